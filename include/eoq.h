@@ -67,12 +67,14 @@ typedef enum {
 
 /* Bits of the device status word returned by eoq_last_status(). */
 #define EOQ_DEV_TIMEOUT 1u   /* a bounded wait inside a kernel ran out; results of that call are invalid */
-#define EOQ_DEV_NONFINITE 2u /* eoq_quantize met a NaN or an infinity */
+#define EOQ_DEV_NONFINITE 2u /* eoq_quantize, eoq_ckpt_save or eoq_gn_fwd (its 8-bit form) met a NaN or an infinity */
 #define EOQ_DEV_SQ_ZERO 4u   /* a scale quantizer saw an all-zero tensor (codes 0, exponent passed through) */
 #define EOQ_DEV_RANGE 8u     /* an input exponent outside the supported range */
 
 typedef enum { EOQ_Q = 0, EOQ_CQ = 1, EOQ_SQ = 2 } eoq_qmode_t;
 typedef enum { EOQ_ROUND_RNE = 0, EOQ_ROUND_STOCHASTIC = 1 } eoq_round_t;
+typedef enum { EOQ_F32 = 0, EOQ_F16 = 1, EOQ_BF16 = 2, EOQ_I32 = 3 } eoq_dtype_t;
+typedef enum { EOQ_ACT_NONE = 0, EOQ_ACT_RELU = 1, EOQ_ACT_SILU = 2 } eoq_act_t;
 typedef enum { EOQ_PASS_FWD = 0, EOQ_PASS_DGRAD = 1, EOQ_PASS_WGRAD = 2 } eoq_pass_t;
 
 /* Geometry of one convolution: input [n,h,w,c_in], filter kh x kw, square stride and padding.
@@ -413,6 +415,68 @@ EOQ_API int eoq_bn_bwd(eoq_handle_t handle, const int8_t *e, const int32_t *e_ex
                int acc_exp, size_t pixels, int c, const float *gamma, void *workspace, size_t workspace_bytes, float *da,
                float *dgamma, float *dbeta, void *stream);
 /*
+ * Activations kept in 8 bits between the passes: the scale quantizer of Sec. 3.2.2 with a step per block of EOQ_CKPT_BLOCK
+ * neighbouring columns of a row (channels of a pixel) instead of one for the tensor, for what a training step keeps of
+ * tensors that are not 8-bit codes already.
+ *   codes  int8 [rows][cols];  exps  one byte s per block, [rows][ceil(cols / 32)], a row's last block may be shorter.
+ *   value = code * 2^(s - 127) with s >= 1 the smallest byte for which the block's largest magnitude is at most 127 steps;
+ *   code = R(v / 2^(s - 127)), so a value is off by half a step at most.  Blocks whose largest magnitude is above
+ *   127 * 2^121 take s = 249 and codes up to 63 (one step).  A block that holds a NaN or an infinity has s = 255 and codes
+ *   0, reads back as NaN and raises EOQ_DEV_NONFINITE.
+ * eoq_ckpt_save: src [rows][stride] of `dtype`, stride >= cols elements from row to row (0 = cols).  EOQ_I32 stands for
+ *   integer sums at exponent src_exp in [-60, 60] (rounded to fp32 first; src_exp must be 0 for the other types).
+ * eoq_ckpt_load: dst [rows][stride] of EOQ_F32, EOQ_F16 or EOQ_BF16; what lies between cols and stride is left as it is.  Exact, except
+ *   that fp16 rounds what is below its normal numbers and holds magnitudes above 65504 at 65504.
+ * Pointers of the values aligned to their elements; 16-byte aligned pointers with cols and strides in multiples of 16 bytes
+ * run several times faster.  Tensors must not overlap.
+ * Errors: BAD_ARG (null pointer, no rows or columns, stride < cols, unknown type), ALIGNMENT, UNSUPPORTED (cols > 2^20, rows > 2^40),
+ * RANGE (src_exp), BAD_ARG when the handle's device is not the current one.
+ */
+#define EOQ_CKPT_BLOCK 32
+EOQ_API int eoq_ckpt_save(eoq_handle_t handle, const void *src, int dtype, int src_exp, size_t rows, int cols, size_t stride,
+                  int8_t *codes, uint8_t *exps, void *stream);
+EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_t *exps, size_t rows, int cols, void *dst, int dtype,
+                  size_t stride, void *stream);
+
+/*
+ * Group normalisation with an activation, channels last: the normalisation beside eoq_bn_* that does not look over the batch
+ * (Sec. 5.3 compares with the one that does; small-batch training has no batch to look over).  Per sample and group of
+ * c / groups neighbouring channels, over all `hw` pixels:
+ *   u = (x - mean) * rstd,  rstd = 1 / sqrt(variance + eps) (biased variance),  y = act(gamma[c] u + beta[c]).
+ * eoq_gn_desc_t: n samples, hw pixels each, c channels, `groups` dividing c.  dtype is that of x: EOQ_F32, EOQ_F16 or EOQ_BF16, with
+ * y, dy and dx in the same type; or EOQ_I32, the exact sums of a convolution (acc_dump of eoq_conv_fwd) at exponent x_exp (-14 there;
+ * within [-60, 60], 0 for the other types), with y = Q_a2 of the result, int8 codes at exponent -7, dy int8 codes at *dy_exp
+ * (device, within [-120, 120], else EOQ_DEV_RANGE) and dx fp32 (quantize it with eoq_quantize(EOQ_SQ) for the passes of the layer in
+ * front).  act: EOQ_ACT_NONE, EOQ_ACT_RELU, EOQ_ACT_SILU (z / (1 + exp(-z))).  Strides: elements from pixel to pixel of each tensor, so
+ * that a tensor may be part of the channels of a wider one; 0 = c.  Samples follow one another (hw * stride elements apart).
+ * eoq_gn_fwd: gamma, beta fp32 [c], NULL = 1 and 0.  stats (fp32 [n][groups][2]: mean, rstd; NULL when no backward pass follows).
+ *   codes and exps (both or neither): the 8-bit form of x, as eoq_ckpt_save(x, rows = n * hw, cols = c) writes it.
+ * eoq_gn_bwd: either x, or codes and exps with x = NULL: the gradients are then those at the values the 8-bit form stands for, with the
+ *   forward pass's mean and rstd (an element is off by at most half a step of its block times rstd in u; ReLU's gate goes by the
+ *   same u).  gamma, beta, stats as in the forward pass.  With dz = dy * act'(z):
+ *   dgamma = sum dz u, dbeta = sum dz (fp32 [c], each may be NULL), dx = rstd (gamma dz - S1 - u S2), S1 and S2 the means of
+ *   gamma dz and gamma dz u over the sample's group.
+ * All arithmetic in fp32 and more; sums run in an order that depends on the sizes alone, so results are reproducible bit for bit.
+ * NaN and infinity spread to their sample's group and to the sums that hold them.  Tensors must not overlap.
+ * workspace: eoq_gn_workspace_size() bytes, 256-byte aligned, the same for both directions; nothing is kept in it between calls.
+ * Pointers aligned to their elements (stats to 8 bytes); 16-byte aligned tensors with c and strides in multiples of 16 bytes run
+ * several times faster.
+ * Errors: BAD_ARG (null pointer, non-positive size, groups not dividing c, stride < c, unknown type or activation, eps negative or
+ * NaN, x and codes both given, the handle's device not the current one), ALIGNMENT, UNSUPPORTED (n or hw > 2^30, c > 2^20), RANGE
+ * (x_exp), WORKSPACE.
+ */
+typedef struct {
+    int n, hw, c, groups, dtype, x_exp, act;
+    float eps;
+    size_t x_stride, y_stride, dy_stride, dx_stride;
+} eoq_gn_desc_t;
+EOQ_API int eoq_gn_workspace_size(const eoq_gn_desc_t *desc, size_t *bytes);
+EOQ_API int eoq_gn_fwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const void *x, const float *gamma, const float *beta, void *y,
+               float *stats, int8_t *codes, uint8_t *exps, void *workspace, size_t workspace_bytes, void *stream);
+EOQ_API int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const void *dy, const int32_t *dy_exp, const void *x,
+               const int8_t *codes, const uint8_t *exps, const float *gamma, const float *beta, const float *stats, void *dx,
+               float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+/*
  * Update of `num` scalar parameters (gamma, b1, b2; Sec. 3.2.3 applied to a single value): g = Q_g({total}) with
  * total the exact sum behind the gradient at exponent *total_exp[i] + exp_bias[i]; u = Q_u(lr g);
  * theta <- Q(theta - u) saturated to 16 bits, rounding as in eoq_update (the hash counter of scalar i is
@@ -441,7 +505,7 @@ EOQ_API int eoq_last_status(eoq_handle_t handle, void *stream, unsigned *bits);
 #define EOQ_PROF_DGRAD_AUX 4     /* Q_e phase 2 */
 #define EOQ_PROF_WGRAD_AUX 5     /* slice sum + b1 term + Q_g behind the weight-gradient GEMM */
 #define EOQ_PROF_FWD_AUX 6       /* b1 weight table, weight row padding (eoq_weight_prep, or per call without it) */
-#define EOQ_PROF_OTHER 7         /* eoq_quantize, eoq_bn_fwd, eoq_bn_bwd */
+#define EOQ_PROF_OTHER 7         /* eoq_quantize, eoq_bn_*, eoq_gn_*, eoq_ckpt_* */
 #define EOQ_PROF_UPDATE 8        /* eoq_update */
 #define EOQ_PROF_INPUT_Q 9       /* eoq_quantize_image */
 #define EOQ_PROF_WGRAD_TAPS 10   /* b1 error sums of the weight gradient (none for a layer without a bias in front) */

@@ -2243,6 +2243,171 @@ extern "C" int eoq_bn_bwd(eoq_handle_t handle, const int8_t *e, const int32_t *e
                                    dgamma, dbeta, h->sm_count, s));
 }
 
+// ================================================================================= activations in 8 bits, group normalisation
+
+static bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+static int dtype_size(int dtype) { return dtype == EOQ_F16 || dtype == EOQ_BF16 ? 2 : 4; }
+
+// These calls may stand between other libraries' work, so a device that is not the handle's is refused instead of assumed away.
+static bool on_handle_device(const Handle *h)
+{
+    int device = -1;
+    return h && cudaGetDevice(&device) == cudaSuccess && device == h->device;
+}
+
+// what can be told without a handle
+static int ckpt_check(const void *values, int dtype, int last_dtype, size_t rows, int cols, size_t stride, const void *codes, const void *exps)
+{
+    if (!values || !codes || !exps || rows == 0 || cols <= 0 || stride < (size_t)cols || dtype < EOQ_F32 || dtype > last_dtype)
+        return EOQ_ERR_BAD_ARG;
+    if (cols > (1 << 20) || rows > (size_t)1 << 40 || stride > (size_t)1 << 40) return EOQ_ERR_UNSUPPORTED;
+    if (!aligned_to(values, dtype_size(dtype))) return EOQ_ERR_ALIGNMENT;
+    return EOQ_OK;
+}
+
+extern "C" int eoq_ckpt_save(eoq_handle_t handle, const void *src, int dtype, int src_exp, size_t rows, int cols, size_t stride,
+                             int8_t *codes, uint8_t *exps, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    if (stride == 0 && cols > 0) stride = cols;
+    const int chk = ckpt_check(src, dtype, EOQ_I32, rows, cols, stride, codes, exps);
+    if (chk != EOQ_OK) return chk;
+    if (dtype == EOQ_I32 ? src_exp < -60 || src_exp > 60 : src_exp != 0) return EOQ_ERR_RANGE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    count_launches(h, 1);
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    return record(h, launch_ckpt_save(src, dtype, src_exp, rows, cols, stride, codes, exps, h->dev, h->sm_count, s));
+}
+
+extern "C" int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_t *exps, size_t rows, int cols, void *dst, int dtype,
+                             size_t stride, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    if (stride == 0 && cols > 0) stride = cols;
+    const int chk = ckpt_check(dst, dtype, EOQ_BF16, rows, cols, stride, codes, exps);
+    if (chk != EOQ_OK) return chk;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    count_launches(h, 1);
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    return record(h, launch_ckpt_load(codes, exps, rows, cols, dst, dtype, stride, h->dev, h->sm_count, s));
+}
+
+// The descriptor of a call with its strides filled in.
+static int gn_check(const eoq_gn_desc_t *desc, eoq_gn_desc_t *d)
+{
+    if (!desc) return EOQ_ERR_BAD_ARG;
+    *d = *desc;
+    if (d->n <= 0 || d->hw <= 0 || d->c <= 0 || d->groups <= 0 || d->c % d->groups || d->dtype < EOQ_F32 || d->dtype > EOQ_I32 ||
+        d->act < EOQ_ACT_NONE || d->act > EOQ_ACT_SILU || !(d->eps >= 0.0f))
+        return EOQ_ERR_BAD_ARG;
+    if (d->n > 1 << 30 || d->hw > 1 << 30 || d->c > 1 << 20) return EOQ_ERR_UNSUPPORTED;
+    size_t *strides[4] = {&d->x_stride, &d->y_stride, &d->dy_stride, &d->dx_stride};
+    for (size_t *s : strides) {
+        if (*s == 0) *s = d->c;
+        if (*s < (size_t)d->c) return EOQ_ERR_BAD_ARG;
+        if (*s > (size_t)1 << 30) return EOQ_ERR_UNSUPPORTED;
+    }
+    if (d->dtype == EOQ_I32 ? d->x_exp < -60 || d->x_exp > 60 : d->x_exp != 0) return EOQ_ERR_RANGE;
+    return EOQ_OK;
+}
+
+static GnArgs gn_args(const Handle *h, const eoq_gn_desc_t &d, const float *gamma, const float *beta, const float *stats)
+{
+    GnArgs a = {};
+    a.gamma = gamma;
+    a.beta = beta;
+    a.stats = reinterpret_cast<float2 *>(const_cast<float *>(stats));
+    a.dev = h->dev;
+    a.x_stride = d.x_stride;
+    a.y_stride = d.y_stride;
+    a.dy_stride = d.dy_stride;
+    a.dx_stride = d.dx_stride;
+    a.eps = d.eps;
+    a.x_scale = ldexpf(1.0f, d.x_exp);
+    a.n = d.n;
+    a.hw = d.hw;
+    a.c = d.c;
+    a.groups = d.groups;
+    a.cpg = d.c / d.groups;
+    a.act = d.act;
+    a.blocks = (d.c + kBlock8 - 1) / kBlock8;
+    a.x_exp = d.x_exp;
+    a.sm_count = h->sm_count;
+    return a;
+}
+
+extern "C" int eoq_gn_workspace_size(const eoq_gn_desc_t *desc, size_t *bytes)
+{
+    eoq_gn_desc_t d;
+    if (!bytes) return EOQ_ERR_BAD_ARG;
+    const int chk = gn_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    *bytes = round256(gn_workspace_bytes(d));
+    return EOQ_OK;
+}
+
+extern "C" int eoq_gn_fwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const void *x, const float *gamma, const float *beta, void *y,
+                          float *stats, int8_t *codes, uint8_t *exps, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    eoq_gn_desc_t d;
+    const int chk = gn_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    if (!x || !y || (codes == nullptr) != (exps == nullptr)) return EOQ_ERR_BAD_ARG;
+    const size_t e = dtype_size(d.dtype), ey = d.dtype == EOQ_I32 ? 1 : e;
+    if (!aligned_to(x, e) || !aligned_to(y, ey) || !aligned_to(gamma, 4) || !aligned_to(beta, 4) || !aligned_to(stats, 8))
+        return EOQ_ERR_ALIGNMENT;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < gn_workspace_bytes(d)) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    GnArgs a = gn_args(h, d, gamma, beta, stats);
+    a.x = x;
+    a.y = y;
+    a.codes_out = codes;
+    a.exps_out = exps;
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    const cudaError_t err = launch_gn_fwd(a, d.dtype, workspace, &launches, s);
+    count_launches(h, launches);
+    return record(h, err);
+}
+
+extern "C" int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const void *dy, const int32_t *dy_exp, const void *x,
+                          const int8_t *codes, const uint8_t *exps, const float *gamma, const float *beta, const float *stats, void *dx,
+                          float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    eoq_gn_desc_t d;
+    const int chk = gn_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    if (!dy || !dx || !stats || (codes == nullptr) != (exps == nullptr) || (x == nullptr) == (codes == nullptr) ||
+        (d.dtype == EOQ_I32) != (dy_exp != nullptr))
+        return EOQ_ERR_BAD_ARG;
+    const size_t e = dtype_size(d.dtype), ey = d.dtype == EOQ_I32 ? 1 : e;
+    if (!aligned_to(x, e) || !aligned_to(dy, ey) || !aligned_to(dx, e) || !aligned_to(gamma, 4) || !aligned_to(beta, 4) ||
+        !aligned_to(stats, 8) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4) || !aligned_to(dy_exp, 4))
+        return EOQ_ERR_ALIGNMENT;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < gn_workspace_bytes(d)) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    GnArgs a = gn_args(h, d, gamma, beta, stats);
+    a.x = x;
+    a.dy = dy;
+    a.dy_exp = dy_exp;
+    a.dx = dx;
+    a.codes = codes;
+    a.exps = exps;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    const cudaError_t err = launch_gn_bwd(a, d.dtype, workspace, &launches, s);
+    count_launches(h, launches);
+    return record(h, err);
+}
+
 extern "C" int eoq_aux_avgpool_sum(eoq_handle_t handle, const int8_t *x, int n, int hw, int c, int32_t *sums, void *stream)
 {
     Handle *h = reinterpret_cast<Handle *>(handle);

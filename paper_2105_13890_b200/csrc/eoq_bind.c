@@ -238,9 +238,70 @@ static PyObject *weight_prep(PyObject *self, PyObject *const *a, Py_ssize_t n)
     return ok ? PyLong_FromLong(st) : NULL;
 }
 
+static PyObject *ckpt_save(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle src dtype src_exp rows cols stride | codes exps stream */
+    void *h, *src, *p[3];
+    long long v[5];
+    if (!want(n, 10) || !get_ptr(a[0], &h) || !get_ptr(a[1], &src)) return NULL;
+    for (int i = 0; i < 5; ++i)
+        if (!get_int(a[2 + i], &v[i])) return NULL;
+    PTRS(7, 3);
+    CALL(eoq_ckpt_save((eoq_handle_t)h, src, (int)v[0], (int)v[1], (size_t)v[2], (int)v[3], (size_t)v[4], (int8_t *)p[0], (uint8_t *)p[1], p[2]));
+}
+
+static PyObject *ckpt_load(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle | codes exps | rows cols dst dtype stride stream */
+    void *h, *p[2], *dst, *stream;
+    long long rows, cols, dtype, stride;
+    if (!want(n, 9) || !get_ptr(a[0], &h) || !get_int(a[3], &rows) || !get_int(a[4], &cols) || !get_ptr(a[5], &dst) ||
+        !get_int(a[6], &dtype) || !get_int(a[7], &stride) || !get_ptr(a[8], &stream))
+        return NULL;
+    PTRS(1, 2);
+    CALL(eoq_ckpt_load((eoq_handle_t)h, (const int8_t *)p[0], (const uint8_t *)p[1], (size_t)rows, (int)cols, dst, (int)dtype, (size_t)stride,
+                       stream));
+}
+
+static int get_gn_desc(PyObject *o, eoq_gn_desc_t *out)
+{
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE)) return 0;
+    const int ok = view.len == (Py_ssize_t)sizeof(*out);
+    if (ok) memcpy(out, view.buf, sizeof(*out));
+    else PyErr_SetString(PyExc_TypeError, "not a group norm descriptor");
+    PyBuffer_Release(&view);
+    return ok;
+}
+
+static PyObject *gn_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle desc | x gamma beta y stats codes exps workspace stream */
+    void *h, *p[9];
+    eoq_gn_desc_t d;
+    size_t bytes;
+    if (!want(n, 11) || !get_ptr(a[0], &h) || !get_gn_desc(a[1], &d) || !get_bytes(a[9], &bytes)) return NULL;
+    PTRS(2, 9);
+    CALL(eoq_gn_fwd((eoq_handle_t)h, &d, p[0], (const float *)p[1], (const float *)p[2], p[3], (float *)p[4], (int8_t *)p[5],
+                    (uint8_t *)p[6], p[7], bytes, p[8]));
+}
+
+static PyObject *gn_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle desc | dy dy_exp x codes exps gamma beta stats dx dgamma dbeta workspace stream */
+    void *h, *p[13];
+    eoq_gn_desc_t d;
+    size_t bytes;
+    if (!want(n, 15) || !get_ptr(a[0], &h) || !get_gn_desc(a[1], &d) || !get_bytes(a[13], &bytes)) return NULL;
+    PTRS(2, 13);
+    CALL(eoq_gn_bwd((eoq_handle_t)h, &d, p[0], (const int32_t *)p[1], p[2], (const int8_t *)p[3], (const uint8_t *)p[4],
+                    (const float *)p[5], (const float *)p[6], (const float *)p[7], p[8], (float *)p[9], (float *)p[10], p[11], bytes, p[12]));
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(conv_fwd_dev), METHOD(conv_dgrad), METHOD(conv_wgrad_dev), METHOD(err_prescale_dev),
-                                METHOD(quantize), METHOD(update_dev), METHOD(weight_prep), {NULL, NULL, 0, NULL}};
+                                METHOD(quantize), METHOD(update_dev), METHOD(weight_prep), METHOD(ckpt_save), METHOD(ckpt_load),
+                                METHOD(gn_fwd), METHOD(gn_bwd), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_eoqbind", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__eoqbind(void)

@@ -1,0 +1,519 @@
+// Group normalisation with an activation on channels-last tensors, forward and backward (eoq_gn_fwd, eoq_gn_bwd).  Beside
+// eoq_bn.cu, the comparison case of arXiv 2105.13890, Sec. 5.3, it is the normalisation that does not look over the batch, which
+// is what the paper's small-batch training needs:
+//   u = (x - mean) rstd over the pixels and channels of a (sample, group),  z = gamma u + beta,  y = act(z);
+//   dz = dy act'(z),  dbeta = sum dz,  dgamma = sum dz u,  dx = rstd (gamma dz - S1 - u S2),
+//   S1 and S2 the means of gamma dz and gamma dz u over the (sample, group).
+//
+// The kernels here are the form for every size: a pass that reduces, a small one that joins, a pass that writes.  A thread owns kV
+// neighbouring channels (16 bytes of x, or one element where widths or addresses rule that out) and walks pixels of one sample, so
+// that what depends on the channel stays in registers.  Sums never leave the thread as raw squares: a batch of pixels gives its mean
+// and its squares about that mean, and (count, mean, squares) are joined pairwise, so a mean far from zero costs no digits.
+#include "eoq_gn.cuh"
+
+namespace eoq {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;
+
+template <int kType, int kV>
+__global__ void __launch_bounds__(kThreads) gn_stats_kernel(const __grid_constant__ GnArgs a)
+{
+    extern __shared__ float2 cell[];   // [slots][channels of the chunk]: mean, squares
+    ptx::grid_dep_wait();
+    const int smp = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
+    const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
+    constexpr int kB = kV * Elem<kType>::kSize;
+    float mean[kV], sq[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) mean[i] = sq[i] = 0.0f;
+    if (slot < a.slots && ch < a.c) {
+        const char *src = reinterpret_cast<const char *>(a.x) + ((size_t)smp * a.hw * a.x_stride + ch) * Elem<kType>::kSize;
+        int count = 0;
+        for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
+            Raw<kB> raw[kUnroll];
+            float v[kUnroll][kV];
+            int m = 0;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + u * a.slots;
+                raw[u] = p < p_end ? load_raw<kB>(src + (size_t)p * a.x_stride * Elem<kType>::kSize) : zero_raw<kB>();
+                m += p < p_end;
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
+            const float inv_m = 1.0f / (float)m, share = (float)m / (float)(count + m), both = (float)count * share;
+            count += m;
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                // about the first pixel: equal values have exactly themselves as their mean
+                const float k = v[0][i];
+                float s = 0.0f, q = 0.0f;
+#pragma unroll
+                for (int u = 1; u < kUnroll; ++u) s += u < m ? v[u][i] - k : 0.0f;   // (the valid pixels come first)
+                s = __fmaf_rn(s, inv_m, k);
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    const float d = u < m ? v[u][i] - s : 0.0f;
+                    q = __fmaf_rn(d, d, q);
+                }
+                const float d = s - mean[i];
+                mean[i] = __fmaf_rn(d, share, mean[i]);
+                sq[i] += __fmaf_rn(d * d, both, q);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kV; ++i) cell[(slot * a.cv + cv) * kV + i] = make_float2(mean[i], sq[i]);
+    }
+    __syncthreads();
+    // a thread per channel joins the slots: the mean of the means by their counts, then the squares about it
+    const int width = a.cv * kV, total = p_end - p_begin;
+    for (int k = threadIdx.x; k < width; k += kThreads) {
+        const int c = blockIdx.y * width + k;
+        if (c >= a.c) break;
+        float s = 0.0f, q = 0.0f;
+        const int full = total / a.slots, more = total % a.slots;   // slot j has `full` pixels, the first `more` one more
+        const float first = cell[k].x;
+        for (int j = 1; j < a.slots; ++j) s = __fmaf_rn(full + (j < more) ? cell[j * width + k].x - first : 0.0f, (float)(full + (j < more)), s);
+        s = first + s / (float)total;
+        for (int j = 0; j < a.slots; ++j) {
+            const float2 e = cell[j * width + k];
+            const int cnt = full + (j < more);
+            if (cnt) q += __fmaf_rn((e.x - s) * (e.x - s), (float)cnt, e.y);
+        }
+        a.part[((size_t)smp * a.splits + split) * a.c + c] = make_float2(s, q);
+    }
+}
+
+// a warp per (sample, group): mean and 1 / sqrt(variance + eps)
+__global__ void __launch_bounds__(kThreads) gn_join_kernel(const __grid_constant__ GnArgs a)
+{
+    ptx::grid_dep_wait_launch_small();
+    const int lane = threadIdx.x & 31;
+    const size_t id = (size_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+    if (id >= (size_t)a.n * a.groups) return;
+    const int smp = (int)(id / a.groups), g = (int)(id % a.groups), cells = a.splits * a.cpg;
+    const float2 *part = a.part + (size_t)smp * a.splits * a.c + (size_t)g * a.cpg;
+    auto count_of = [&](int split) { return (double)(min(a.hw, (split + 1) * a.per_split) - split * a.per_split); };
+    double s = 0.0;
+    for (int i = lane; i < cells; i += 32) s += count_of(i / a.cpg) * part[(size_t)(i / a.cpg) * a.c + i % a.cpg].x;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    const double total = (double)a.hw * a.cpg, mean = s / total;
+    double q = 0.0;
+    for (int i = lane; i < cells; i += 32) {
+        const float2 e = part[(size_t)(i / a.cpg) * a.c + i % a.cpg];
+        q += e.y + count_of(i / a.cpg) * (e.x - mean) * (e.x - mean);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+    if (lane == 0) a.stats[id] = make_float2((float)mean, (float)(1.0 / sqrt(q / total + (double)a.eps)));
+}
+
+template <int kType, int kV, bool kSave>
+__global__ void __launch_bounds__(kThreads) gn_apply_kernel(const __grid_constant__ GnArgs a)
+{
+    using Types = GnTypes<kType>;
+    constexpr int kB = kV * Elem<kType>::kSize, kLanes = kBlock8 / kV;
+    ptx::grid_dep_wait_launch_small();
+    const int smp = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
+    const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
+    const bool mine = slot < a.slots && ch < a.c;
+    float mul[kV], add[kV], mean[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) mul[i] = add[i] = mean[i] = 0.0f;
+    if (mine)
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
+            mean[i] = st.x;
+            mul[i] = a.gamma ? st.y * a.gamma[ch + i] : st.y;
+            add[i] = a.beta ? a.beta[ch + i] : 0.0f;
+        }
+    const size_t pix0 = (size_t)smp * a.hw;
+    unsigned bad = 0;
+    for (int p0 = p_begin; p0 < p_end; p0 += kUnroll * a.slots) {
+        Raw<kB> raw[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int p = p0 + slot + u * a.slots;
+            raw[u] = mine && p < p_end ? load_raw<kB>(reinterpret_cast<const char *>(a.x) + ((pix0 + p) * a.x_stride + ch) * Elem<kType>::kSize)
+                                       : zero_raw<kB>();
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int p = p0 + slot + u * a.slots;
+            const bool in = mine && p < p_end;
+            float v[kV];
+            x_values<kType, kV>(raw[u], a.x_scale, v);
+            if constexpr (kSave) {
+                float m = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) m = max_abs(m, v[i]);
+                m = lanes_max_abs<kLanes>(m);
+                const int s = block_exp(m);
+                uint32_t w[(kV + 3) / 4];
+                block_codes(v, s, w);
+                if (in) {
+                    Raw<kV> out;
+#pragma unroll
+                    for (int i = 0; i < (kV + 3) / 4; ++i) set_word(out, i, w[i]);
+                    store_raw(a.codes_out + (pix0 + p) * a.c + ch, out);
+                    if (ch % kBlock8 == 0) a.exps_out[(pix0 + p) * a.blocks + ch / kBlock8] = (uint8_t)s;
+                    bad |= s == 255;
+                }
+            }
+            if (in) {
+#pragma unroll
+                for (int i = 0; i < kV; ++i) v[i] = __fmaf_rn(v[i] - mean[i], mul[i], add[i]);
+                activate(v, a.act);
+                store_raw(reinterpret_cast<char *>(a.y) + ((pix0 + p) * a.y_stride + ch) * Elem<Types::kY>::kSize,
+                          Elem<Types::kY>::from_f32(v));
+            }
+        }
+    }
+    if (kSave && bad) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
+}
+
+// What the backward pass reads of a pixel: x or its 8-bit form, and the error.
+template <int kType, int kV, bool kCodes>
+struct GnInput {
+    using Types = GnTypes<kType>;
+    static constexpr int kXB = kCodes ? kV : kV * Elem<kType>::kSize, kDyB = kV * Elem<Types::kY>::kSize;
+    Raw<kXB> x;
+    Raw<kDyB> dy;
+    int s;
+    __device__ __forceinline__ void load(const GnArgs &a, size_t pix, int ch, bool in)
+    {
+        x = zero_raw<kXB>();
+        dy = zero_raw<kDyB>();
+        s = 1;
+        if (!in) return;
+        if (kCodes) {
+            x = load_raw<kXB>(a.codes + pix * a.c + ch);
+            s = __ldg(a.exps + pix * a.blocks + ch / kBlock8);
+        } else {
+            x = load_raw<kXB>(reinterpret_cast<const char *>(a.x) + (pix * a.x_stride + ch) * Elem<kType>::kSize);
+        }
+        dy = load_raw<kDyB>(reinterpret_cast<const char *>(a.dy) + (pix * a.dy_stride + ch) * Elem<Types::kY>::kSize);
+    }
+    // u = (x - mean) rstd and dz = dy act'(gamma u + beta)
+    __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&mean)[kV], const float (&gamma)[kV],
+                                           const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
+    {
+        float z[kV];
+        if constexpr (kCodes) block_values<kV>(x, s, u);
+        else x_values<kType, kV>(x, a.x_scale, u);
+        Elem<Types::kY>::to_f32(dy, dz);
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            u[i] = (u[i] - mean[i]) * rstd[i];
+            z[i] = __fmaf_rn(u[i], gamma[i], beta[i]);
+            if (kType == EOQ_I32) dz[i] *= dy_scale;
+        }
+        times_slope(dz, z, a.act);
+    }
+};
+
+// 2^*dy_exp of int8 errors
+template <int kType>
+__device__ __forceinline__ float error_scale(const GnArgs &a)
+{
+    if (kType != EOQ_I32) return 1.0f;
+    const int e = *a.dy_exp;
+    if ((e < -120 || e > 120) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(&a.dev->status, EOQ_DEV_RANGE);
+    return ldexpf(1.0f, clampi(e, -120, 120));
+}
+
+template <int kType, int kV, bool kCodes>
+__global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_constant__ GnArgs a)
+{
+    extern __shared__ float2 cell[];   // [slots][channels of the chunk]: sum dz, sum dz u
+    ptx::grid_dep_wait();
+    const int smp = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
+    const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
+    if (slot < a.slots && ch < a.c) {
+        float rstd[kV], mean[kV], gamma[kV], beta[kV], s0[kV], s1[kV];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+            const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
+            rstd[i] = st.y;
+            mean[i] = st.x;
+            gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
+            beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
+            s0[i] = s1[i] = 0.0f;
+        }
+        const float dy_scale = error_scale<kType>(a);
+        const size_t pix0 = (size_t)smp * a.hw;
+        for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
+            GnInput<kType, kV, kCodes> in[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                if (p0 + k * a.slots >= p_end) break;
+                float u[kV], dz[kV];
+                in[k].values(a, rstd, mean, gamma, beta, dy_scale, u, dz);
+#pragma unroll
+                for (int i = 0; i < kV; ++i) {
+                    s0[i] += dz[i];
+                    s1[i] = __fmaf_rn(dz[i], u[i], s1[i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kV; ++i) cell[(slot * a.cv + cv) * kV + i] = make_float2(s0[i], s1[i]);
+    }
+    __syncthreads();
+    const int width = a.cv * kV;
+    for (int k = threadIdx.x; k < width; k += kThreads) {
+        const int c = blockIdx.y * width + k;
+        if (c >= a.c) break;
+        float2 t = make_float2(0.0f, 0.0f);
+        for (int j = 0; j < a.slots; ++j) {
+            const float2 e = cell[j * width + k];
+            t.x += e.x;
+            t.y += e.y;
+        }
+        a.part[((size_t)smp * a.splits + split) * a.c + c] = t;
+    }
+}
+
+// Blocks in front: a warp per (sample, group) forms S1 and S2.  Blocks behind: 32 channels each, dgamma and dbeta over samples and
+// splits, 8 threads a channel in a fixed order.
+__global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_constant__ GnArgs a, int group_blocks)
+{
+    ptx::grid_dep_wait_launch_small();
+    if ((int)blockIdx.x < group_blocks) {
+        const int lane = threadIdx.x & 31;
+        const size_t id = (size_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+        if (id >= (size_t)a.n * a.groups) return;
+        const int smp = (int)(id / a.groups), g = (int)(id % a.groups), cells = a.splits * a.cpg;
+        const float2 *part = a.part + (size_t)smp * a.splits * a.c + (size_t)g * a.cpg;
+        float s0 = 0.0f, s1 = 0.0f;
+        for (int i = lane; i < cells; i += 32) {
+            const float2 e = part[(size_t)(i / a.cpg) * a.c + i % a.cpg];
+            const float gamma = a.gamma ? a.gamma[g * a.cpg + i % a.cpg] : 1.0f;
+            s0 = __fmaf_rn(gamma, e.x, s0);
+            s1 = __fmaf_rn(gamma, e.y, s1);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            s0 += __shfl_xor_sync(0xffffffffu, s0, d);
+            s1 += __shfl_xor_sync(0xffffffffu, s1, d);
+        }
+        const float total = (float)((double)a.hw * a.cpg);
+        if (lane == 0) a.means[id] = make_float2(s0 / total, s1 / total);
+        return;
+    }
+    __shared__ float2 red[8][32];
+    const int k = threadIdx.x & 31, j = threadIdx.x >> 5, c = ((int)blockIdx.x - group_blocks) * 32 + k;
+    float2 t = make_float2(0.0f, 0.0f);
+    if (c < a.c)
+        for (size_t r = j; r < (size_t)a.n * a.splits; r += 8) {
+            const float2 e = a.part[r * a.c + c];
+            t.x += e.x;
+            t.y += e.y;
+        }
+    red[j][k] = t;
+    __syncthreads();
+    if (j == 0 && c < a.c) {
+        for (int i = 1; i < 8; ++i) {
+            t.x += red[i][k].x;
+            t.y += red[i][k].y;
+        }
+        if (a.dbeta) a.dbeta[c] = t.x;
+        if (a.dgamma) a.dgamma[c] = t.y;
+    }
+}
+
+template <int kType, int kV, bool kCodes>
+__global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_constant__ GnArgs a)
+{
+    using Types = GnTypes<kType>;
+    ptx::grid_dep_wait_launch_small();
+    const int smp = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
+    if (slot >= a.slots || ch >= a.c) return;
+    const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
+    float rstd[kV], mean[kV], gamma[kV], beta[kV], k0[kV], k1[kV];
+#pragma unroll
+    for (int i = 0; i < kV; ++i) {
+        const size_t g = (size_t)smp * a.groups + (ch + i) / a.cpg;
+        const float2 st = a.stats[g], m = a.means[g];
+        rstd[i] = st.y;
+        mean[i] = st.x;
+        gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
+        beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
+        k0[i] = -st.y * m.x;
+        k1[i] = -st.y * m.y;
+    }
+    const float dy_scale = error_scale<kType>(a);
+    const size_t pix0 = (size_t)smp * a.hw;
+    for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
+        GnInput<kType, kV, kCodes> in[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            const int p = p0 + k * a.slots;
+            if (p >= p_end) break;
+            float u[kV], dz[kV];
+            in[k].values(a, rstd, mean, gamma, beta, dy_scale, u, dz);
+#pragma unroll
+            for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i] * gamma[i], rstd[i], __fmaf_rn(u[i], k1[i], k0[i]));
+            store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,
+                      Elem<Types::kDx>::from_f32(dz));
+        }
+    }
+}
+
+// How the channels and pixels of a call are dealt out to thread blocks.
+struct GnPlan {
+    int cv, slots, chunks, splits, per_split;
+};
+
+// `blocks`: how many thread blocks are wanted in all.  Splits are whole rounds of the block's pixels.
+GnPlan gn_plan(int n, int hw, int c, int v, int blocks)
+{
+    GnPlan p;
+    const int per_pixel = (c + v - 1) / v, lanes = kBlock8 / v;
+    p.chunks = (per_pixel + kThreads - 1) / kThreads;
+    p.cv = (per_pixel + p.chunks - 1) / p.chunks;
+    if (c % kBlock8 == 0) p.cv = (p.cv + lanes - 1) / lanes * lanes;   // blocks of the 8-bit form stay within a warp
+    p.slots = kThreads / p.cv;
+    const int rounds = (hw + p.slots * kUnroll - 1) / (p.slots * kUnroll);
+    long long splits = (blocks + (long long)n * p.chunks - 1) / ((long long)n * p.chunks);
+    if (splits > rounds) splits = rounds;
+    if (splits < 1) splits = 1;
+    p.per_split = (int)((rounds + splits - 1) / splits) * p.slots * kUnroll;
+    p.splits = (hw + p.per_split - 1) / p.per_split;
+    return p;
+}
+
+constexpr int kStatBlocks = 4 * kPartSms, kApplyBlocks = 8 * kPartSms;
+
+int wide_of(int dtype) { return dtype == EOQ_F32 || dtype == EOQ_I32 ? 4 : 8; }
+
+void use_plan(GnArgs &a, const GnPlan &p)
+{
+    a.cv = p.cv;
+    a.slots = p.slots;
+    a.splits = p.splits;
+    a.per_split = p.per_split;
+}
+
+size_t parts_bytes(int n, int hw, int c, int dtype)
+{
+    // either width may be taken, by the addresses of the call
+    const GnPlan w = gn_plan(n, hw, c, wide_of(dtype), kStatBlocks), s = gn_plan(n, hw, c, 1, kStatBlocks);
+    const size_t splits = (size_t)(w.splits > s.splits ? w.splits : s.splits);
+    return (sizeof(float2) * (size_t)n * splits * c + 255) & ~(size_t)255;
+}
+
+template <int kType, int kV>
+cudaError_t run_fwd(GnArgs a, int *launches, cudaStream_t st)
+{
+    GnPlan p = gn_plan(a.n, a.hw, a.c, kV, kStatBlocks);
+    use_plan(a, p);
+    cudaError_t e = launch_chained(gn_stats_kernel<kType, kV>, dim3(a.n * p.splits, p.chunks), dim3(kThreads),
+                                   sizeof(float2) * p.slots * p.cv * kV, st, a);
+    if (e != cudaSuccess) return e;
+    const size_t warps = (size_t)a.n * a.groups;
+    e = launch_chained(gn_join_kernel, dim3((unsigned)((warps + kThreads / 32 - 1) / (kThreads / 32))), dim3(kThreads), 0, st, a);
+    if (e != cudaSuccess) return e;
+    p = gn_plan(a.n, a.hw, a.c, kV, kApplyBlocks);
+    use_plan(a, p);
+    *launches += 3;
+    const dim3 grid(a.n * p.splits, p.chunks);
+    if (!a.codes_out) return launch_chained(gn_apply_kernel<kType, kV, false>, grid, dim3(kThreads), 0, st, a);
+    if (a.c % kBlock8 == 0) return launch_chained(gn_apply_kernel<kType, kV, true>, grid, dim3(kThreads), 0, st, a);
+    // a row of blocks that ends inside one
+    e = launch_chained(gn_apply_kernel<kType, kV, false>, grid, dim3(kThreads), 0, st, a);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    return launch_ckpt_save(a.x, kType, a.x_exp, (size_t)a.n * a.hw, a.c, a.x_stride, a.codes_out, a.exps_out, a.dev, a.sm_count, st);
+}
+
+template <int kType, int kV, bool kCodes>
+cudaError_t run_bwd(GnArgs a, int *launches, cudaStream_t st)
+{
+    GnPlan p = gn_plan(a.n, a.hw, a.c, kV, kStatBlocks);
+    use_plan(a, p);
+    cudaError_t e = launch_chained(gn_bwd_sums_kernel<kType, kV, kCodes>, dim3(a.n * p.splits, p.chunks), dim3(kThreads),
+                                   sizeof(float2) * p.slots * p.cv * kV, st, a);
+    if (e != cudaSuccess) return e;
+    const size_t warps = (size_t)a.n * a.groups;
+    const int group_blocks = (int)((warps + kThreads / 32 - 1) / (kThreads / 32)), channel_blocks = (a.c + 31) / 32;
+    e = launch_chained(gn_bwd_join_kernel, dim3(group_blocks + channel_blocks), dim3(kThreads), 0, st, a, group_blocks);
+    if (e != cudaSuccess) return e;
+    p = gn_plan(a.n, a.hw, a.c, kV, kApplyBlocks);
+    use_plan(a, p);
+    *launches += 3;
+    return launch_chained(gn_bwd_apply_kernel<kType, kV, kCodes>, dim3(a.n * p.splits, p.chunks), dim3(kThreads), 0, st, a);
+}
+
+bool divides(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+template <int kType>
+cudaError_t fwd_of_type(const GnArgs &a, int *launches, cudaStream_t st)
+{
+    constexpr int kV = GnTypes<kType>::kWide, kY = Elem<GnTypes<kType>::kY>::kSize;
+    const bool wide = a.c % kV == 0 && a.x_stride % kV == 0 && a.y_stride % kV == 0 && divides(a.x, 16) && divides(a.y, kV * kY) &&
+                      divides(a.codes_out, kV);
+    return wide ? run_fwd<kType, kV>(a, launches, st) : run_fwd<kType, 1>(a, launches, st);
+}
+
+template <int kType>
+cudaError_t bwd_of_type(const GnArgs &a, int *launches, cudaStream_t st)
+{
+    constexpr int kV = GnTypes<kType>::kWide, kY = Elem<GnTypes<kType>::kY>::kSize;
+    const bool wide = a.c % kV == 0 && a.dy_stride % kV == 0 && a.dx_stride % kV == 0 && (!a.x || a.x_stride % kV == 0) && divides(a.x, 16) &&
+                      divides(a.codes, kV) && divides(a.dy, kV * kY) && divides(a.dx, 16);
+    if (a.codes) return wide ? run_bwd<kType, kV, true>(a, launches, st) : run_bwd<kType, 1, true>(a, launches, st);
+    return wide ? run_bwd<kType, kV, false>(a, launches, st) : run_bwd<kType, 1, false>(a, launches, st);
+}
+
+}  // namespace
+
+// [partial sums][means of the backward pass, or the statistics of a call that keeps none]
+size_t gn_workspace_bytes(const eoq_gn_desc_t &d)
+{
+    return parts_bytes(d.n, d.hw, d.c, d.dtype) + sizeof(float2) * (size_t)d.n * d.groups;
+}
+
+static void place(GnArgs &a, int dtype, void *workspace)
+{
+    a.part = reinterpret_cast<float2 *>(workspace);
+    a.means = reinterpret_cast<float2 *>(reinterpret_cast<char *>(workspace) + parts_bytes(a.n, a.hw, a.c, dtype));
+}
+
+cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st)
+{
+    place(a, dtype, workspace);
+    if (!a.stats) a.stats = a.means;
+    switch (dtype) {
+        case EOQ_F32: return fwd_of_type<EOQ_F32>(a, launches, st);
+        case EOQ_F16: return fwd_of_type<EOQ_F16>(a, launches, st);
+        case EOQ_BF16: return fwd_of_type<EOQ_BF16>(a, launches, st);
+        default: return fwd_of_type<EOQ_I32>(a, launches, st);
+    }
+}
+
+cudaError_t launch_gn_bwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st)
+{
+    place(a, dtype, workspace);
+    switch (dtype) {
+        case EOQ_F32: return bwd_of_type<EOQ_F32>(a, launches, st);
+        case EOQ_F16: return bwd_of_type<EOQ_F16>(a, launches, st);
+        case EOQ_BF16: return bwd_of_type<EOQ_BF16>(a, launches, st);
+        default: return bwd_of_type<EOQ_I32>(a, launches, st);
+    }
+}
+
+}  // namespace eoq

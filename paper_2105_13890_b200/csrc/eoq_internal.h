@@ -521,6 +521,37 @@ cudaError_t launch_bn_bwd(const int8_t *e, const int32_t *e_exp, const uint8_t *
                           int c, const float *gamma, BnChannel *ch, float *da, float *dgamma, float *dbeta, int sm_count,
                           cudaStream_t st);
 
+// Activations in 8 bits (eoq_ckpt.cu) and group normalisation (eoq_gn.cu)
+constexpr int kBlock8 = EOQ_CKPT_BLOCK;
+cudaError_t launch_ckpt_save(const void *src, int dtype, int src_exp, size_t rows, int cols, size_t stride, int8_t *codes, uint8_t *exps,
+                             DeviceState *dev, int sm_count, cudaStream_t st);
+cudaError_t launch_ckpt_load(const int8_t *codes, const uint8_t *exps, size_t rows, int cols, void *dst, int dtype, size_t stride,
+                             DeviceState *dev, int sm_count, cudaStream_t st);
+
+// One call of eoq_gn_fwd or eoq_gn_bwd; the fields of the second group are filled in by its launcher.
+struct GnArgs {
+    const void *x, *dy;
+    void *y, *dx;
+    const float *gamma, *beta;          // or null
+    float2 *stats;                      // mean, rstd of (sample, group); forward: written
+    int8_t *codes_out;
+    uint8_t *exps_out;
+    const int8_t *codes;
+    const uint8_t *exps;
+    const int32_t *dy_exp;
+    float *dgamma, *dbeta;
+    DeviceState *dev;
+    size_t x_stride, y_stride, dy_stride, dx_stride;
+    float eps, x_scale;                 // x_scale: 2^x_exp of int32 sums
+    int n, hw, c, groups, cpg, act, blocks, x_exp, sm_count;   // cpg: channels of a group; blocks: of a pixel's 8-bit form
+
+    float2 *part, *means;               // workspace
+    int cv, slots, splits, per_split;   // lanes of a chunk of channels, pixels at a time, pixel ranges of a sample, pixels of a range
+};
+size_t gn_workspace_bytes(const eoq_gn_desc_t &d);
+cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
+cudaError_t launch_gn_bwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
+
 cudaError_t launch_scalar_update(const ScalarBatch &b, int32_t lr_mant, int32_t lr_exp, int stochastic, uint64_t seed,
                                  const unsigned long long *step_dev, uint64_t step, cudaStream_t st);
 

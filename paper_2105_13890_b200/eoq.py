@@ -22,6 +22,9 @@ EOQ_OK, EOQ_ERR_BAD_ARG, EOQ_ERR_ALIGNMENT, EOQ_ERR_UNSUPPORTED, EOQ_ERR_WORKSPA
 EOQ_DEV_TIMEOUT, EOQ_DEV_NONFINITE, EOQ_DEV_SQ_ZERO, EOQ_DEV_RANGE = 1, 2, 4, 8
 EOQ_Q, EOQ_CQ, EOQ_SQ = 0, 1, 2
 EOQ_ROUND_RNE, EOQ_ROUND_STOCHASTIC = 0, 1
+EOQ_F32, EOQ_F16, EOQ_BF16, EOQ_I32 = range(4)
+EOQ_ACT_NONE, EOQ_ACT_RELU, EOQ_ACT_SILU = range(3)
+EOQ_CKPT_BLOCK = 32
 EOQ_PASS_FWD, EOQ_PASS_DGRAD, EOQ_PASS_WGRAD = 0, 1, 2
 
 EXPORTS = [
@@ -31,6 +34,7 @@ EXPORTS = [
     "eoq_conv_dgrad_static", "eoq_conv_fwd_dev", "eoq_weight_prep_size", "eoq_weight_prep", "eoq_conv_wgrad_dev",
     "eoq_err_prescale_dev", "eoq_update_dev", "eoq_update_part", "eoq_describe_plan", "eoq_debug_force_wait_timeout", "eoq_probe_mma_i8", "eoq_profile_gemm_only", "eoq_aux_maxpool_fwd", "eoq_aux_maxpool_bwd",
     "eoq_aux_maxpool_bwd_head", "eoq_aux_avgpool_sum", "eoq_aux_join", "eoq_aux_join_head", "eoq_conv_dgrad_head", "eoq_conv_dgrad_join_head", "eoq_conv_wgrad_gemm", "eoq_wgrad_finish", "eoq_aux_head_workspace_size", "eoq_aux_head", "eoq_aux_head_update", "eoq_aux_head_error", "eoq_aux_scalar_update", "eoq_update_wide", "eoq_set_reduce_hook", "eoq_bn_workspace_size", "eoq_bn_fwd", "eoq_bn_bwd",
+    "eoq_ckpt_save", "eoq_ckpt_load", "eoq_gn_workspace_size", "eoq_gn_fwd", "eoq_gn_bwd",
 ]
 EOQ_STATIC_SCRATCH_BYTES = 16 << 20
 EOQ_PROF_IGEMM_FWD, EOQ_PROF_IGEMM_DGRAD, EOQ_PROF_WGRAD = 0, 1, 2
@@ -59,6 +63,15 @@ class eoq_conv_desc_t(C.Structure):
 
 def conv_desc(n, h, w, c_in, c_out, kh, kw, stride=1, pad=0, x_wmargin=0) -> eoq_conv_desc_t:
     return eoq_conv_desc_t(n, h, w, c_in, c_out, kh, kw, stride, pad, x_wmargin)
+
+
+class eoq_gn_desc_t(C.Structure):
+    _fields_ = [(k, C.c_int) for k in ("n", "hw", "c", "groups", "dtype", "x_exp", "act")] + [("eps", C.c_float)] + \
+               [(k, C.c_size_t) for k in ("x_stride", "y_stride", "dy_stride", "dx_stride")]
+
+
+def gn_desc(n, hw, c, groups, dtype, act=EOQ_ACT_NONE, eps=1e-5, x_exp=0, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0) -> eoq_gn_desc_t:
+    return eoq_gn_desc_t(n, hw, c, groups, dtype, x_exp, act, eps, x_stride, y_stride, dy_stride, dx_stride)
 
 
 _lib = None
@@ -132,6 +145,12 @@ def lib() -> C.CDLL:
         L.eoq_bn_workspace_size.argtypes = [ci, C.POINTER(sz)]
         L.eoq_bn_fwd.argtypes = [vp, vp, ci, sz, ci, vp, vp, C.c_float, vp, vp, vp, sz, vp]
         L.eoq_bn_bwd.argtypes = [vp, vp, vp, vp, vp, ci, sz, ci, vp, vp, sz, vp, vp, vp, vp]
+        gp = C.POINTER(eoq_gn_desc_t)
+        L.eoq_ckpt_save.argtypes = [vp, vp, ci, ci, sz, ci, sz, vp, vp, vp]
+        L.eoq_ckpt_load.argtypes = [vp, vp, vp, sz, ci, vp, ci, sz, vp]
+        L.eoq_gn_workspace_size.argtypes = [gp, C.POINTER(sz)]
+        L.eoq_gn_fwd.argtypes = [vp, gp] + [vp] * 8 + [sz, vp]
+        L.eoq_gn_bwd.argtypes = [vp, gp] + [vp] * 12 + [sz, vp]
         L.eoq_profile_gemm_only.argtypes = [vp, C.c_int]
         L.eoq_probe_mma_i8.argtypes = [vp, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_double), vp]
         L.eoq_status_string.argtypes = [C.c_int]
@@ -469,6 +488,44 @@ def eoq_bn_bwd(handle, e, e_exp, relu_mask, acc, acc_exp, pixels, c, gamma, work
     _check(lib().eoq_bn_bwd(handle, _ptr(e), _ptr(e_exp), _ptr(relu_mask), _ptr(acc), acc_exp, int(pixels), c, _ptr(gamma),
                             _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(da), _ptr(dgamma), _ptr(dbeta),
                             _stream(stream)), "eoq_bn_bwd")
+
+
+# ------------------------------------------------------------------------------- activations in 8 bits, group normalisation
+
+def eoq_ckpt_save(handle, src, dtype, src_exp, rows, cols, stride, codes, exps, stream=None, check: bool = True) -> int:
+    st = (_native or native()).ckpt_save(handle, src, dtype, src_exp, rows, cols, stride, codes, exps, _stream(stream))
+    if check:
+        _check(st, "eoq_ckpt_save")
+    return st
+
+
+def eoq_ckpt_load(handle, codes, exps, rows, cols, dst, dtype, stride, stream=None, check: bool = True) -> int:
+    st = (_native or native()).ckpt_load(handle, codes, exps, rows, cols, dst, dtype, stride, _stream(stream))
+    if check:
+        _check(st, "eoq_ckpt_load")
+    return st
+
+
+def eoq_gn_workspace_size(desc: eoq_gn_desc_t) -> int:
+    out = C.c_size_t(0)
+    _check(lib().eoq_gn_workspace_size(C.byref(desc), C.byref(out)), "eoq_gn_workspace_size")
+    return out.value
+
+
+def eoq_gn_fwd(handle, desc, x, gamma, beta, y, stats=None, codes=None, exps=None, workspace=None, stream=None, check: bool = True) -> int:
+    st = (_native or native()).gn_fwd(handle, desc, x, gamma, beta, y, stats, codes, exps, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_gn_fwd")
+    return st
+
+
+def eoq_gn_bwd(handle, desc, dy, dy_exp, x, codes, exps, gamma, beta, stats, dx, dgamma=None, dbeta=None, workspace=None, stream=None,
+               check: bool = True) -> int:
+    st = (_native or native()).gn_bwd(handle, desc, dy, dy_exp, x, codes, exps, gamma, beta, stats, dx, dgamma, dbeta, workspace,
+                                      _stream(stream))
+    if check:
+        _check(st, "eoq_gn_bwd")
+    return st
 
 
 def eoq_aux_avgpool_sum(handle, x, n, hw, c, sums, stream=None) -> None:
