@@ -439,6 +439,24 @@ EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_
                   size_t stride, void *stream);
 
 /*
+ * Weight gradient of a linear layer (a 1x1 convolution) whose input was kept in 8 bits:
+ *   dw[o][i] = sum over r of dy[r][o] * code[r][i] * 2^(s[r][i / 32] - 127).
+ * device in : dy [rows][dy_stride] (dtype EOQ_F32, EOQ_F16 or EOQ_BF16; dy_stride >= c_out elements, 0 = c_out); codes
+ *             [rows][c_in] and exps as eoq_ckpt_save wrote them.
+ * device out: dw fp32 [c_out][c_in], 16-byte aligned.
+ * Every product is exact (dy in two or three bf16 parts where its type has more bits), sums are fp32, in an order that depends on the
+ * sizes alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
+ * workspace: eoq_ckpt_wgrad_workspace_size() bytes (may be 0), 256-byte aligned; nothing is kept in it between calls.
+ * eoq_set_gemm_ctas does not apply.  16-byte aligned tensors with c_out a multiple of 8, c_in of 16 and dy_stride of 16 bytes run
+ * several times faster.
+ * Errors: BAD_ARG (null pointer, non-positive size, dy_stride < c_out, unknown type, the handle's device not the current one),
+ * ALIGNMENT, UNSUPPORTED (rows > 2^36, c_out or c_in > 2^20), WORKSPACE.
+ */
+EOQ_API int eoq_ckpt_wgrad_workspace_size(size_t rows, int c_out, int c_in, int dtype, size_t *bytes);
+EOQ_API int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_t rows, int c_out, size_t dy_stride, const int8_t *codes,
+                   const uint8_t *exps, int c_in, float *dw, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Group normalisation with an activation, channels last: the normalisation beside eoq_bn_* that does not look over the batch
  * (Sec. 5.3 compares with the one that does; small-batch training has no batch to look over).  Per sample and group of
  * c / groups neighbouring channels, over all `hw` pixels:

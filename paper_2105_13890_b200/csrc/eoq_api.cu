@@ -2294,6 +2294,53 @@ extern "C" int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uin
     return record(h, launch_ckpt_load(codes, exps, rows, cols, dst, dtype, stride, h->dev, h->sm_count, s));
 }
 
+static int ckpt_wgrad_check(size_t rows, int c_out, int c_in, int dtype)
+{
+    if (rows == 0 || c_out <= 0 || c_in <= 0 || dtype < EOQ_F32 || dtype > EOQ_BF16) return EOQ_ERR_BAD_ARG;
+    // (tiles of 128 x 256 where either is this long: at most 2^25 of them, and splits only below 148)
+    if (rows > (size_t)1 << 36 || c_out > 1 << 20 || c_in > 1 << 20) return EOQ_ERR_UNSUPPORTED;
+    return EOQ_OK;
+}
+
+extern "C" int eoq_ckpt_wgrad_workspace_size(size_t rows, int c_out, int c_in, int dtype, size_t *bytes)
+{
+    if (!bytes) return EOQ_ERR_BAD_ARG;
+    const int chk = ckpt_wgrad_check(rows, c_out, c_in, dtype);
+    if (chk != EOQ_OK) return chk;
+    *bytes = round256(ckpt_wgrad_workspace_bytes(rows, c_out, c_in));
+    return EOQ_OK;
+}
+
+extern "C" int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_t rows, int c_out, size_t dy_stride, const int8_t *codes,
+                              const uint8_t *exps, int c_in, float *dw, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    const int chk = ckpt_wgrad_check(rows, c_out, c_in, dtype);
+    if (chk != EOQ_OK) return chk;
+    if (dy_stride == 0) dy_stride = c_out;
+    if (!dy || !codes || !exps || !dw || dy_stride < (size_t)c_out) return EOQ_ERR_BAD_ARG;
+    if (dy_stride > (size_t)1 << 30) return EOQ_ERR_UNSUPPORTED;
+    if (!aligned_to(dy, dtype_size(dtype)) || !aligned16(dw)) return EOQ_ERR_ALIGNMENT;
+    const size_t need = ckpt_wgrad_workspace_bytes(rows, c_out, c_in);
+    if (need && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need)) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    CkptWgradArgs a = {};
+    a.dy = dy;
+    a.codes = codes;
+    a.exps = exps;
+    a.rows = rows;
+    a.dy_stride = dy_stride;
+    a.c_out = c_out;
+    a.c_in = c_in;
+    a.dev = h->dev;
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    const cudaError_t err = launch_ckpt_wgrad(a, dtype, dw, workspace, &launches, s);
+    count_launches(h, launches);
+    return record(h, err);
+}
+
 // The descriptor of a call with its strides filled in.
 static int gn_check(const eoq_gn_desc_t *desc, eoq_gn_desc_t *d)
 {

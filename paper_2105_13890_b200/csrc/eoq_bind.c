@@ -263,6 +263,22 @@ static PyObject *ckpt_load(PyObject *self, PyObject *const *a, Py_ssize_t n)
                        stream));
 }
 
+static PyObject *ckpt_wgrad(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle dy dtype rows c_out dy_stride | codes exps | c_in | dw workspace stream */
+    void *h, *dy, *p[2], *q[3];
+    long long v[4], c_in;
+    size_t bytes;
+    if (!want(n, 12) || !get_ptr(a[0], &h) || !get_ptr(a[1], &dy) || !get_int(a[8], &c_in) || !get_bytes(a[10], &bytes)) return NULL;
+    for (int i = 0; i < 4; ++i)
+        if (!get_int(a[2 + i], &v[i])) return NULL;
+    PTRS(6, 2);
+    for (int i = 0; i < 3; ++i)
+        if (!get_ptr(a[9 + i], &q[i])) return NULL;
+    CALL(eoq_ckpt_wgrad((eoq_handle_t)h, dy, (int)v[0], (size_t)v[1], (int)v[2], (size_t)v[3], (const int8_t *)p[0], (const uint8_t *)p[1],
+                        (int)c_in, (float *)q[0], q[1], bytes, q[2]));
+}
+
 static int get_gn_desc(PyObject *o, eoq_gn_desc_t *out)
 {
     Py_buffer view;
@@ -300,7 +316,7 @@ static PyObject *gn_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
 
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(conv_fwd_dev), METHOD(conv_dgrad), METHOD(conv_wgrad_dev), METHOD(err_prescale_dev),
-                                METHOD(quantize), METHOD(update_dev), METHOD(weight_prep), METHOD(ckpt_save), METHOD(ckpt_load),
+                                METHOD(quantize), METHOD(update_dev), METHOD(weight_prep), METHOD(ckpt_save), METHOD(ckpt_load), METHOD(ckpt_wgrad),
                                 METHOD(gn_fwd), METHOD(gn_bwd), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_eoqbind", NULL, -1, methods, NULL, NULL, NULL, NULL};
 

@@ -528,6 +528,21 @@ cudaError_t launch_ckpt_save(const void *src, int dtype, int src_exp, size_t row
 cudaError_t launch_ckpt_load(const int8_t *codes, const uint8_t *exps, size_t rows, int cols, void *dst, int dtype, size_t stride,
                              DeviceState *dev, int sm_count, cudaStream_t st);
 
+struct CkptWgradArgs {
+    const void *dy;
+    const int8_t *codes;
+    const uint8_t *exps;
+    size_t rows, dy_stride;
+    int c_out, c_in;
+    DeviceState *dev;
+    // filled in by the launcher
+    float *out;                     // [split][c_out][c_in]
+    size_t rows_per_split;
+    int blocks, m_tiles, n_tiles;   // blocks: of a row of codes
+};
+size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in);
+cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st);
+
 // One call of eoq_gn_fwd or eoq_gn_bwd; the fields of the second group are filled in by its launcher.
 struct GnArgs {
     const void *x, *dy;

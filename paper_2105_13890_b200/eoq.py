@@ -34,7 +34,7 @@ EXPORTS = [
     "eoq_conv_dgrad_static", "eoq_conv_fwd_dev", "eoq_weight_prep_size", "eoq_weight_prep", "eoq_conv_wgrad_dev",
     "eoq_err_prescale_dev", "eoq_update_dev", "eoq_update_part", "eoq_describe_plan", "eoq_debug_force_wait_timeout", "eoq_probe_mma_i8", "eoq_profile_gemm_only", "eoq_aux_maxpool_fwd", "eoq_aux_maxpool_bwd",
     "eoq_aux_maxpool_bwd_head", "eoq_aux_avgpool_sum", "eoq_aux_join", "eoq_aux_join_head", "eoq_conv_dgrad_head", "eoq_conv_dgrad_join_head", "eoq_conv_wgrad_gemm", "eoq_wgrad_finish", "eoq_aux_head_workspace_size", "eoq_aux_head", "eoq_aux_head_update", "eoq_aux_head_error", "eoq_aux_scalar_update", "eoq_update_wide", "eoq_set_reduce_hook", "eoq_bn_workspace_size", "eoq_bn_fwd", "eoq_bn_bwd",
-    "eoq_ckpt_save", "eoq_ckpt_load", "eoq_gn_workspace_size", "eoq_gn_fwd", "eoq_gn_bwd",
+    "eoq_ckpt_save", "eoq_ckpt_load", "eoq_ckpt_wgrad_workspace_size", "eoq_ckpt_wgrad", "eoq_gn_workspace_size", "eoq_gn_fwd", "eoq_gn_bwd",
 ]
 EOQ_STATIC_SCRATCH_BYTES = 16 << 20
 EOQ_PROF_IGEMM_FWD, EOQ_PROF_IGEMM_DGRAD, EOQ_PROF_WGRAD = 0, 1, 2
@@ -148,6 +148,8 @@ def lib() -> C.CDLL:
         gp = C.POINTER(eoq_gn_desc_t)
         L.eoq_ckpt_save.argtypes = [vp, vp, ci, ci, sz, ci, sz, vp, vp, vp]
         L.eoq_ckpt_load.argtypes = [vp, vp, vp, sz, ci, vp, ci, sz, vp]
+        L.eoq_ckpt_wgrad_workspace_size.argtypes = [sz, ci, ci, ci, C.POINTER(sz)]
+        L.eoq_ckpt_wgrad.argtypes = [vp, vp, ci, sz, ci, sz, vp, vp, ci, vp, vp, sz, vp]
         L.eoq_gn_workspace_size.argtypes = [gp, C.POINTER(sz)]
         L.eoq_gn_fwd.argtypes = [vp, gp] + [vp] * 8 + [sz, vp]
         L.eoq_gn_bwd.argtypes = [vp, gp] + [vp] * 12 + [sz, vp]
@@ -503,6 +505,19 @@ def eoq_ckpt_load(handle, codes, exps, rows, cols, dst, dtype, stride, stream=No
     st = (_native or native()).ckpt_load(handle, codes, exps, rows, cols, dst, dtype, stride, _stream(stream))
     if check:
         _check(st, "eoq_ckpt_load")
+    return st
+
+
+def eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, dtype) -> int:
+    out = C.c_size_t(0)
+    _check(lib().eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, dtype, C.byref(out)), "eoq_ckpt_wgrad_workspace_size")
+    return out.value
+
+
+def eoq_ckpt_wgrad(handle, dy, dtype, rows, c_out, dy_stride, codes, exps, c_in, dw, workspace=None, stream=None, check: bool = True) -> int:
+    st = (_native or native()).ckpt_wgrad(handle, dy, dtype, rows, c_out, dy_stride, codes, exps, c_in, dw, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_ckpt_wgrad")
     return st
 
 

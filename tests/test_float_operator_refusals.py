@@ -93,3 +93,19 @@ def test_eight_bit_form():
     assert save(src=At(4097)) == eoq.EOQ_ERR_ALIGNMENT and load(dst=At(4098), dtype=eoq.EOQ_F32) == eoq.EOQ_ERR_ALIGNMENT
     assert save(cols=(1 << 20) + 1, stride=0) == eoq.EOQ_ERR_UNSUPPORTED and save(rows=(1 << 40) + 1) == eoq.EOQ_ERR_UNSUPPORTED
     assert save(src_exp=-14) == eoq.EOQ_ERR_RANGE and save(dtype=eoq.EOQ_I32, src_exp=-61) == eoq.EOQ_ERR_RANGE
+
+
+def test_weight_gradient():
+    def call(dy=A, dtype=eoq.EOQ_BF16, rows=4096, c_out=32, dy_stride=32, codes=A, exps=A, c_in=64, dw=A, ws=A):
+        return eoq.eoq_ckpt_wgrad(0, dy, dtype, rows, c_out, dy_stride, codes, exps, c_in, dw, ws, stream=0, check=False)
+
+    for k in (dict(), dict(dy=None), dict(rows=0), dict(c_out=0), dict(c_in=-1), dict(dy_stride=31), dict(dtype=eoq.EOQ_I32), dict(dtype=-1),
+              dict(codes=None), dict(exps=None), dict(dw=None)):
+        assert call(**k) == eoq.EOQ_ERR_BAD_ARG, k
+    assert call(dy=At(4097)) == eoq.EOQ_ERR_ALIGNMENT and call(dw=At(4100)) == eoq.EOQ_ERR_ALIGNMENT
+    assert call(rows=(1 << 36) + 1) == eoq.EOQ_ERR_UNSUPPORTED and call(c_in=(1 << 20) + 1) == eoq.EOQ_ERR_UNSUPPORTED
+    need = eoq.eoq_ckpt_wgrad_workspace_size(4096, 32, 64, eoq.EOQ_BF16)
+    assert need > 0 and need % 256 == 0
+    assert call(ws=None) == eoq.EOQ_ERR_WORKSPACE and call(ws=At(1 << 12, need // 2)) == eoq.EOQ_ERR_WORKSPACE and call(ws=At(4112)) == eoq.EOQ_ERR_WORKSPACE
+    with pytest.raises(eoq.EoqError):
+        eoq.eoq_ckpt_wgrad_workspace_size(0, 32, 64, eoq.EOQ_BF16)
