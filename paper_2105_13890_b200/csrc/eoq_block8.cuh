@@ -166,14 +166,13 @@ template <> struct Elem<kElemI8> {
         int q[kN];
 #pragma unroll
         for (int i = 0; i < kN; ++i) q[i] = clampi(__float2int_rn(v[i] * 128.0f), -127, 127);
-        if constexpr (kN == 1) {
-            set_word(r, 0, (uint32_t)q[0]);
-            return r;
+        if constexpr (kN < 4) {
+            set_word(r, 0, kN == 1 ? (uint32_t)q[0] : __byte_perm((uint32_t)q[0], (uint32_t)q[kN - 1], 0x0040));
         } else {
 #pragma unroll
             for (int i = 0; i < kN / 4; ++i) set_word(r, i, pack4(q[4 * i], q[4 * i + 1], q[4 * i + 2], q[4 * i + 3]));
-            return r;
         }
+        return r;
     }
 };
 
@@ -198,7 +197,7 @@ __device__ __forceinline__ int block_exp(float amax)
 }
 __device__ __forceinline__ float block_step(int s) { return __uint_as_float((uint32_t)s << 23); }
 
-// the codes of kN values of a block, packed in words (the single code of kN = 1 in the low byte)
+// the codes of kN values of a block, packed in words (one or two codes in the low bytes)
 template <int kN>
 __device__ __forceinline__ void block_codes(const float (&v)[kN], int s, uint32_t (&w)[(kN + 3) / 4])
 {
@@ -212,8 +211,8 @@ __device__ __forceinline__ void block_codes(const float (&v)[kN], int s, uint32_
 #pragma unroll
         for (int i = 0; i < kN; ++i) q[i] = s == 255 ? 0u : (uint32_t)clampi((int)(q[i] - 0x4B400000u), -63, 63);
     }
-    if constexpr (kN == 1) {
-        w[0] = q[0] & 0xffu;
+    if constexpr (kN < 4) {
+        w[0] = kN == 1 ? q[0] : __byte_perm(q[0], q[kN - 1], 0x0040);
     } else {
 #pragma unroll
         for (int i = 0; i < kN / 4; ++i)

@@ -179,56 +179,6 @@ __global__ void __launch_bounds__(kThreads) gn_apply_kernel(const __grid_constan
     if (kSave && bad) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
 }
 
-// What the backward pass reads of a pixel: x or its 8-bit form, and the error.
-template <int kType, int kV, bool kCodes>
-struct GnInput {
-    using Types = GnTypes<kType>;
-    static constexpr int kXB = kCodes ? kV : kV * Elem<kType>::kSize, kDyB = kV * Elem<Types::kY>::kSize;
-    Raw<kXB> x;
-    Raw<kDyB> dy;
-    int s;
-    __device__ __forceinline__ void load(const GnArgs &a, size_t pix, int ch, bool in)
-    {
-        x = zero_raw<kXB>();
-        dy = zero_raw<kDyB>();
-        s = 1;
-        if (!in) return;
-        if (kCodes) {
-            x = load_raw<kXB>(a.codes + pix * a.c + ch);
-            s = __ldg(a.exps + pix * a.blocks + ch / kBlock8);
-        } else {
-            x = load_raw<kXB>(reinterpret_cast<const char *>(a.x) + (pix * a.x_stride + ch) * Elem<kType>::kSize);
-        }
-        dy = load_raw<kDyB>(reinterpret_cast<const char *>(a.dy) + (pix * a.dy_stride + ch) * Elem<Types::kY>::kSize);
-    }
-    // u = (x - mean) rstd and dz = dy act'(gamma u + beta)
-    __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&mean)[kV], const float (&gamma)[kV],
-                                           const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
-    {
-        float z[kV];
-        if constexpr (kCodes) block_values<kV>(x, s, u);
-        else x_values<kType, kV>(x, a.x_scale, u);
-        Elem<Types::kY>::to_f32(dy, dz);
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            u[i] = (u[i] - mean[i]) * rstd[i];
-            z[i] = __fmaf_rn(u[i], gamma[i], beta[i]);
-            if (kType == EOQ_I32) dz[i] *= dy_scale;
-        }
-        times_slope(dz, z, a.act);
-    }
-};
-
-// 2^*dy_exp of int8 errors
-template <int kType>
-__device__ __forceinline__ float error_scale(const GnArgs &a)
-{
-    if (kType != EOQ_I32) return 1.0f;
-    const int e = *a.dy_exp;
-    if ((e < -120 || e > 120) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(&a.dev->status, EOQ_DEV_RANGE);
-    return ldexpf(1.0f, clampi(e, -120, 120));
-}
-
 template <int kType, int kV, bool kCodes>
 __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_constant__ GnArgs a)
 {
@@ -251,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
         const float dy_scale = error_scale<kType>(a);
         const size_t pix0 = (size_t)smp * a.hw;
         for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-            GnInput<kType, kV, kCodes> in[kUnroll];
+            GnInput<kType, kV, kCodes, false> in[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
@@ -356,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
     const float dy_scale = error_scale<kType>(a);
     const size_t pix0 = (size_t)smp * a.hw;
     for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-        GnInput<kType, kV, kCodes> in[kUnroll];
+        GnInput<kType, kV, kCodes, false> in[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
@@ -458,14 +408,12 @@ cudaError_t run_bwd(GnArgs a, int *launches, cudaStream_t st)
     return launch_chained(gn_bwd_apply_kernel<kType, kV, kCodes>, dim3(a.n * p.splits, p.chunks), dim3(kThreads), 0, st, a);
 }
 
-bool divides(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
 template <int kType>
 cudaError_t fwd_of_type(const GnArgs &a, int *launches, cudaStream_t st)
 {
     constexpr int kV = GnTypes<kType>::kWide, kY = Elem<GnTypes<kType>::kY>::kSize;
-    const bool wide = a.c % kV == 0 && a.x_stride % kV == 0 && a.y_stride % kV == 0 && divides(a.x, 16) && divides(a.y, kV * kY) &&
-                      divides(a.codes_out, kV);
+    const bool wide = a.c % kV == 0 && a.x_stride % kV == 0 && a.y_stride % kV == 0 && aligned_at(a.x, 16) && aligned_at(a.y, kV * kY) &&
+                      aligned_at(a.codes_out, kV);
     return wide ? run_fwd<kType, kV>(a, launches, st) : run_fwd<kType, 1>(a, launches, st);
 }
 
@@ -473,13 +421,19 @@ template <int kType>
 cudaError_t bwd_of_type(const GnArgs &a, int *launches, cudaStream_t st)
 {
     constexpr int kV = GnTypes<kType>::kWide, kY = Elem<GnTypes<kType>::kY>::kSize;
-    const bool wide = a.c % kV == 0 && a.dy_stride % kV == 0 && a.dx_stride % kV == 0 && (!a.x || a.x_stride % kV == 0) && divides(a.x, 16) &&
-                      divides(a.codes, kV) && divides(a.dy, kV * kY) && divides(a.dx, 16);
+    const bool wide = a.c % kV == 0 && a.dy_stride % kV == 0 && a.dx_stride % kV == 0 && (!a.x || a.x_stride % kV == 0) && aligned_at(a.x, 16) &&
+                      aligned_at(a.codes, kV) && aligned_at(a.dy, kV * kY) && aligned_at(a.dx, 16);
     if (a.codes) return wide ? run_bwd<kType, kV, true>(a, launches, st) : run_bwd<kType, 1, true>(a, launches, st);
     return wide ? run_bwd<kType, kV, false>(a, launches, st) : run_bwd<kType, 1, false>(a, launches, st);
 }
 
 }  // namespace
+
+cudaError_t launch_gn_channel_sums(GnArgs a, cudaStream_t st)
+{
+    a.splits = 1;
+    return launch_chained(gn_bwd_join_kernel, dim3((a.c + 31) / 32), dim3(kThreads), 0, st, a, 0);
+}
 
 // [partial sums][means of the backward pass, or the statistics of a call that keeps none]
 size_t gn_workspace_bytes(const eoq_gn_desc_t &d)
@@ -496,6 +450,8 @@ static void place(GnArgs &a, int dtype, void *workspace)
 cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st)
 {
     place(a, dtype, workspace);
+    cudaError_t e;
+    if (gn_fused_fwd(a, dtype, &e, launches, st)) return e;
     if (!a.stats) a.stats = a.means;
     switch (dtype) {
         case EOQ_F32: return fwd_of_type<EOQ_F32>(a, launches, st);
@@ -508,6 +464,8 @@ cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, c
 cudaError_t launch_gn_bwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st)
 {
     place(a, dtype, workspace);
+    cudaError_t e;
+    if (gn_fused_bwd(a, dtype, &e, launches, st)) return e;
     switch (dtype) {
         case EOQ_F32: return bwd_of_type<EOQ_F32>(a, launches, st);
         case EOQ_F16: return bwd_of_type<EOQ_F16>(a, launches, st);

@@ -562,8 +562,14 @@ struct GnArgs {
 
     float2 *part, *means;               // workspace
     int cv, slots, splits, per_split;   // lanes of a chunk of channels, pixels at a time, pixel ranges of a sample, pixels of a range
+    // the one-pass kernels: chunks of channels, blocks of a cluster, of them those of a sample, vectors of a thread
+    int chunks, cluster, ranks, vecs;
 };
 size_t gn_workspace_bytes(const eoq_gn_desc_t &d);
+cudaError_t launch_gn_channel_sums(GnArgs a, cudaStream_t st);   // dgamma, dbeta from part [n][c]
+// The forms that read every element once (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu); false when a sample's chunk of groups does not fit.
+bool gn_fused_fwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
+bool gn_fused_bwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
 cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
 cudaError_t launch_gn_bwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
 

@@ -103,6 +103,17 @@ def test_shapes_and_types(n, hw, c, groups, extra, name):
         check(x, dy, gamma, beta, c, groups, name, "silu", kept)
 
 
+@pytest.mark.parametrize("name", sorted(TYPES))
+@pytest.mark.parametrize("n,hw,c,groups,extra", [(1, 40000, 64, 1, 0), (1, 25000, 96, 1, 1), (2, 3000, 301, 1, 0), (1, 30, 4096, 2, 0), (2, 1500, 22, 2, 0),
+                                                 (2, 1500, 22, 1, 4), (8, 20, 64, 8, 0), (5, 64, 24, 3, 0), (9, 700, 32, 4, 0), (1, 9, 32, 2, 0),
+                                                 (1, 6000, 256, 1, 0), (3, 4000, 24, 8, 0), (2, 12544, 64, 16, 0)])
+def test_groups_of_every_size(n, hw, c, groups, extra, name):
+    """Groups that stay on one SM, on a cluster's, on none; pairs of channels; samples that share a cluster and that do not."""
+    x, dy, gamma, beta = make(n, hw, c, extra, name, n * 37 + hw * 7 + c)
+    for kept in ("input", "codes"):
+        check(x, dy, gamma, beta, c, groups, name, "silu", kept)
+
+
 @pytest.mark.parametrize("kind", ["none", "relu"])
 @pytest.mark.parametrize("n,hw,c,groups,extra", [(2, 50, 64, 8, 0), (3, 45, 120, 8, 24), (2, 61, 35, 5, 3), (1, 12000, 64, 32, 0)])
 def test_activations_and_missing_parameters(n, hw, c, groups, extra, kind):
