@@ -188,12 +188,12 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
     if (slot < a.slots && ch < a.c) {
-        float rstd[kV], mean[kV], gamma[kV], beta[kV], s0[kV], s1[kV];
+        float rstd[kV], off[kV], gamma[kV], beta[kV], s0[kV], s1[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
             rstd[i] = st.y;
-            mean[i] = st.x;
+            off[i] = -st.x * st.y;
             gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
             beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
             s0[i] = s1[i] = 0.0f;
@@ -201,14 +201,14 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
         const float dy_scale = error_scale<kType>(a);
         const size_t pix0 = (size_t)smp * a.hw;
         for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-            GnInput<kType, kV, kCodes, false> in[kUnroll];
+            GnInput<kType, kV, kCodes> in[kUnroll];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
             for (int k = 0; k < kUnroll; ++k) {
                 if (p0 + k * a.slots >= p_end) break;
                 float u[kV], dz[kV];
-                in[k].values(a, rstd, mean, gamma, beta, dy_scale, u, dz);
+                in[k].values(a, rstd, off, gamma, beta, dy_scale, u, dz);
 #pragma unroll
                 for (int i = 0; i < kV; ++i) {
                     s0[i] += dz[i];
@@ -291,13 +291,13 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     if (slot >= a.slots || ch >= a.c) return;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
-    float rstd[kV], mean[kV], gamma[kV], beta[kV], k0[kV], k1[kV];
+    float rstd[kV], off[kV], gamma[kV], beta[kV], k0[kV], k1[kV];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
         const size_t g = (size_t)smp * a.groups + (ch + i) / a.cpg;
         const float2 st = a.stats[g], m = a.means[g];
         rstd[i] = st.y;
-        mean[i] = st.x;
+        off[i] = -st.x * st.y;
         gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
         beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
         k0[i] = -st.y * m.x;
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
     const float dy_scale = error_scale<kType>(a);
     const size_t pix0 = (size_t)smp * a.hw;
     for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-        GnInput<kType, kV, kCodes, false> in[kUnroll];
+        GnInput<kType, kV, kCodes> in[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
             const int p = p0 + k * a.slots;
             if (p >= p_end) break;
             float u[kV], dz[kV];
-            in[k].values(a, rstd, mean, gamma, beta, dy_scale, u, dz);
+            in[k].values(a, rstd, off, gamma, beta, dy_scale, u, dz);
 #pragma unroll
             for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i] * gamma[i], rstd[i], __fmaf_rn(u[i], k1[i], k0[i]));
             store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,

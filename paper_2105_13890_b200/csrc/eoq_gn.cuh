@@ -12,8 +12,64 @@ template <> struct GnTypes<EOQ_I32> {
     static constexpr int kY = kElemI8, kDx = EOQ_F32, kWide = 4;
 };
 
-// x / (1 + exp(-x)); the slope of it below.  (An exp that overflows leaves 0, as the limit does.)
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// Two fp32 operations in one instruction (each rounded as by itself): these kernels have more to compute per byte than the memory's
+// rate leaves issue slots for one by one.
+struct Pair {
+    float x, y;
+};
+__device__ __forceinline__ Pair operator+(Pair a, Pair b)
+{
+    Pair r;
+    asm("{\n\t.reg .b64 a, b, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 r, a, b;\n\tmov.b64 {%0, %1}, r;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b)
+{
+    Pair r;
+    asm("{\n\t.reg .b64 a, b, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 r, a, b;\n\tmov.b64 {%0, %1}, r;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("{\n\t.reg .b64 a, b, c, r;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 r, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, r;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ Pair both(float v) { return {v, v}; }
+// elements 2 i and 2 i + 1 (of a single element: itself twice)
+template <int kN>
+__device__ __forceinline__ Pair pair_of(const float (&v)[kN], int i) { return {v[2 * i], v[kN == 1 ? 0 : 2 * i + 1]}; }
+template <int kN>
+__device__ __forceinline__ void set_pair(float (&v)[kN], int i, Pair p)
+{
+    v[2 * i] = p.x;
+    if (kN > 1) v[kN == 1 ? 0 : 2 * i + 1] = p.y;
+}
+template <int kN> constexpr int kPairs = (kN + 1) / 2;
+
+__device__ __forceinline__ float ex2_approx(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float v)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// 1 / (1 + exp(-z)); an exp that overflows leaves 0, as the limit does.
+__device__ __forceinline__ Pair sigmoid2(Pair z)
+{
+    const Pair t = z * both(-1.44269504f);
+    const Pair a = Pair{ex2_approx(t.x), ex2_approx(t.y)} + both(1.0f);
+    return Pair{rcp_approx(a.x), rcp_approx(a.y)};
+}
 
 template <int kN>
 __device__ __forceinline__ void activate(float (&z)[kN], int act)
@@ -23,7 +79,10 @@ __device__ __forceinline__ void activate(float (&z)[kN], int act)
         for (int i = 0; i < kN; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];   // (a NaN stays one)
     } else if (act == EOQ_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) z[i] *= sigmoid(z[i]);
+        for (int i = 0; i < kPairs<kN>; ++i) {
+            const Pair v = pair_of(z, i), q = sigmoid2(v);
+            set_pair(z, i, v * q);
+        }
     }
 }
 
@@ -36,9 +95,9 @@ __device__ __forceinline__ void times_slope(float (&e)[kN], const float (&z)[kN]
         for (int i = 0; i < kN; ++i) e[i] = z[i] > 0.0f ? e[i] : z[i] != z[i] ? z[i] : 0.0f;
     } else if (act == EOQ_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float q = sigmoid(z[i]);
-            e[i] *= q * __fmaf_rn(z[i], 1.0f - q, 1.0f);
+        for (int i = 0; i < kPairs<kN>; ++i) {
+            const Pair v = pair_of(z, i), q = sigmoid2(v);
+            set_pair(e, i, pair_of(e, i) * (q * fma2(v, fma2(q, both(-1.0f), both(1.0f)), both(1.0f))));
         }
     }
 }
@@ -54,27 +113,38 @@ __device__ __forceinline__ void x_values(const Raw<kN * Elem<kType>::kSize> &r, 
 }
 
 // u = (x - mean) rstd and dz = dy act'(gamma u + beta) of kN neighbouring channels; x from the kept tensor, or from its 8-bit form with
-// the byte s of their block.  kUni: the channels are of one group, whose mean and rstd come first in their arrays.
-template <int kType, int kN, bool kCodes, bool kUni>
+// the byte s of their block.  Of kW neighbouring channels all are of one group: mean and rstd come once for each kW.  off = -mean rstd:
+// the step of the 8-bit form goes into the factor of u (a power of two, so exactly).
+template <int kType, int kN, bool kCodes, int kW>
 __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType>::kSize> &x, int s, const Raw<kN * Elem<GnTypes<kType>::kY>::kSize> &dy,
-                                         float x_scale, float dy_scale, int act, const float *mean, const float *rstd, const float (&gamma)[kN],
-                                         const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
+                                         float x_scale, float dy_scale, int act, const float (&off)[kN / kW], const float (&rstd)[kN / kW],
+                                         const float (&gamma)[kN], const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
 {
     float z[kN];
-    if constexpr (kCodes) block_values<kN>(x, s, u);
-    else x_values<kType, kN>(x, x_scale, u);
-    Elem<GnTypes<kType>::kY>::to_f32(dy, dz);
+    if constexpr (kCodes) {
+        // 2^23 + (code + 128) is a float whose bits are put together from the byte
 #pragma unroll
-    for (int i = 0; i < kN; ++i) {
-        u[i] = (u[i] - mean[kUni ? 0 : i]) * rstd[kUni ? 0 : i];
-        z[i] = __fmaf_rn(u[i], gamma[i], beta[i]);
-        if (kType == EOQ_I32) dz[i] *= dy_scale;
+        for (int i = 0; i < kN; ++i) u[i] = __uint_as_float(__byte_perm(raw_word(x, i / 4) ^ 0x80808080u, 0x4B000000u, 0x7650 + (i & 3)));
+#pragma unroll
+        for (int i = 0; i < kPairs<kN>; ++i) set_pair(u, i, pair_of(u, i) + both(-8388736.0f));
+    } else {
+        Elem<kType>::to_f32(x, u);
+    }
+    Elem<GnTypes<kType>::kY>::to_f32(dy, dz);
+    const float scale = kCodes ? block_step(s) : kType == EOQ_I32 ? x_scale : 1.0f;
+#pragma unroll
+    for (int i = 0; i < kPairs<kN>; ++i) {
+        const int j = 2 * i / kW, k = kN == 1 ? 0 : (2 * i + 1) / kW;
+        const Pair v = fma2(pair_of(u, i), Pair{rstd[j] * scale, rstd[k] * scale}, Pair{off[j], off[k]});
+        set_pair(u, i, v);
+        set_pair(z, i, fma2(v, pair_of(gamma, i), pair_of(beta, i)));
+        if (kType == EOQ_I32) set_pair(dz, i, pair_of(dz, i) * both(dy_scale));
     }
     times_slope(dz, z, act);
 }
 
 // What the backward pass reads of a pixel: x or its 8-bit form, and the error.
-template <int kType, int kV, bool kCodes, bool kUni>
+template <int kType, int kV, bool kCodes>
 struct GnInput {
     using Types = GnTypes<kType>;
     static constexpr int kXB = kCodes ? kV : kV * Elem<kType>::kSize, kDyB = kV * Elem<Types::kY>::kSize;
@@ -95,10 +165,10 @@ struct GnInput {
         }
         dy = load_raw<kDyB>(reinterpret_cast<const char *>(a.dy) + (pix * a.dy_stride + ch) * Elem<Types::kY>::kSize);
     }
-    __device__ __forceinline__ void values(const GnArgs &a, const float *rstd, const float *mean, const float (&gamma)[kV],
+    __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&off)[kV], const float (&gamma)[kV],
                                            const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
     {
-        gn_terms<kType, kV, kCodes, kUni>(x, s, dy, a.x_scale, dy_scale, a.act, mean, rstd, gamma, beta, u, dz);
+        gn_terms<kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
     }
 };
 

@@ -1,148 +1,192 @@
-// Group normalisation forward, every element read once (eoq_gn_fwd): see eoq_gn_fused.cuh for how the data stays on the chip.
-// Mean and squares about it come from two looks at the kept vectors, joined as (count, mean, squares), so a mean far from zero costs
-// no digits and a group of equal values has exactly that value as its mean.
+// Group normalisation forward in one launch (eoq_gn_fwd): see eoq_gn_fused.cuh for how a sample is dealt out.
+// Batches of a thread's vectors give their mean and the squares about it; (count, mean, squares) are joined pairwise, so a mean far from
+// zero costs no digits, and a group of equal values has exactly that value as its mean.
+#include <type_traits>
+
 #include "eoq_gn_fused.cuh"
 
 namespace eoq {
 
 namespace {
 
-// shared memory behind the vectors: cells of the threads, (mean, squares) of the block's groups, (mean, rstd), gamma, beta
-template <int kV, bool kUni>
+// shared memory: cells of the threads, (mean, squares) of every block of the cluster, (mean, rstd), gamma, beta
+template <int kV, int kW>
 struct FwdLayout {
-    static constexpr int kCells = kGnThreads * (kUni ? 1 : kV);
-    // (a group has at least one channel)
-    __host__ __device__ static size_t bytes(int cv) { return sizeof(float2) * (kCells + 3 * (size_t)cv * kV); }
+    static constexpr int kCells = kGnThreads * (kV / kW);
+    __host__ __device__ static size_t bytes(int cv, int groups) { return sizeof(float2) * (kCells + (8 + 1) * (size_t)groups + (size_t)cv * kV); }
 };
 
-template <int kType, int kV, bool kUni, bool kSave>
+// kW: so many neighbouring channels of a vector are always of one group (the common divisor of both widths)
+template <int kType, int kV, int kW, bool kSave, bool kKeep>
 __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __grid_constant__ GnArgs a)
 {
     using Types = GnTypes<kType>;
-    constexpr int kE = Elem<kType>::kSize, kB = kV * kE, kLanes = kBlock8 / kV, kG = kUni ? 1 : kV;
+    constexpr int kE = Elem<kType>::kSize, kB = kV * kE, kLanes = kBlock8 / kV, kG = kV / kW;
     extern __shared__ __align__(16) uint8_t smem[];
-    const OwnVectors<kB> own(smem);
-    const int width = a.cv * kV;   // channels of a chunk
-    float2 *cell = reinterpret_cast<float2 *>(smem + (size_t)a.vecs * kGnThreads * kB);
-    float2 *mine = cell + FwdLayout<kV, kUni>::kCells, *final = mine + width;
-    float *gamma = reinterpret_cast<float *>(final + width), *beta = gamma + width;
+    const int width = a.cv * kV, most = a.by_cpg(width);   // channels and groups of a chunk (the last one may have fewer)
+    float2 *cell = reinterpret_cast<float2 *>(smem + (kKeep ? (size_t)a.vecs * kGnThreads * kB : 0));
+    float2 *parts = cell + FwdLayout<kV, kW>::kCells, *final = parts + 8 * most;   // parts [rank][group]
+    float *gamma = reinterpret_cast<float *>(final + most), *beta = gamma + width;
 
-    const int rank = blockIdx.x % a.ranks, id = blockIdx.x / a.ranks, chunk = id % a.chunks, smp = id / a.chunks;
-    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch0 = chunk * width, ch = ch0 + cv * kV;
-    const int per = (a.hw + a.ranks - 1) / a.ranks, p_begin = min(rank * per, a.hw), pixels = min(a.hw, p_begin + per) - p_begin;
-    const int channels = min(width, a.c - ch0), groups = channels / a.cpg;
-    const int vecs = slot < a.slots && ch < a.c && slot < pixels ? (pixels - slot + a.slots - 1) / a.slots : 0;   // of this thread
+    const int id = a.by_ranks(blockIdx.x), rank = blockIdx.x - id * a.ranks, smp = a.by_chunks(id), chunk = id - smp * a.chunks;
+    const int slot = a.by_cv(threadIdx.x), cv = threadIdx.x - slot * a.cv, ch0 = chunk * width, ch = ch0 + cv * kV;
+    const int per = a.per, p_begin = min(rank * per, a.hw), pixels = min(a.hw, p_begin + per) - p_begin;
+    const int channels = min(width, a.c - ch0), groups = a.by_cpg(channels);
+    const int full = a.by_slots(pixels), more = pixels - full * a.slots;   // slot j has `full` pixels, the first `more` one more
+    const bool active = slot < a.slots && ch < a.c;
+    const int vecs = active ? full + (slot < more) : 0;                  // of this thread
     const size_t pix0 = (size_t)smp * a.hw + p_begin + slot;
+    const Vectors<kB, kKeep> x(reinterpret_cast<const char *>(a.x) + (pix0 * a.x_stride + ch) * kE, a.slots * a.x_stride * kE, smem);
 
     ptx::grid_dep_wait_launch_small();
-    own.fetch(vecs, [&](int i) { return reinterpret_cast<const char *>(a.x) + ((pix0 + (size_t)i * a.slots) * a.x_stride + ch) * kE; });
+    x.fetch(vecs);
     for (int k = threadIdx.x; k < channels; k += kGnThreads) {
         gamma[k] = a.gamma ? __ldg(a.gamma + ch0 + k) : 1.0f;
         beta[k] = a.beta ? __ldg(a.beta + ch0 + k) : 0.0f;
     }
-    copy_wait();
 
-    // ---- the thread's vectors: mean about the first value, squares about the mean
+    if (kKeep) copy_wait();
+
+    // ---- the thread's vectors
     {
-        float first[kG], s[kG], q[kG];
+        constexpr int kA = kW == 1 ? kPairs<kV> : kG;   // accumulators: a channel to a lane of a pair, or a group to a pair
+        Pair mean[kA], sq[kA];   // mean: with its sign turned
 #pragma unroll
-        for (int j = 0; j < kG; ++j) first[j] = s[j] = q[j] = 0.0f;
-        if (vecs > 0) {
-            float v[kV];
-            x_values<kType, kV>(own.get(0), a.x_scale, v);
+        for (int j = 0; j < kA; ++j) mean[j] = sq[j] = both(0.0f);
+        auto acc = [](int i) { return kW == 1 ? i : 2 * i / kW; };   // of pair i of a vector
+        auto batch = [&](const char *&at, int i0, auto count, float inv) {   // inv: 1 / values of the batch
+            constexpr int kCount = decltype(count)::value;
+            Raw<kB> raw[kCount];
+            float v[kCount][kV];
+            Pair s[kA], q[kA], first[kA];
+            x.get(raw, i0, at);
 #pragma unroll
-            for (int j = 0; j < kG; ++j) first[j] = v[j];
-#pragma unroll 4
-            for (int i = 0; i < vecs; ++i) {
-                x_values<kType, kV>(own.get(i), a.x_scale, v);
+            for (int u = 0; u < kCount; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
+            // (about the first value, so that equal values have themselves as their mean; sums of a few 16-bit values are exact anyway)
+            constexpr bool kShift = kE > 2;
 #pragma unroll
-                for (int j = 0; j < kV; ++j) s[kUni ? 0 : j] += v[j] - first[kUni ? 0 : j];
+            for (int j = 0; j < kA; ++j) {
+                s[j] = q[j] = both(0.0f);
+                first[j] = kW == 1 ? pair_of(v[0], j) * both(-1.0f) : both(-v[0][j * kW]);
             }
-            const float per_value = 1.0f / (float)(kUni ? vecs * kV : vecs);
 #pragma unroll
-            for (int j = 0; j < kG; ++j) s[j] = __fmaf_rn(s[j], per_value, first[j]);
-#pragma unroll 4
-            for (int i = 0; i < vecs; ++i) {
-                x_values<kType, kV>(own.get(i), a.x_scale, v);
+            for (int u = 0; u < kCount; ++u)
 #pragma unroll
-                for (int j = 0; j < kV; ++j) {
-                    const float d = v[j] - s[kUni ? 0 : j];
-                    q[kUni ? 0 : j] = __fmaf_rn(d, d, q[kUni ? 0 : j]);
+                for (int j = 0; j < kPairs<kV>; ++j) s[acc(j)] = s[acc(j)] + (kShift ? pair_of(v[u], j) + first[acc(j)] : pair_of(v[u], j));
+#pragma unroll
+            for (int j = 0; j < kA; ++j) {   // s: minus the mean
+                if (kW > 1) s[j] = both(s[j].x + s[j].y);
+                s[j] = kShift ? fma2(s[j], both(-inv), first[j]) : s[j] * both(-inv);
+            }
+#pragma unroll
+            for (int u = 0; u < kCount; ++u)
+#pragma unroll
+                for (int j = 0; j < kPairs<kV>; ++j) {
+                    const Pair d = pair_of(v[u], j) + s[acc(j)];
+                    q[acc(j)] = fma2(d, d, q[acc(j)]);
                 }
+            const float share = __fdividef((float)kCount, (float)(i0 + kCount)), between = (float)(i0 * kW) * share;
+            // (each lane of a pair holds half of a group's squares: half of what the means' distance adds goes to each)
+#pragma unroll
+            for (int j = 0; j < kA; ++j) {
+                const Pair d = fma2(mean[j], both(-1.0f), s[j]);
+                mean[j] = i0 ? fma2(d, both(share), mean[j]) : s[j];
+                sq[j] = sq[j] + fma2(d * d, both(kW > 1 ? 0.5f * between : between), q[j]);
             }
+        };
+        const char *at = x.first();
+        int i = 0;
+        for (; i + kGnBatch <= vecs; i += kGnBatch) batch(at, i, std::integral_constant<int, kGnBatch>(), 1.0f / (kGnBatch * kW));
+        if (i + 2 <= vecs) {
+            batch(at, i, std::integral_constant<int, 2>(), 0.5f / kW);
+            i += 2;
         }
+        if (i < vecs) batch(at, i, std::integral_constant<int, 1>(), 1.0f / kW);
         if (slot < a.slots)
 #pragma unroll
-            for (int j = 0; j < kG; ++j) cell[(slot * a.cv + cv) * kG + j] = make_float2(s[j], q[j]);
+            for (int j = 0; j < kG; ++j) {
+                const Pair m = mean[kW == 1 ? j / 2 : j], e = sq[kW == 1 ? j / 2 : j];
+                cell[(slot * a.cv + cv) * kG + j] = kW == 1 ? (j % 2 ? make_float2(-m.y, e.y) : make_float2(-m.x, e.x)) : make_float2(-m.x, e.x + e.y);
+            }
     }
+    if (!kKeep) copy_wait();
     __syncthreads();
+    if (a.ranks > 1) ptx::cluster_wait();
 
-    // ---- a warp per group joins the block's cells
-    const int per_group = kUni ? a.cpg / kV : a.cpg, row = a.cv * kG, used = min(a.slots, pixels);   // (cells of a group in a slot, of a slot)
-    const int full = pixels / a.slots, more = pixels % a.slots;
+    // ---- a warp per group joins the block's cells and hands the result to every block of the sample
+    const int per_group = a.cpg / kW, row = a.cv * kG, used = min(a.slots, pixels);   // (cells of a group in a slot, of a slot)
     const int lane = threadIdx.x & 31;
     for (int g = threadIdx.x / 32; g < groups; g += kGnWarps) {
-        const float2 *src = cell + g * per_group;
-        const float first = src[0].x;
+        const float2 *cells = cell + g * per_group;
+        const float first = cells[0].x;
         float s = 0.0f, q = 0.0f;
         for (int i = lane; i < used * per_group; i += 32) {
-            const int j = i / per_group;
-            s = __fmaf_rn(src[j * row + i - j * per_group].x - first, (float)(full + (j < more)), s);
+            const int j = a.by_part(i);
+            s = __fmaf_rn(cells[j * row + i - j * per_group].x - first, (float)(full + (j < more)), s);
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
         s = pixels ? first + s / ((float)pixels * (float)per_group) : 0.0f;
-        constexpr float kValues = kUni ? (float)kV : 1.0f;   // values a pixel adds to a cell
         for (int i = lane; i < used * per_group; i += 32) {
-            const int j = i / per_group;
-            const float2 e = src[j * row + i - j * per_group];
-            q += __fmaf_rn((e.x - s) * (e.x - s), kValues * (float)(full + (j < more)), e.y);
+            const int j = a.by_part(i);
+            const float2 e = cells[j * row + i - j * per_group];
+            q += __fmaf_rn((e.x - s) * (e.x - s), (float)((full + (j < more)) * kW), e.y);
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-        if (lane == 0) mine[g] = make_float2(s, q);
+        if (a.ranks == 1) {
+            if (lane == 0) parts[g] = make_float2(s, q);
+        } else if (lane < a.ranks) {
+            st_cluster_f2(parts + rank * most + g, lane, make_float2(s, q));
+        }
     }
     if (a.ranks > 1) ptx::cluster_sync();
     else __syncthreads();
 
     // ---- the blocks of the sample; every one joins them for itself
     for (int g = threadIdx.x; g < groups; g += kGnThreads) {
-        const uint32_t at = ptx::smem_u32(mine + g);
-        auto part = [&](int r) { return a.ranks > 1 ? ld_cluster_f2(ptx::cluster_addr(at, (uint32_t)r)) : mine[g]; };
         auto count = [&](int r) { return (float)(min(a.hw, (r + 1) * per) - min(a.hw, r * per)); };
-        const float first = part(0).x;
+        const float first = parts[g].x;
         float s = 0.0f, q = 0.0f;
-        for (int r = 1; r < a.ranks; ++r) s = __fmaf_rn(count(r) > 0.0f ? part(r).x - first : 0.0f, count(r), s);
+        for (int r = 1; r < a.ranks; ++r) s = __fmaf_rn(count(r) > 0.0f ? parts[r * most + g].x - first : 0.0f, count(r), s);
         s = first + s / (float)a.hw;
         for (int r = 0; r < a.ranks; ++r) {
-            const float2 e = part(r);
+            const float2 e = parts[r * most + g];
             if (count(r) > 0.0f) q += __fmaf_rn((e.x - s) * (e.x - s), count(r) * (float)a.cpg, e.y);
         }
-        const float rstd = (float)(1.0 / sqrt((double)q / ((double)a.hw * a.cpg) + (double)a.eps));
+        const float rstd = __frsqrt_rn(q / ((float)a.hw * (float)a.cpg) + a.eps);
         final[g] = make_float2(s, rstd);
-        if (rank == 0 && a.stats) a.stats[(size_t)smp * a.groups + ch0 / a.cpg + g] = make_float2(s, rstd);
+        if (rank == 0 && a.stats) a.stats[(size_t)smp * a.groups + a.by_cpg(ch0) + g] = make_float2(s, rstd);
     }
     __syncthreads();
-    if (a.ranks > 1) ptx::cluster_arrive();   // (this block has read what it needs of the others)
 
     // ---- y, and the 8-bit form
     float mul[kV], add[kV], mean[kG];
+    int g = a.by_cpg(cv * kV), in_g = cv * kV - g * a.cpg;   // group of the next kW channels, and where in it
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
-        const bool in = ch + j < a.c && slot < a.slots;
-        const float2 st = in ? final[(cv * kV + j) / a.cpg] : make_float2(0.0f, 0.0f);
-        if (j < kG) mean[j] = st.x;
-        mul[j] = in ? st.y * gamma[cv * kV + j] : 0.0f;
-        add[j] = in ? beta[cv * kV + j] : 0.0f;
+    for (int k = 0; k < kG; ++k) {
+        const float2 st = active ? final[g] : make_float2(0.0f, 0.0f);
+        mean[k] = -st.x;
+#pragma unroll
+        for (int j = k * kW; j < (k + 1) * kW; ++j) {
+            mul[j] = active ? st.y * gamma[cv * kV + j] : 0.0f;
+            add[j] = active ? beta[cv * kV + j] : 0.0f;
+        }
+        in_g += kW;
+        if (in_g == a.cpg) {
+            in_g = 0;
+            ++g;
+        }
     }
+    constexpr int kYE = Elem<Types::kY>::kSize;
+    char *y = reinterpret_cast<char *>(a.y) + (pix0 * a.y_stride + ch) * kYE;
+    int8_t *codes = kSave ? a.codes_out + pix0 * a.c + ch : nullptr;
+    uint8_t *exps = kSave ? a.exps_out + pix0 * a.blocks + ch / kBlock8 : nullptr;
+    const size_t y_step = a.slots * a.y_stride * kYE, codes_step = (size_t)a.slots * a.c, exps_step = (size_t)a.slots * a.blocks;
     unsigned bad = 0;
-    const int rounds = kSave ? a.vecs : vecs;   // (lanes that share a block of the 8-bit form stay together)
-#pragma unroll 2
-    for (int i = 0; i < rounds; ++i) {
-        const bool in = !kSave || i < vecs;
-        const size_t pix = pix0 + (size_t)i * a.slots;
+    auto emit = [&](const Raw<kB> &raw, bool in) {
         float v[kV];
-        x_values<kType, kV>(in ? own.get(i) : zero_raw<kB>(), a.x_scale, v);
+        x_values<kType, kV>(raw, a.x_scale, v);
         if constexpr (kSave) {
             float m = 0.0f;
 #pragma unroll
@@ -155,52 +199,81 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
                 Raw<kV> out;
 #pragma unroll
                 for (int j = 0; j < (kV + 3) / 4; ++j) set_word(out, j, w[j]);
-                store_raw(a.codes_out + pix * a.c + ch, out);
-                if (ch % kBlock8 == 0) a.exps_out[pix * a.blocks + ch / kBlock8] = (uint8_t)s;
+                store_raw(codes, out);
+                if (ch % kBlock8 == 0) *exps = (uint8_t)s;
                 bad |= s == 255;
             }
+            codes += codes_step;
+            exps += exps_step;
         }
         if (in) {
 #pragma unroll
-            for (int j = 0; j < kV; ++j) v[j] = __fmaf_rn(v[j] - mean[kUni ? 0 : j], mul[j], add[j]);
+            for (int j = 0; j < kPairs<kV>; ++j) {
+                const Pair m = {mean[2 * j / kW], mean[kV == 1 ? 0 : (2 * j + 1) / kW]};
+                set_pair(v, j, fma2(pair_of(v, j) + m, pair_of(mul, j), pair_of(add, j)));
+            }
             activate(v, a.act);
-            store_raw(reinterpret_cast<char *>(a.y) + (pix * a.y_stride + ch) * Elem<Types::kY>::kSize, Elem<Types::kY>::from_f32(v));
+            store_raw(y, Elem<Types::kY>::from_f32(v));
         }
+        y += y_step;
+    };
+    // Lanes that share a block of the 8-bit form stay together: full batches are those of the whole warp.
+    const int least = kSave ? (int)__reduce_min_sync(0xffffffffu, (unsigned)vecs) : vecs;
+    const int rounds = kSave ? (int)__reduce_max_sync(0xffffffffu, (unsigned)vecs) : vecs;
+    const char *at = x.first();
+    int i = 0;
+    for (; i + kGnBatch <= least; i += kGnBatch) {
+        Raw<kB> raw[kGnBatch];
+        x.get(raw, i, at);
+#pragma unroll
+        for (int u = 0; u < kGnBatch; ++u) emit(raw[u], true);
+    }
+    for (; i < rounds; ++i) {
+        Raw<kB> raw[1] = {zero_raw<kB>()};
+        if (i < vecs) x.get(raw, i, at);
+        emit(raw[0], i < vecs);
     }
     if (kSave && bad) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
-    if (a.ranks > 1) ptx::cluster_wait();
 }
 
-template <int kType, int kV, bool kUni, bool kSave>
+template <int kType, int kV, int kW, bool kSave, bool kKeep>
 cudaError_t launch(GnArgs a, const FusedPlan &p, cudaStream_t st)
 {
+    const auto kernel = gn_fused_fwd_kernel<kType, kV, kW, kSave, kKeep>;
+    use_plan(a, p, kW);
     static std::atomic<unsigned long long> allowed;
-    const auto kernel = gn_fused_fwd_kernel<kType, kV, kUni, kSave>;
-    const cudaError_t e = allow_fused((const void *)kernel, allowed);
+    const cudaError_t e = allow_smem((const void *)kernel, 200 * 1024, allowed);
     if (e != cudaSuccess) return e;
-    a.cv = p.cv;
-    a.slots = p.slots;
-    a.chunks = p.chunks;
-    a.ranks = p.ranks;
-    a.vecs = p.vecs;
     return launch_chained_clusters(p.ranks, kernel, dim3((unsigned)((size_t)a.n * p.chunks * p.ranks)), dim3(kGnThreads), p.smem, st, a);
+}
+
+template <int kType, int kV, int kW>
+bool of_part(const GnArgs &a, cudaError_t *result, cudaStream_t st)
+{
+    constexpr int kB = kV * Elem<kType>::kSize;
+    const bool save = a.codes_out != nullptr && a.c % kBlock8 == 0;
+    int unit = a.cpg / kW * kV;
+    if (save) unit = unit / gcd_of(unit, kBlock8) * kBlock8;
+    // four blocks to an SM
+    constexpr size_t kLimit = 56 * 1024;
+    FusedPlan p;
+    if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kLimit, [&](int cv) { return FwdLayout<kV, kW>::bytes(cv, cv * kV / a.cpg); })) return false;
+    if (p.keep) *result = save ? launch<kType, kV, kW, true, true>(a, p, st) : launch<kType, kV, kW, false, true>(a, p, st);
+    else *result = save ? launch<kType, kV, kW, true, false>(a, p, st) : launch<kType, kV, kW, false, false>(a, p, st);
+    return true;
 }
 
 template <int kType, int kV>
 bool of_width(const GnArgs &a, cudaError_t *result, cudaStream_t st)
 {
-    constexpr int kE = Elem<kType>::kSize;
-    const bool uni = a.cpg % kV == 0, save = a.codes_out != nullptr && a.c % kBlock8 == 0;
-    int unit = a.cpg / gcd_of(a.cpg, kV) * kV;
-    if (save) unit = unit / gcd_of(unit, kBlock8) * kBlock8;
-    FusedPlan p;
-    if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kV * kE, kV * kE,
-                    [&](int cv) { return uni ? FwdLayout<kV, true>::bytes(cv) : FwdLayout<kV, false>::bytes(cv); }) ||
-        (size_t)a.n * p.chunks * p.ranks > 0x7fffffffull)
-        return false;
-    if (kV == 1 || uni) *result = save ? launch<kType, kV, true, true>(a, p, st) : launch<kType, kV, true, false>(a, p, st);
-    else if constexpr (kV > 1) *result = save ? launch<kType, kV, false, true>(a, p, st) : launch<kType, kV, false, false>(a, p, st);
-    return true;
+    const int w = gcd_of(a.cpg, kV);
+    if constexpr (kV == 8)
+        if (w == 8) return of_part<kType, kV, 8>(a, result, st);
+    if constexpr (kV >= 4)
+        if (w == 4) return of_part<kType, kV, 4>(a, result, st);
+    if constexpr (kV >= 2)
+        if (w == 2) return of_part<kType, kV, 2>(a, result, st);
+    return of_part<kType, kV, 1>(a, result, st);
 }
 
 template <int kType>

@@ -1,15 +1,25 @@
-// Group normalisation that reads every element once: what its forward and backward kernels share.
+// Group normalisation in one launch: what its forward and backward kernels share.
 //
-// A sample's chunk of whole groups stays on the chip between the sums and their use, dealt out by pixels to the blocks of a cluster.
-// A thread copies its vectors to shared memory (asynchronously where they have 4 bytes or more) and only ever reads back what it
-// copied itself, so the data needs no barrier; sums meet in shared memory, and over the cluster through distributed shared memory.
+// A sample's chunk of whole groups belongs to a cluster, dealt out by pixels to its blocks.  The blocks read their pixels once for the
+// sums, which meet in shared memory and, over the cluster, in distributed shared memory, and look at them once more for the results.
+// Between the two looks the vectors stay in shared memory where that leaves room for four blocks on an SM; larger samples are read
+// again, from the L2 cache as far as what the resident clusters work on has room there.  (256 channels 56 x 56, 32 fp16 samples: 25 us
+// kept, 30 read again; 64 channels 112 x 112, 64 bf16 samples: kept in 104 KB by two blocks an SM 73 us forward and 209 backward, read
+// again 83 and 117.)
 #pragma once
 #include "eoq_gn.cuh"
 
 namespace eoq {
 
 constexpr int kGnThreads = 256, kGnWarps = kGnThreads / 32;
+constexpr int kGnBatch = 4;   // vectors of a thread at a time
 
+// to the same place in shared memory of block `rank` of the cluster
+__device__ __forceinline__ void st_cluster_f2(const float2 *at, int rank, float2 v)
+{
+    const uint32_t to = ptx::cluster_addr(ptx::smem_u32(at), (uint32_t)rank);
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+}
 template <int kBytes>
 __device__ __forceinline__ void copy_in(uint32_t smem, const void *src)
 {
@@ -19,57 +29,64 @@ __device__ __forceinline__ void copy_in(uint32_t smem, const void *src)
 }
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t addr)
-{
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-    return v;
-}
-
-// A thread's vectors of a tensor: element i at base[i * kGnThreads + thread].
-template <int kBytes>
-struct OwnVectors {
+// A thread's vectors of a tensor, `step` bytes apart from `at` on; kept: vector i at base[i * kGnThreads] of shared memory, where the
+// thread only ever reads back what it copied itself, so that no barrier is needed.
+template <int kBytes, bool kKeep>
+struct Vectors {
     using Word = decltype(Raw<kBytes>::w);
+    const char *at;
+    size_t step;
     Word *base;
-    __device__ __forceinline__ explicit OwnVectors(void *smem) : base(reinterpret_cast<Word *>(smem) + threadIdx.x) {}
-    __device__ __forceinline__ Raw<kBytes> get(int i) const
+    __device__ __forceinline__ Vectors(const void *from, size_t step_, void *smem)
+        : at(reinterpret_cast<const char *>(from)), step(step_), base(reinterpret_cast<Word *>(smem) + threadIdx.x)
     {
-        Raw<kBytes> r;
-        r.w = base[i * kGnThreads];
-        return r;
     }
-    // vectors first, first + step, ... of `count`; `at(i)` is their address
-    template <typename At>
-    __device__ __forceinline__ void fetch(int count, At at) const
+    __device__ __forceinline__ void fetch(int count) const
     {
-        if constexpr (kBytes >= 4) {
-            for (int i = 0; i < count; ++i) copy_in<kBytes>(ptx::smem_u32(base + i * kGnThreads), at(i));
-        } else {
-            constexpr int kBatch = 8;
-            for (int i0 = 0; i0 < count; i0 += kBatch) {
-                Raw<kBytes> r[kBatch];
+        if constexpr (kKeep) {
+            const char *p = at;
+            if constexpr (kBytes >= 4) {
+                uint32_t to = ptx::smem_u32(base);
+                for (int i = 0; i < count; ++i, p += step, to += kGnThreads * kBytes) copy_in<kBytes>(to, p);
+            } else {
+                constexpr int kMany = 8;
+                for (int i0 = 0; i0 < count; i0 += kMany, p += kMany * step) {
+                    Raw<kBytes> r[kMany];
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j)
-                    if (i0 + j < count) r[j] = load_raw<kBytes>(at(i0 + j));
+                    for (int j = 0; j < kMany; ++j)
+                        if (i0 + j < count) r[j] = load_raw<kBytes>(p + j * step);
 #pragma unroll
-                for (int j = 0; j < kBatch; ++j)
-                    if (i0 + j < count) base[(i0 + j) * kGnThreads] = r[j].w;
+                    for (int j = 0; j < kMany; ++j)
+                        if (i0 + j < count) base[(i0 + j) * kGnThreads] = r[j].w;
+                }
             }
         }
+    }
+    // vectors i, i + 1, ... of which `p` (vectors_at(0), moved on by next) is the first's address
+    __device__ __forceinline__ const char *first() const { return at; }
+    template <int kCount>
+    __device__ __forceinline__ void get(Raw<kBytes> (&r)[kCount], int i, const char *&p) const
+    {
+#pragma unroll
+        for (int u = 0; u < kCount; ++u) {
+            if constexpr (kKeep) r[u].w = base[(i + u) * kGnThreads];
+            else r[u] = load_raw<kBytes>(p + u * step);
+        }
+        if constexpr (!kKeep) p += kCount * step;
     }
 };
 
 // How a call is dealt out.
 struct FusedPlan {
     int cv, slots, chunks, ranks, vecs;
+    bool keep;
     size_t smem;
 };
 
-// v: channels of a vector; bytes: what a thread keeps of one; unit: channels that must stay together (a multiple of v); fixed(cv):
-// further bytes of shared memory.  Blocks want to share an SM, so that one loads while another stores: the first limit that some
-// cluster meets is taken, small blocks before large ones, clusters of up to 8 before 16.
+// v: channels of a vector, x_bytes long; unit: channels that must stay together (a multiple of v); kept: bytes of a vector in shared
+// memory, as long as a block needs no more than `limit`; fixed(cv): further bytes of it.
 template <typename Fixed>
-bool fused_plan(FusedPlan &p, int n, int hw, int c, int v, int unit, int bytes, int x_bytes, Fixed fixed)
+bool fused_plan(FusedPlan &p, int n, int hw, int c, int v, int unit, int x_bytes, int kept, size_t limit, Fixed fixed)
 {
     const int total = c / v, unit_v = unit / v;
     if (unit_v > kGnThreads) return false;
@@ -84,43 +101,34 @@ bool fused_plan(FusedPlan &p, int n, int hw, int c, int v, int unit, int bytes, 
     p.cv = m * unit_v;
     p.chunks = (units + m - 1) / m;
     p.slots = kGnThreads / p.cv;
-    const size_t rest = fixed(p.cv);
-    auto fits = [&](int ranks, size_t limit) {
-        const int per = (hw + ranks - 1) / ranks;
-        p.ranks = ranks;
-        p.vecs = (per + p.slots - 1) / p.slots;
-        p.smem = (size_t)p.vecs * kGnThreads * bytes + rest;
-        return p.smem <= limit;
-    };
-    const size_t kQuarter = 54 * 1024, kHalf = 110 * 1024, kWhole = 220 * 1024;
-    const struct {
-        size_t limit;
-        int most;
-    } tries[] = {{kQuarter, 8}, {kHalf, 8}, {kQuarter, 16}, {kHalf, 16}, {kWhole, 16}};
-    for (const auto &t : tries)
-        for (int ranks = 1; ranks <= t.most; ranks *= 2)
-            if (fits(ranks, t.limit)) {
-                // few blocks: spread them over more SMs as long as every thread has two vectors
-                while (ranks < 8 && p.vecs > 2 && (long long)n * p.chunks * ranks < 2 * kPartSms) fits(ranks *= 2, t.limit);
-                return true;
-            }
-    return false;
+    p.ranks = 1;
+    // (more blocks to a sample while the vectors do not fit, and while there are few and every thread has more than two)
+    auto vecs = [&] { return p.vecs = ((hw + p.ranks - 1) / p.ranks + p.slots - 1) / p.slots; };
+    auto size = [&] { return (size_t)vecs() * kGnThreads * kept + fixed(p.cv); };
+    while (p.ranks < 8 && (size() > limit || (vecs() > 2 && (long long)n * p.chunks * p.ranks < 2 * kPartSms))) p.ranks *= 2;
+    p.keep = size() <= limit;
+    p.smem = p.keep ? size() : fixed(p.cv);
+    if (p.smem > 200 * 1024) return false;
+    // (divisions by multiplication: dividend times divisor below 2^32)
+    return (size_t)n * p.chunks * p.ranks < (1ull << 32) / (p.chunks > 8 ? p.chunks : 8) && (size_t)p.slots * hw < (1ull << 32);
+}
+
+inline void use_plan(GnArgs &a, const FusedPlan &p, int kw)
+{
+    a.cv = p.cv;
+    a.slots = p.slots;
+    a.chunks = p.chunks;
+    a.ranks = p.ranks;
+    a.vecs = p.vecs;
+    a.per = (a.hw + p.ranks - 1) / p.ranks;
+    a.by_slots = FastDiv(p.slots);
+    a.by_chunks = FastDiv(p.chunks);
+    a.by_ranks = FastDiv(p.ranks);
+    a.by_cv = FastDiv(p.cv);
+    a.by_cpg = FastDiv(a.cpg);
+    a.by_part = FastDiv(a.cpg / kw);
 }
 
 inline int gcd_of(int a, int b) { return b ? gcd_of(b, a % b) : a; }
-
-// Allows a kernel its shared memory and clusters of 16, once per device.
-inline cudaError_t allow_fused(const void *kernel, std::atomic<unsigned long long> &done)
-{
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    const unsigned long long bit = device < 64 ? 1ull << device : 0ull;
-    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
-    return e;
-}
 
 }  // namespace eoq

@@ -1,87 +1,129 @@
-// Group normalisation backward, every element read once (eoq_gn_bwd): see eoq_gn_fused.cuh for how the data stays on the chip, and
-// eoq_gn.cu for the formulas.  The first look at the kept vectors sums dz and dz u per channel, which is all that S1, S2, dgamma and
-// dbeta need; the second writes dx.  When all samples of a chunk fit a cluster it also adds dgamma and dbeta over them, and the call is
-// one launch; otherwise a small kernel behind adds the samples in their order.
+// Group normalisation backward in one launch, or two (eoq_gn_bwd): see eoq_gn_fused.cuh for how a sample is dealt out, and eoq_gn.cu for
+// the formulas.  The first look at a block's pixels sums dz and dz u per channel, which is all that S1, S2, dgamma and dbeta need; the
+// second writes dx.  When all samples of a chunk fit a cluster it also adds dgamma and dbeta over them, and the call is one launch;
+// otherwise a small kernel behind adds the samples in their order.
+#include <type_traits>
+
 #include "eoq_gn_fused.cuh"
 
 namespace eoq {
 
+
 namespace {
 
-// shared memory behind the vectors: cells of the threads, rows of sums by warp, sums of the block, of the sample, (S1, S2), gamma
+// shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2), gamma, beta
 template <int kV>
 struct BwdLayout {
     __host__ __device__ static size_t bytes(int cv)
     {
         const int slots = kGnThreads / cv, width = cv * kV;
-        return sizeof(float2) * ((size_t)kGnThreads * kV + (size_t)(slots < kGnWarps ? slots : kGnWarps) * width + (size_t)width * 7 / 2);
+        return sizeof(float2) * ((size_t)kGnThreads * kV + (size_t)(slots < kGnWarps ? slots : kGnWarps) * width + (8 + 3) * (size_t)width);
     }
 };
 
-template <int kType, int kV, bool kUni, bool kCodes>
-__global__ void __launch_bounds__(kGnThreads, 2) gn_fused_bwd_kernel(const __grid_constant__ GnArgs a)
+// kW: so many neighbouring channels of a vector are always of one group (the common divisor of both widths)
+template <int kType, int kV, int kW, bool kCodes, bool kKeep>
+__global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __grid_constant__ GnArgs a)
 {
     using Types = GnTypes<kType>;
-    using Input = GnInput<kType, kV, kCodes, kUni>;
-    constexpr int kE = Elem<kType>::kSize, kDyE = Elem<Types::kY>::kSize, kG = kUni ? 1 : kV;
+    using Input = GnInput<kType, kV, kCodes>;
+    constexpr int kE = Elem<kType>::kSize, kDyE = Elem<Types::kY>::kSize, kG = kV / kW;
     extern __shared__ __align__(16) uint8_t smem[];
-    const size_t all = (size_t)a.vecs * kGnThreads;
-    const OwnVectors<Input::kDyB> own_dy(smem);
-    const OwnVectors<Input::kXB> own_x(smem + all * Input::kDyB);
-    uint8_t *own_s = smem + all * (Input::kDyB + Input::kXB) + threadIdx.x;
     const int width = a.cv * kV, rows = min(a.slots, kGnWarps);
+    const size_t all = kKeep ? (size_t)a.vecs * kGnThreads : 0;
     float2 *cell = reinterpret_cast<float2 *>(smem + all * (Input::kDyB + Input::kXB + (kCodes ? 1 : 0)));
-    float2 *by_warp = cell + kGnThreads * kV, *mine = by_warp + rows * width, *total = mine + width, *means = total + width;
-    float *gamma_s = reinterpret_cast<float *>(means + width);
+    float2 *by_warp = cell + kGnThreads * kV, *parts = by_warp + rows * width, *total = parts + 8 * width, *means = total + width;   // parts [rank][channel]
+    float *gamma_s = reinterpret_cast<float *>(means + width), *beta_s = gamma_s + width;
 
-    const int rank = blockIdx.x % a.cluster, id = blockIdx.x / a.cluster, chunk = id % a.chunks, samples = a.cluster / a.ranks;
-    const int smp = id / a.chunks * samples + rank / a.ranks, part = rank % a.ranks;
-    const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch0 = chunk * width, ch = ch0 + cv * kV;
-    const int per = (a.hw + a.ranks - 1) / a.ranks, p_begin = min(part * per, a.hw), pixels = min(a.hw, p_begin + per) - p_begin;
-    const int channels = min(width, a.c - ch0), groups = channels / a.cpg;
+    const int id = a.by_cluster(blockIdx.x), rank = blockIdx.x - id * a.cluster, set = a.by_chunks(id), chunk = id - set * a.chunks;
+    const int samples = a.by_ranks(a.cluster), own = a.by_ranks(rank), smp = set * samples + own, part = rank - own * a.ranks;
+    const int slot = a.by_cv(threadIdx.x), cv = threadIdx.x - slot * a.cv, ch0 = chunk * width, ch = ch0 + cv * kV;
+    const int per = a.per, p_begin = min(part * per, a.hw), pixels = min(a.hw, p_begin + per) - p_begin;
+    const int channels = min(width, a.c - ch0), groups = a.by_cpg(channels);
     const bool active = slot < a.slots && ch < a.c;
-    const int vecs = active && slot < pixels ? (pixels - slot + a.slots - 1) / a.slots : 0;
+    const int vecs = active && slot < pixels ? 1 + a.by_slots(pixels - 1 - slot) : 0;
     const size_t pix0 = (size_t)smp * a.hw + p_begin + slot;
 
+    const Vectors<Input::kDyB, kKeep> dys(reinterpret_cast<const char *>(a.dy) + (pix0 * a.dy_stride + ch) * kDyE, a.slots * a.dy_stride * kDyE, smem);
+    const Vectors<Input::kXB, kKeep> xs(kCodes ? reinterpret_cast<const char *>(a.codes + pix0 * a.c + ch)
+                                               : reinterpret_cast<const char *>(a.x) + (pix0 * a.x_stride + ch) * kE,
+                                        kCodes ? (size_t)a.slots * a.c : a.slots * a.x_stride * kE, smem + all * Input::kDyB);
+    const Vectors<1, kKeep> bytes(kCodes ? a.exps + pix0 * a.blocks + ch / kBlock8 : nullptr, (size_t)a.slots * a.blocks,
+                                  smem + all * (Input::kDyB + Input::kXB));
+
+    if (a.cluster > 1) ptx::cluster_arrive();   // (waited for below: the others have started when their memory is written)
     ptx::grid_dep_wait_launch_small();
-    own_dy.fetch(vecs, [&](int i) { return reinterpret_cast<const char *>(a.dy) + ((pix0 + (size_t)i * a.slots) * a.dy_stride + ch) * kDyE; });
-    if constexpr (kCodes) {
-        own_x.fetch(vecs, [&](int i) { return a.codes + (pix0 + (size_t)i * a.slots) * a.c + ch; });
-        OwnVectors<1> bytes(own_s - threadIdx.x);
-        bytes.fetch(vecs, [&](int i) { return a.exps + (pix0 + (size_t)i * a.slots) * a.blocks + ch / kBlock8; });
-    } else {
-        own_x.fetch(vecs, [&](int i) { return reinterpret_cast<const char *>(a.x) + ((pix0 + (size_t)i * a.slots) * a.x_stride + ch) * kE; });
-    }
-    float gamma[kV], beta[kV], mean[kG], rstd[kG];
+    dys.fetch(vecs);
+    xs.fetch(vecs);
+    if (kCodes) bytes.fetch(vecs);
+    float off[kG], rstd[kG];
+    const int g0 = a.by_cpg(cv * kV), in_g0 = cv * kV - g0 * a.cpg;   // group of the first channel within the chunk, and where in it
+    const float2 *stats = a.stats + (size_t)smp * a.groups + a.by_cpg(ch0);
+    int g = g0, in_g = in_g0;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) {
-        gamma[j] = active && a.gamma ? __ldg(a.gamma + ch + j) : 1.0f;
-        beta[j] = active && a.beta ? __ldg(a.beta + ch + j) : 0.0f;
-        if (j < kG) {
-            const float2 st = active ? a.stats[(size_t)smp * a.groups + (ch + j) / a.cpg] : make_float2(0.0f, 0.0f);
-            mean[j] = st.x;
-            rstd[j] = st.y;
+    for (int k = 0; k < kG; ++k) {
+        const float2 st = active ? __ldg(stats + g) : make_float2(0.0f, 0.0f);
+        off[k] = -st.x * st.y;
+        rstd[k] = st.y;
+        in_g += kW;
+        if (in_g == a.cpg) {
+            in_g = 0;
+            ++g;
         }
     }
-    for (int k = threadIdx.x; k < channels; k += kGnThreads) gamma_s[k] = a.gamma ? __ldg(a.gamma + ch0 + k) : 1.0f;
+    for (int k = threadIdx.x; k < width; k += kGnThreads) {
+        gamma_s[k] = a.gamma && k < channels ? __ldg(a.gamma + ch0 + k) : 1.0f;
+        beta_s[k] = a.beta && k < channels ? __ldg(a.beta + ch0 + k) : 0.0f;
+    }
     const float dy_scale = error_scale<kType>(a);
-    copy_wait();
+
+    if (kKeep) copy_wait();
+
+    __syncthreads();   // (gamma and beta)
+
+    // Both looks: a few vectors at a time.  use(u, dz, gamma) gets what a vector holds.
+    const float *const gamma_at = gamma_s + cv * kV, *const beta_at = beta_s + cv * kV;
+    auto look = [&](auto use) {
+        const char *dy_at = dys.first(), *x_at = xs.first(), *s_at = bytes.first();
+        auto batch = [&](int i, auto count) {
+            constexpr int kCount = decltype(count)::value;
+            Raw<Input::kXB> x[kCount];
+            Raw<Input::kDyB> dy[kCount];
+            Raw<1> s[kCount] = {};
+            dys.get(dy, i, dy_at);
+            xs.get(x, i, x_at);
+            if (kCodes) bytes.get(s, i, s_at);
+            float gamma[kV], beta[kV];
+#pragma unroll
+            for (int j = 0; j < kV; ++j) {
+                gamma[j] = gamma_at[j];
+                beta[j] = beta_at[j];
+            }
+#pragma unroll
+            for (int j = 0; j < kCount; ++j) {
+                float u[kV], dz[kV];
+                gn_terms<kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
+                use(u, dz, gamma);
+            }
+        };
+        int i = 0;
+#pragma unroll 1
+        for (; i + kGnBatch <= vecs; i += kGnBatch) batch(i, std::integral_constant<int, kGnBatch>());
+#pragma unroll 1
+        for (; i < vecs; ++i) batch(i, std::integral_constant<int, 1>());
+    };
 
     {
         float s0[kV], s1[kV];
 #pragma unroll
         for (int j = 0; j < kV; ++j) s0[j] = s1[j] = 0.0f;
-#pragma unroll 2
-        for (int i = 0; i < vecs; ++i) {
-            float u[kV], dz[kV];
-            gn_terms<kType, kV, kCodes, kUni>(own_x.get(i), kCodes ? own_s[i * kGnThreads] : 0, own_dy.get(i), a.x_scale, dy_scale, a.act, mean, rstd,
-                                              gamma, beta, u, dz);
+        look([&](const float (&u)[kV], const float (&dz)[kV], const float (&)[kV]) {
 #pragma unroll
-            for (int j = 0; j < kV; ++j) {
-                s0[j] += dz[j];
-                s1[j] = __fmaf_rn(dz[j], u[j], s1[j]);
+            for (int j = 0; j < kPairs<kV>; ++j) {
+                set_pair(s0, j, pair_of(s0, j) + pair_of(dz, j));
+                set_pair(s1, j, fma2(pair_of(dz, j), pair_of(u, j), pair_of(s1, j)));
             }
-        }
+        });
         if (slot < a.slots)
 #pragma unroll
             for (int j = 0; j < kV; ++j) cell[(slot * a.cv + cv) * kV + j] = make_float2(s0[j], s1[j]);
@@ -100,30 +142,37 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fused_bwd_kernel(const __gri
             by_warp[warp * width + k] = t;
         }
     __syncthreads();
+    if (a.cluster > 1) ptx::cluster_wait();
+    // who needs a block's sums: the blocks of its sample, and the first block where that adds the samples up
+    const bool whole = samples == a.n;
     for (int k = threadIdx.x; k < channels; k += kGnThreads) {
         float2 t = make_float2(0.0f, 0.0f);
         for (int j = 0; j < rows; ++j) {
             t.x += by_warp[j * width + k].x;
             t.y += by_warp[j * width + k].y;
         }
-        mine[k] = t;
+        if (a.cluster == 1) {
+            parts[k] = t;
+        } else {
+            for (int r = rank - part; r < rank - part + a.ranks; ++r) st_cluster_f2(parts + rank * width + k, r, t);
+            if (whole && rank >= a.ranks) st_cluster_f2(parts + rank * width + k, 0, t);
+        }
     }
     if (a.cluster > 1) ptx::cluster_sync();
     else __syncthreads();
 
     for (int k = threadIdx.x; k < channels; k += kGnThreads) {
-        const uint32_t at = ptx::smem_u32(mine + k);
-        auto add = [&](float2 &t, int r) {
-            const float2 e = a.cluster > 1 ? ld_cluster_f2(ptx::cluster_addr(at, (uint32_t)r)) : mine[k];
+        float2 t = make_float2(0.0f, 0.0f);
+        auto add = [&](int r) {
+            const float2 e = parts[r * width + k];
             t.x += e.x;
             t.y += e.y;
         };
-        float2 t = make_float2(0.0f, 0.0f);
-        for (int r = 0; r < a.ranks; ++r) add(t, rank - part + r);
+        for (int r = 0; r < a.ranks; ++r) add(rank - part + r);
         total[k] = t;
-        if (samples == a.n) {   // the cluster has every sample
+        if (whole) {
             if (rank == 0) {
-                for (int r = a.ranks; r < a.cluster; ++r) add(t, r);
+                for (int r = a.ranks; r < a.cluster; ++r) add(r);
                 if (a.dbeta) a.dbeta[ch0 + k] = t.x;
                 if (a.dgamma) a.dgamma[ch0 + k] = t.y;
             }
@@ -132,58 +181,62 @@ __global__ void __launch_bounds__(kGnThreads, 2) gn_fused_bwd_kernel(const __gri
         }
     }
     __syncthreads();
-    if (a.cluster > 1) ptx::cluster_arrive();   // (this block has read what it needs of the others)
-    const float inv = (float)(1.0 / ((double)a.hw * a.cpg));
-    for (int g = warp; g < groups; g += kGnWarps) {
+    const float inv = 1.0f / ((float)a.hw * (float)a.cpg);
+    for (int k = warp; k < groups; k += kGnWarps) {
         float s0 = 0.0f, s1 = 0.0f;
         for (int i = lane; i < a.cpg; i += 32) {
-            const float2 e = total[g * a.cpg + i];
-            s0 = __fmaf_rn(gamma_s[g * a.cpg + i], e.x, s0);
-            s1 = __fmaf_rn(gamma_s[g * a.cpg + i], e.y, s1);
+            const float2 e = total[k * a.cpg + i];
+            s0 = __fmaf_rn(gamma_s[k * a.cpg + i], e.x, s0);
+            s1 = __fmaf_rn(gamma_s[k * a.cpg + i], e.y, s1);
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
             s0 += __shfl_xor_sync(0xffffffffu, s0, d);
             s1 += __shfl_xor_sync(0xffffffffu, s1, d);
         }
-        if (lane == 0) means[g] = make_float2(s0 * inv, s1 * inv);
+        if (lane == 0) means[k] = make_float2(s0 * inv, s1 * inv);
     }
     __syncthreads();
     float k0[kG], k1[kG];
+    g = g0;
+    in_g = in_g0;
 #pragma unroll
-    for (int j = 0; j < kG; ++j) {
-        const float2 m = active ? means[(cv * kV + j) / a.cpg] : make_float2(0.0f, 0.0f);
-        k0[j] = -rstd[j] * m.x;
-        k1[j] = -rstd[j] * m.y;
+    for (int k = 0; k < kG; ++k) {
+        const float2 m = active ? means[g] : make_float2(0.0f, 0.0f);
+        k0[k] = -rstd[k] * m.x;
+        k1[k] = -rstd[k] * m.y;
+        in_g += kW;
+        if (in_g == a.cpg) {
+            in_g = 0;
+            ++g;
+        }
     }
-#pragma unroll 2
-    for (int i = 0; i < vecs; ++i) {
-        float u[kV], dz[kV];
-        gn_terms<kType, kV, kCodes, kUni>(own_x.get(i), kCodes ? own_s[i * kGnThreads] : 0, own_dy.get(i), a.x_scale, dy_scale, a.act, mean, rstd, gamma,
-                                          beta, u, dz);
+    constexpr int kDxE = Elem<Types::kDx>::kSize;
+    char *dx = reinterpret_cast<char *>(a.dx) + (pix0 * a.dx_stride + ch) * kDxE;
+    const size_t dx_step = a.slots * a.dx_stride * kDxE;
+    look([&](const float (&u)[kV], float (&dz)[kV], const float (&gamma)[kV]) {
 #pragma unroll
-        for (int j = 0; j < kV; ++j)
-            dz[j] = __fmaf_rn(dz[j] * gamma[j], rstd[kUni ? 0 : j], __fmaf_rn(u[j], k1[kUni ? 0 : j], k0[kUni ? 0 : j]));
-        store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + (size_t)i * a.slots) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,
-                  Elem<Types::kDx>::from_f32(dz));
-    }
-    if (a.cluster > 1) ptx::cluster_wait();
+        for (int j = 0; j < kPairs<kV>; ++j) {
+            const int l = 2 * j / kW, h = kV == 1 ? 0 : (2 * j + 1) / kW;
+            const Pair e = pair_of(dz, j) * pair_of(gamma, j);
+            set_pair(dz, j, fma2(e, Pair{rstd[l], rstd[h]}, fma2(pair_of(u, j), Pair{k1[l], k1[h]}, Pair{k0[l], k0[h]})));
+        }
+        store_raw(dx, Elem<Types::kDx>::from_f32(dz));
+        dx += dx_step;
+    });
 }
 
-template <int kType, int kV, bool kUni, bool kCodes>
+template <int kType, int kV, int kW, bool kCodes, bool kKeep>
 cudaError_t launch(GnArgs a, const FusedPlan &p, int *launches, cudaStream_t st)
 {
-    static std::atomic<unsigned long long> allowed;
-    const auto kernel = gn_fused_bwd_kernel<kType, kV, kUni, kCodes>;
-    cudaError_t e = allow_fused((const void *)kernel, allowed);
-    if (e != cudaSuccess) return e;
-    a.cv = p.cv;
-    a.slots = p.slots;
-    a.chunks = p.chunks;
-    a.ranks = p.ranks;
-    a.vecs = p.vecs;
+    const auto kernel = gn_fused_bwd_kernel<kType, kV, kW, kCodes, kKeep>;
+    use_plan(a, p, kW);
     const bool together = a.n == 1 || (long long)a.n * p.ranks <= 8;   // all samples of a chunk in one cluster
     a.cluster = together ? a.n * p.ranks : p.ranks;
+    a.by_cluster = FastDiv(a.cluster);
+    static std::atomic<unsigned long long> allowed;
+    cudaError_t e = allow_smem((const void *)kernel, 200 * 1024, allowed);
+    if (e != cudaSuccess) return e;
     e = launch_chained_clusters(a.cluster, kernel, dim3((unsigned)((size_t)a.n * p.chunks * p.ranks)), dim3(kGnThreads), p.smem, st, a);
     ++*launches;
     if (e != cudaSuccess || together || (!a.dgamma && !a.dbeta)) return e;
@@ -191,18 +244,26 @@ cudaError_t launch(GnArgs a, const FusedPlan &p, int *launches, cudaStream_t st)
     return launch_gn_channel_sums(a, st);
 }
 
+template <int kType, int kV, int kW, bool kCodes>
+bool of_part(const GnArgs &a, cudaError_t *result, int *launches, cudaStream_t st)
+{
+    constexpr int kB = kV * Elem<kType>::kSize, kKept = kV * Elem<GnTypes<kType>::kY>::kSize + (kCodes ? kV + 1 : kB);
+    constexpr size_t kLimit = 56 * 1024;   // four blocks to an SM
+    FusedPlan p;
+    if (!fused_plan(p, a.n, a.hw, a.c, kV, a.cpg / kW * kV, kB, kKept, kLimit, [](int cv) { return BwdLayout<kV>::bytes(cv); })) return false;
+    *result = p.keep ? launch<kType, kV, kW, kCodes, true>(a, p, launches, st) : launch<kType, kV, kW, kCodes, false>(a, p, launches, st);
+    return true;
+}
+
 template <int kType, int kV, bool kCodes>
 bool of_width(const GnArgs &a, cudaError_t *result, int *launches, cudaStream_t st)
 {
-    constexpr int kE = Elem<kType>::kSize, kDyB = kV * Elem<GnTypes<kType>::kY>::kSize, kXB = kCodes ? kV : kV * kE;
-    const int unit = a.cpg / gcd_of(a.cpg, kV) * kV;
-    FusedPlan p;
-    if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kDyB + kXB + (kCodes ? 1 : 0), kV * kE, [&](int cv) { return BwdLayout<kV>::bytes(cv); }) ||
-        (size_t)a.n * p.chunks * p.ranks > 0x7fffffffull)
-        return false;
-    if (kV == 1 || a.cpg % kV == 0) *result = launch<kType, kV, true, kCodes>(a, p, launches, st);
-    else if constexpr (kV > 1) *result = launch<kType, kV, false, kCodes>(a, p, launches, st);
-    return true;
+    const int w = gcd_of(a.cpg, kV);
+    if constexpr (kV >= 4)
+        if (w == 4) return of_part<kType, kV, 4, kCodes>(a, result, launches, st);
+    if constexpr (kV >= 2)
+        if (w == 2) return of_part<kType, kV, 2, kCodes>(a, result, launches, st);
+    return of_part<kType, kV, 1, kCodes>(a, result, launches, st);
 }
 
 template <int kType, bool kCodes>
@@ -213,7 +274,9 @@ bool of_source(const GnArgs &a, cudaError_t *result, int *launches, cudaStream_t
         return a.c % v == 0 && a.dy_stride % v == 0 && a.dx_stride % v == 0 && (kCodes || (a.x_stride % v == 0 && aligned_at(a.x, v * kE))) &&
                aligned_at(a.codes, v) && aligned_at(a.dy, v * kY) && aligned_at(a.dx, v * kDx);
     };
-    if (of(GnTypes<kType>::kWide)) return of_width<kType, GnTypes<kType>::kWide, kCodes>(a, result, launches, st);
+    // (eight 16-bit channels a thread take more registers than four blocks on an SM leave: 145 us instead of 117 for 64 channels 112 x 112,
+    // 64 bf16 samples)
+    if (of(4)) return of_width<kType, 4, kCodes>(a, result, launches, st);
     if (of(2)) return of_width<kType, 2, kCodes>(a, result, launches, st);
     return of_width<kType, 1, kCodes>(a, result, launches, st);
 }

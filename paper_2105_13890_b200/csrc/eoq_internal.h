@@ -543,6 +543,16 @@ struct CkptWgradArgs {
 size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in);
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st);
 
+// Division by a number that a launch keeps: exact as long as dividend times divisor stays below 2^32.
+struct FastDiv {
+    unsigned d, m;
+    FastDiv() = default;
+    explicit FastDiv(unsigned div) : d(div), m(div > 1 ? 0xffffffffu / div + 1u : 0u) {}
+#ifdef __CUDACC__
+    __device__ __forceinline__ int operator()(int v) const { return d > 1 ? (int)__umulhi((unsigned)v, m) : v; }
+#endif
+};
+
 // One call of eoq_gn_fwd or eoq_gn_bwd; the fields of the second group are filled in by its launcher.
 struct GnArgs {
     const void *x, *dy;
@@ -562,12 +572,13 @@ struct GnArgs {
 
     float2 *part, *means;               // workspace
     int cv, slots, splits, per_split;   // lanes of a chunk of channels, pixels at a time, pixel ranges of a sample, pixels of a range
-    // the one-pass kernels: chunks of channels, blocks of a cluster, of them those of a sample, vectors of a thread
-    int chunks, cluster, ranks, vecs;
+    // the one-launch kernels: chunks of channels, blocks of a cluster, of them those of a sample
+    int chunks, cluster, ranks, vecs, per;   // vecs: vectors of a thread; per: pixels of a block
+    FastDiv by_cv, by_cpg, by_part, by_slots, by_chunks, by_ranks, by_cluster;   // by_part: cells of a group in a pixel
 };
 size_t gn_workspace_bytes(const eoq_gn_desc_t &d);
 cudaError_t launch_gn_channel_sums(GnArgs a, cudaStream_t st);   // dgamma, dbeta from part [n][c]
-// The forms that read every element once (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu); false when a sample's chunk of groups does not fit.
+// The forms in one launch (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu); false when a group is wider than a thread block.
 bool gn_fused_fwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
 bool gn_fused_bwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
 cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
