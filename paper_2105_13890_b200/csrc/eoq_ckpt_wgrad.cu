@@ -5,9 +5,16 @@
 // (11 = 8 + 3 and 24 = 8 + 8 + 8 bits), and every part is an operand of its own: products are exact whatever the type, sums are fp32.
 //
 // The reduction runs over rows, the slow axis of both operands, so both are MN-major tiles [rows][64 columns], 128 bytes a row,
-// swizzled.  Eight warps read dy and codes from global memory a stage ahead into registers, convert and write the tiles; one warp issues
-// the MMAs; the eight store the accumulators.  Row ranges are split over blocks where there are few tiles; their sums stand side by
-// side in the workspace and a second kernel adds them in a fixed order.  All waits are bounded.
+// swizzled.  Roles: eight warps bring dy and codes in (asynchronous copies, three stages ahead), convert and write the operand tiles; one
+// warp issues the MMAs; four move the accumulator on.  Row ranges are split over blocks where there are few tiles; their sums stand side
+// by side in the workspace and a second kernel adds them in a fixed order.  All waits are bounded.
+//
+// The tensor core adds to its fp32 accumulator without rounding to nearest: sums lose about 2^-27 of themselves with every step of 16
+// rows, always towards zero (16,384 rows: 8e-6 of the result's norm).  So every kSteps steps the accumulator is added to a second one in
+// tensor memory, in ordinary fp32 additions, and starts again: 5e-7, as a library product in fp32.
+//
+// A copied chunk is only ever read back by the thread that copied it.  Where rows are not 16-byte aligned, the aligned words around a
+// chunk are copied and shifted into place; a word is only touched when it holds part of the row.
 #include "eoq_block8.cuh"
 #include "eoq_epilogue.cuh"
 
@@ -15,11 +22,11 @@ namespace eoq {
 
 namespace {
 
-constexpr int kProducers = 256;             // threads of the eight warps
-constexpr int kThreads = kProducers + 32;   // and the MMA warp, the last one
-constexpr int kRows = 64;                   // rows of a stage
-constexpr int kSub = kRows * 128;           // bytes of a tile of 64 columns
-constexpr int kStagesMax = 4;
+constexpr int kProducers = 256;                  // threads of the eight warps
+constexpr int kMmaWarp = kProducers / 32;        // then the MMA warp, then four that move the accumulator on
+constexpr int kThreads = kProducers + 32 + 128;
+constexpr int kAhead = 3;                        // stages that copies run ahead
+constexpr int kSteps = 64;                       // MMA steps before the accumulator moves on
 
 // bf16 parts that hold an error of the type
 template <int kType> struct DyParts;
@@ -27,11 +34,53 @@ template <> struct DyParts<EOQ_BF16> { static constexpr int kParts = 1; };
 template <> struct DyParts<EOQ_F16> { static constexpr int kParts = 2; };
 template <> struct DyParts<EOQ_F32> { static constexpr int kParts = 3; };
 
+// Shapes and shared memory of a kernel.  Errors in bf16 with aligned rows are copied straight into their operand tiles.
+template <int kType, int kN, bool kWide>
+struct Shape {
+    static constexpr int kE = Elem<kType>::kSize, kParts = DyParts<kType>::kParts;
+    static constexpr bool kDirect = kType == EOQ_BF16 && kWide;
+    static constexpr int kRows = kDirect ? 64 : 32;                      // rows of a stage
+    static constexpr int kSub = kRows * 128;                             // bytes of a tile of 64 columns
+    static constexpr int kATile = kTileM / 64 * kSub, kA = kParts * kATile, kB = kN / 64 * kSub;
+    static constexpr int kASlots = kDirect ? kAhead + 2 : 2, kBSlots = 2, kRaw = kAhead + 1;
+    static constexpr int kDyLanes = kTileM / 8, kXLanes = kN / 16;       // threads of a row: eight errors, 16 codes each
+    static constexpr int kDy = kDyLanes * kRows / kProducers, kX = (kXLanes * kRows + kProducers - 1) / kProducers;
+    // words of a chunk as copied: an unaligned one of 16 bytes touches five
+    static constexpr int kDyWords = kDirect ? 0 : kE == 4 ? 8 : kWide ? 4 : 5, kXWords = kWide ? 4 : 5;
+    static constexpr int kRawBytes = kProducers * 4 * (kDy * kDyWords + kX * kXWords);
+    static constexpr int kBytes = kASlots * kA + kBSlots * kB + kRaw * kRawBytes + 1024;
+    static constexpr int kChunk = kSteps / (kRows / 16 * kParts);        // stages before the accumulator moves on
+    static constexpr int kBars = 5;                                      // stages that barriers tell apart
+};
+
 // byte offset of eight columns (16 bytes) of a row within an operand tile
+template <int kSub>
 __device__ __forceinline__ uint32_t tile_at(int col8, int row)
 {
     return (uint32_t)((col8 >> 3) * kSub + row * 128 + (((col8 & 7) ^ (row & 7)) << 4));
 }
+// asynchronous copies that write zeros where `in` is false
+__device__ __forceinline__ void copy_16(uint32_t to, const void *from, bool in)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_4(uint32_t to, const void *from, bool in)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(in ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+          "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+          "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+          "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void st_shared_128(uint32_t addr, uint4 v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -55,188 +104,241 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t halves, __nv_bfloat162 st
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// What a thread carries of a stage: kDy chunks of eight errors and kX chunks of 16 codes, rows apart.
+// What a thread of the eight warps does to a stage.
 template <int kType, int kN, bool kWide>
-struct StageRegs {
-    static constexpr int kE = Elem<kType>::kSize;
-    static constexpr int kDy = kTileM / 8 * kRows / kProducers;     // 4
-    static constexpr int kXLanes = kN / 16, kX = kXLanes * kRows / kProducers;
-    uint4 dy[kDy][kE / 2];
-    uint4 x[kX];
-    uint32_t s[kX];
+struct Feeder {
+    using S = Shape<kType, kN, kWide>;
+    const CkptWgradArgs &a;
+    size_t row_begin, row_end;
+    int o, i;            // first error and first code of the thread's chunks
+    uint32_t raw;        // its first copied word in shared memory: word j of chunk k at (k * words + j) * kProducers
+    uint32_t a_base;
 
-    __device__ __forceinline__ void load(const CkptWgradArgs &a, size_t row0, size_t row_end, int o0, int i0)
+    __device__ __forceinline__ Feeder(const CkptWgradArgs &args, size_t begin, size_t end, int o0, int i0, uint32_t smem_base)
+        : a(args), row_begin(begin), row_end(end), o(o0 + (int)(threadIdx.x % S::kDyLanes) * 8), i(i0 + (int)(threadIdx.x % S::kXLanes) * 16),
+          raw(smem_base + S::kASlots * S::kA + S::kBSlots * S::kB + threadIdx.x * (kWide ? 16 : 4)), a_base(smem_base)
     {
-        const int t = threadIdx.x;
-        const int o = o0 + (t % (kTileM / 8)) * 8;
+    }
+    static __device__ __forceinline__ int dy_row(int k) { return threadIdx.x / S::kDyLanes + k * (kProducers / S::kDyLanes); }
+    static __device__ __forceinline__ int x_row(int k) { return threadIdx.x / S::kXLanes + k * (kProducers / S::kXLanes); }
+    // (kN = 64 has fewer chunks of codes in a stage of 32 rows than there are threads)
+    static __device__ __forceinline__ bool x_mine() { return S::kXLanes * S::kRows >= kProducers || (int)threadIdx.x < S::kXLanes * S::kRows; }
+
+    // words from `row` + `offset` bytes on, of which those up to `end` hold something; word j goes to at + j * kProducers * 4
+    template <int kWords>
+    __device__ __forceinline__ void copy_words(uint32_t at, const char *row, size_t offset, size_t end, bool in) const
+    {
+        const uintptr_t first = reinterpret_cast<uintptr_t>(row) + offset, last = reinterpret_cast<uintptr_t>(row) + end;
+        const uintptr_t p = first & ~(uintptr_t)3;
 #pragma unroll
-        for (int k = 0; k < kDy; ++k) {
-            const size_t r = row0 + t / (kTileM / 8) + k * (kProducers / (kTileM / 8));
-            const char *src = reinterpret_cast<const char *>(a.dy) + (r * a.dy_stride + o) * kE;
-#pragma unroll
-            for (int j = 0; j < kE / 2; ++j) dy[k][j] = make_uint4(0, 0, 0, 0);
-            if (r < row_end && o < a.c_out) {
-                if (kWide) {
-#pragma unroll
-                    for (int j = 0; j < kE / 2; ++j) dy[k][j] = __ldg(reinterpret_cast<const uint4 *>(src) + j);
-                } else {
-                    uint32_t w[4 * (kE / 2)];
-#pragma unroll
-                    for (int j = 0; j < 2 * kE; ++j) w[j] = 0;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (o + j < a.c_out) {
-                            if (kE == 2) w[j / 2] |= (uint32_t)__ldg(reinterpret_cast<const uint16_t *>(src) + j) << (16 * (j & 1));
-                            else w[j % (2 * kE)] = __ldg(reinterpret_cast<const uint32_t *>(src) + j);
-                        }
-#pragma unroll
-                    for (int j = 0; j < kE / 2; ++j) dy[k][j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-                }
-            }
-        }
-        const int i = i0 + (t % kXLanes) * 16;
-#pragma unroll
-        for (int k = 0; k < kX; ++k) {
-            const size_t r = row0 + t / kXLanes + k * (kProducers / kXLanes);
-            x[k] = make_uint4(0, 0, 0, 0);
-            s[k] = 1;
-            if (r < row_end && i < a.c_in) {
-                const int8_t *src = a.codes + r * a.c_in + i;
-                if (kWide) x[k] = __ldg(reinterpret_cast<const uint4 *>(src));
-                else {
-                    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (i + j < a.c_in) w[j / 4] |= (uint32_t)(uint8_t)__ldg(src + j) << (8 * (j & 3));
-                    x[k] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                s[k] = __ldg(a.exps + r * a.blocks + i / kBlock8);
-            }
+        for (int j = 0; j < kWords; ++j) {
+            const bool has = in && p + 4 * j < last;
+            copy_4(at + j * kProducers * 4, reinterpret_cast<const void *>(has ? p + 4 * j : reinterpret_cast<uintptr_t>(a.codes) & ~(uintptr_t)3), has);
         }
     }
 
-    // converts and writes the stage's tiles: the parts of dy one after the other at `at`, then x
-    __device__ __forceinline__ void store(uint32_t at) const
+    // starts the copies of stage `it`; s: the bytes of its chunks of codes (loaded, on their way)
+    __device__ __forceinline__ void start(int it, int stages, uint32_t (&s)[S::kX]) const
     {
-        constexpr int kParts = DyParts<kType>::kParts;
-        const int t = threadIdx.x;
+        if (it < stages) {
+            const size_t r0 = row_begin + (size_t)it * S::kRows;
+            uint32_t at = raw + (it % S::kRaw) * S::kRawBytes;
 #pragma unroll
-        for (int k = 0; k < kDy; ++k) {
-            const uint32_t dst = at + tile_at(t % (kTileM / 8), t / (kTileM / 8) + k * (kProducers / (kTileM / 8)));
-            if (kType == EOQ_BF16) {
-                st_shared_128(dst, dy[k][0]);
-            } else {
-                float v[8];
-                if (kE == 2) {
-                    Raw<16> r;
-                    r.w = dy[k][0];
-                    Elem<EOQ_F16>::to_f32(r, v);
+            for (int k = 0; k < S::kDy; ++k) {
+                const size_t r = r0 + dy_row(k);
+                const bool in = r < row_end && o < a.c_out;
+                const char *row = reinterpret_cast<const char *>(a.dy) + (in ? r * a.dy_stride * S::kE : 0);
+                const size_t off = in ? (size_t)o * S::kE : 0;
+                if constexpr (S::kDirect) {
+                    copy_16(a_base + (it % S::kASlots) * S::kA + tile_at<S::kSub>(threadIdx.x % S::kDyLanes, dy_row(k)), row + off, in);
+                } else if constexpr (kWide) {
+#pragma unroll
+                    for (int j = 0; j < S::kDyWords / 4; ++j) copy_16(at + j * kProducers * 16, row + off + 16 * j, in);
+                    at += S::kDyWords * kProducers * 4;
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        v[4 * j] = __uint_as_float(dy[k][j % (kE / 2)].x);
-                        v[4 * j + 1] = __uint_as_float(dy[k][j % (kE / 2)].y);
-                        v[4 * j + 2] = __uint_as_float(dy[k][j % (kE / 2)].z);
-                        v[4 * j + 3] = __uint_as_float(dy[k][j % (kE / 2)].w);
-                    }
+                    copy_words<S::kDyWords>(at, row, off, (size_t)a.c_out * S::kE, in);
+                    at += S::kDyWords * kProducers * 4;
                 }
+            }
 #pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    uint32_t w[4];
+            for (int k = 0; k < S::kX; ++k) {
+                const size_t r = r0 + x_row(k);
+                const bool in = x_mine() && r < row_end && i < a.c_in;
+                const char *row = reinterpret_cast<const char *>(a.codes) + (in ? r * a.c_in : 0);
+                if constexpr (kWide) copy_16(at, row + (in ? i : 0), in);
+                else copy_words<S::kXWords>(at, row, i, a.c_in, in);
+                at += S::kXWords * kProducers * 4;
+                s[k] = in ? __ldg(a.exps + r * a.blocks + i / kBlock8) : 1u;
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    template <int kWords>
+    __device__ __forceinline__ void copied(uint32_t at, uint32_t (&w)[kWords]) const
+    {
+        if constexpr (kWide) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) w[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
-                    st_shared_128(dst + p * (kTileM / 64 * kSub), make_uint4(w[0], w[1], w[2], w[3]));
-                    // what the upper halves leave: exact; nothing of an infinity
+            for (int j = 0; j < kWords; j += 4) {
+                const int4 v = ptx::ld_shared_128(at + j / 4 * kProducers * 16);
+                w[j] = v.x;
+                w[j + 1] = v.y;
+                w[j + 2] = v.z;
+                w[j + 3] = v.w;
+            }
+        } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                        v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
+            for (int j = 0; j < kWords; ++j) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[j]) : "r"(at + j * kProducers * 4) : "memory");
+        }
+    }
+    // five aligned words to the 16 bytes that begin `bytes` into the first
+    static __device__ __forceinline__ uint4 shifted(const uint32_t (&w)[5], uint32_t bytes)
+    {
+        const uint32_t n = 8 * bytes;
+        return make_uint4(__funnelshift_r(w[0], w[1], n), __funnelshift_r(w[1], w[2], n), __funnelshift_r(w[2], w[3], n), __funnelshift_r(w[3], w[4], n));
+    }
+
+    // converts stage `it`, whose copies have arrived, into its operand tiles
+    __device__ __forceinline__ void convert(int it, const uint32_t (&s)[S::kX]) const
+    {
+        uint32_t at = raw + (it % S::kRaw) * S::kRawBytes;
+        const size_t r0 = row_begin + (size_t)it * S::kRows;
+        if constexpr (!S::kDirect) {
+            const uint32_t a_tile = a_base + (it % S::kASlots) * S::kA;
+#pragma unroll
+            for (int k = 0; k < S::kDy; ++k) {
+                uint32_t w[S::kDyWords];
+                copied(at, w);
+                at += S::kDyWords * kProducers * 4;
+                const uint32_t dst = a_tile + tile_at<S::kSub>(threadIdx.x % S::kDyLanes, dy_row(k));
+                uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
+                if constexpr (S::kDyWords == 5) {
+                    const uintptr_t p = reinterpret_cast<uintptr_t>(a.dy) + ((r0 + dy_row(k)) * a.dy_stride + o) * S::kE;
+                    c = shifted(w, (uint32_t)p & 3u);
+                }
+                if constexpr (kType == EOQ_BF16) {
+                    st_shared_128(dst, c);
+                } else {
+                    float v[8];
+                    if constexpr (S::kE == 2) {
+                        Raw<16> r;
+                        r.w = c;
+                        Elem<EOQ_F16>::to_f32(r, v);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+                    }
+#pragma unroll
+                    for (int p = 0; p < S::kParts; ++p) {
+                        uint32_t h[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) h[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
+                        st_shared_128(dst + p * S::kATile, make_uint4(h[0], h[1], h[2], h[3]));
+                        // what the upper halves leave: exact; nothing of an infinity
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                            v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
+                        }
                     }
                 }
             }
         }
-        const uint32_t at_x = at + kParts * (kTileM / 64 * kSub);
+        const uint32_t b_tile = a_base + S::kASlots * S::kA + (it % S::kBSlots) * S::kB;
+        if (!x_mine()) return;
 #pragma unroll
-        for (int k = 0; k < kX; ++k) {
-            const int g = t % kXLanes, row = t / kXLanes + k * (kProducers / kXLanes);
+        for (int k = 0; k < S::kX; ++k) {
+            uint32_t w[S::kXWords];
+            copied(at, w);
+            at += S::kXWords * kProducers * 4;
+            const int g = threadIdx.x % S::kXLanes, row = x_row(k);
+            uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
+            if constexpr (S::kXWords == 5) c = shifted(w, (uint32_t)(reinterpret_cast<uintptr_t>(a.codes) + (r0 + row) * a.c_in + i) & 3u);
             const uint32_t sw = s[k] << 7 | s[k] << 23;
             const __nv_bfloat162 step = *reinterpret_cast<const __nv_bfloat162 *>(&sw);
-            const uint32_t c[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-            uint4 half[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                half[h] = make_uint4(two_codes(__byte_perm(c[2 * h], 0, 0x4140), step), two_codes(__byte_perm(c[2 * h], 0, 0x4342), step),
-                                     two_codes(__byte_perm(c[2 * h + 1], 0, 0x4140), step), two_codes(__byte_perm(c[2 * h + 1], 0, 0x4342), step));
+            const uint4 lo = make_uint4(two_codes(__byte_perm(c.x, 0, 0x4140), step), two_codes(__byte_perm(c.x, 0, 0x4342), step),
+                                        two_codes(__byte_perm(c.y, 0, 0x4140), step), two_codes(__byte_perm(c.y, 0, 0x4342), step));
+            const uint4 hi = make_uint4(two_codes(__byte_perm(c.z, 0, 0x4140), step), two_codes(__byte_perm(c.z, 0, 0x4342), step),
+                                        two_codes(__byte_perm(c.w, 0, 0x4140), step), two_codes(__byte_perm(c.w, 0, 0x4342), step));
             // neighbouring tiles begin at the same bank: every other one takes its odd chunks first
             const int first = (g >> 2) & 1;
-            st_shared_128(at_x + tile_at(2 * g + first, row), first ? half[1] : half[0]);
-            st_shared_128(at_x + tile_at(2 * g + 1 - first, row), first ? half[0] : half[1]);
+            st_shared_128(b_tile + tile_at<S::kSub>(2 * g + first, row), first ? hi : lo);
+            st_shared_128(b_tile + tile_at<S::kSub>(2 * g + 1 - first, row), first ? lo : hi);
         }
     }
-};
-
-template <int kType, int kN> struct StageSize {
-    static constexpr uint32_t kA = DyParts<kType>::kParts * (kTileM / 64) * kSub, kBytes = kA + kN / 64 * kSub;
-    static constexpr int kFit = (int)((200u * 1024u) / kBytes), kStages = kFit < kStagesMax ? kFit : kStagesMax;
 };
 
 template <int kType, int kN, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_constant__ CkptWgradArgs a)
 {
-    using Size = StageSize<kType, kN>;
-    constexpr int kStages = Size::kStages, kParts = DyParts<kType>::kParts;
+    using S = Shape<kType, kN, kWide>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStagesMax + 1];
+    __shared__ __align__(8) uint64_t bars[2 * S::kBars + 3];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t abort_s;
 
     const int warp = warp_index_uniform(), lane = threadIdx.x & 31;
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = ptx::smem_u32(bars);
-    auto full_bar = [&](int s) { return bar0 + 8u * s; };
-    auto empty_bar = [&](int s) { return bar0 + 8u * (kStagesMax + s); };
-    const uint32_t done_bar = bar0 + 8u * (2 * kStagesMax);
+    // of stage `it`: operands written; MMAs done.  Of the chunks of steps: sums complete; sums moved on.  All done.
+    auto full_bar = [&](int it) { return bar0 + 8u * (it % S::kBars); };
+    auto done_bar = [&](int it) { return bar0 + 8u * (S::kBars + it % S::kBars); };
+    auto parity = [](int it) { return (uint32_t)(it / S::kBars) & 1u; };
+    const uint32_t sums_bar = bar0 + 8u * (2 * S::kBars), moved_bar = sums_bar + 8, end_bar = sums_bar + 16;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < S::kBars; ++s) {
             ptx::mbar_init(full_bar(s), kProducers / 32);
-            ptx::mbar_init(empty_bar(s), 1);
+            ptx::mbar_init(done_bar(s), 1);
         }
-        ptx::mbar_init(done_bar, 1);
+        ptx::mbar_init(sums_bar, 1);
+        ptx::mbar_init(moved_bar, 4);
+        ptx::mbar_init(end_bar, 1);
         abort_s = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == kProducers / 32) {
-        ptx::tmem_alloc(ptx::smem_u32(&tmem_base_s), kN);
+    if (warp == kMmaWarp) {
+        ptx::tmem_alloc(ptx::smem_u32(&tmem_base_s), 2 * kN);
         ptx::tmem_relinquish();
     }
     const int tiles = a.m_tiles * a.n_tiles, split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
     const int o0 = tile / a.n_tiles * kTileM, i0 = tile % a.n_tiles * kN;
     const size_t row_begin = (size_t)split * a.rows_per_split, row_end = min(a.rows, row_begin + a.rows_per_split);
-    const int stages = (int)((row_end - row_begin + kRows - 1) / kRows);
+    const int stages = (int)((row_end - row_begin + S::kRows - 1) / S::kRows), chunks = (stages + S::kChunk - 1) / S::kChunk;
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
-    const uint32_t tmem_base = tmem_base_s;
+    const uint32_t tmem_base = tmem_base_s, tmem_run = tmem_base + kN;
     const RoleCtx ctx{&abort_s, a.dev};
 
-    if (warp < kProducers / 32) {
-        StageRegs<kType, kN, kWide> cur, next;
-        cur.load(a, row_begin, row_end, o0, i0);
-        int stage = 0;
-        uint32_t phase = 0;
-        for (int it = 0; it < stages; ++it) {
-            if (it + 1 < stages) next.load(a, row_begin + (size_t)(it + 1) * kRows, row_end, o0, i0);
-            if (!__all_sync(0xffffffffu, wait_bar(empty_bar(stage), phase ^ 1u, ctx))) break;
-            cur.store(smem_base + stage * Size::kBytes);
+    if (warp < kMmaWarp) {
+        const Feeder<kType, kN, kWide> feed(a, row_begin, row_end, o0, i0, smem_base);
+        uint32_t s[kAhead + 1][S::kX];
+        feed.start(0, stages, s[0]);
+        feed.start(1, stages, s[1]);
+        feed.start(2, stages, s[2]);
+        static_assert(kAhead == 3, "three stages ahead");
+        bool ok = true;
+        auto turn = [&](int it, const uint32_t (&now)[S::kX], uint32_t (&later)[S::kX]) {
+            // stage it - 2 has left the tiles that stage `it` and, three ahead, its errors go to
+            if (it >= 2) ok = __all_sync(0xffffffffu, wait_bar(done_bar(it - 2), parity(it - 2), ctx));
+            if (!ok) return;
+            feed.start(it + kAhead, stages, later);
+            asm volatile("cp.async.wait_group 3;" ::: "memory");
+            feed.convert(it, now);
             ptx::fence_proxy_async();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full_bar(stage));
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
-            cur = next;
+            if (lane == 0) ptx::mbar_arrive(full_bar(it));
+        };
+        for (int it = 0; it < stages && ok; it += 4) {
+            turn(it, s[0], s[3]);
+            if (ok && it + 1 < stages) turn(it + 1, s[1], s[0]);
+            if (ok && it + 2 < stages) turn(it + 2, s[2], s[1]);
+            if (ok && it + 3 < stages) turn(it + 3, s[3], s[2]);
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         // a row of the tile a lane; two warps share 32 rows, half of the columns each
         const int quad = warp & 3, o = o0 + quad * 32 + lane;
-        const bool ok = __all_sync(0xffffffffu, wait_bar<64>(done_bar, 0, ctx));
+        ok = __all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx));
         if (ok) {
             ptx::tc_fence_after();
             float *dst = a.out + (size_t)split * a.c_out * a.c_in + (size_t)o * a.c_in;
@@ -246,6 +348,13 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
                 uint32_t r[32];
                 ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(quad * 32) << 16) + c0, r);
                 ptx::tmem_ld_wait();
+                if (chunks > 1) {
+                    uint32_t run[32];
+                    ptx::tmem_ld_32x32(tmem_run + ((uint32_t)(quad * 32) << 16) + c0, run);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
+                }
                 if (o < a.c_out) {
                     if (a.c_in % 4 == 0) {
 #pragma unroll
@@ -260,40 +369,70 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
                 }
             }
         }
-    } else {
+    } else if (warp == kMmaWarp) {
         const uint32_t leader = elect_one();
         // fp32 accumulator, bf16 operands, both MN-major
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
-        const uint64_t proto = make_smem_desc(0, kSub, 1024, 2);
+        const uint64_t proto = make_smem_desc(0, S::kSub, 1024, 2);
         const uint32_t hi = (uint32_t)(proto >> 32), lead = (uint32_t)proto;
-        int stage = 0;
-        uint32_t phase = 0, accumulate = 0;
         bool ok = true;
+        int chunk = 0, in_chunk = 0;
         for (int it = 0; it < stages; ++it) {
-            if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(stage), phase, ctx)))) break;
+            if (in_chunk == S::kChunk) {   // hand the sums over and wait until they have been taken
+                ptx::mma_commit(sums_bar, leader);
+                if (!(ok = __all_sync(0xffffffffu, wait_bar(moved_bar, chunk & 1, ctx)))) break;
+                ptx::tc_fence_after();
+                ++chunk;
+                in_chunk = 0;
+            }
+            if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(it), parity(it), ctx)))) break;
             ptx::tc_fence_after();
-            const uint32_t a16 = ((smem_base + stage * Size::kBytes) >> 4) | lead, b16 = ((smem_base + stage * Size::kBytes + Size::kA) >> 4) | lead;
+            const uint32_t a16 = ((smem_base + (it % S::kASlots) * S::kA) >> 4) | lead;
+            const uint32_t b16 = ((smem_base + S::kASlots * S::kA + (it % S::kBSlots) * S::kB) >> 4) | lead;
 #pragma unroll
-            for (int k = 0; k < kRows / 16; ++k)
+            for (int k = 0; k < S::kRows / 16; ++k)
 #pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    mma_bf16(tmem_base, smem_desc_join(a16 + p * ((kTileM / 64 * kSub) >> 4) + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc,
-                             accumulate, leader);
-                    accumulate = 1;
-                }
-            ptx::mma_commit(empty_bar(stage), leader);
-            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                for (int p = 0; p < S::kParts; ++p)
+                    mma_bf16(tmem_base, smem_desc_join(a16 + p * (S::kATile >> 4) + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc,
+                             (k | p | in_chunk) != 0 ? 1u : 0u, leader);
+            ptx::mma_commit(done_bar(it), leader);
+            ++in_chunk;
         }
-        ptx::mma_commit(done_bar, leader);
+        ptx::mma_commit(end_bar, leader);
         if (!ok)
             for (uint32_t i = 0; i < kSpinLimit; ++i)
-                if (ptx::mbar_try_wait(done_bar, 0)) break;
+                if (ptx::mbar_try_wait(end_bar, 0)) break;
+    } else {
+        const int quad = warp & 3;
+        const uint32_t row = (uint32_t)(quad * 32) << 16;
+        for (int chunk = 0; chunk + 1 < chunks; ++chunk) {
+            if (!__all_sync(0xffffffffu, wait_bar<64>(sums_bar, chunk & 1, ctx))) break;
+            ptx::tc_fence_after();
+#pragma unroll 1
+            for (int c0 = 0; c0 < kN; c0 += 32) {
+                uint32_t r[32];
+                ptx::tmem_ld_32x32(tmem_base + row + c0, r);
+                ptx::tmem_ld_wait();
+                if (chunk) {
+                    uint32_t run[32];
+                    ptx::tmem_ld_32x32(tmem_run + row + c0, run);
+                    ptx::tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
+                }
+                tmem_st_32x32(tmem_run + row + c0, r);
+            }
+            tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(moved_bar);
+        }
     }
     ptx::tc_fence_before();
     __syncthreads();
-    if (warp == kProducers / 32) {
+    if (warp == kMmaWarp) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem_base, kN);
+        ptx::tmem_dealloc(tmem_base, 2 * kN);
     }
 }
 
@@ -316,6 +455,8 @@ __global__ void __launch_bounds__(256) ckpt_wgrad_join_kernel(const float *__res
     }
 }
 
+constexpr int kPlanRows = 64;   // (whole stages of every kernel)
+
 struct WgradPlan8 {
     int n_tile, m_tiles, n_tiles, splits;
     size_t rows_per_split;
@@ -327,20 +468,20 @@ WgradPlan8 plan_of(size_t rows, int c_out, int c_in)
     p.n_tile = c_in <= 64 ? 64 : c_in <= 128 ? 128 : 256;
     p.m_tiles = (c_out + kTileM - 1) / kTileM;
     p.n_tiles = (c_in + p.n_tile - 1) / p.n_tile;
-    const size_t tiles = (size_t)p.m_tiles * p.n_tiles, stages = (rows + kRows - 1) / kRows;
+    const size_t tiles = (size_t)p.m_tiles * p.n_tiles, stages = (rows + kPlanRows - 1) / kPlanRows;
     size_t splits = tiles < (size_t)kPartSms ? kPartSms / tiles : 1;
     if (splits > stages) splits = stages;
     const size_t per = (stages + splits - 1) / splits;
     p.splits = (int)((stages + per - 1) / per);
-    p.rows_per_split = per * kRows;
+    p.rows_per_split = per * kPlanRows;
     return p;
 }
 
 template <int kType, int kN, bool kWide>
 cudaError_t launch(const CkptWgradArgs &a, int grid, cudaStream_t st)
 {
-    using Size = StageSize<kType, kN>;
-    constexpr int bytes = Size::kBytes * Size::kStages + 1024;
+    constexpr int bytes = Shape<kType, kN, kWide>::kBytes;
+    static_assert(bytes <= 227 * 1024, "shared memory of a block");
     static std::atomic<unsigned long long> allowed;
     const cudaError_t e = allow_smem((const void *)ckpt_wgrad_kernel<kType, kN, kWide>, bytes, allowed);
     if (e != cudaSuccess) return e;
