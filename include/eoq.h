@@ -450,7 +450,7 @@ EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_
  * eoq_set_gemm_ctas does not apply.  16-byte aligned tensors with c_out a multiple of 8, c_in of 16 and dy_stride of 16 bytes run
  * several times faster.
  * Errors: BAD_ARG (null pointer, non-positive size, dy_stride < c_out, unknown type, the handle's device not the current one),
- * ALIGNMENT, UNSUPPORTED (rows > 2^36, c_out or c_in > 2^20), WORKSPACE.
+ * ALIGNMENT, UNSUPPORTED (rows > 2^30, c_out or c_in > 2^20), WORKSPACE.
  */
 EOQ_API int eoq_ckpt_wgrad_workspace_size(size_t rows, int c_out, int c_in, int dtype, size_t *bytes);
 EOQ_API int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_t rows, int c_out, size_t dy_stride, const int8_t *codes,

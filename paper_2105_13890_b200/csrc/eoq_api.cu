@@ -2298,7 +2298,7 @@ static int ckpt_wgrad_check(size_t rows, int c_out, int c_in, int dtype)
 {
     if (rows == 0 || c_out <= 0 || c_in <= 0 || dtype < EOQ_F32 || dtype > EOQ_BF16) return EOQ_ERR_BAD_ARG;
     // (tiles of 128 x 256 where either is this long: at most 2^25 of them, and splits only below 148)
-    if (rows > (size_t)1 << 36 || c_out > 1 << 20 || c_in > 1 << 20) return EOQ_ERR_UNSUPPORTED;
+    if (rows > (size_t)1 << 30 || c_out > 1 << 20 || c_in > 1 << 20) return EOQ_ERR_UNSUPPORTED;
     return EOQ_OK;
 }
 

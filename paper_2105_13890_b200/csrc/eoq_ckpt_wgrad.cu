@@ -5,7 +5,7 @@
 // (11 = 8 + 3 and 24 = 8 + 8 + 8 bits), and every part is an operand of its own: products are exact whatever the type, sums are fp32.
 //
 // The reduction runs over rows, the slow axis of both operands, so both are MN-major tiles [rows][64 columns], 128 bytes a row,
-// swizzled.  Roles: eight warps bring dy and codes in (asynchronous copies, three stages ahead), convert and write the operand tiles; one
+// swizzled.  Roles: sixteen warps bring dy and codes in (asynchronous copies, some stages ahead), convert and write the operand tiles; one
 // warp issues the MMAs; four move the accumulator on.  Row ranges are split over blocks where there are few tiles; their sums stand side
 // by side in the workspace and a second kernel adds them in a fixed order.  All waits are bounded.
 //
@@ -22,11 +22,11 @@ namespace eoq {
 
 namespace {
 
-constexpr int kProducers = 256;                  // threads of the eight warps
+constexpr int kProducers = 512;                  // threads of the sixteen warps
 constexpr int kMmaWarp = kProducers / 32;        // then the MMA warp, then four that move the accumulator on
 constexpr int kThreads = kProducers + 32 + 128;
-constexpr int kAhead = 3;                        // stages that copies run ahead
 constexpr int kSteps = 64;                       // MMA steps before the accumulator moves on
+constexpr int kMaxSmem = 226 * 1024;   // (of dynamic shared memory)
 
 // bf16 parts that hold an error of the type
 template <int kType> struct DyParts;
@@ -42,15 +42,21 @@ struct Shape {
     static constexpr int kRows = kDirect ? 64 : 32;                      // rows of a stage
     static constexpr int kSub = kRows * 128;                             // bytes of a tile of 64 columns
     static constexpr int kATile = kTileM / 64 * kSub, kA = kParts * kATile, kB = kN / 64 * kSub;
-    static constexpr int kASlots = kDirect ? kAhead + 2 : 2, kBSlots = 2, kRaw = kAhead + 1;
-    static constexpr int kDyLanes = kTileM / 8, kXLanes = kN / 16;       // threads of a row: eight errors, 16 codes each
-    static constexpr int kDy = kDyLanes * kRows / kProducers, kX = (kXLanes * kRows + kProducers - 1) / kProducers;
-    // words of a chunk as copied: an unaligned one of 16 bytes touches five
-    static constexpr int kDyWords = kDirect ? 0 : kE == 4 ? 8 : kWide ? 4 : 5, kXWords = kWide ? 4 : 5;
-    static constexpr int kRawBytes = kProducers * 4 * (kDy * kDyWords + kX * kXWords);
-    static constexpr int kBytes = kASlots * kA + kBSlots * kB + kRaw * kRawBytes + 1024;
+    // A thread's share of a stage: kDy times eight errors, and kCodes neighbouring codes of a row (of threads without any there may be some).
+    static constexpr int kDyLanes = kTileM / 8, kDyPass = kProducers / kDyLanes, kDy = kRows / kDyPass;
+    static constexpr int kCodes = kN * kRows / kProducers >= 32 ? 32 : 16, kXLanes = kN / kCodes;
+    static_assert(kDyPass % 8 == 0 && kDy * kDyPass == kRows, "rows of a thread's chunks share their swizzle");
+    static_assert(kXLanes * kRows <= kProducers, "one piece of codes a thread");
+    // words of a chunk as copied: an unaligned one of n words touches n + 1
+    static constexpr int kDyWords = kDirect ? 0 : kE == 4 ? 8 : kWide ? 4 : 5, kXWords = kCodes / 4 + (kWide ? 0 : 1);
+    static constexpr int kRawBytes = kProducers * 4 * (kDy * kDyWords + kXWords);
+    // Stages of operand tiles, of copies and of barriers, all of which divide four, so that a loop over four stages knows its slots.
+    // Copied errors run kAhead = 2 stages ahead of tiles that kOps = 2 stages are at work on.
+    static constexpr int kRing = 4;
+    static constexpr int size(int ops) { return (kDirect ? kRing : ops) * kA + ops * kB + kRing * kRawBytes + 1024; }
+    static constexpr int kOps = !kDirect && size(4) <= kMaxSmem ? 4 : 2, kASlots = kDirect ? kRing : kOps, kAhead = kDirect ? 2 : 3;
+    static constexpr int kBytes = size(kOps);
     static constexpr int kChunk = kSteps / (kRows / 16 * kParts);        // stages before the accumulator moves on
-    static constexpr int kBars = 5;                                      // stages that barriers tell apart
 };
 
 // byte offset of eight columns (16 bytes) of a row within an operand tile
@@ -104,74 +110,91 @@ __device__ __forceinline__ uint32_t two_codes(uint32_t halves, __nv_bfloat162 st
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// What a thread of the eight warps does to a stage.
+// What a thread of the sixteen warps does to a stage.
 template <int kType, int kN, bool kWide>
 struct Feeder {
     using S = Shape<kType, kN, kWide>;
-    const CkptWgradArgs &a;
-    size_t row_begin, row_end;
-    int o, i;            // first error and first code of the thread's chunks
-    uint32_t raw;        // its first copied word in shared memory: word j of chunk k at (k * words + j) * kProducers
-    uint32_t a_base;
+    const void *safe;
+    const char *dy, *x;                  // the thread's first chunks of the next stage to copy
+    const uint8_t *exps;
+    size_t dy_pass, dy_step, x_step, exps_step;   // to its next chunk, S::kDyPass rows on; to the next stage
+    int dy_left, x_left;                 // rows from that chunk to the end of the range; 0 where the columns are past the end
+    int dy_cols, x_cols;                 // bytes from the chunk to the end of its row
+    uint32_t smem, raw;                  // operand tiles; the thread's first copied word: word j of its chunks at j * kProducers
+    uint32_t dy_tile, x_tile;            // places of the first chunks in their tiles
+    uint32_t dy_bytes, x_bytes;          // addresses of the chunks to convert next, of which two bits count
 
-    __device__ __forceinline__ Feeder(const CkptWgradArgs &args, size_t begin, size_t end, int o0, int i0, uint32_t smem_base)
-        : a(args), row_begin(begin), row_end(end), o(o0 + (int)(threadIdx.x % S::kDyLanes) * 8), i(i0 + (int)(threadIdx.x % S::kXLanes) * 16),
-          raw(smem_base + S::kASlots * S::kA + S::kBSlots * S::kB + threadIdx.x * (kWide ? 16 : 4)), a_base(smem_base)
+    __device__ __forceinline__ Feeder(const CkptWgradArgs &a, size_t begin, size_t end, int o0, int i0, uint32_t smem_base)
+        : safe(a.safe), smem(smem_base), raw(smem_base + S::kASlots * S::kA + S::kOps * S::kB + threadIdx.x * (kWide ? 16 : 4))
     {
+        // Eight lanes that store together should meet eight different places of 16 bytes: of codes, the even (or a quarter of the) chunks
+        // of a tile's row, in neighbouring rows, which the swizzle turns against one another.
+        constexpr int kInTile = 64 / S::kCodes, kRowBits = 8 / kInTile;   // pieces of a row in a tile; rows of eight lanes
+        const int t = threadIdx.x, o8 = t % S::kDyLanes, dy_row = t / S::kDyLanes;
+        const int piece = t % kInTile + t / 8 % (S::kXLanes / kInTile) * kInTile, x_row = t / kInTile % kRowBits + t / (8 * (S::kXLanes / kInTile)) * kRowBits;
+        const int o = o0 + o8 * 8, i = i0 + piece * S::kCodes, rows = (int)(end - begin);
+        dy = reinterpret_cast<const char *>(a.dy) + ((begin + dy_row) * a.dy_stride + o) * S::kE;
+        x = reinterpret_cast<const char *>(a.codes) + (begin + x_row) * a.c_in + i;
+        exps = a.exps + (begin + x_row) * a.blocks + i / kBlock8;
+        dy_pass = (size_t)S::kDyPass * a.dy_stride * S::kE;
+        dy_step = (size_t)S::kRows * a.dy_stride * S::kE;
+        x_step = (size_t)S::kRows * a.c_in;
+        exps_step = (size_t)S::kRows * a.blocks;
+        dy_left = o < a.c_out ? rows - dy_row : 0;
+        x_left = i < a.c_in && x_row < S::kRows ? rows - x_row : 0;
+        dy_cols = (a.c_out - o) * S::kE;
+        x_cols = a.c_in - i;
+        dy_tile = tile_at<S::kSub>(o8, dy_row);
+        x_tile = x_row < S::kRows ? tile_at<S::kSub>(piece * (S::kCodes / 8), x_row) : ~0u;
+        dy_bytes = (uint32_t)reinterpret_cast<uintptr_t>(dy);
+        x_bytes = (uint32_t)reinterpret_cast<uintptr_t>(x);
     }
-    static __device__ __forceinline__ int dy_row(int k) { return threadIdx.x / S::kDyLanes + k * (kProducers / S::kDyLanes); }
-    static __device__ __forceinline__ int x_row(int k) { return threadIdx.x / S::kXLanes + k * (kProducers / S::kXLanes); }
-    // (kN = 64 has fewer chunks of codes in a stage of 32 rows than there are threads)
-    static __device__ __forceinline__ bool x_mine() { return S::kXLanes * S::kRows >= kProducers || (int)threadIdx.x < S::kXLanes * S::kRows; }
 
-    // words from `row` + `offset` bytes on, of which those up to `end` hold something; word j goes to at + j * kProducers * 4
+    // words that hold the bytes from p to p + valid; word j goes to at + j * kProducers * 4
     template <int kWords>
-    __device__ __forceinline__ void copy_words(uint32_t at, const char *row, size_t offset, size_t end, bool in) const
+    __device__ __forceinline__ void copy_words(uint32_t at, const char *p, int valid, bool in) const
     {
-        const uintptr_t first = reinterpret_cast<uintptr_t>(row) + offset, last = reinterpret_cast<uintptr_t>(row) + end;
-        const uintptr_t p = first & ~(uintptr_t)3;
+        const uintptr_t first = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3;
+        const int bytes = in ? valid + (int)(reinterpret_cast<uintptr_t>(p) & 3) : 0;
 #pragma unroll
         for (int j = 0; j < kWords; ++j) {
-            const bool has = in && p + 4 * j < last;
-            copy_4(at + j * kProducers * 4, reinterpret_cast<const void *>(has ? p + 4 * j : reinterpret_cast<uintptr_t>(a.codes) & ~(uintptr_t)3), has);
+            const bool has = 4 * j < bytes;
+            copy_4(at + j * kProducers * 4, has ? reinterpret_cast<const void *>(first + 4 * j) : safe, has);
+        }
+    }
+    // pieces of 16 bytes that hold the bytes from p to p + valid (a multiple of 16)
+    template <int kWords>
+    __device__ __forceinline__ void copy_wide(uint32_t at, const char *p, int valid, bool in) const
+    {
+#pragma unroll
+        for (int j = 0; j < kWords / 4; ++j) {
+            const bool has = in && (j == 0 || 16 * j < valid);
+            copy_16(at + j * kProducers * 16, has ? p + 16 * j : safe, has);
         }
     }
 
-    // starts the copies of stage `it`; s: the bytes of its chunks of codes (loaded, on their way)
-    __device__ __forceinline__ void start(int it, int stages, uint32_t (&s)[S::kX]) const
+    // starts the copies of the next stage, whose slot of the copies (and of copied errors) is `slot`; the byte of its codes is on its way
+    __device__ __forceinline__ void start(int slot, uint32_t &s)
     {
-        if (it < stages) {
-            const size_t r0 = row_begin + (size_t)it * S::kRows;
-            uint32_t at = raw + (it % S::kRaw) * S::kRawBytes;
+        uint32_t at = raw + slot * S::kRawBytes;
+        const char *p = dy;
 #pragma unroll
-            for (int k = 0; k < S::kDy; ++k) {
-                const size_t r = r0 + dy_row(k);
-                const bool in = r < row_end && o < a.c_out;
-                const char *row = reinterpret_cast<const char *>(a.dy) + (in ? r * a.dy_stride * S::kE : 0);
-                const size_t off = in ? (size_t)o * S::kE : 0;
-                if constexpr (S::kDirect) {
-                    copy_16(a_base + (it % S::kASlots) * S::kA + tile_at<S::kSub>(threadIdx.x % S::kDyLanes, dy_row(k)), row + off, in);
-                } else if constexpr (kWide) {
-#pragma unroll
-                    for (int j = 0; j < S::kDyWords / 4; ++j) copy_16(at + j * kProducers * 16, row + off + 16 * j, in);
-                    at += S::kDyWords * kProducers * 4;
-                } else {
-                    copy_words<S::kDyWords>(at, row, off, (size_t)a.c_out * S::kE, in);
-                    at += S::kDyWords * kProducers * 4;
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < S::kX; ++k) {
-                const size_t r = r0 + x_row(k);
-                const bool in = x_mine() && r < row_end && i < a.c_in;
-                const char *row = reinterpret_cast<const char *>(a.codes) + (in ? r * a.c_in : 0);
-                if constexpr (kWide) copy_16(at, row + (in ? i : 0), in);
-                else copy_words<S::kXWords>(at, row, i, a.c_in, in);
-                at += S::kXWords * kProducers * 4;
-                s[k] = in ? __ldg(a.exps + r * a.blocks + i / kBlock8) : 1u;
-            }
+        for (int k = 0; k < S::kDy; ++k, p += dy_pass) {
+            const bool in = k * S::kDyPass < dy_left;
+            if constexpr (S::kDirect) copy_16(smem + slot * S::kA + dy_tile + k * S::kDyPass * 128, in ? p : safe, in);
+            else if constexpr (kWide) copy_wide<S::kDyWords>(at, p, dy_cols, in);
+            else copy_words<S::kDyWords>(at, p, dy_cols, in);
+            at += S::kDyWords * kProducers * 4;
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        const bool in = x_left > 0;
+        if constexpr (kWide) copy_wide<S::kXWords>(at, x, x_cols, in);
+        else copy_words<S::kXWords>(at, x, x_cols, in);
+        s = in ? __ldg(exps) : 1u;
+        dy += dy_step;
+        x += x_step;
+        exps += exps_step;
+        dy_left -= S::kRows;
+        x_left -= S::kRows;
     }
 
     template <int kWords>
@@ -191,38 +214,33 @@ struct Feeder {
             for (int j = 0; j < kWords; ++j) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[j]) : "r"(at + j * kProducers * 4) : "memory");
         }
     }
-    // five aligned words to the 16 bytes that begin `bytes` into the first
-    static __device__ __forceinline__ uint4 shifted(const uint32_t (&w)[5], uint32_t bytes)
+    // aligned words to the ones that begin at an address of that remainder in the first
+    template <int kWords>
+    static __device__ __forceinline__ void shift(uint32_t (&w)[kWords], uint32_t bytes)
     {
-        const uint32_t n = 8 * bytes;
-        return make_uint4(__funnelshift_r(w[0], w[1], n), __funnelshift_r(w[1], w[2], n), __funnelshift_r(w[2], w[3], n), __funnelshift_r(w[3], w[4], n));
+#pragma unroll
+        for (int j = 0; j + 1 < kWords; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], 8 * (bytes & 3u));
     }
 
-    // converts stage `it`, whose copies have arrived, into its operand tiles
-    __device__ __forceinline__ void convert(int it, const uint32_t (&s)[S::kX]) const
+    // converts the next stage, whose copies have arrived in `raw_slot`, into its operand tiles
+    __device__ __forceinline__ void convert(int raw_slot, int slot, uint32_t s)
     {
-        uint32_t at = raw + (it % S::kRaw) * S::kRawBytes;
-        const size_t r0 = row_begin + (size_t)it * S::kRows;
+        uint32_t at = raw + raw_slot * S::kRawBytes;
         if constexpr (!S::kDirect) {
-            const uint32_t a_tile = a_base + (it % S::kASlots) * S::kA;
 #pragma unroll
             for (int k = 0; k < S::kDy; ++k) {
                 uint32_t w[S::kDyWords];
                 copied(at, w);
                 at += S::kDyWords * kProducers * 4;
-                const uint32_t dst = a_tile + tile_at<S::kSub>(threadIdx.x % S::kDyLanes, dy_row(k));
-                uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
-                if constexpr (S::kDyWords == 5) {
-                    const uintptr_t p = reinterpret_cast<uintptr_t>(a.dy) + ((r0 + dy_row(k)) * a.dy_stride + o) * S::kE;
-                    c = shifted(w, (uint32_t)p & 3u);
-                }
+                const uint32_t dst = smem + slot * S::kA + dy_tile + k * S::kDyPass * 128;
+                if constexpr (S::kDyWords == 5) shift(w, dy_bytes + k * (uint32_t)dy_pass);
                 if constexpr (kType == EOQ_BF16) {
-                    st_shared_128(dst, c);
+                    st_shared_128(dst, make_uint4(w[0], w[1], w[2], w[3]));
                 } else {
                     float v[8];
                     if constexpr (S::kE == 2) {
                         Raw<16> r;
-                        r.w = c;
+                        r.w = make_uint4(w[0], w[1], w[2], w[3]);
                         Elem<EOQ_F16>::to_f32(r, v);
                     } else {
 #pragma unroll
@@ -235,36 +253,33 @@ struct Feeder {
                         for (int j = 0; j < 4; ++j) h[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
                         st_shared_128(dst + p * S::kATile, make_uint4(h[0], h[1], h[2], h[3]));
                         // what the upper halves leave: exact; nothing of an infinity
+                        if (p + 1 < S::kParts)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                            v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
-                        }
+                            for (int j = 0; j < 8; ++j) {
+                                const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                                v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
+                            }
                     }
                 }
             }
+            dy_bytes += (uint32_t)dy_step;
         }
-        const uint32_t b_tile = a_base + S::kASlots * S::kA + (it % S::kBSlots) * S::kB;
-        if (!x_mine()) return;
-#pragma unroll
-        for (int k = 0; k < S::kX; ++k) {
+        if (S::kXLanes * S::kRows == kProducers || x_tile != ~0u) {
             uint32_t w[S::kXWords];
             copied(at, w);
-            at += S::kXWords * kProducers * 4;
-            const int g = threadIdx.x % S::kXLanes, row = x_row(k);
-            uint4 c = make_uint4(w[0], w[1], w[2], w[3]);
-            if constexpr (S::kXWords == 5) c = shifted(w, (uint32_t)(reinterpret_cast<uintptr_t>(a.codes) + (r0 + row) * a.c_in + i) & 3u);
-            const uint32_t sw = s[k] << 7 | s[k] << 23;
+            if constexpr (!kWide) shift(w, x_bytes);
+            const uint32_t sw = s << 7 | s << 23;
             const __nv_bfloat162 step = *reinterpret_cast<const __nv_bfloat162 *>(&sw);
-            const uint4 lo = make_uint4(two_codes(__byte_perm(c.x, 0, 0x4140), step), two_codes(__byte_perm(c.x, 0, 0x4342), step),
-                                        two_codes(__byte_perm(c.y, 0, 0x4140), step), two_codes(__byte_perm(c.y, 0, 0x4342), step));
-            const uint4 hi = make_uint4(two_codes(__byte_perm(c.z, 0, 0x4140), step), two_codes(__byte_perm(c.z, 0, 0x4342), step),
-                                        two_codes(__byte_perm(c.w, 0, 0x4140), step), two_codes(__byte_perm(c.w, 0, 0x4342), step));
-            // neighbouring tiles begin at the same bank: every other one takes its odd chunks first
-            const int first = (g >> 2) & 1;
-            st_shared_128(b_tile + tile_at<S::kSub>(2 * g + first, row), first ? hi : lo);
-            st_shared_128(b_tile + tile_at<S::kSub>(2 * g + 1 - first, row), first ? lo : hi);
+            const uint32_t dst = smem + S::kASlots * S::kA + slot % S::kOps * S::kB + x_tile;
+#pragma unroll
+            for (int j = 0; j < S::kCodes / 8; ++j) {
+                const uint32_t c0 = w[2 * j], c1 = w[2 * j + 1];
+                // (the pieces of a row begin at a multiple of their number: chunk j differs in bits of the swizzled place)
+                st_shared_128(dst ^ (j << 4), make_uint4(two_codes(__byte_perm(c0, 0, 0x4140), step), two_codes(__byte_perm(c0, 0, 0x4342), step),
+                                                         two_codes(__byte_perm(c1, 0, 0x4140), step), two_codes(__byte_perm(c1, 0, 0x4342), step)));
+            }
         }
+        x_bytes += (uint32_t)x_step;
     }
 };
 
@@ -273,19 +288,19 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
 {
     using S = Shape<kType, kN, kWide>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kBars + 3];
+    __shared__ __align__(8) uint64_t bars[2 * S::kRing + 3];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t abort_s;
 
     const int warp = warp_index_uniform(), lane = threadIdx.x & 31;
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = ptx::smem_u32(bars);
     // of stage `it`: operands written; MMAs done.  Of the chunks of steps: sums complete; sums moved on.  All done.
-    auto full_bar = [&](int it) { return bar0 + 8u * (it % S::kBars); };
-    auto done_bar = [&](int it) { return bar0 + 8u * (S::kBars + it % S::kBars); };
-    auto parity = [](int it) { return (uint32_t)(it / S::kBars) & 1u; };
-    const uint32_t sums_bar = bar0 + 8u * (2 * S::kBars), moved_bar = sums_bar + 8, end_bar = sums_bar + 16;
+    auto full_bar = [&](int it) { return bar0 + 8u * (it % S::kRing); };
+    auto done_bar = [&](int it) { return bar0 + 8u * (S::kRing + it % S::kRing); };
+    auto parity = [](int it) { return (uint32_t)(it / S::kRing) & 1u; };
+    const uint32_t sums_bar = bar0 + 8u * (2 * S::kRing), moved_bar = sums_bar + 8, end_bar = sums_bar + 16;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kBars; ++s) {
+        for (int s = 0; s < S::kRing; ++s) {
             ptx::mbar_init(full_bar(s), kProducers / 32);
             ptx::mbar_init(done_bar(s), 1);
         }
@@ -311,35 +326,36 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
     const RoleCtx ctx{&abort_s, a.dev};
 
     if (warp < kMmaWarp) {
-        const Feeder<kType, kN, kWide> feed(a, row_begin, row_end, o0, i0, smem_base);
-        uint32_t s[kAhead + 1][S::kX];
-        feed.start(0, stages, s[0]);
-        feed.start(1, stages, s[1]);
-        feed.start(2, stages, s[2]);
-        static_assert(kAhead == 3, "three stages ahead");
+        Feeder<kType, kN, kWide> feed(a, row_begin, row_end, o0, i0, smem_base);
+        uint32_t s[S::kRing] = {};
+        auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
+#pragma unroll
+        for (int j = 0; j < S::kAhead; ++j) {
+            if (j < stages) feed.start(j, s[j]);
+            commit();
+        }
         bool ok = true;
-        auto turn = [&](int it, const uint32_t (&now)[S::kX], uint32_t (&later)[S::kX]) {
-            // stage it - 2 has left the tiles that stage `it` and, three ahead, its errors go to
-            if (it >= 2) ok = __all_sync(0xffffffffu, wait_bar(done_bar(it - 2), parity(it - 2), ctx));
-            if (!ok) return;
-            feed.start(it + kAhead, stages, later);
-            asm volatile("cp.async.wait_group 3;" ::: "memory");
-            feed.convert(it, now);
-            ptx::fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full_bar(it));
-        };
-        for (int it = 0; it < stages && ok; it += 4) {
-            turn(it, s[0], s[3]);
-            if (ok && it + 1 < stages) turn(it + 1, s[1], s[0]);
-            if (ok && it + 2 < stages) turn(it + 2, s[2], s[1]);
-            if (ok && it + 3 < stages) turn(it + 3, s[3], s[2]);
+        for (int it0 = 0; it0 < stages && ok; it0 += S::kRing) {
+#pragma unroll
+            for (int j = 0; j < S::kRing; ++j) {
+                const int it = it0 + j, ahead = (j + S::kAhead) % S::kRing;
+                if (it >= stages || !ok) break;
+                // stage it - kOps has left the tiles that stage `it` and, kAhead on, copied errors go to
+                if (it >= S::kOps) ok = __all_sync(0xffffffffu, wait_bar(done_bar(j + S::kRing - S::kOps), parity(it - S::kOps), ctx));
+                if (!ok) break;
+                if (it + S::kAhead < stages) feed.start(ahead, s[ahead]);
+                commit();
+                asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead) : "memory");
+                feed.convert(j, j % S::kASlots, s[j]);
+                ptx::fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(full_bar(j));
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        // a row of the tile a lane; two warps share 32 rows, half of the columns each
+        // a row of the tile a lane; the first eight warps: two share 32 rows, half of the columns each
         const int quad = warp & 3, o = o0 + quad * 32 + lane;
-        ok = __all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx));
-        if (ok) {
+        if (warp < 8 && __all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx))) {
             ptx::tc_fence_after();
             float *dst = a.out + (size_t)split * a.c_out * a.c_in + (size_t)o * a.c_in;
             constexpr int kHalf = kN / 2;
@@ -388,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(it), parity(it), ctx)))) break;
             ptx::tc_fence_after();
             const uint32_t a16 = ((smem_base + (it % S::kASlots) * S::kA) >> 4) | lead;
-            const uint32_t b16 = ((smem_base + S::kASlots * S::kA + (it % S::kBSlots) * S::kB) >> 4) | lead;
+            const uint32_t b16 = ((smem_base + S::kASlots * S::kA + (it % S::kOps) * S::kB) >> 4) | lead;
 #pragma unroll
             for (int k = 0; k < S::kRows / 16; ++k)
 #pragma unroll
@@ -481,7 +497,7 @@ template <int kType, int kN, bool kWide>
 cudaError_t launch(const CkptWgradArgs &a, int grid, cudaStream_t st)
 {
     constexpr int bytes = Shape<kType, kN, kWide>::kBytes;
-    static_assert(bytes <= 227 * 1024, "shared memory of a block");
+    static_assert(bytes <= kMaxSmem, "shared memory of a block");
     static std::atomic<unsigned long long> allowed;
     const cudaError_t e = allow_smem((const void *)ckpt_wgrad_kernel<kType, kN, kWide>, bytes, allowed);
     if (e != cudaSuccess) return e;
@@ -519,6 +535,7 @@ cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *works
     a.m_tiles = p.m_tiles;
     a.n_tiles = p.n_tiles;
     a.rows_per_split = p.rows_per_split;
+    a.safe = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(a.exps) & ~(uintptr_t)15);   // (never read: copies of nothing)
     a.out = p.splits > 1 ? reinterpret_cast<float *>(workspace) : dw;
     const int grid = p.m_tiles * p.n_tiles * p.splits;
     const cudaError_t e = dtype == EOQ_F32   ? of_type<EOQ_F32>(a, p.n_tile, grid, st)

@@ -536,6 +536,7 @@ struct CkptWgradArgs {
     int c_out, c_in;
     DeviceState *dev;
     // filled in by the launcher
+    const void *safe;               // an aligned address for copies of nothing
     float *out;                     // [split][c_out][c_in]
     size_t rows_per_split;
     int blocks, m_tiles, n_tiles;   // blocks: of a row of codes
