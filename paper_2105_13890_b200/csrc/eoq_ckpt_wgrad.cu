@@ -34,7 +34,7 @@ template <> struct DyParts<EOQ_BF16> { static constexpr int kParts = 1; };
 template <> struct DyParts<EOQ_F16> { static constexpr int kParts = 2; };
 template <> struct DyParts<EOQ_F32> { static constexpr int kParts = 3; };
 
-// Shapes and shared memory of a kernel.  Errors in bf16 with aligned rows are copied straight into their operand tiles.
+// Shapes and shared memory of a kernel.
 template <int kType, int kN, bool kWide>
 struct Shape {
     static constexpr int kE = Elem<kType>::kSize, kParts = DyParts<kType>::kParts;
@@ -283,6 +283,78 @@ struct Feeder {
     }
 };
 
+// fp32 accumulator, bf16 operands, both MN-major, 128 x n
+__device__ __forceinline__ uint32_t wgrad_idesc(int n)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+}
+
+// The first eight warps, once everything is done: the tile to memory.  A row of the tile a lane; two warps share 32 rows, half of the
+// columns each.
+template <int kN>
+__device__ __forceinline__ void store_tile(const CkptWgradArgs &a, int split, int o0, int i0, uint32_t tmem_base, uint32_t tmem_run, int chunks,
+                                           uint32_t end_bar, const RoleCtx &ctx)
+{
+    const int warp = warp_index_uniform(), quad = warp & 3, o = o0 + quad * 32 + (threadIdx.x & 31);
+    if (warp >= 8 || !__all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx))) return;
+    ptx::tc_fence_after();
+    float *dst = a.out + (size_t)split * a.c_out * a.c_in + (size_t)o * a.c_in;
+    constexpr int kHalf = kN / 2;
+#pragma unroll 1
+    for (int c0 = (warp >> 2) * kHalf; c0 < (warp >> 2) * kHalf + kHalf; c0 += 32) {
+        uint32_t r[32];
+        ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(quad * 32) << 16) + c0, r);
+        ptx::tmem_ld_wait();
+        if (chunks > 1) {
+            uint32_t run[32];
+            ptx::tmem_ld_32x32(tmem_run + ((uint32_t)(quad * 32) << 16) + c0, run);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
+        }
+        if (o < a.c_out) {
+            if (a.c_in % 4 == 0) {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4)
+                    if (i0 + c0 + j < a.c_in) *reinterpret_cast<uint4 *>(dst + i0 + c0 + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (i0 + c0 + j < a.c_in) dst[i0 + c0 + j] = __uint_as_float(r[j]);
+            }
+        }
+    }
+}
+
+// The four warps that add the accumulator to the one of the chunks before.
+template <int kN>
+__device__ __forceinline__ void move_sums(uint32_t tmem_base, uint32_t tmem_run, int chunks, uint32_t sums_bar, uint32_t moved_bar, const RoleCtx &ctx)
+{
+    const uint32_t row = (uint32_t)((warp_index_uniform() & 3) * 32) << 16;
+    for (int chunk = 0; chunk + 1 < chunks; ++chunk) {
+        if (!__all_sync(0xffffffffu, wait_bar<64>(sums_bar, chunk & 1, ctx))) break;
+        ptx::tc_fence_after();
+#pragma unroll 1
+        for (int c0 = 0; c0 < kN; c0 += 32) {
+            uint32_t r[32];
+            ptx::tmem_ld_32x32(tmem_base + row + c0, r);
+            ptx::tmem_ld_wait();
+            if (chunk) {
+                uint32_t run[32];
+                ptx::tmem_ld_32x32(tmem_run + row + c0, run);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
+            }
+            tmem_st_32x32(tmem_run + row + c0, r);
+        }
+        tmem_st_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(moved_bar);
+    }
+}
+
 template <int kType, int kN, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_constant__ CkptWgradArgs a)
 {
@@ -353,42 +425,10 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        // a row of the tile a lane; the first eight warps: two share 32 rows, half of the columns each
-        const int quad = warp & 3, o = o0 + quad * 32 + lane;
-        if (warp < 8 && __all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx))) {
-            ptx::tc_fence_after();
-            float *dst = a.out + (size_t)split * a.c_out * a.c_in + (size_t)o * a.c_in;
-            constexpr int kHalf = kN / 2;
-#pragma unroll 1
-            for (int c0 = (warp >> 2) * kHalf; c0 < (warp >> 2) * kHalf + kHalf; c0 += 32) {
-                uint32_t r[32];
-                ptx::tmem_ld_32x32(tmem_base + ((uint32_t)(quad * 32) << 16) + c0, r);
-                ptx::tmem_ld_wait();
-                if (chunks > 1) {
-                    uint32_t run[32];
-                    ptx::tmem_ld_32x32(tmem_run + ((uint32_t)(quad * 32) << 16) + c0, run);
-                    ptx::tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
-                }
-                if (o < a.c_out) {
-                    if (a.c_in % 4 == 0) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4)
-                            if (i0 + c0 + j < a.c_in)
-                                *reinterpret_cast<uint4 *>(dst + i0 + c0 + j) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (i0 + c0 + j < a.c_in) dst[i0 + c0 + j] = __uint_as_float(r[j]);
-                    }
-                }
-            }
-        }
+        store_tile<kN>(a, split, o0, i0, tmem_base, tmem_run, chunks, end_bar, ctx);
     } else if (warp == kMmaWarp) {
         const uint32_t leader = elect_one();
-        // fp32 accumulator, bf16 operands, both MN-major
-        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(kN >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+        const uint32_t idesc = wgrad_idesc(kN);
         const uint64_t proto = make_smem_desc(0, S::kSub, 1024, 2);
         const uint32_t hi = (uint32_t)(proto >> 32), lead = (uint32_t)proto;
         bool ok = true;
@@ -419,30 +459,191 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             for (uint32_t i = 0; i < kSpinLimit; ++i)
                 if (ptx::mbar_try_wait(end_bar, 0)) break;
     } else {
-        const int quad = warp & 3;
-        const uint32_t row = (uint32_t)(quad * 32) << 16;
-        for (int chunk = 0; chunk + 1 < chunks; ++chunk) {
-            if (!__all_sync(0xffffffffu, wait_bar<64>(sums_bar, chunk & 1, ctx))) break;
-            ptx::tc_fence_after();
-#pragma unroll 1
-            for (int c0 = 0; c0 < kN; c0 += 32) {
-                uint32_t r[32];
-                ptx::tmem_ld_32x32(tmem_base + row + c0, r);
-                ptx::tmem_ld_wait();
-                if (chunk) {
-                    uint32_t run[32];
-                    ptx::tmem_ld_32x32(tmem_run + row + c0, run);
-                    ptx::tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(run[j]) + __uint_as_float(r[j]));
-                }
-                tmem_st_32x32(tmem_run + row + c0, r);
-            }
-            tmem_st_wait();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(moved_bar);
+        move_sums<kN>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem_base, 2 * kN);
+    }
+}
+
+// ------------------------------------------------------------------ bf16 errors, 16-byte rows: tensor copies
+// The same with both operands brought in by tensor copies (one thread's work), errors straight into their operand tiles and codes as
+// they are, four to five stages ahead; the sixteen converting warps only convert.  With copies of their own between the conversions
+// 1024 to 4096 channels, 16,384 rows took 250 us: 159 of it for the copies alone, which two stages in flight do not feed, 96 for the MMAs alone.
+template <int kN>
+struct TmaShape {
+    static constexpr int kRows = 64, kSub = kRows * 128, kA = kTileM / 64 * kSub, kB = kN / 64 * kSub, kCodesBytes = kRows * kN;
+    static constexpr int kOps = 2;                                        // stages of converted tiles
+    static constexpr int kRing = (kMaxSmem - 1024 - kOps * kB) / (kA + kCodesBytes) < 8 ? (kMaxSmem - 1024 - kOps * kB) / (kA + kCodesBytes) : 8;
+    static constexpr int kBytes = kRing * (kA + kCodesBytes) + kOps * kB + 1024;
+    static constexpr int kChunk = kSteps / (kRows / 16);
+    static constexpr int kPieces = kProducers / kRows, kCodes = kN / kPieces, kChunks8 = kCodes / 8;   // codes of a thread: a piece of a row
+    static_assert(kPieces == 8 && kChunks8 >= 1 && kCodes <= kBlock8, "a row's pieces are those of eight lanes");
+};
+constexpr int kTmaThreads = kThreads + 32;   // one more warp, for the copies
+
+template <int kN>
+__global__ void __launch_bounds__(kTmaThreads, 1)
+ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x)
+{
+    using S = TmaShape<kN>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S::kRing + 2 * S::kOps + 3];
+    __shared__ uint32_t tmem_base_s;
+    __shared__ volatile uint32_t abort_s;
+
+    const int warp = warp_index_uniform(), lane = threadIdx.x & 31;
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = ptx::smem_u32(bars);
+    const uint32_t b_base = smem_base + S::kRing * S::kA, code_base = b_base + S::kOps * S::kB;
+    // by slot of the ring: copies landed; codes read and MMAs on the errors done.  By slot of converted tiles: written; MMAs done.
+    auto in_bar = [&](int s) { return bar0 + 8u * s; };
+    auto free_bar = [&](int s) { return bar0 + 8u * (S::kRing + s); };
+    auto full_bar = [&](int s) { return bar0 + 8u * (2 * S::kRing + s); };
+    auto done_bar = [&](int s) { return bar0 + 8u * (2 * S::kRing + S::kOps + s); };
+    const uint32_t sums_bar = bar0 + 8u * (2 * S::kRing + 2 * S::kOps), moved_bar = sums_bar + 8, end_bar = sums_bar + 16;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kRing; ++s) {
+            ptx::mbar_init(in_bar(s), 1);
+            ptx::mbar_init(free_bar(s), kProducers / 32 + 1);
         }
+        for (int s = 0; s < S::kOps; ++s) {
+            ptx::mbar_init(full_bar(s), kProducers / 32);
+            ptx::mbar_init(done_bar(s), 1);
+        }
+        ptx::mbar_init(sums_bar, 1);
+        ptx::mbar_init(moved_bar, 4);
+        ptx::mbar_init(end_bar, 1);
+        abort_s = 0;
+        ptx::fence_barrier_init();
+        ptx::prefetch_tensormap(&map_dy);
+        ptx::prefetch_tensormap(&map_x);
+    }
+    if (warp == kMmaWarp) {
+        ptx::tmem_alloc(ptx::smem_u32(&tmem_base_s), 2 * kN);
+        ptx::tmem_relinquish();
+    }
+    const int tiles = a.m_tiles * a.n_tiles, split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
+    const int o0 = tile / a.n_tiles * kTileM, i0 = tile % a.n_tiles * kN;
+    const size_t row_begin = (size_t)split * a.rows_per_split, row_end = min(a.rows, row_begin + a.rows_per_split);
+    const int stages = (int)((row_end - row_begin + S::kRows - 1) / S::kRows), chunks = (stages + S::kChunk - 1) / S::kChunk;
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    ptx::grid_dep_wait();
+    const uint32_t tmem_base = tmem_base_s, tmem_run = tmem_base + kN;
+    const RoleCtx ctx{&abort_s, a.dev};
+
+    if (warp < kMmaWarp) {
+        const int piece = threadIdx.x % S::kPieces, row = threadIdx.x / S::kPieces, i = i0 + piece * S::kCodes;
+        int left = i < a.c_in ? (int)(row_end - row_begin) - row : 0;
+        const uint8_t *exps = a.exps + (row_begin + row) * a.blocks + i / kBlock8;
+        const size_t step = (size_t)S::kRows * a.blocks;
+        auto next_byte = [&] {
+            const uint32_t s = left > 0 ? __ldg(exps) : 1u;
+            exps += step;
+            left -= S::kRows;
+            return s;
+        };
+        uint32_t s0 = next_byte(), s1 = next_byte();
+        // Each lane takes its chunks of eight codes in an order of its own, so that lanes that store (and load) together meet different banks.
+        const int turn = piece * S::kChunks8 / 8 + (row & 1);
+        uint32_t from[S::kChunks8], to[S::kChunks8];
+#pragma unroll
+        for (int j = 0; j < S::kChunks8; ++j) {
+            const int c = (j + turn) % S::kChunks8;
+            from[j] = (uint32_t)(row * kN + piece * S::kCodes + c * 8);
+            to[j] = tile_at<S::kSub>(piece * S::kChunks8 + c, row);
+        }
+        int slot = 0, op = 0;
+        uint32_t ring_phase = 0, op_phase = 0;
+        for (int it = 0; it < stages; ++it) {
+            const uint32_t s2 = next_byte();
+            if (!__all_sync(0xffffffffu, wait_bar(in_bar(slot), ring_phase, ctx))) break;
+            const uint32_t src = code_base + slot * S::kCodesBytes;
+            uint4 v[S::kChunks8];
+            const uint32_t sw = s0 << 7 | s0 << 23;
+            const __nv_bfloat162 unit = *reinterpret_cast<const __nv_bfloat162 *>(&sw);
+#pragma unroll
+            for (int j = 0; j < S::kChunks8; ++j) {
+                uint32_t c0, c1;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c0), "=r"(c1) : "r"(src + from[j]) : "memory");
+                v[j] = make_uint4(two_codes(__byte_perm(c0, 0, 0x4140), unit), two_codes(__byte_perm(c0, 0, 0x4342), unit),
+                                  two_codes(__byte_perm(c1, 0, 0x4140), unit), two_codes(__byte_perm(c1, 0, 0x4342), unit));
+            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(free_bar(slot));
+            if (!__all_sync(0xffffffffu, wait_bar(done_bar(op), op_phase ^ 1u, ctx))) break;
+            const uint32_t dst = b_base + op * S::kB;
+#pragma unroll
+            for (int j = 0; j < S::kChunks8; ++j) st_shared_128(dst + to[j], v[j]);
+            ptx::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(full_bar(op));
+            s0 = s1;
+            s1 = s2;
+            if (++slot == S::kRing) { slot = 0; ring_phase ^= 1u; }
+            if (++op == S::kOps) { op = 0; op_phase ^= 1u; }
+        }
+        store_tile<kN>(a, split, o0, i0, tmem_base, tmem_run, chunks, end_bar, ctx);
+    } else if (warp == kMmaWarp) {
+        const uint32_t leader = elect_one();
+        const uint32_t idesc = wgrad_idesc(kN);
+        const uint64_t proto = make_smem_desc(0, S::kSub, 1024, 2);
+        const uint32_t hi = (uint32_t)(proto >> 32), lead = (uint32_t)proto;
+        bool ok = true;
+        int chunk = 0, in_chunk = 0, slot = 0, op = 0;
+        uint32_t ring_phase = 0, op_phase = 0;
+        for (int it = 0; it < stages; ++it) {
+            if (in_chunk == S::kChunk) {   // hand the sums over and wait until they have been taken
+                ptx::mma_commit(sums_bar, leader);
+                if (!(ok = __all_sync(0xffffffffu, wait_bar(moved_bar, chunk & 1, ctx)))) break;
+                ptx::tc_fence_after();
+                ++chunk;
+                in_chunk = 0;
+            }
+            if (!(ok = __all_sync(0xffffffffu, wait_bar(in_bar(slot), ring_phase, ctx)))) break;
+            if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(op), op_phase, ctx)))) break;
+            ptx::tc_fence_after();
+            const uint32_t a16 = ((smem_base + slot * S::kA) >> 4) | lead, b16 = ((b_base + op * S::kB) >> 4) | lead;
+#pragma unroll
+            for (int k = 0; k < S::kRows / 16; ++k)
+                mma_bf16(tmem_base, smem_desc_join(a16 + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc, (k | in_chunk) != 0 ? 1u : 0u, leader);
+            ptx::mma_commit(done_bar(op), leader);
+            ptx::mma_commit(free_bar(slot), leader);
+            ++in_chunk;
+            if (++slot == S::kRing) { slot = 0; ring_phase ^= 1u; }
+            if (++op == S::kOps) { op = 0; op_phase ^= 1u; }
+        }
+        ptx::mma_commit(end_bar, leader);
+        if (!ok)
+            for (uint32_t i = 0; i < kSpinLimit; ++i)
+                if (ptx::mbar_try_wait(end_bar, 0)) break;
+    } else if (warp < kMmaWarp + 5) {
+        move_sums<kN>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
+    } else {
+        bool ok = true;
+        int slot = 0, started = 0;
+        uint32_t ring_phase = 0;
+        for (int it = 0; it < stages; ++it) {
+            if (!(ok = __all_sync(0xffffffffu, wait_bar<32>(free_bar(slot), ring_phase ^ 1u, ctx)))) break;
+            if (lane == 0) {
+                const int r = (int)row_begin + it * S::kRows;
+                ptx::mbar_expect_tx(in_bar(slot), S::kA + S::kCodesBytes);
+#pragma unroll
+                for (int j = 0; j < kTileM / 64; ++j) ptx::tma_load_2d(smem_base + slot * S::kA + j * S::kSub, &map_dy, in_bar(slot), o0 + 64 * j, r);
+                ptx::tma_load_2d(code_base + slot * S::kCodesBytes, &map_x, in_bar(slot), i0, r);
+            }
+            __syncwarp();
+            ++started;
+            if (++slot == S::kRing) { slot = 0; ring_phase ^= 1u; }
+        }
+        if (!ok && lane == 0)   // (copies still in flight land before the block ends)
+            for (int it = started > S::kRing ? started - S::kRing : 0; it < started; ++it)
+                for (uint32_t i = 0; i < kSpinLimit; ++i)
+                    if (ptx::mbar_try_wait(in_bar(it % S::kRing), (uint32_t)(it / S::kRing) & 1u)) break;
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -504,6 +705,21 @@ cudaError_t launch(const CkptWgradArgs &a, int grid, cudaStream_t st)
     return launch_chained(ckpt_wgrad_kernel<kType, kN, kWide>, dim3(grid), dim3(kThreads), bytes, st, a);
 }
 
+template <int kN>
+cudaError_t launch_tma(const CkptWgradArgs &a, int grid, cudaStream_t st)
+{
+    CUtensorMap map_dy, map_x;
+    if (!tiled_map_2d(&map_dy, a.dy, true, a.c_out, a.rows, a.dy_stride * 2, 64, TmaShape<kN>::kRows, true) ||
+        !tiled_map_2d(&map_x, a.codes, false, a.c_in, a.rows, a.c_in, kN, TmaShape<kN>::kRows, false))
+        return cudaErrorInvalidValue;
+    constexpr int bytes = TmaShape<kN>::kBytes;
+    static_assert(bytes <= kMaxSmem, "shared memory of a block");
+    static std::atomic<unsigned long long> allowed;
+    const cudaError_t e = allow_smem((const void *)ckpt_wgrad_tma_kernel<kN>, bytes, allowed);
+    if (e != cudaSuccess) return e;
+    return launch_chained(ckpt_wgrad_tma_kernel<kN>, dim3(grid), dim3(kTmaThreads), bytes, st, a, map_dy, map_x);
+}
+
 template <int kType, bool kWide>
 cudaError_t of_width(const CkptWgradArgs &a, int n_tile, int grid, cudaStream_t st)
 {
@@ -517,7 +733,14 @@ cudaError_t of_type(const CkptWgradArgs &a, int n_tile, int grid, cudaStream_t s
 {
     const bool wide = a.c_out % 8 == 0 && a.c_in % 16 == 0 && a.dy_stride % (16 / Elem<kType>::kSize) == 0 &&
                       reinterpret_cast<uintptr_t>(a.dy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 16 == 0;
-    return wide ? of_width<kType, true>(a, n_tile, grid, st) : of_width<kType, false>(a, n_tile, grid, st);
+    if (!wide) return of_width<kType, false>(a, n_tile, grid, st);
+    if constexpr (kType == EOQ_BF16) {
+        if (n_tile == 64) return launch_tma<64>(a, grid, st);
+        if (n_tile == 128) return launch_tma<128>(a, grid, st);
+        return launch_tma<256>(a, grid, st);
+    } else {
+        return of_width<kType, true>(a, n_tile, grid, st);
+    }
 }
 
 }  // namespace

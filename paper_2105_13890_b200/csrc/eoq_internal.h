@@ -528,6 +528,10 @@ cudaError_t launch_ckpt_save(const void *src, int dtype, int src_exp, size_t row
 cudaError_t launch_ckpt_load(const int8_t *codes, const uint8_t *exps, size_t rows, int cols, void *dst, int dtype, size_t stride,
                              DeviceState *dev, int sm_count, cudaStream_t st);
 
+// Tensor map of a matrix of bf16 (or bytes): `cols` x `rows`, rows `pitch` bytes apart, boxes of box_cols x box_rows, rows of a box swizzled over
+// 128 bytes or as they are (eoq_api.cu).
+bool tiled_map_2d(CUtensorMap *map, const void *ptr, bool bf16, size_t cols, size_t rows, size_t pitch, int box_cols, int box_rows, bool swizzle);
+
 struct CkptWgradArgs {
     const void *dy;
     const int8_t *codes;
