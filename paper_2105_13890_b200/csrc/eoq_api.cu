@@ -2318,7 +2318,7 @@ extern "C" int eoq_ckpt_wgrad_workspace_size(size_t rows, int c_out, int c_in, i
     if (!bytes) return EOQ_ERR_BAD_ARG;
     const int chk = ckpt_wgrad_check(rows, c_out, c_in, dtype);
     if (chk != EOQ_OK) return chk;
-    *bytes = round256(ckpt_wgrad_workspace_bytes(rows, c_out, c_in));
+    *bytes = round256(ckpt_wgrad_workspace_bytes(rows, c_out, c_in, dtype));
     return EOQ_OK;
 }
 
@@ -2332,7 +2332,7 @@ extern "C" int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, si
     if (!dy || !codes || !exps || !dw || dy_stride < (size_t)c_out) return EOQ_ERR_BAD_ARG;
     if (dy_stride > (size_t)1 << 30) return EOQ_ERR_UNSUPPORTED;
     if (!aligned_to(dy, dtype_size(dtype)) || !aligned16(dw)) return EOQ_ERR_ALIGNMENT;
-    const size_t need = ckpt_wgrad_workspace_bytes(rows, c_out, c_in);
+    const size_t need = ckpt_wgrad_workspace_bytes(rows, c_out, c_in, dtype);
     if (need && (!workspace || !aligned_to(workspace, 256) || workspace_bytes < need)) return EOQ_ERR_WORKSPACE;
     if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

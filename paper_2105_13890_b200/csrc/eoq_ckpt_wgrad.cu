@@ -38,8 +38,7 @@ template <> struct DyParts<EOQ_F32> { static constexpr int kParts = 3; };
 template <int kType, int kN, bool kWide>
 struct Shape {
     static constexpr int kE = Elem<kType>::kSize, kParts = DyParts<kType>::kParts;
-    static constexpr bool kDirect = kType == EOQ_BF16 && kWide;
-    static constexpr int kRows = kDirect ? 64 : 32;                      // rows of a stage
+    static constexpr int kRows = kE == 2 && kN <= 128 ? 64 : 32;         // rows of a stage
     static constexpr int kSub = kRows * 128;                             // bytes of a tile of 64 columns
     static constexpr int kATile = kTileM / 64 * kSub, kA = kParts * kATile, kB = kN / 64 * kSub;
     // A thread's share of a stage: kDy times eight errors, and kCodes neighbouring codes of a row (of threads without any there may be some).
@@ -48,13 +47,12 @@ struct Shape {
     static_assert(kDyPass % 8 == 0 && kDy * kDyPass == kRows, "rows of a thread's chunks share their swizzle");
     static_assert(kXLanes * kRows <= kProducers, "one piece of codes a thread");
     // words of a chunk as copied: an unaligned one of n words touches n + 1
-    static constexpr int kDyWords = kDirect ? 0 : kE == 4 ? 8 : kWide ? 4 : 5, kXWords = kCodes / 4 + (kWide ? 0 : 1);
+    static constexpr int kDyWords = kE == 4 ? 8 : kWide ? 4 : 5, kXWords = kCodes / 4 + (kWide ? 0 : 1);
     static constexpr int kRawBytes = kProducers * 4 * (kDy * kDyWords + kXWords);
     // Stages of operand tiles, of copies and of barriers, all of which divide four, so that a loop over four stages knows its slots.
-    // Copied errors run kAhead = 2 stages ahead of tiles that kOps = 2 stages are at work on.
-    static constexpr int kRing = 4;
-    static constexpr int size(int ops) { return (kDirect ? kRing : ops) * kA + ops * kB + kRing * kRawBytes + 1024; }
-    static constexpr int kOps = !kDirect && size(4) <= kMaxSmem ? 4 : 2, kASlots = kDirect ? kRing : kOps, kAhead = kDirect ? 2 : 3;
+    static constexpr int kRing = 4, kAhead = 3;
+    static constexpr int size(int ops) { return ops * (kA + kB) + kRing * kRawBytes + 1024; }
+    static constexpr int kOps = size(4) <= kMaxSmem ? 4 : 2;
     static constexpr int kBytes = size(kOps);
     static constexpr int kChunk = kSteps / (kRows / 16 * kParts);        // stages before the accumulator moves on
 };
@@ -92,14 +90,86 @@ __device__ __forceinline__ void st_shared_128(uint32_t addr, uint4 v)
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// kPair: over the operands of two blocks, issued by the first
+template <bool kPair>
 __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t leader)
 {
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "setp.ne.b32 q, %5, 0;\n\t"
-        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader));
+    if constexpr (kPair)
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader));
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader));
+}
+// the barrier at the same place of every block receives one arrival when the MMAs issued so far are done
+template <bool kPair>
+__device__ __forceinline__ void commit_both(uint32_t bar, uint32_t leader)
+{
+    if constexpr (kPair)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t"
+            "setp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %2;\n\t}"
+            ::"r"(bar), "r"(leader), "h"((uint16_t)3) : "memory");
+    else
+        ptx::mma_commit(bar, leader);
+}
+// An arrival at the first block's barrier.  (In the default scope: what it announces lies in this block's shared memory, written and fenced
+// towards the asynchronous proxy by then.  With the scope of the cluster, which waits for more than that, the kernel takes 288 us where it
+// takes 135: 1024 to 4096 channels, 16,384 rows.)
+template <bool kPair>
+__device__ __forceinline__ void arrive_first(uint32_t bar)
+{
+    if constexpr (kPair)
+        asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(ptx::cluster_addr(bar, 0)) : "memory");
+    else
+        ptx::mbar_arrive(bar);
+}
+// wait_bar for a barrier that threads of both blocks arrive at: what they wrote before is visible behind it
+template <bool kPair>
+__device__ __forceinline__ bool wait_both(uint32_t bar, uint32_t parity, const RoleCtx &c)
+{
+    if constexpr (!kPair) return wait_bar(bar, parity, c);
+    for (uint32_t i = 0; i < kSpinLimit; ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (done) return true;
+        if (*c.abort_flag) return false;
+    }
+    *c.abort_flag = 1u;
+    atomicOr(&c.dev->status, EOQ_DEV_TIMEOUT);
+    return false;
+}
+template <bool kPair>
+__device__ __forceinline__ void tmem_take(uint32_t result, uint32_t columns)
+{
+    if constexpr (kPair) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(result), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        ptx::tmem_alloc(result, columns);
+        ptx::tmem_relinquish();
+    }
+}
+template <bool kPair>
+__device__ __forceinline__ void tmem_return(uint32_t base, uint32_t columns)
+{
+    if constexpr (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(columns) : "memory");
+    else ptx::tmem_dealloc(base, columns);
 }
 
 // bf16 pair of two codes: 128 + (low seven bits) less 128 or, for a negative code, 256; both are bf16 numbers, and so is the result
@@ -125,7 +195,7 @@ struct Feeder {
     uint32_t dy_bytes, x_bytes;          // addresses of the chunks to convert next, of which two bits count
 
     __device__ __forceinline__ Feeder(const CkptWgradArgs &a, size_t begin, size_t end, int o0, int i0, uint32_t smem_base)
-        : safe(a.safe), smem(smem_base), raw(smem_base + S::kASlots * S::kA + S::kOps * S::kB + threadIdx.x * (kWide ? 16 : 4))
+        : safe(a.safe), smem(smem_base), raw(smem_base + S::kOps * S::kA + S::kOps * S::kB + threadIdx.x * (kWide ? 16 : 4))
     {
         // Eight lanes that store together should meet eight different places of 16 bytes: of codes, the even (or a quarter of the) chunks
         // of a tile's row, in neighbouring rows, which the swizzle turns against one another.
@@ -173,7 +243,7 @@ struct Feeder {
         }
     }
 
-    // starts the copies of the next stage, whose slot of the copies (and of copied errors) is `slot`; the byte of its codes is on its way
+    // starts the copies of the next stage, whose slot of the copies is `slot`; the byte of its codes is on its way
     __device__ __forceinline__ void start(int slot, uint32_t &s)
     {
         uint32_t at = raw + slot * S::kRawBytes;
@@ -181,8 +251,7 @@ struct Feeder {
 #pragma unroll
         for (int k = 0; k < S::kDy; ++k, p += dy_pass) {
             const bool in = k * S::kDyPass < dy_left;
-            if constexpr (S::kDirect) copy_16(smem + slot * S::kA + dy_tile + k * S::kDyPass * 128, in ? p : safe, in);
-            else if constexpr (kWide) copy_wide<S::kDyWords>(at, p, dy_cols, in);
+            if constexpr (kWide) copy_wide<S::kDyWords>(at, p, dy_cols, in);
             else copy_words<S::kDyWords>(at, p, dy_cols, in);
             at += S::kDyWords * kProducers * 4;
         }
@@ -226,51 +295,49 @@ struct Feeder {
     __device__ __forceinline__ void convert(int raw_slot, int slot, uint32_t s)
     {
         uint32_t at = raw + raw_slot * S::kRawBytes;
-        if constexpr (!S::kDirect) {
 #pragma unroll
-            for (int k = 0; k < S::kDy; ++k) {
-                uint32_t w[S::kDyWords];
-                copied(at, w);
-                at += S::kDyWords * kProducers * 4;
-                const uint32_t dst = smem + slot * S::kA + dy_tile + k * S::kDyPass * 128;
-                if constexpr (S::kDyWords == 5) shift(w, dy_bytes + k * (uint32_t)dy_pass);
-                if constexpr (kType == EOQ_BF16) {
-                    st_shared_128(dst, make_uint4(w[0], w[1], w[2], w[3]));
+        for (int k = 0; k < S::kDy; ++k) {
+            uint32_t w[S::kDyWords];
+            copied(at, w);
+            at += S::kDyWords * kProducers * 4;
+            const uint32_t dst = smem + slot * S::kA + dy_tile + k * S::kDyPass * 128;
+            if constexpr (S::kDyWords == 5) shift(w, dy_bytes + k * (uint32_t)dy_pass);
+            if constexpr (kType == EOQ_BF16) {
+                st_shared_128(dst, make_uint4(w[0], w[1], w[2], w[3]));
+            } else {
+                float v[8];
+                if constexpr (S::kE == 2) {
+                    Raw<16> r;
+                    r.w = make_uint4(w[0], w[1], w[2], w[3]);
+                    Elem<EOQ_F16>::to_f32(r, v);
                 } else {
-                    float v[8];
-                    if constexpr (S::kE == 2) {
-                        Raw<16> r;
-                        r.w = make_uint4(w[0], w[1], w[2], w[3]);
-                        Elem<EOQ_F16>::to_f32(r, v);
-                    } else {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
-                    }
+                    for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+                }
 #pragma unroll
-                    for (int p = 0; p < S::kParts; ++p) {
-                        uint32_t h[4];
+                for (int p = 0; p < S::kParts; ++p) {
+                    uint32_t h[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) h[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
-                        st_shared_128(dst + p * S::kATile, make_uint4(h[0], h[1], h[2], h[3]));
-                        // what the upper halves leave: exact; nothing of an infinity
-                        if (p + 1 < S::kParts)
+                    for (int j = 0; j < 4; ++j) h[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
+                    st_shared_128(dst + p * S::kATile, make_uint4(h[0], h[1], h[2], h[3]));
+                    // what the upper halves leave: exact; nothing of an infinity
+                    if (p + 1 < S::kParts)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                                v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
-                            }
-                    }
+                        for (int j = 0; j < 8; ++j) {
+                            const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                            v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
+                        }
                 }
             }
-            dy_bytes += (uint32_t)dy_step;
         }
+        dy_bytes += (uint32_t)dy_step;
         if (S::kXLanes * S::kRows == kProducers || x_tile != ~0u) {
             uint32_t w[S::kXWords];
             copied(at, w);
             if constexpr (!kWide) shift(w, x_bytes);
             const uint32_t sw = s << 7 | s << 23;
             const __nv_bfloat162 step = *reinterpret_cast<const __nv_bfloat162 *>(&sw);
-            const uint32_t dst = smem + S::kASlots * S::kA + slot % S::kOps * S::kB + x_tile;
+            const uint32_t dst = smem + S::kOps * S::kA + slot % S::kOps * S::kB + x_tile;
 #pragma unroll
             for (int j = 0; j < S::kCodes / 8; ++j) {
                 const uint32_t c0 = w[2 * j], c1 = w[2 * j + 1];
@@ -283,10 +350,10 @@ struct Feeder {
     }
 };
 
-// fp32 accumulator, bf16 operands, both MN-major, 128 x n
-__device__ __forceinline__ uint32_t wgrad_idesc(int n)
+// fp32 accumulator, bf16 operands, both MN-major, m x n
+__device__ __forceinline__ uint32_t wgrad_idesc(int m, int n)
 {
-    return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+    return (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
 
 // The first eight warps, once everything is done: the tile to memory.  A row of the tile a lane; two warps share 32 rows, half of the
@@ -327,7 +394,7 @@ __device__ __forceinline__ void store_tile(const CkptWgradArgs &a, int split, in
 }
 
 // The four warps that add the accumulator to the one of the chunks before.
-template <int kN>
+template <int kN, bool kPair>
 __device__ __forceinline__ void move_sums(uint32_t tmem_base, uint32_t tmem_run, int chunks, uint32_t sums_bar, uint32_t moved_bar, const RoleCtx &ctx)
 {
     const uint32_t row = (uint32_t)((warp_index_uniform() & 3) * 32) << 16;
@@ -351,7 +418,7 @@ __device__ __forceinline__ void move_sums(uint32_t tmem_base, uint32_t tmem_run,
         tmem_st_wait();
         ptx::tc_fence_before();
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(moved_bar);
+        if ((threadIdx.x & 31) == 0) arrive_first<kPair>(moved_bar);
     }
 }
 
@@ -412,13 +479,13 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             for (int j = 0; j < S::kRing; ++j) {
                 const int it = it0 + j, ahead = (j + S::kAhead) % S::kRing;
                 if (it >= stages || !ok) break;
-                // stage it - kOps has left the tiles that stage `it` and, kAhead on, copied errors go to
+                // stage it - kOps has left the tiles that stage `it` goes to
                 if (it >= S::kOps) ok = __all_sync(0xffffffffu, wait_bar(done_bar(j + S::kRing - S::kOps), parity(it - S::kOps), ctx));
                 if (!ok) break;
                 if (it + S::kAhead < stages) feed.start(ahead, s[ahead]);
                 commit();
                 asm volatile("cp.async.wait_group %0;" ::"n"(S::kAhead) : "memory");
-                feed.convert(j, j % S::kASlots, s[j]);
+                feed.convert(j, j % S::kOps, s[j]);
                 ptx::fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(full_bar(j));
@@ -428,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
         store_tile<kN>(a, split, o0, i0, tmem_base, tmem_run, chunks, end_bar, ctx);
     } else if (warp == kMmaWarp) {
         const uint32_t leader = elect_one();
-        const uint32_t idesc = wgrad_idesc(kN);
+        const uint32_t idesc = wgrad_idesc(kTileM, kN);
         const uint64_t proto = make_smem_desc(0, S::kSub, 1024, 2);
         const uint32_t hi = (uint32_t)(proto >> 32), lead = (uint32_t)proto;
         bool ok = true;
@@ -443,13 +510,13 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             }
             if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(it), parity(it), ctx)))) break;
             ptx::tc_fence_after();
-            const uint32_t a16 = ((smem_base + (it % S::kASlots) * S::kA) >> 4) | lead;
-            const uint32_t b16 = ((smem_base + S::kASlots * S::kA + (it % S::kOps) * S::kB) >> 4) | lead;
+            const uint32_t a16 = ((smem_base + (it % S::kOps) * S::kA) >> 4) | lead;
+            const uint32_t b16 = ((smem_base + S::kOps * S::kA + (it % S::kOps) * S::kB) >> 4) | lead;
 #pragma unroll
             for (int k = 0; k < S::kRows / 16; ++k)
 #pragma unroll
                 for (int p = 0; p < S::kParts; ++p)
-                    mma_bf16(tmem_base, smem_desc_join(a16 + p * (S::kATile >> 4) + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc,
+                    mma_bf16<false>(tmem_base, smem_desc_join(a16 + p * (S::kATile >> 4) + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc,
                              (k | p | in_chunk) != 0 ? 1u : 0u, leader);
             ptx::mma_commit(done_bar(it), leader);
             ++in_chunk;
@@ -459,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
             for (uint32_t i = 0; i < kSpinLimit; ++i)
                 if (ptx::mbar_try_wait(end_bar, 0)) break;
     } else {
-        move_sums<kN>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
+        move_sums<kN, false>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
     }
     ptx::tc_fence_before();
     __syncthreads();
@@ -473,23 +540,29 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
 // The same with both operands brought in by tensor copies (one thread's work), errors straight into their operand tiles and codes as
 // they are, four to five stages ahead; the sixteen converting warps only convert.  With copies of their own between the conversions
 // 1024 to 4096 channels, 16,384 rows took 250 us: 159 of it for the copies alone, which two stages in flight do not feed, 96 for the MMAs alone.
-template <int kN>
+//
+// kPair: two blocks, a cluster, work on a tile of 256 x 256 as one.  Each brings in its 128 columns of dy and of codes, converts its
+// codes and holds its 128 rows of the accumulator; the MMAs are the first block's, over both blocks' operands.  What bounds the kernel is
+// the conversion, and a pair converts half as much for the same MMAs.
+template <int kN, bool kPair>
 struct TmaShape {
-    static constexpr int kRows = 64, kSub = kRows * 128, kA = kTileM / 64 * kSub, kB = kN / 64 * kSub, kCodesBytes = kRows * kN;
-    static constexpr int kOps = 2;                                        // stages of converted tiles
+    static constexpr int kOwn = kPair ? kN / 2 : kN;                      // columns of codes of a block
+    static constexpr int kRows = 64, kSub = kRows * 128, kA = kTileM / 64 * kSub, kB = kOwn / 64 * kSub, kCodesBytes = kRows * kOwn;
+    static constexpr int kOps = kOwn <= 128 ? 3 : 2;                      // stages of converted tiles
     static constexpr int kRing = (kMaxSmem - 1024 - kOps * kB) / (kA + kCodesBytes) < 8 ? (kMaxSmem - 1024 - kOps * kB) / (kA + kCodesBytes) : 8;
     static constexpr int kBytes = kRing * (kA + kCodesBytes) + kOps * kB + 1024;
     static constexpr int kChunk = kSteps / (kRows / 16);
-    static constexpr int kPieces = kProducers / kRows, kCodes = kN / kPieces, kChunks8 = kCodes / 8;   // codes of a thread: a piece of a row
+    static constexpr int kPieces = kProducers / kRows, kCodes = kOwn / kPieces, kChunks8 = kCodes / 8;   // codes of a thread: a piece of a row
     static_assert(kPieces == 8 && kChunks8 >= 1 && kCodes <= kBlock8, "a row's pieces are those of eight lanes");
 };
 constexpr int kTmaThreads = kThreads + 32;   // one more warp, for the copies
 
-template <int kN>
+template <int kN, bool kPair>
 __global__ void __launch_bounds__(kTmaThreads, 1)
 ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_constant__ CUtensorMap map_dy, const __grid_constant__ CUtensorMap map_x)
 {
-    using S = TmaShape<kN>;
+    using S = TmaShape<kN, kPair>;
+    constexpr int kBlocks = kPair ? 2 : 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kRing + 2 * S::kOps + 3];
     __shared__ uint32_t tmem_base_s;
@@ -510,34 +583,33 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
             ptx::mbar_init(free_bar(s), kProducers / 32 + 1);
         }
         for (int s = 0; s < S::kOps; ++s) {
-            ptx::mbar_init(full_bar(s), kProducers / 32);
+            ptx::mbar_init(full_bar(s), kBlocks * kProducers / 32);
             ptx::mbar_init(done_bar(s), 1);
         }
         ptx::mbar_init(sums_bar, 1);
-        ptx::mbar_init(moved_bar, 4);
+        ptx::mbar_init(moved_bar, kBlocks * 4);
         ptx::mbar_init(end_bar, 1);
         abort_s = 0;
         ptx::fence_barrier_init();
         ptx::prefetch_tensormap(&map_dy);
         ptx::prefetch_tensormap(&map_x);
     }
-    if (warp == kMmaWarp) {
-        ptx::tmem_alloc(ptx::smem_u32(&tmem_base_s), 2 * kN);
-        ptx::tmem_relinquish();
-    }
-    const int tiles = a.m_tiles * a.n_tiles, split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-    const int o0 = tile / a.n_tiles * kTileM, i0 = tile % a.n_tiles * kN;
+    if (warp == kMmaWarp) tmem_take<kPair>(ptx::smem_u32(&tmem_base_s), 2 * kN);
+    const int rank = kPair ? blockIdx.x & 1 : 0, id = blockIdx.x / kBlocks;
+    const int tiles = a.m_tiles * a.n_tiles, split = id / tiles, tile = id % tiles;
+    const int o0 = (tile / a.n_tiles * kBlocks + rank) * kTileM, i0 = tile % a.n_tiles * kN, own_i0 = i0 + rank * S::kOwn;
     const size_t row_begin = (size_t)split * a.rows_per_split, row_end = min(a.rows, row_begin + a.rows_per_split);
     const int stages = (int)((row_end - row_begin + S::kRows - 1) / S::kRows), chunks = (stages + S::kChunk - 1) / S::kChunk;
     ptx::tc_fence_before();
-    __syncthreads();
+    if (kPair) ptx::cluster_sync();   // (the other block's barriers are ready)
+    else __syncthreads();
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
     const uint32_t tmem_base = tmem_base_s, tmem_run = tmem_base + kN;
     const RoleCtx ctx{&abort_s, a.dev};
 
     if (warp < kMmaWarp) {
-        const int piece = threadIdx.x % S::kPieces, row = threadIdx.x / S::kPieces, i = i0 + piece * S::kCodes;
+        const int piece = threadIdx.x % S::kPieces, row = threadIdx.x / S::kPieces, i = own_i0 + piece * S::kCodes;
         int left = i < a.c_in ? (int)(row_end - row_begin) - row : 0;
         const uint8_t *exps = a.exps + (row_begin + row) * a.blocks + i / kBlock8;
         const size_t step = (size_t)S::kRows * a.blocks;
@@ -554,7 +626,7 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
 #pragma unroll
         for (int j = 0; j < S::kChunks8; ++j) {
             const int c = (j + turn) % S::kChunks8;
-            from[j] = (uint32_t)(row * kN + piece * S::kCodes + c * 8);
+            from[j] = (uint32_t)(row * S::kOwn + piece * S::kCodes + c * 8);
             to[j] = tile_at<S::kSub>(piece * S::kChunks8 + c, row);
         }
         int slot = 0, op = 0;
@@ -581,16 +653,16 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
             for (int j = 0; j < S::kChunks8; ++j) st_shared_128(dst + to[j], v[j]);
             ptx::fence_proxy_async();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(full_bar(op));
+            if (lane == 0) arrive_first<kPair>(full_bar(op));
             s0 = s1;
             s1 = s2;
             if (++slot == S::kRing) { slot = 0; ring_phase ^= 1u; }
             if (++op == S::kOps) { op = 0; op_phase ^= 1u; }
         }
         store_tile<kN>(a, split, o0, i0, tmem_base, tmem_run, chunks, end_bar, ctx);
-    } else if (warp == kMmaWarp) {
+    } else if (warp == kMmaWarp && rank == 0) {
         const uint32_t leader = elect_one();
-        const uint32_t idesc = wgrad_idesc(kN);
+        const uint32_t idesc = wgrad_idesc(kBlocks * kTileM, kN);
         const uint64_t proto = make_smem_desc(0, S::kSub, 1024, 2);
         const uint32_t hi = (uint32_t)(proto >> 32), lead = (uint32_t)proto;
         bool ok = true;
@@ -598,31 +670,33 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
         uint32_t ring_phase = 0, op_phase = 0;
         for (int it = 0; it < stages; ++it) {
             if (in_chunk == S::kChunk) {   // hand the sums over and wait until they have been taken
-                ptx::mma_commit(sums_bar, leader);
-                if (!(ok = __all_sync(0xffffffffu, wait_bar(moved_bar, chunk & 1, ctx)))) break;
+                commit_both<kPair>(sums_bar, leader);
+                if (!(ok = __all_sync(0xffffffffu, wait_both<kPair>(moved_bar, chunk & 1, ctx)))) break;
                 ptx::tc_fence_after();
                 ++chunk;
                 in_chunk = 0;
             }
             if (!(ok = __all_sync(0xffffffffu, wait_bar(in_bar(slot), ring_phase, ctx)))) break;
-            if (!(ok = __all_sync(0xffffffffu, wait_bar(full_bar(op), op_phase, ctx)))) break;
+            if (!(ok = __all_sync(0xffffffffu, wait_both<kPair>(full_bar(op), op_phase, ctx)))) break;
             ptx::tc_fence_after();
             const uint32_t a16 = ((smem_base + slot * S::kA) >> 4) | lead, b16 = ((b_base + op * S::kB) >> 4) | lead;
 #pragma unroll
             for (int k = 0; k < S::kRows / 16; ++k)
-                mma_bf16(tmem_base, smem_desc_join(a16 + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc, (k | in_chunk) != 0 ? 1u : 0u, leader);
-            ptx::mma_commit(done_bar(op), leader);
-            ptx::mma_commit(free_bar(slot), leader);
+                mma_bf16<kPair>(tmem_base, smem_desc_join(a16 + k * 128, hi), smem_desc_join(b16 + k * 128, hi), idesc, (k | in_chunk) != 0 ? 1u : 0u, leader);
+            commit_both<kPair>(done_bar(op), leader);
+            commit_both<kPair>(free_bar(slot), leader);
             ++in_chunk;
             if (++slot == S::kRing) { slot = 0; ring_phase ^= 1u; }
             if (++op == S::kOps) { op = 0; op_phase ^= 1u; }
         }
-        ptx::mma_commit(end_bar, leader);
+        commit_both<kPair>(end_bar, leader);
         if (!ok)
             for (uint32_t i = 0; i < kSpinLimit; ++i)
                 if (ptx::mbar_try_wait(end_bar, 0)) break;
+    } else if (warp == kMmaWarp) {
+        // (the other block of a pair: its MMAs are issued by the first)
     } else if (warp < kMmaWarp + 5) {
-        move_sums<kN>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
+        move_sums<kN, kPair>(tmem_base, tmem_run, chunks, sums_bar, moved_bar, ctx);
     } else {
         bool ok = true;
         int slot = 0, started = 0;
@@ -634,7 +708,7 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
                 ptx::mbar_expect_tx(in_bar(slot), S::kA + S::kCodesBytes);
 #pragma unroll
                 for (int j = 0; j < kTileM / 64; ++j) ptx::tma_load_2d(smem_base + slot * S::kA + j * S::kSub, &map_dy, in_bar(slot), o0 + 64 * j, r);
-                ptx::tma_load_2d(code_base + slot * S::kCodesBytes, &map_x, in_bar(slot), i0, r);
+                ptx::tma_load_2d(code_base + slot * S::kCodesBytes, &map_x, in_bar(slot), own_i0, r);
             }
             __syncwarp();
             ++started;
@@ -646,12 +720,14 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
                     if (ptx::mbar_try_wait(in_bar(it % S::kRing), (uint32_t)(it / S::kRing) & 1u)) break;
     }
     ptx::tc_fence_before();
-    __syncthreads();
+    if (kPair) ptx::cluster_sync();   // (neither block ends while the other's MMAs or arrivals may reach it)
+    else __syncthreads();
     if (warp == kMmaWarp) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem_base, 2 * kN);
+        tmem_return<kPair>(tmem_base, 2 * kN);
     }
 }
+
 
 // dw = the splits' sums, added in their order
 template <int kV>
@@ -675,23 +751,33 @@ __global__ void __launch_bounds__(256) ckpt_wgrad_join_kernel(const float *__res
 constexpr int kPlanRows = 64;   // (whole stages of every kernel)
 
 struct WgradPlan8 {
+    bool pair;
     int n_tile, m_tiles, n_tiles, splits;
     size_t rows_per_split;
 };
 
-WgradPlan8 plan_of(size_t rows, int c_out, int c_in)
+// wide: rows of both operands 16-byte aligned
+WgradPlan8 plan_of(size_t rows, int c_out, int c_in, int dtype, bool wide)
 {
     WgradPlan8 p;
+    p.pair = wide && dtype == EOQ_BF16 && c_out > kTileM && c_in > 128;
     p.n_tile = c_in <= 64 ? 64 : c_in <= 128 ? 128 : 256;
-    p.m_tiles = (c_out + kTileM - 1) / kTileM;
+    const int m_tile = p.pair ? 2 * kTileM : kTileM;
+    p.m_tiles = (c_out + m_tile - 1) / m_tile;
     p.n_tiles = (c_in + p.n_tile - 1) / p.n_tile;
-    const size_t tiles = (size_t)p.m_tiles * p.n_tiles, stages = (rows + kPlanRows - 1) / kPlanRows;
-    size_t splits = tiles < (size_t)kPartSms ? kPartSms / tiles : 1;
+    const size_t tiles = (size_t)p.m_tiles * p.n_tiles, stages = (rows + kPlanRows - 1) / kPlanRows, room = kPartSms / (p.pair ? 2 : 1);
+    size_t splits = tiles < room ? room / tiles : 1;
     if (splits > stages) splits = stages;
     const size_t per = (stages + splits - 1) / splits;
     p.splits = (int)((stages + per - 1) / per);
     p.rows_per_split = per * kPlanRows;
     return p;
+}
+
+bool wide_rows(const void *dy, int dtype, int c_out, size_t dy_stride, const void *codes, int c_in)
+{
+    return c_out % 8 == 0 && c_in % 16 == 0 && dy_stride % (dtype == EOQ_F32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(codes) % 16 == 0;
 }
 
 template <int kType, int kN, bool kWide>
@@ -705,19 +791,19 @@ cudaError_t launch(const CkptWgradArgs &a, int grid, cudaStream_t st)
     return launch_chained(ckpt_wgrad_kernel<kType, kN, kWide>, dim3(grid), dim3(kThreads), bytes, st, a);
 }
 
-template <int kN>
+template <int kN, bool kPair>
 cudaError_t launch_tma(const CkptWgradArgs &a, int grid, cudaStream_t st)
 {
+    using S = TmaShape<kN, kPair>;
     CUtensorMap map_dy, map_x;
-    if (!tiled_map_2d(&map_dy, a.dy, true, a.c_out, a.rows, a.dy_stride * 2, 64, TmaShape<kN>::kRows, true) ||
-        !tiled_map_2d(&map_x, a.codes, false, a.c_in, a.rows, a.c_in, kN, TmaShape<kN>::kRows, false))
+    if (!tiled_map_2d(&map_dy, a.dy, true, a.c_out, a.rows, a.dy_stride * 2, 64, S::kRows, true) ||
+        !tiled_map_2d(&map_x, a.codes, false, a.c_in, a.rows, a.c_in, S::kOwn, S::kRows, false))
         return cudaErrorInvalidValue;
-    constexpr int bytes = TmaShape<kN>::kBytes;
-    static_assert(bytes <= kMaxSmem, "shared memory of a block");
+    static_assert(S::kBytes <= kMaxSmem, "shared memory of a block");
     static std::atomic<unsigned long long> allowed;
-    const cudaError_t e = allow_smem((const void *)ckpt_wgrad_tma_kernel<kN>, bytes, allowed);
+    const cudaError_t e = allow_smem((const void *)ckpt_wgrad_tma_kernel<kN, kPair>, S::kBytes, allowed);
     if (e != cudaSuccess) return e;
-    return launch_chained(ckpt_wgrad_tma_kernel<kN>, dim3(grid), dim3(kTmaThreads), bytes, st, a, map_dy, map_x);
+    return launch_chained_clusters(kPair ? 2 : 1, ckpt_wgrad_tma_kernel<kN, kPair>, dim3(grid), dim3(kTmaThreads), S::kBytes, st, a, map_dy, map_x);
 }
 
 template <int kType, bool kWide>
@@ -729,15 +815,14 @@ cudaError_t of_width(const CkptWgradArgs &a, int n_tile, int grid, cudaStream_t 
 }
 
 template <int kType>
-cudaError_t of_type(const CkptWgradArgs &a, int n_tile, int grid, cudaStream_t st)
+cudaError_t of_type(const CkptWgradArgs &a, int n_tile, bool wide, bool pair, int grid, cudaStream_t st)
 {
-    const bool wide = a.c_out % 8 == 0 && a.c_in % 16 == 0 && a.dy_stride % (16 / Elem<kType>::kSize) == 0 &&
-                      reinterpret_cast<uintptr_t>(a.dy) % 16 == 0 && reinterpret_cast<uintptr_t>(a.codes) % 16 == 0;
     if (!wide) return of_width<kType, false>(a, n_tile, grid, st);
     if constexpr (kType == EOQ_BF16) {
-        if (n_tile == 64) return launch_tma<64>(a, grid, st);
-        if (n_tile == 128) return launch_tma<128>(a, grid, st);
-        return launch_tma<256>(a, grid, st);
+        if (pair) return launch_tma<256, true>(a, 2 * grid, st);
+        if (n_tile == 64) return launch_tma<64, false>(a, grid, st);
+        if (n_tile == 128) return launch_tma<128, false>(a, grid, st);
+        return launch_tma<256, false>(a, grid, st);
     } else {
         return of_width<kType, true>(a, n_tile, grid, st);
     }
@@ -745,15 +830,18 @@ cudaError_t of_type(const CkptWgradArgs &a, int n_tile, int grid, cudaStream_t s
 
 }  // namespace
 
-size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in)
+// for either alignment of the call's tensors
+size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in, int dtype)
 {
-    const WgradPlan8 p = plan_of(rows, c_out, c_in);
-    return p.splits > 1 ? sizeof(float) * (size_t)p.splits * c_out * c_in : 0;
+    const WgradPlan8 w = plan_of(rows, c_out, c_in, dtype, true), n = plan_of(rows, c_out, c_in, dtype, false);
+    const int splits = w.splits > n.splits ? w.splits : n.splits;
+    return splits > 1 ? sizeof(float) * (size_t)splits * c_out * c_in : 0;
 }
 
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st)
 {
-    const WgradPlan8 p = plan_of(a.rows, a.c_out, a.c_in);
+    const bool wide = wide_rows(a.dy, dtype, a.c_out, a.dy_stride, a.codes, a.c_in);
+    const WgradPlan8 p = plan_of(a.rows, a.c_out, a.c_in, dtype, wide);
     a.blocks = (a.c_in + kBlock8 - 1) / kBlock8;
     a.m_tiles = p.m_tiles;
     a.n_tiles = p.n_tiles;
@@ -761,9 +849,9 @@ cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *works
     a.safe = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(a.exps) & ~(uintptr_t)15);   // (never read: copies of nothing)
     a.out = p.splits > 1 ? reinterpret_cast<float *>(workspace) : dw;
     const int grid = p.m_tiles * p.n_tiles * p.splits;
-    const cudaError_t e = dtype == EOQ_F32   ? of_type<EOQ_F32>(a, p.n_tile, grid, st)
-                          : dtype == EOQ_F16 ? of_type<EOQ_F16>(a, p.n_tile, grid, st)
-                                             : of_type<EOQ_BF16>(a, p.n_tile, grid, st);
+    const cudaError_t e = dtype == EOQ_F32   ? of_type<EOQ_F32>(a, p.n_tile, wide, p.pair, grid, st)
+                          : dtype == EOQ_F16 ? of_type<EOQ_F16>(a, p.n_tile, wide, p.pair, grid, st)
+                                             : of_type<EOQ_BF16>(a, p.n_tile, wide, p.pair, grid, st);
     ++*launches;
     if (e != cudaSuccess || p.splits == 1) return e;
     ++*launches;

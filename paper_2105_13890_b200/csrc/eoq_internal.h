@@ -545,7 +545,7 @@ struct CkptWgradArgs {
     size_t rows_per_split;
     int blocks, m_tiles, n_tiles;   // blocks: of a row of codes
 };
-size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in);
+size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in, int dtype);
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st);
 
 // Division by a number that a launch keeps: exact as long as dividend times divisor stays below 2^32.

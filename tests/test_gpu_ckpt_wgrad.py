@@ -1,4 +1,6 @@
 """Weight gradients from errors and the 8-bit form of the input (eoq_ckpt_wgrad) against sums in 64 bits."""
+import itertools
+
 import numpy as np
 import pytest
 import torch
@@ -51,14 +53,21 @@ def test_shapes_and_types(rows, c_out, c_in, extra, name):
     check(*make(rows, c_out, c_in, name, rows + c_in, extra), name, c_out)
 
 
+@pytest.mark.parametrize("name", sorted(TYPES))
+@pytest.mark.parametrize("rows,c_out,c_in", [(1, 136, 144), (64, 256, 256), (1000, 264, 528), (5000, 512, 272), (2500, 1024, 256), (9000, 136, 1040)])
+def test_tiles_of_two_blocks(rows, c_out, c_in, name):
+    """More than 128 columns on both sides: in bf16, blocks work in pairs; ends inside either block's half; sums that move on."""
+    check(*make(rows, c_out, c_in, name, rows + c_in), name, c_out)
+
+
 def test_every_operand_has_its_place():
     """One row at a time against the outer product: exact, so that a swapped row, column or part shows."""
-    for name in sorted(TYPES):
+    for name, c_out in itertools.product(sorted(TYPES), (128, 256)):
         for row in (0, 1, 7, 8, 15, 16, 63, 64, 100):
-            dy, codes, exps, back = make(101, 128, 256, name, 7)
+            dy, codes, exps, back = make(101, c_out, 256, name, 7)
             keep = torch.zeros_like(dy)
             keep[row] = dy[row]
-            got = call(keep, codes, exps, name, 128).double().cpu().numpy()
+            got = call(keep, codes, exps, name, c_out).double().cpu().numpy()
             want = np.outer(keep[row].double().cpu().numpy(), back[row])
             # three parts are added in two roundings; with one or two parts the last of them rounds
             R.within(got, want, {"bf16": 0, "fp16": 2.0 ** -23, "fp32": 2.0 ** -22}[name] * np.abs(want))
