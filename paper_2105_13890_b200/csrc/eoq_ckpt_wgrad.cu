@@ -321,12 +321,11 @@ struct Feeder {
                     for (int j = 0; j < 4; ++j) h[j] = __byte_perm(__float_as_uint(v[2 * j]), __float_as_uint(v[2 * j + 1]), 0x7632);
                     st_shared_128(dst + p * S::kATile, make_uint4(h[0], h[1], h[2], h[3]));
                     // what the upper halves leave: exact; nothing of an infinity
-                    if (p + 1 < S::kParts)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
-                            v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
+                        v[j] = fabsf(v[j]) == INFINITY ? 0.0f : v[j] - hi;
+                    }
                 }
             }
         }
@@ -365,7 +364,7 @@ __device__ __forceinline__ void store_tile(const CkptWgradArgs &a, int split, in
     const int warp = warp_index_uniform(), quad = warp & 3, o = o0 + quad * 32 + (threadIdx.x & 31);
     if (warp >= 8 || !__all_sync(0xffffffffu, wait_bar<64>(end_bar, 0, ctx))) return;
     ptx::tc_fence_after();
-    float *dst = a.out + (size_t)split * a.c_out * a.c_in + (size_t)o * a.c_in;
+    float *dst = a.out + (size_t)split * a.pitch + (size_t)o * a.c_in;
     constexpr int kHalf = kN / 2;
 #pragma unroll 1
     for (int c0 = (warp >> 2) * kHalf; c0 < (warp >> 2) * kHalf + kHalf; c0 += 32) {
@@ -461,6 +460,7 @@ __global__ void __launch_bounds__(kThreads, 1) ckpt_wgrad_kernel(const __grid_co
     __syncthreads();
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
+    if (a.joins) ptx::grid_dep_launch();   // (the joining kernel comes up beside this one)
     const uint32_t tmem_base = tmem_base_s, tmem_run = tmem_base + kN;
     const RoleCtx ctx{&abort_s, a.dev};
 
@@ -605,6 +605,7 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
     else __syncthreads();
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
+    if (a.joins) ptx::grid_dep_launch();   // (the joining kernel comes up beside this one)
     const uint32_t tmem_base = tmem_base_s, tmem_run = tmem_base + kN;
     const RoleCtx ctx{&abort_s, a.dev};
 
@@ -729,22 +730,43 @@ ckpt_wgrad_tma_kernel(const __grid_constant__ CkptWgradArgs a, const __grid_cons
 }
 
 
-// dw = the splits' sums, added in their order
-template <int kV>
-__global__ void __launch_bounds__(256) ckpt_wgrad_join_kernel(const float *__restrict__ part, size_t n, int splits, float *__restrict__ dw)
+// dw = the splits' sums, which stand `pitch` floats apart: four neighbouring ones a thread, kShares warps of a block to the same ones, each
+// with every kShares-th split in order, then the shares in order.  (One share leaves too few loads in flight where the matrix is small.)
+template <int kShares>
+__global__ void __launch_bounds__(256) ckpt_wgrad_join_kernel(const float *__restrict__ part, size_t n, size_t pitch, int splits, float *__restrict__ dw)
 {
+    __shared__ float4 share[kShares][256 / kShares];
     ptx::grid_dep_wait_launch_small();
-    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * kV; i < n; i += (size_t)gridDim.x * 256 * kV) {
-        float t[kV];
-#pragma unroll
-        for (int j = 0; j < kV; ++j) t[j] = 0.0f;
-        for (int s = 0; s < splits; ++s) {
-            float v[kV];
-            Elem<EOQ_F32>::to_f32(load_raw<4 * kV>(part + (size_t)s * n + i), v);
-#pragma unroll
-            for (int j = 0; j < kV; ++j) t[j] += v[j];
+    constexpr int kPieces = 256 / kShares;
+    const int piece = threadIdx.x % kPieces, own = threadIdx.x / kPieces;
+    for (size_t i0 = (size_t)blockIdx.x * kPieces * 4; i0 < n; i0 += (size_t)gridDim.x * kPieces * 4) {
+        const size_t i = i0 + piece * 4;
+        float4 t = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        auto add = [&](const float4 &v) {
+            t.x += v.x;
+            t.y += v.y;
+            t.z += v.z;
+            t.w += v.w;
+        };
+        if (i < n)
+#pragma unroll 4
+            for (int s = own; s < splits; s += kShares) add(__ldg(reinterpret_cast<const float4 *>(part + (size_t)s * pitch + i)));
+        if (kShares > 1) {
+            share[own][piece] = t;
+            __syncthreads();
+            t = share[0][piece];
+            if (own == 0)
+                for (int w = 1; w < kShares; ++w) add(share[w][piece]);
+            __syncthreads();
         }
-        store_raw(dw + i, Elem<EOQ_F32>::from_f32(t));
+        if (own == 0 && i < n) {
+            if (i + 4 <= n) {
+                *reinterpret_cast<float4 *>(dw + i) = t;
+            } else {
+                const float v[3] = {t.x, t.y, t.z};
+                for (int j = 0; j < (int)(n - i); ++j) dw[i + j] = v[j];
+            }
+        }
     }
 }
 
@@ -756,22 +778,53 @@ struct WgradPlan8 {
     size_t rows_per_split;
 };
 
-// wide: rows of both operands 16-byte aligned
+// Microseconds of a block for 64 rows, by the width of its tile (64, 128, 256), as measured with every SM at work: what the conversions
+// take, not the MMAs (0.27 at 256).
+double rows_time(int dtype, bool wide, int width)
+{
+    static const double kTimes[2][3][3] = {{{2.3, 2.45, 2.8}, {1.2, 1.45, 1.85}, {1.07, 1.13, 1.69}},    // fp32, fp16, bf16
+                                           {{1.85, 1.85, 2.1}, {0.8, 0.86, 1.33}, {0.35, 0.43, 0.5}}};
+    return kTimes[wide ? 1 : 0][dtype == EOQ_F32 ? 0 : dtype == EOQ_F16 ? 1 : 2][width];
+}
+
+// The tile and the number of splits that take the least time by that: waves of blocks, each with some 6 us in front of and behind its
+// rows, and the joining kernel's launch and reading (512 to 2048 channels, 1,568 rows of bf16: 14 us without splits in tiles of 64,
+// 17 us in four splits of tiles of two blocks).  wide: rows of both operands 16-byte aligned; bf16 then has a tile of 256 x 256 for two
+// blocks, and none of 128 x 256.
 WgradPlan8 plan_of(size_t rows, int c_out, int c_in, int dtype, bool wide)
 {
-    WgradPlan8 p;
-    p.pair = wide && dtype == EOQ_BF16 && c_out > kTileM && c_in > 128;
-    p.n_tile = c_in <= 64 ? 64 : c_in <= 128 ? 128 : 256;
-    const int m_tile = p.pair ? 2 * kTileM : kTileM;
-    p.m_tiles = (c_out + m_tile - 1) / m_tile;
-    p.n_tiles = (c_in + p.n_tile - 1) / p.n_tile;
-    const size_t tiles = (size_t)p.m_tiles * p.n_tiles, stages = (rows + kPlanRows - 1) / kPlanRows, room = kPartSms / (p.pair ? 2 : 1);
-    size_t splits = tiles < room ? room / tiles : 1;
-    if (splits > stages) splits = stages;
-    const size_t per = (stages + splits - 1) / splits;
-    p.splits = (int)((stages + per - 1) / per);
-    p.rows_per_split = per * kPlanRows;
-    return p;
+    const bool tma = wide && dtype == EOQ_BF16;
+    const size_t stages = (rows + kPlanRows - 1) / kPlanRows;
+    WgradPlan8 best = {};
+    double best_time = 0.0;
+    for (int width = 0; width < 3; ++width) {
+        WgradPlan8 p;
+        p.n_tile = 64 << width;
+        p.pair = tma && width == 2;
+        if (p.pair && (c_out <= kTileM || c_in <= 128)) continue;
+        if (width > 0 && c_in <= p.n_tile / 2) continue;
+        const int m_tile = p.pair ? 2 * kTileM : kTileM;
+        p.m_tiles = (c_out + m_tile - 1) / m_tile;
+        p.n_tiles = (c_in + p.n_tile - 1) / p.n_tile;
+        const size_t tiles = (size_t)p.m_tiles * p.n_tiles, room = kPartSms / (p.pair ? 2 : 1);
+        for (size_t fill = 0; fill <= 2; ++fill) {
+            size_t splits = fill == 0 ? 1 : fill * room / tiles;
+            if (splits < 1 || (fill > 0 && splits == 1)) continue;
+            if (splits > stages) splits = stages;
+            const size_t per = (stages + splits - 1) / splits;
+            splits = (stages + per - 1) / per;
+            p.splits = (int)splits;
+            p.rows_per_split = per * kPlanRows;
+            const double waves = (double)((tiles * splits + room - 1) / room);
+            const double time = waves * (6.0 + (double)per * rows_time(dtype, wide, width)) +
+                                (splits > 1 ? 3.0 + (double)splits * c_out * c_in * 4.0 / 4e6 : 0.0);
+            if (best_time == 0.0 || time < best_time) {
+                best = p;
+                best_time = time;
+            }
+        }
+    }
+    return best;
 }
 
 bool wide_rows(const void *dy, int dtype, int c_out, size_t dy_stride, const void *codes, int c_in)
@@ -820,9 +873,7 @@ cudaError_t of_type(const CkptWgradArgs &a, int n_tile, bool wide, bool pair, in
     if (!wide) return of_width<kType, false>(a, n_tile, grid, st);
     if constexpr (kType == EOQ_BF16) {
         if (pair) return launch_tma<256, true>(a, 2 * grid, st);
-        if (n_tile == 64) return launch_tma<64, false>(a, grid, st);
-        if (n_tile == 128) return launch_tma<128, false>(a, grid, st);
-        return launch_tma<256, false>(a, grid, st);
+        return n_tile == 64 ? launch_tma<64, false>(a, grid, st) : launch_tma<128, false>(a, grid, st);
     } else {
         return of_width<kType, true>(a, n_tile, grid, st);
     }
@@ -830,12 +881,15 @@ cudaError_t of_type(const CkptWgradArgs &a, int n_tile, bool wide, bool pair, in
 
 }  // namespace
 
+// floats of a split's sums: whole pieces of 16 bytes
+static size_t split_pitch(int c_out, int c_in) { return ((size_t)c_out * c_in + 3) & ~(size_t)3; }
+
 // for either alignment of the call's tensors
 size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in, int dtype)
 {
     const WgradPlan8 w = plan_of(rows, c_out, c_in, dtype, true), n = plan_of(rows, c_out, c_in, dtype, false);
     const int splits = w.splits > n.splits ? w.splits : n.splits;
-    return splits > 1 ? sizeof(float) * (size_t)splits * c_out * c_in : 0;
+    return splits > 1 ? sizeof(float) * (size_t)splits * split_pitch(c_out, c_in) : 0;
 }
 
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st)
@@ -847,6 +901,8 @@ cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *works
     a.n_tiles = p.n_tiles;
     a.rows_per_split = p.rows_per_split;
     a.safe = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(a.exps) & ~(uintptr_t)15);   // (never read: copies of nothing)
+    a.joins = p.splits > 1;
+    a.pitch = split_pitch(a.c_out, a.c_in);
     a.out = p.splits > 1 ? reinterpret_cast<float *>(workspace) : dw;
     const int grid = p.m_tiles * p.n_tiles * p.splits;
     const cudaError_t e = dtype == EOQ_F32   ? of_type<EOQ_F32>(a, p.n_tile, wide, p.pair, grid, st)
@@ -855,10 +911,12 @@ cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *works
     ++*launches;
     if (e != cudaSuccess || p.splits == 1) return e;
     ++*launches;
-    const size_t n = (size_t)a.c_out * a.c_in, per = n % 4 == 0 ? 4 : 1, blocks = (n / per + 255) / 256, cap = 8 * kPartSms;
+    const size_t n = (size_t)a.c_out * a.c_in, pieces = (n + 3) / 4, cap = 8 * kPartSms;
+    const bool small = pieces < (size_t)kPartSms * 256;
+    const size_t blocks = small ? (pieces + 31) / 32 : (pieces + 255) / 256;
     const dim3 join((unsigned)(blocks < cap ? blocks : cap));
-    if (per == 4) return launch_chained(ckpt_wgrad_join_kernel<4>, join, dim3(256), 0, st, (const float *)a.out, n, p.splits, dw);
-    return launch_chained(ckpt_wgrad_join_kernel<1>, join, dim3(256), 0, st, (const float *)a.out, n, p.splits, dw);
+    if (small) return launch_chained(ckpt_wgrad_join_kernel<8>, join, dim3(256), 0, st, (const float *)a.out, n, a.pitch, p.splits, dw);
+    return launch_chained(ckpt_wgrad_join_kernel<1>, join, dim3(256), 0, st, (const float *)a.out, n, a.pitch, p.splits, dw);
 }
 
 }  // namespace eoq

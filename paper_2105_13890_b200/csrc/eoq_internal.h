@@ -541,9 +541,11 @@ struct CkptWgradArgs {
     DeviceState *dev;
     // filled in by the launcher
     const void *safe;               // an aligned address for copies of nothing
-    float *out;                     // [split][c_out][c_in]
+    float *out;                     // [c_out][c_in] of every split, `pitch` floats apart
+    size_t pitch;
     size_t rows_per_split;
     int blocks, m_tiles, n_tiles;   // blocks: of a row of codes
+    bool joins;                     // several splits, whose sums another kernel adds
 };
 size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in, int dtype);
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st);

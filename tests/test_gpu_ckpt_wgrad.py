@@ -60,6 +60,13 @@ def test_tiles_of_two_blocks(rows, c_out, c_in, name):
     check(*make(rows, c_out, c_in, name, rows + c_in), name, c_out)
 
 
+@pytest.mark.parametrize("rows,c_out,c_in", [(3000, 3, 7), (9000, 33, 31), (700, 1, 5)])
+def test_splits_of_odd_matrices(rows, c_out, c_in):
+    """Several splits of a matrix whose elements are no multiple of four."""
+    assert c_out * c_in % 4 and eoq.eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, eoq.EOQ_F16) > 0
+    check(*make(rows, c_out, c_in, "fp16", rows), "fp16", c_out)
+
+
 def test_every_operand_has_its_place():
     """One row at a time against the outer product: exact, so that a swapped row, column or part shows."""
     for name, c_out in itertools.product(sorted(TYPES), (128, 256)):
