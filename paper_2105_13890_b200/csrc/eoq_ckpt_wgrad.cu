@@ -137,22 +137,25 @@ __device__ __forceinline__ void arrive_first(uint32_t bar)
 template <bool kPair>
 __device__ __forceinline__ bool wait_both(uint32_t bar, uint32_t parity, const RoleCtx &c)
 {
-    if constexpr (!kPair) return wait_bar(bar, parity, c);
-    for (uint32_t i = 0; i < kSpinLimit; ++i) {
-        uint32_t done;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-        if (done) return true;
-        if (*c.abort_flag) return false;
+    if constexpr (!kPair) {
+        return wait_bar(bar, parity, c);
+    } else {
+        for (uint32_t i = 0; i < kSpinLimit; ++i) {
+            uint32_t done;
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t"
+                "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\t}"
+                : "=r"(done)
+                : "r"(bar), "r"(parity)
+                : "memory");
+            if (done) return true;
+            if (*c.abort_flag) return false;
+        }
+        *c.abort_flag = 1u;
+        atomicOr(&c.dev->status, EOQ_DEV_TIMEOUT);
+        return false;
     }
-    *c.abort_flag = 1u;
-    atomicOr(&c.dev->status, EOQ_DEV_TIMEOUT);
-    return false;
 }
 template <bool kPair>
 __device__ __forceinline__ void tmem_take(uint32_t result, uint32_t columns)

@@ -131,51 +131,53 @@ __global__ void __launch_bounds__(kThreads) gn_apply_kernel(const __grid_constan
         for (int i = 0; i < kV; ++i) {
             const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
             mean[i] = st.x;
-            mul[i] = a.gamma ? st.y * a.gamma[ch + i] : st.y;
-            add[i] = a.beta ? a.beta[ch + i] : 0.0f;
+            mul[i] = (a.gamma ? st.y * a.gamma[ch + i] : st.y) * act_scale(a.act);
+            add[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
         }
     const size_t pix0 = (size_t)smp * a.hw;
     unsigned bad = 0;
-    for (int p0 = p_begin; p0 < p_end; p0 += kUnroll * a.slots) {
-        Raw<kB> raw[kUnroll];
+    with_act(a.act, [&](auto kind) {
+        for (int p0 = p_begin; p0 < p_end; p0 += kUnroll * a.slots) {
+            Raw<kB> raw[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int p = p0 + slot + u * a.slots;
-            raw[u] = mine && p < p_end ? load_raw<kB>(reinterpret_cast<const char *>(a.x) + ((pix0 + p) * a.x_stride + ch) * Elem<kType>::kSize)
-                                       : zero_raw<kB>();
-        }
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + slot + u * a.slots;
+                raw[u] = mine && p < p_end ? load_raw<kB>(reinterpret_cast<const char *>(a.x) + ((pix0 + p) * a.x_stride + ch) * Elem<kType>::kSize)
+                                           : zero_raw<kB>();
+            }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int p = p0 + slot + u * a.slots;
-            const bool in = mine && p < p_end;
-            float v[kV];
-            x_values<kType, kV>(raw[u], a.x_scale, v);
-            if constexpr (kSave) {
-                float m = 0.0f;
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + slot + u * a.slots;
+                const bool in = mine && p < p_end;
+                float v[kV];
+                x_values<kType, kV>(raw[u], a.x_scale, v);
+                if constexpr (kSave) {
+                    float m = 0.0f;
 #pragma unroll
-                for (int i = 0; i < kV; ++i) m = max_abs(m, v[i]);
-                m = lanes_max_abs<kLanes>(m);
-                const int s = block_exp(m);
-                uint32_t w[(kV + 3) / 4];
-                block_codes(v, s, w);
+                    for (int i = 0; i < kV; ++i) m = max_abs(m, v[i]);
+                    m = lanes_max_abs<kLanes>(m);
+                    const int s = block_exp(m);
+                    uint32_t w[(kV + 3) / 4];
+                    block_codes(v, s, w);
+                    if (in) {
+                        Raw<kV> out;
+#pragma unroll
+                        for (int i = 0; i < (kV + 3) / 4; ++i) set_word(out, i, w[i]);
+                        store_raw(a.codes_out + (pix0 + p) * a.c + ch, out);
+                        if (ch % kBlock8 == 0) a.exps_out[(pix0 + p) * a.blocks + ch / kBlock8] = (uint8_t)s;
+                        bad |= s == 255;
+                    }
+                }
                 if (in) {
-                    Raw<kV> out;
 #pragma unroll
-                    for (int i = 0; i < (kV + 3) / 4; ++i) set_word(out, i, w[i]);
-                    store_raw(a.codes_out + (pix0 + p) * a.c + ch, out);
-                    if (ch % kBlock8 == 0) a.exps_out[(pix0 + p) * a.blocks + ch / kBlock8] = (uint8_t)s;
-                    bad |= s == 255;
+                    for (int i = 0; i < kV; ++i) v[i] = __fmaf_rn(v[i] - mean[i], mul[i], add[i]);
+                    activate<decltype(kind)::value>(v);
+                    store_raw(reinterpret_cast<char *>(a.y) + ((pix0 + p) * a.y_stride + ch) * Elem<Types::kY>::kSize,
+                              Elem<Types::kY>::from_f32(v));
                 }
             }
-            if (in) {
-#pragma unroll
-                for (int i = 0; i < kV; ++i) v[i] = __fmaf_rn(v[i] - mean[i], mul[i], add[i]);
-                activate(v, a.act);
-                store_raw(reinterpret_cast<char *>(a.y) + ((pix0 + p) * a.y_stride + ch) * Elem<Types::kY>::kSize,
-                          Elem<Types::kY>::from_f32(v));
-            }
         }
-    }
+    });
     if (kSave && bad) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
 }
 
@@ -194,28 +196,30 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
             const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
             rstd[i] = st.y;
             off[i] = -st.x * st.y;
-            gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
-            beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
+            gamma[i] = (a.gamma ? a.gamma[ch + i] : 1.0f) * act_scale(a.act);
+            beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
             s0[i] = s1[i] = 0.0f;
         }
         const float dy_scale = error_scale<kType>(a);
         const size_t pix0 = (size_t)smp * a.hw;
-        for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-            GnInput<kType, kV, kCodes> in[kUnroll];
+        with_act(a.act, [&](auto kind) {
+            for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
+                GnInput<kType, kV, kCodes> in[kUnroll];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
+                for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                if (p0 + k * a.slots >= p_end) break;
-                float u[kV], dz[kV];
-                in[k].values(a, rstd, off, gamma, beta, dy_scale, u, dz);
+                for (int k = 0; k < kUnroll; ++k) {
+                    if (p0 + k * a.slots >= p_end) break;
+                    float u[kV], dz[kV];
+                    in[k].template values<decltype(kind)::value>(a, rstd, off, gamma, beta, dy_scale, u, dz);
 #pragma unroll
-                for (int i = 0; i < kV; ++i) {
-                    s0[i] += dz[i];
-                    s1[i] = __fmaf_rn(dz[i], u[i], s1[i]);
+                    for (int i = 0; i < kV; ++i) {
+                        s0[i] += dz[i];
+                        s1[i] = __fmaf_rn(dz[i], u[i], s1[i]);
+                    }
                 }
             }
-        }
+        });
 #pragma unroll
         for (int i = 0; i < kV; ++i) cell[(slot * a.cv + cv) * kV + i] = make_float2(s0[i], s1[i]);
     }
@@ -291,36 +295,39 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     if (slot >= a.slots || ch >= a.c) return;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
-    float rstd[kV], off[kV], gamma[kV], beta[kV], k0[kV], k1[kV];
+    float rstd[kV], off[kV], gamma[kV], beta[kV], by[kV], k0[kV], k1[kV];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
         const size_t g = (size_t)smp * a.groups + (ch + i) / a.cpg;
         const float2 st = a.stats[g], m = a.means[g];
         rstd[i] = st.y;
         off[i] = -st.x * st.y;
-        gamma[i] = a.gamma ? a.gamma[ch + i] : 1.0f;
-        beta[i] = a.beta ? a.beta[ch + i] : 0.0f;
+        gamma[i] = (a.gamma ? a.gamma[ch + i] : 1.0f) * act_scale(a.act);
+        by[i] = a.gamma ? st.y * a.gamma[ch + i] : st.y;
+        beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
         k0[i] = -st.y * m.x;
         k1[i] = -st.y * m.y;
     }
     const float dy_scale = error_scale<kType>(a);
     const size_t pix0 = (size_t)smp * a.hw;
-    for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-        GnInput<kType, kV, kCodes> in[kUnroll];
+    with_act(a.act, [&](auto kind) {
+        for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
+            GnInput<kType, kV, kCodes> in[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
+            for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-            const int p = p0 + k * a.slots;
-            if (p >= p_end) break;
-            float u[kV], dz[kV];
-            in[k].values(a, rstd, off, gamma, beta, dy_scale, u, dz);
+            for (int k = 0; k < kUnroll; ++k) {
+                const int p = p0 + k * a.slots;
+                if (p >= p_end) break;
+                float u[kV], dz[kV];
+                in[k].template values<decltype(kind)::value>(a, rstd, off, gamma, beta, dy_scale, u, dz);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i] * gamma[i], rstd[i], __fmaf_rn(u[i], k1[i], k0[i]));
-            store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,
-                      Elem<Types::kDx>::from_f32(dz));
+                for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i], by[i], __fmaf_rn(u[i], k1[i], k0[i]));
+                store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,
+                          Elem<Types::kDx>::from_f32(dz));
+            }
         }
-    }
+    });
 }
 
 // How the channels and pixels of a call are dealt out to thread blocks.

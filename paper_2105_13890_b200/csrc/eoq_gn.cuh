@@ -1,5 +1,7 @@
 // Group normalisation: what its kernels share.
 #pragma once
+#include <type_traits>
+
 #include "eoq_block8.cuh"
 
 namespace eoq {
@@ -63,41 +65,54 @@ __device__ __forceinline__ float rcp_approx(float v)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// 1 / (1 + exp(-z)); an exp that overflows leaves 0, as the limit does.
-__device__ __forceinline__ Pair sigmoid2(Pair z)
+// Activations work on s z, s = act_scale(): for SiLU -log2(e), so that the exponential's argument takes no multiplication of its own; it
+// rides on gamma and beta.
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+__device__ __forceinline__ float act_scale(int act) { return act == EOQ_ACT_SILU ? -kLog2e : 1.0f; }
+
+// Calls f with the activation as a compile-time constant, so that no vector of a batch waits for a test of it; kAnyAct leaves the test to
+// each vector, which keeps the vectors apart and takes fewer registers.
+constexpr int kAnyAct = -1;
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f)
 {
-    const Pair t = z * both(-1.44269504f);
-    const Pair a = Pair{ex2_approx(t.x), ex2_approx(t.y)} + both(1.0f);
-    return Pair{rcp_approx(a.x), rcp_approx(a.y)};
+    if (act == EOQ_ACT_SILU) f(std::integral_constant<int, EOQ_ACT_SILU>());
+    else if (act == EOQ_ACT_RELU) f(std::integral_constant<int, EOQ_ACT_RELU>());
+    else f(std::integral_constant<int, EOQ_ACT_NONE>());
 }
 
-template <int kN>
-__device__ __forceinline__ void activate(float (&z)[kN], int act)
+// act(z), in the place of s z.  SiLU: s z / (s (1 + 2^(s z))); an exponential that overflows leaves 0, as the limit does.
+template <int kAct, int kN>
+__device__ __forceinline__ void activate(float (&z)[kN])
 {
-    if (act == EOQ_ACT_RELU) {
+    if (kAct == EOQ_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) z[i] = z[i] < 0.0f ? 0.0f : z[i];   // (a NaN stays one)
-    } else if (act == EOQ_ACT_SILU) {
+    } else if (kAct == EOQ_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < kPairs<kN>; ++i) {
-            const Pair v = pair_of(z, i), q = sigmoid2(v);
-            set_pair(z, i, v * q);
+            const Pair v = pair_of(z, i);
+            const Pair a = fma2(Pair{ex2_approx(v.x), ex2_approx(v.y)}, both(-kLog2e), both(-kLog2e));
+            set_pair(z, i, v * Pair{rcp_approx(a.x), rcp_approx(a.y)});
         }
     }
 }
 
-// e[i] *= slope of the activation at z[i]
-template <int kN>
-__device__ __forceinline__ void times_slope(float (&e)[kN], const float (&z)[kN], int act)
+// e[i] *= slope of the activation where z[i] is s z.  SiLU: q (1 + z (1 - q)), q = 1 / (1 + 2^(s z)).
+template <int kAct, int kN>
+__device__ __forceinline__ void times_slope(float (&e)[kN], const float (&z)[kN], int any_act)
 {
+    const int act = kAct == kAnyAct ? any_act : kAct;
     if (act == EOQ_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < kN; ++i) e[i] = z[i] > 0.0f ? e[i] : z[i] != z[i] ? z[i] : 0.0f;
     } else if (act == EOQ_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < kPairs<kN>; ++i) {
-            const Pair v = pair_of(z, i), q = sigmoid2(v);
-            set_pair(e, i, pair_of(e, i) * (q * fma2(v, fma2(q, both(-1.0f), both(1.0f)), both(1.0f))));
+            const Pair v = pair_of(z, i);
+            const Pair a = Pair{ex2_approx(v.x), ex2_approx(v.y)} + both(1.0f);
+            const Pair q = {rcp_approx(a.x), rcp_approx(a.y)};
+            set_pair(e, i, pair_of(e, i) * (q * fma2(v, fma2(q, both(kLn2), both(-kLn2)), both(1.0f))));
         }
     }
 }
@@ -113,9 +128,9 @@ __device__ __forceinline__ void x_values(const Raw<kN * Elem<kType>::kSize> &r, 
 }
 
 // u = (x - mean) rstd and dz = dy act'(gamma u + beta) of kN neighbouring channels; x from the kept tensor, or from its 8-bit form with
-// the byte s of their block.  Of kW neighbouring channels all are of one group: mean and rstd come once for each kW.  off = -mean rstd:
-// the step of the 8-bit form goes into the factor of u (a power of two, so exactly).
-template <int kType, int kN, bool kCodes, int kW>
+// the byte s of their block; gamma and beta times act_scale().  Of kW neighbouring channels all are of one group: mean and rstd come once
+// for each kW.  off = -mean rstd: the step of the 8-bit form goes into the factor of u (a power of two, so exactly).
+template <int kAct, int kType, int kN, bool kCodes, int kW>
 __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType>::kSize> &x, int s, const Raw<kN * Elem<GnTypes<kType>::kY>::kSize> &dy,
                                          float x_scale, float dy_scale, int act, const float (&off)[kN / kW], const float (&rstd)[kN / kW],
                                          const float (&gamma)[kN], const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
@@ -140,7 +155,7 @@ __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType
         set_pair(z, i, fma2(v, pair_of(gamma, i), pair_of(beta, i)));
         if (kType == EOQ_I32) set_pair(dz, i, pair_of(dz, i) * both(dy_scale));
     }
-    times_slope(dz, z, act);
+    times_slope<kAct>(dz, z, act);
 }
 
 // What the backward pass reads of a pixel: x or its 8-bit form, and the error.
@@ -165,10 +180,11 @@ struct GnInput {
         }
         dy = load_raw<kDyB>(reinterpret_cast<const char *>(a.dy) + (pix * a.dy_stride + ch) * Elem<Types::kY>::kSize);
     }
+    template <int kAct>
     __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&off)[kV], const float (&gamma)[kV],
                                            const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
     {
-        gn_terms<kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
+        gn_terms<kAct, kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
     }
 };
 

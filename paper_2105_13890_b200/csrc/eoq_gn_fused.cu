@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
 
     // ---- y, and the 8-bit form
     float mul[kV], add[kV], mean[kG];
+    const float scale = act_scale(a.act);
     int g = a.by_cpg(cv * kV), in_g = cv * kV - g * a.cpg;   // group of the next kW channels, and where in it
 #pragma unroll
     for (int k = 0; k < kG; ++k) {
@@ -169,8 +170,8 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
         mean[k] = -st.x;
 #pragma unroll
         for (int j = k * kW; j < (k + 1) * kW; ++j) {
-            mul[j] = active ? st.y * gamma[cv * kV + j] : 0.0f;
-            add[j] = active ? beta[cv * kV + j] : 0.0f;
+            mul[j] = active ? st.y * gamma[cv * kV + j] * scale : 0.0f;
+            add[j] = active ? beta[cv * kV + j] * scale : 0.0f;
         }
         in_g += kW;
         if (in_g == a.cpg) {
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
     uint8_t *exps = kSave ? a.exps_out + pix0 * a.blocks + ch / kBlock8 : nullptr;
     const size_t y_step = a.slots * a.y_stride * kYE, codes_step = (size_t)a.slots * a.c, exps_step = (size_t)a.slots * a.blocks;
     unsigned bad = 0;
-    auto emit = [&](const Raw<kB> &raw, bool in) {
+    auto emit = [&](auto kind, const Raw<kB> &raw, bool in) {
         float v[kV];
         x_values<kType, kV>(raw, a.x_scale, v);
         if constexpr (kSave) {
@@ -212,7 +213,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
                 const Pair m = {mean[2 * j / kW], mean[kV == 1 ? 0 : (2 * j + 1) / kW]};
                 set_pair(v, j, fma2(pair_of(v, j) + m, pair_of(mul, j), pair_of(add, j)));
             }
-            activate(v, a.act);
+            activate<decltype(kind)::value>(v);
             store_raw(y, Elem<Types::kY>::from_f32(v));
         }
         y += y_step;
@@ -220,19 +221,21 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
     // Lanes that share a block of the 8-bit form stay together: full batches are those of the whole warp.
     const int least = kSave ? (int)__reduce_min_sync(0xffffffffu, (unsigned)vecs) : vecs;
     const int rounds = kSave ? (int)__reduce_max_sync(0xffffffffu, (unsigned)vecs) : vecs;
-    const char *at = x.first();
-    int i = 0;
-    for (; i + kGnBatch <= least; i += kGnBatch) {
-        Raw<kB> raw[kGnBatch];
-        x.get(raw, i, at);
+    with_act(a.act, [&](auto kind) {
+        const char *at = x.first();
+        int i = 0;
+        for (; i + kGnBatch <= least; i += kGnBatch) {
+            Raw<kB> raw[kGnBatch];
+            x.get(raw, i, at);
 #pragma unroll
-        for (int u = 0; u < kGnBatch; ++u) emit(raw[u], true);
-    }
-    for (; i < rounds; ++i) {
-        Raw<kB> raw[1] = {zero_raw<kB>()};
-        if (i < vecs) x.get(raw, i, at);
-        emit(raw[0], i < vecs);
-    }
+            for (int u = 0; u < kGnBatch; ++u) emit(kind, raw[u], true);
+        }
+        for (; i < rounds; ++i) {
+            Raw<kB> raw[1] = {zero_raw<kB>()};
+            if (i < vecs) x.get(raw, i, at);
+            emit(kind, raw[0], i < vecs);
+        }
+    });
     if (kSave && bad) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
 }
 

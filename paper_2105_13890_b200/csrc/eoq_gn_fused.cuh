@@ -47,6 +47,7 @@ struct Vectors {
             const char *p = at;
             if constexpr (kBytes >= 4) {
                 uint32_t to = ptx::smem_u32(base);
+#pragma unroll 4
                 for (int i = 0; i < count; ++i, p += step, to += kGnThreads * kBytes) copy_in<kBytes>(to, p);
             } else {
                 constexpr int kMany = 8;

@@ -11,19 +11,20 @@ namespace eoq {
 
 namespace {
 
-// shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2), gamma, beta
+// shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2); gamma, gamma and beta times
+// act_scale(), gamma times rstd
 template <int kV>
 struct BwdLayout {
     __host__ __device__ static size_t bytes(int cv)
     {
         const int slots = kGnThreads / cv, width = cv * kV;
-        return sizeof(float2) * ((size_t)kGnThreads * kV + (size_t)(slots < kGnWarps ? slots : kGnWarps) * width + (8 + 3) * (size_t)width);
+        return sizeof(float2) * ((size_t)kGnThreads * kV + (size_t)(slots < kGnWarps ? slots : kGnWarps) * width + (8 + 4) * (size_t)width);
     }
 };
 
 // kW: so many neighbouring channels of a vector are always of one group (the common divisor of both widths)
 template <int kType, int kV, int kW, bool kCodes, bool kKeep>
-__global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __grid_constant__ GnArgs a)
+__global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_kernel(const __grid_constant__ GnArgs a)
 {
     using Types = GnTypes<kType>;
     using Input = GnInput<kType, kV, kCodes>;
@@ -31,9 +32,9 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
     extern __shared__ __align__(16) uint8_t smem[];
     const int width = a.cv * kV, rows = min(a.slots, kGnWarps);
     const size_t all = kKeep ? (size_t)a.vecs * kGnThreads : 0;
-    float2 *cell = reinterpret_cast<float2 *>(smem + all * (Input::kDyB + Input::kXB + (kCodes ? 1 : 0)));
+    float2 *cell = reinterpret_cast<float2 *>(smem + all * (Input::kDyB + Input::kXB));
     float2 *by_warp = cell + kGnThreads * kV, *parts = by_warp + rows * width, *total = parts + 8 * width, *means = total + width;   // parts [rank][channel]
-    float *gamma_s = reinterpret_cast<float *>(means + width), *beta_s = gamma_s + width;
+    float *gamma_s = reinterpret_cast<float *>(means + width), *gamma_z = gamma_s + width, *beta_z = gamma_z + width, *gamma_r = beta_z + width;
 
     const int id = a.by_cluster(blockIdx.x), rank = blockIdx.x - id * a.cluster, set = a.by_chunks(id), chunk = id - set * a.chunks;
     const int samples = a.by_ranks(a.cluster), own = a.by_ranks(rank), smp = set * samples + own, part = rank - own * a.ranks;
@@ -48,14 +49,17 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
     const Vectors<Input::kXB, kKeep> xs(kCodes ? reinterpret_cast<const char *>(a.codes + pix0 * a.c + ch)
                                                : reinterpret_cast<const char *>(a.x) + (pix0 * a.x_stride + ch) * kE,
                                         kCodes ? (size_t)a.slots * a.c : a.slots * a.x_stride * kE, smem + all * Input::kDyB);
-    const Vectors<1, kKeep> bytes(kCodes ? a.exps + pix0 * a.blocks + ch / kBlock8 : nullptr, (size_t)a.slots * a.blocks,
-                                  smem + all * (Input::kDyB + Input::kXB));
+    const Vectors<1, false> bytes(kCodes ? a.exps + pix0 * a.blocks + ch / kBlock8 : nullptr, (size_t)a.slots * a.blocks, smem);
 
     if (a.cluster > 1) ptx::cluster_arrive();   // (waited for below: the others have started when their memory is written)
     ptx::grid_dep_wait_launch_small();
     dys.fetch(vecs);
     xs.fetch(vecs);
-    if (kCodes) bytes.fetch(vecs);
+    if (kKeep && kCodes) {   // (into the L1 cache, where both looks find them)
+        const char *p = bytes.first();
+#pragma unroll 4
+        for (int i = 0; i < vecs; ++i, p += bytes.step) ptx::prefetch_l1(p);
+    }
     float off[kG], rstd[kG];
     const int g0 = a.by_cpg(cv * kV), in_g0 = cv * kV - g0 * a.cpg;   // group of the first channel within the chunk, and where in it
     const float2 *stats = a.stats + (size_t)smp * a.groups + a.by_cpg(ch0);
@@ -72,8 +76,12 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
         }
     }
     for (int k = threadIdx.x; k < width; k += kGnThreads) {
-        gamma_s[k] = a.gamma && k < channels ? __ldg(a.gamma + ch0 + k) : 1.0f;
-        beta_s[k] = a.beta && k < channels ? __ldg(a.beta + ch0 + k) : 0.0f;
+        const bool in = k < channels;
+        const float gamma = in && a.gamma ? __ldg(a.gamma + ch0 + k) : 1.0f, r = in ? __ldg(stats + a.by_cpg(k)).y : 0.0f;
+        gamma_s[k] = gamma;
+        gamma_z[k] = gamma * act_scale(a.act);
+        beta_z[k] = (in && a.beta ? __ldg(a.beta + ch0 + k) : 0.0f) * act_scale(a.act);
+        gamma_r[k] = gamma * r;
     }
     const float dy_scale = error_scale<kType>(a);
 
@@ -81,9 +89,9 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
 
     __syncthreads();   // (gamma and beta)
 
-    // Both looks: a few vectors at a time.  use(u, dz, gamma) gets what a vector holds.
-    const float *const gamma_at = gamma_s + cv * kV, *const beta_at = beta_s + cv * kV;
-    auto look = [&](auto use) {
+    // Both looks: a few vectors at a time.  use(u, dz, gamma rstd) gets what a vector holds.
+    const float *const gamma_at = gamma_z + cv * kV, *const beta_at = beta_z + cv * kV, *const gamma_r_at = gamma_r + cv * kV;
+    auto look = [&](auto kind, auto use) {
         const char *dy_at = dys.first(), *x_at = xs.first(), *s_at = bytes.first();
         auto batch = [&](int i, auto count) {
             constexpr int kCount = decltype(count)::value;
@@ -93,17 +101,18 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
             dys.get(dy, i, dy_at);
             xs.get(x, i, x_at);
             if (kCodes) bytes.get(s, i, s_at);
-            float gamma[kV], beta[kV];
+            float gamma[kV], beta[kV], by[kV];
 #pragma unroll
             for (int j = 0; j < kV; ++j) {
                 gamma[j] = gamma_at[j];
                 beta[j] = beta_at[j];
+                by[j] = gamma_r_at[j];
             }
 #pragma unroll
             for (int j = 0; j < kCount; ++j) {
                 float u[kV], dz[kV];
-                gn_terms<kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
-                use(u, dz, gamma);
+                gn_terms<decltype(kind)::value, kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
+                use(u, dz, by);
             }
         };
         int i = 0;
@@ -113,16 +122,26 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
         for (; i < vecs; ++i) batch(i, std::integral_constant<int, 1>());
     };
 
+    // Vectors read again from the cache are worked on one by one, with what registers the loads of a batch leave (64 channels 112 x 112, 64 bf16
+    // samples: 117 us; a batch at a time 138, with three blocks on an SM 153); kept ones a batch at a time (256 channels 56 x 56, 32 bf16
+    // samples: 68 us instead of 70).
+    auto by_act = [&](auto f) {
+        if constexpr (kKeep) with_act(a.act, f);
+        else f(std::integral_constant<int, kAnyAct>());
+    };
+
     {
         float s0[kV], s1[kV];
 #pragma unroll
         for (int j = 0; j < kV; ++j) s0[j] = s1[j] = 0.0f;
-        look([&](const float (&u)[kV], const float (&dz)[kV], const float (&)[kV]) {
+        by_act([&](auto kind) {
+            look(kind, [&](const float (&u)[kV], const float (&dz)[kV], const float (&)[kV]) {
 #pragma unroll
-            for (int j = 0; j < kPairs<kV>; ++j) {
-                set_pair(s0, j, pair_of(s0, j) + pair_of(dz, j));
-                set_pair(s1, j, fma2(pair_of(dz, j), pair_of(u, j), pair_of(s1, j)));
-            }
+                for (int j = 0; j < kPairs<kV>; ++j) {
+                    set_pair(s0, j, pair_of(s0, j) + pair_of(dz, j));
+                    set_pair(s1, j, fma2(pair_of(dz, j), pair_of(u, j), pair_of(s1, j)));
+                }
+            });
         });
         if (slot < a.slots)
 #pragma unroll
@@ -214,15 +233,16 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_bwd_kernel(const __gri
     constexpr int kDxE = Elem<Types::kDx>::kSize;
     char *dx = reinterpret_cast<char *>(a.dx) + (pix0 * a.dx_stride + ch) * kDxE;
     const size_t dx_step = a.slots * a.dx_stride * kDxE;
-    look([&](const float (&u)[kV], float (&dz)[kV], const float (&gamma)[kV]) {
+    by_act([&](auto kind) {
+        look(kind, [&](const float (&u)[kV], float (&dz)[kV], const float (&by)[kV]) {
 #pragma unroll
-        for (int j = 0; j < kPairs<kV>; ++j) {
-            const int l = 2 * j / kW, h = kV == 1 ? 0 : (2 * j + 1) / kW;
-            const Pair e = pair_of(dz, j) * pair_of(gamma, j);
-            set_pair(dz, j, fma2(e, Pair{rstd[l], rstd[h]}, fma2(pair_of(u, j), Pair{k1[l], k1[h]}, Pair{k0[l], k0[h]})));
-        }
-        store_raw(dx, Elem<Types::kDx>::from_f32(dz));
-        dx += dx_step;
+            for (int j = 0; j < kPairs<kV>; ++j) {
+                const int l = 2 * j / kW, h = kV == 1 ? 0 : (2 * j + 1) / kW;
+                set_pair(dz, j, fma2(pair_of(dz, j), pair_of(by, j), fma2(pair_of(u, j), Pair{k1[l], k1[h]}, Pair{k0[l], k0[h]})));
+            }
+            store_raw(dx, Elem<Types::kDx>::from_f32(dz));
+            dx += dx_step;
+        });
     });
 }
 
@@ -247,7 +267,7 @@ cudaError_t launch(GnArgs a, const FusedPlan &p, int *launches, cudaStream_t st)
 template <int kType, int kV, int kW, bool kCodes>
 bool of_part(const GnArgs &a, cudaError_t *result, int *launches, cudaStream_t st)
 {
-    constexpr int kB = kV * Elem<kType>::kSize, kKept = kV * Elem<GnTypes<kType>::kY>::kSize + (kCodes ? kV + 1 : kB);
+    constexpr int kB = kV * Elem<kType>::kSize, kKept = kV * Elem<GnTypes<kType>::kY>::kSize + (kCodes ? kV : kB);
     constexpr size_t kLimit = 56 * 1024;   // four blocks to an SM
     FusedPlan p;
     if (!fused_plan(p, a.n, a.hw, a.c, kV, a.cpg / kW * kV, kB, kKept, kLimit, [](int cv) { return BwdLayout<kV>::bytes(cv); })) return false;
