@@ -111,6 +111,42 @@ def test_range_of_the_steps():
     check(tiny, codes, np.full_like(exps, 127), codes.astype(np.float64), "fp16", c_out)
 
 
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+def test_addresses_beyond_32_bits(name):
+    """Rows of errors 2^30 elements apart."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of free device memory")
+    rows, c_out, c_in, stride = 6, 136, 144, 1 << 30
+    dy, codes, exps, back = make(rows, c_out, c_in, name, 43)
+    big = torch.empty(5 * stride + c_out, dtype=dy.dtype, device="cuda:0")
+    far = torch.as_strided(big, (rows, c_out), (stride, 1))
+    far.copy_(dy)
+    out = G.zeros((c_out, c_in), torch.float32)
+    ws = G.empty(max(eoq.eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, TYPES[name][1]), 256), torch.uint8)
+    eoq.eoq_ckpt_wgrad(G.handle(), far, TYPES[name][1], rows, c_out, stride, G.dev(codes), G.dev(exps), c_in, out, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(out, call(dy, codes, exps, name, c_out))
+
+
+def test_two_calls_at_once():
+    """Two streams, one handle, a workspace each: nothing of one call reaches the other."""
+    a, b = make(5000, 256, 272, "bf16", 51), make(4000, 130, 65, "fp16", 52)
+    want = [call(dy, codes, exps, name, dy.shape[1]) for (dy, codes, exps, _), name in ((a, "bf16"), (b, "fp16"))]
+    jobs = []
+    for (dy, codes, exps, _), name in ((a, "bf16"), (b, "fp16")):
+        c_out, c_in = dy.shape[1], codes.shape[1]
+        jobs.append((dy, name, c_out, G.dev(codes), G.dev(exps), c_in, G.zeros((c_out, c_in), torch.float32),
+                     G.empty(eoq.eoq_ckpt_wgrad_workspace_size(dy.shape[0], c_out, c_in, TYPES[name][1]), torch.uint8), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for dy, name, c_out, codes, exps, c_in, out, ws, stream in jobs:
+            with torch.cuda.stream(stream):
+                eoq.eoq_ckpt_wgrad(G.handle(), dy, TYPES[name][1], dy.shape[0], c_out, c_out, codes, exps, c_in, out, ws)
+    torch.cuda.synchronize()
+    for job, w in zip(jobs, want):
+        assert torch.equal(job[6], w)
+
+
 def test_the_same_bits_every_time_and_replayed():
     rows, c_out, c_in = 3000, 192, 160
     dy, codes, exps, _ = make(rows, c_out, c_in, "bf16", 11)

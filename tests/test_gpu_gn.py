@@ -210,6 +210,38 @@ def test_the_same_bits_every_time_on_any_stream_and_replayed(kept):
     assert not torch.equal(third["y"], first["y"])
 
 
+@pytest.mark.parametrize("name", ["bf16", "fp32"])
+def test_pairs_of_channels_with_the_eight_bit_form(name):
+    """Rows that only pairs of elements are aligned in, and channels in whole blocks: the 8-bit form is written beside the output."""
+    x, dy, gamma, beta = make(2, 50, 64, 2, name, 41)
+    check(x, dy, gamma, beta, 64, 8, name, "silu", "codes")
+
+
+def test_addresses_beyond_32_bits():
+    """Pixels 2^30 elements apart: the last ones lie beyond 2^32 elements."""
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of free device memory")
+    hw, c, groups, stride = 6, 64, 8, 1 << 30
+    rng = np.random.default_rng(43)
+    big = torch.empty(5 * stride + c, dtype=torch.bfloat16, device="cuda:0")
+    x = torch.as_strided(big, (hw, c), (stride, 1))
+    x.copy_(torch.from_numpy(rng.normal(size=(hw, c))))
+    dy = torch.from_numpy(rng.normal(size=(hw, c))).bfloat16().to("cuda:0")
+    d = eoq.gn_desc(1, hw, c, groups, eoq.EOQ_BF16, eoq.EOQ_ACT_SILU, x_stride=stride)
+    flat = eoq.gn_desc(1, hw, c, groups, eoq.EOQ_BF16, eoq.EOQ_ACT_SILU)
+    got = []
+    for desc, src in ((d, x), (flat, x.contiguous())):
+        o = {k: torch.empty(hw, c, dtype=torch.bfloat16, device="cuda:0") for k in ("y", "dx")}
+        o["stats"], o["dg"], o["db"] = G.zeros((1, groups, 2), torch.float32), G.zeros(c, torch.float32), G.zeros(c, torch.float32)
+        ws = G.empty(eoq.eoq_gn_workspace_size(desc), torch.uint8)
+        eoq.eoq_gn_fwd(G.handle(), desc, src, None, None, o["y"], o["stats"], None, None, ws)
+        eoq.eoq_gn_bwd(G.handle(), desc, dy, None, src, None, None, None, None, o["stats"], o["dx"], o["dg"], o["db"], ws)
+        got.append(o)
+    torch.cuda.synchronize()
+    for k in got[0]:
+        assert torch.equal(got[0][k], got[1][k]), k
+
+
 def test_directional_derivative():
     """<gradient, direction> against differences of the GPU's own forward pass.  Central differences are off by h^2 / 6 of the third
     derivative and by the forward pass's rounding over h: with h = 2^-6, u of order one and 2,000 terms summed in 64 bits, well under 1%."""
