@@ -444,8 +444,8 @@ EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_
  * device in : dy [rows][dy_stride] (dtype EOQ_F32, EOQ_F16 or EOQ_BF16; dy_stride >= c_out elements, 0 = c_out); codes
  *             [rows][c_in] and exps as eoq_ckpt_save wrote them.
  * device out: dw fp32 [c_out][c_in], 16-byte aligned.
- * Every product is exact (dy in two or three bf16 parts where its type has more bits), sums are fp32, in an order that depends on the
- * sizes alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
+ * Every product is exact (dy in two or three bf16 parts where its type has more bits; fp32 errors below 2^-110 to 2^-133), sums are
+ * fp32, in an order that depends on the sizes alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
  * workspace: eoq_ckpt_wgrad_workspace_size() bytes (may be 0), 256-byte aligned; nothing is kept in it between calls.
  * eoq_set_gemm_ctas does not apply.  16-byte aligned tensors with c_out a multiple of 8, c_in of 16 and dy_stride of 16 bytes run
  * several times faster.

@@ -1,7 +1,7 @@
 // A tensor in 8 bits and back (eoq_ckpt_save, eoq_ckpt_load): the scale quantizer of arXiv 2105.13890, Sec. 3.2.2, with a step per
 // block of 32 neighbouring columns instead of one for the tensor, chosen so that nothing clips.  See eoq_block8.cuh for the form.
 //
-// Both directions are bound by memory (a bf16 element: 2 bytes in, 1 + 1/32 out).  A block belongs to 32 / kV neighbouring lanes,
+// Both directions are bound by memory (a bf16 element: 2 bytes in, 1 + 1/32 out; 200,704 rows of 128 bf16 there and back: 29 us, 5.3 TB/s).  A block belongs to 32 / kV neighbouring lanes,
 // each with kV elements (16 bytes of the wider side); rows are dealt out to thread groups of fixed width, so that no element needs a
 // division.  Columns, strides or addresses that rule 16-byte loads out take kV = 1, a lane per element and a warp per block.
 #include "eoq_block8.cuh"

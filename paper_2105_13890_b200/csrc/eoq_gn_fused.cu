@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
     const size_t pix0 = (size_t)smp * a.hw + p_begin + slot;
     const Vectors<kB, kKeep> x(reinterpret_cast<const char *>(a.x) + (pix0 * a.x_stride + ch) * kE, a.slots * a.x_stride * kE, smem);
 
+    if (a.ranks > 1) ptx::cluster_arrive();   // (waited for below: the others have started when their memory is written)
     ptx::grid_dep_wait_launch_small();
     x.fetch(vecs);
     for (int k = threadIdx.x; k < channels; k += kGnThreads) {

@@ -8,7 +8,6 @@
 
 namespace eoq {
 
-
 namespace {
 
 // shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2); gamma, gamma and beta times

@@ -585,7 +585,7 @@ struct GnArgs {
 };
 size_t gn_workspace_bytes(const eoq_gn_desc_t &d);
 cudaError_t launch_gn_channel_sums(GnArgs a, cudaStream_t st);   // dgamma, dbeta from part [n][c]
-// The forms in one launch (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu); false when a group is wider than a thread block.
+// The forms in one launch (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu); false when a group is wider than a thread block or its shared memory.
 bool gn_fused_fwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
 bool gn_fused_bwd(GnArgs a, int dtype, cudaError_t *result, int *launches, cudaStream_t st);
 cudaError_t launch_gn_fwd(GnArgs a, int dtype, void *workspace, int *launches, cudaStream_t st);
