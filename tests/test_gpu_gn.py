@@ -217,6 +217,14 @@ def test_pairs_of_channels_with_the_eight_bit_form(name):
     check(x, dy, gamma, beta, 64, 8, name, "silu", "codes")
 
 
+@pytest.mark.parametrize("n", [3, 160])
+@pytest.mark.parametrize("c,groups,name,kept", [(96, 16, "bf16", "codes"), (120, 8, "fp16", "input"), (40, 2, "fp16", "codes"), (24, 2, "fp32", "input")])
+def test_groups_that_cut_vectors(n, c, groups, name, kept):
+    """Groups that are no whole vectors, in few blocks and in many: the width of the vectors goes by both."""
+    x, dy, gamma, beta = make(n, 65, c, 0, name, 47)
+    check(x, dy, gamma, beta, c, groups, name, "silu", kept)
+
+
 def test_addresses_beyond_32_bits():
     """Pixels 2^30 elements apart: the last ones lie beyond 2^32 elements."""
     if torch.cuda.mem_get_info()[0] < 24 << 30:
