@@ -258,10 +258,11 @@ bool of_part(const GnArgs &a, cudaError_t *result, cudaStream_t st, bool all_sms
     const bool save = a.codes_out != nullptr && a.c % kBlock8 == 0;
     int unit = a.cpg / kW * kV;
     if (save) unit = unit / gcd_of(unit, kBlock8) * kBlock8;
-    // four blocks to an SM
-    constexpr size_t kLimit = 56 * 1024;
+    constexpr size_t kFour = 56 * 1024, kTwo = 112 * 1024;   // blocks to an SM
     FusedPlan p;
-    if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kLimit, [&](int cv) { return FwdLayout<kV, kW>::bytes(cv, cv * kV / a.cpg); })) return false;
+    auto fixed = [&](int cv) { return FwdLayout<kV, kW>::bytes(cv, cv * kV / a.cpg); };
+    if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kFour, fixed)) return false;
+    if (!p.keep && !fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kTwo, fixed)) return false;
     if (all_sms && (size_t)a.n * p.chunks * p.ranks < kPartSms) return false;
     if (p.keep) *result = save ? launch<kType, kV, kW, true, true>(a, p, st) : launch<kType, kV, kW, false, true>(a, p, st);
     else *result = save ? launch<kType, kV, kW, true, false>(a, p, st) : launch<kType, kV, kW, false, false>(a, p, st);

@@ -2,10 +2,10 @@
 //
 // A sample's chunk of whole groups belongs to a cluster, dealt out by pixels to its blocks.  The blocks read their pixels once for the
 // sums, which meet in shared memory and, over the cluster, in distributed shared memory, and look at them once more for the results.
-// Between the two looks the vectors stay in shared memory where that leaves room for four blocks on an SM; larger samples are read
-// again, from the L2 cache as far as what the resident clusters work on has room there.  (256 channels 56 x 56, 32 fp16 samples: 25 us
-// kept, 30 read again; 64 channels 112 x 112, 64 bf16 samples: kept in 104 KB by two blocks an SM 73 us forward and 209 backward, read
-// again 83 and 117.)
+// Between the two looks the vectors stay in shared memory where that leaves room for four blocks on an SM, forward also where it leaves
+// room for two; larger samples are read again, from the L2 cache as far as what the resident clusters work on has room there.  (256
+// channels 56 x 56, 32 fp16 samples: 25 us kept, 30 read again; 64 channels 112 x 112, 64 bf16 samples: kept in 104 KB by two blocks an
+// SM 72 us forward and 209 backward, read again 83 and 119.)
 #pragma once
 #include "eoq_gn.cuh"
 
