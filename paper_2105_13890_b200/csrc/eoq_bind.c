@@ -4,6 +4,7 @@
  * single layers: a 16-channel layer's forward, backward and update took 67 us for 45 us of kernels. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <limits.h>
 #include <stdint.h>
 #include <string.h>
 
@@ -40,6 +41,19 @@ static int get_int(PyObject *o, long long *out)
         Py_DECREF(v);
     }
     return *out != -1 || !PyErr_Occurred();
+}
+
+/* an argument that the call takes as an int */
+static int get_i32(PyObject *o, int *out)
+{
+    long long v;
+    if (!get_int(o, &v)) return 0;
+    if (v < INT_MIN || v > INT_MAX) {
+        PyErr_SetString(PyExc_OverflowError, "integer argument out of range");
+        return 0;
+    }
+    *out = (int)v;
+    return 1;
 }
 
 static int get_u64(PyObject *o, uint64_t *out)
@@ -242,24 +256,26 @@ static PyObject *ckpt_save(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     /* handle src dtype src_exp rows cols stride | codes exps stream */
     void *h, *src, *p[3];
-    long long v[5];
-    if (!want(n, 10) || !get_ptr(a[0], &h) || !get_ptr(a[1], &src)) return NULL;
-    for (int i = 0; i < 5; ++i)
-        if (!get_int(a[2 + i], &v[i])) return NULL;
+    int dtype, src_exp, cols;
+    long long rows, stride;
+    if (!want(n, 10) || !get_ptr(a[0], &h) || !get_ptr(a[1], &src) || !get_i32(a[2], &dtype) || !get_i32(a[3], &src_exp) ||
+        !get_int(a[4], &rows) || !get_i32(a[5], &cols) || !get_int(a[6], &stride))
+        return NULL;
     PTRS(7, 3);
-    CALL(eoq_ckpt_save((eoq_handle_t)h, src, (int)v[0], (int)v[1], (size_t)v[2], (int)v[3], (size_t)v[4], (int8_t *)p[0], (uint8_t *)p[1], p[2]));
+    CALL(eoq_ckpt_save((eoq_handle_t)h, src, dtype, src_exp, (size_t)rows, cols, (size_t)stride, (int8_t *)p[0], (uint8_t *)p[1], p[2]));
 }
 
 static PyObject *ckpt_load(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     /* handle | codes exps | rows cols dst dtype stride stream */
     void *h, *p[2], *dst, *stream;
-    long long rows, cols, dtype, stride;
-    if (!want(n, 9) || !get_ptr(a[0], &h) || !get_int(a[3], &rows) || !get_int(a[4], &cols) || !get_ptr(a[5], &dst) ||
-        !get_int(a[6], &dtype) || !get_int(a[7], &stride) || !get_ptr(a[8], &stream))
+    long long rows, stride;
+    int cols, dtype;
+    if (!want(n, 9) || !get_ptr(a[0], &h) || !get_int(a[3], &rows) || !get_i32(a[4], &cols) || !get_ptr(a[5], &dst) ||
+        !get_i32(a[6], &dtype) || !get_int(a[7], &stride) || !get_ptr(a[8], &stream))
         return NULL;
     PTRS(1, 2);
-    CALL(eoq_ckpt_load((eoq_handle_t)h, (const int8_t *)p[0], (const uint8_t *)p[1], (size_t)rows, (int)cols, dst, (int)dtype, (size_t)stride,
+    CALL(eoq_ckpt_load((eoq_handle_t)h, (const int8_t *)p[0], (const uint8_t *)p[1], (size_t)rows, cols, dst, dtype, (size_t)stride,
                        stream));
 }
 
@@ -267,16 +283,17 @@ static PyObject *ckpt_wgrad(PyObject *self, PyObject *const *a, Py_ssize_t n)
 {
     /* handle dy dtype rows c_out dy_stride | codes exps | c_in | dw workspace stream */
     void *h, *dy, *p[2], *q[3];
-    long long v[4], c_in;
+    long long rows, dy_stride;
+    int dtype, c_out, c_in;
     size_t bytes;
-    if (!want(n, 12) || !get_ptr(a[0], &h) || !get_ptr(a[1], &dy) || !get_int(a[8], &c_in) || !get_bytes(a[10], &bytes)) return NULL;
-    for (int i = 0; i < 4; ++i)
-        if (!get_int(a[2 + i], &v[i])) return NULL;
+    if (!want(n, 12) || !get_ptr(a[0], &h) || !get_ptr(a[1], &dy) || !get_i32(a[2], &dtype) || !get_int(a[3], &rows) || !get_i32(a[4], &c_out) ||
+        !get_int(a[5], &dy_stride) || !get_i32(a[8], &c_in) || !get_bytes(a[10], &bytes))
+        return NULL;
     PTRS(6, 2);
     for (int i = 0; i < 3; ++i)
         if (!get_ptr(a[9 + i], &q[i])) return NULL;
-    CALL(eoq_ckpt_wgrad((eoq_handle_t)h, dy, (int)v[0], (size_t)v[1], (int)v[2], (size_t)v[3], (const int8_t *)p[0], (const uint8_t *)p[1],
-                        (int)c_in, (float *)q[0], q[1], bytes, q[2]));
+    CALL(eoq_ckpt_wgrad((eoq_handle_t)h, dy, dtype, (size_t)rows, c_out, (size_t)dy_stride, (const int8_t *)p[0], (const uint8_t *)p[1],
+                        c_in, (float *)q[0], q[1], bytes, q[2]));
 }
 
 static int get_gn_desc(PyObject *o, eoq_gn_desc_t *out)

@@ -71,6 +71,8 @@ class eoq_gn_desc_t(C.Structure):
 
 
 def gn_desc(n, hw, c, groups, dtype, act=EOQ_ACT_NONE, eps=1e-5, x_exp=0, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0) -> eoq_gn_desc_t:
+    if max(abs(v) for v in (n, hw, c, groups, dtype, x_exp, act)) >= 1 << 31 or min(x_stride, y_stride, dy_stride, dx_stride) < 0:
+        raise OverflowError("gn_desc: a size that its field does not hold")   # (ctypes would cut it)
     return eoq_gn_desc_t(n, hw, c, groups, dtype, x_exp, act, eps, x_stride, y_stride, dy_stride, dx_stride)
 
 

@@ -95,6 +95,20 @@ def test_eight_bit_form():
     assert save(src_exp=-14) == eoq.EOQ_ERR_RANGE and save(dtype=eoq.EOQ_I32, src_exp=-61) == eoq.EOQ_ERR_RANGE
 
 
+
+def test_sizes_that_no_int_holds():
+    """Not cut to 32 bits on their way into the library."""
+    for cols in (40 + (1 << 32), 40 - (1 << 32)):
+        with pytest.raises(OverflowError):
+            eoq.eoq_ckpt_save(0, A, eoq.EOQ_F16, 0, 4, cols, 40, A, A, stream=0, check=False)
+        with pytest.raises(OverflowError):
+            eoq.eoq_ckpt_load(0, A, A, 4, cols, A, eoq.EOQ_F16, 0, stream=0, check=False)
+        with pytest.raises(OverflowError):
+            eoq.eoq_ckpt_wgrad(0, A, eoq.EOQ_BF16, 64, cols, 0, A, A, 64, A, A, stream=0, check=False)
+    with pytest.raises(OverflowError):
+        eoq.gn_desc(1 + (1 << 32), 4, 8, 2, eoq.EOQ_F16)
+
+
 def test_weight_gradient():
     def call(dy=A, dtype=eoq.EOQ_BF16, rows=4096, c_out=32, dy_stride=32, codes=A, exps=A, c_in=64, dw=A, ws=A):
         return eoq.eoq_ckpt_wgrad(0, dy, dtype, rows, c_out, dy_stride, codes, exps, c_in, dw, ws, stream=0, check=False)
