@@ -241,8 +241,9 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
     }
 }
 
-// Blocks in front: a warp per (sample, group) forms S1 and S2.  Blocks behind: 32 channels each, dgamma and dbeta over samples and
-// splits, 8 threads a channel in a fixed order.
+// Blocks in front: a warp per (sample, group) forms S1 and S2.  Blocks behind: kJoin channels each, dgamma and dbeta over samples and
+// splits, 32 threads a channel in a fixed order.
+constexpr int kJoin = 8;
 __global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_constant__ GnArgs a, int group_blocks)
 {
     ptx::grid_dep_wait_launch_small();
@@ -268,19 +269,26 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_cons
         if (lane == 0) a.means[id] = make_float2(s0 / total, s1 / total);
         return;
     }
-    __shared__ float2 red[8][32];
-    const int k = threadIdx.x & 31, j = threadIdx.x >> 5, c = ((int)blockIdx.x - group_blocks) * 32 + k;
+    __shared__ float2 red[kThreads / 32][kJoin];
+    const int k = threadIdx.x % kJoin, j = threadIdx.x / kJoin, c = ((int)blockIdx.x - group_blocks) * kJoin + k;
     float2 t = make_float2(0.0f, 0.0f);
     if (c < a.c)
-        for (size_t r = j; r < (size_t)a.n * a.splits; r += 8) {
+#pragma unroll 4
+        for (size_t r = j; r < (size_t)a.n * a.splits; r += kThreads / kJoin) {
             const float2 e = a.part[r * a.c + c];
             t.x += e.x;
             t.y += e.y;
         }
-    red[j][k] = t;
+#pragma unroll
+    for (int d = kJoin; d < 32; d *= 2) {
+        t.x += __shfl_xor_sync(0xffffffffu, t.x, d);
+        t.y += __shfl_xor_sync(0xffffffffu, t.y, d);
+    }
+    if (threadIdx.x % 32 < kJoin) red[threadIdx.x / 32][k] = t;
     __syncthreads();
-    if (j == 0 && c < a.c) {
-        for (int i = 1; i < 8; ++i) {
+    if (threadIdx.x < kJoin && c < a.c) {
+#pragma unroll
+        for (int i = 1; i < kThreads / 32; ++i) {
             t.x += red[i][k].x;
             t.y += red[i][k].y;
         }
@@ -409,7 +417,7 @@ cudaError_t run_bwd(GnArgs a, int *launches, cudaStream_t st)
                                    sizeof(float2) * p.slots * p.cv * kV, st, a);
     if (e != cudaSuccess) return e;
     const size_t warps = (size_t)a.n * a.groups;
-    const int group_blocks = (int)((warps + kThreads / 32 - 1) / (kThreads / 32)), channel_blocks = (a.c + 31) / 32;
+    const int group_blocks = (int)((warps + kThreads / 32 - 1) / (kThreads / 32)), channel_blocks = (a.c + kJoin - 1) / kJoin;
     e = launch_chained(gn_bwd_join_kernel, dim3(group_blocks + channel_blocks), dim3(kThreads), 0, st, a, group_blocks);
     if (e != cudaSuccess) return e;
     p = gn_plan(a.n, a.hw, a.c, kV, kApplyBlocks);
@@ -442,7 +450,7 @@ cudaError_t bwd_of_type(const GnArgs &a, int *launches, cudaStream_t st)
 cudaError_t launch_gn_channel_sums(GnArgs a, cudaStream_t st)
 {
     a.splits = 1;
-    return launch_chained(gn_bwd_join_kernel, dim3((a.c + 31) / 32), dim3(kThreads), 0, st, a, 0);
+    return launch_chained(gn_bwd_join_kernel, dim3((a.c + kJoin - 1) / kJoin), dim3(kThreads), 0, st, a, 0);
 }
 
 // [partial sums][means of the backward pass, or the statistics of a call that keeps none]
