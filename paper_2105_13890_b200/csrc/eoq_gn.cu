@@ -193,13 +193,13 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
     if (slot < a.slots && ch < a.c) {
-        float rstd[kV], off[kV], gamma[kV], beta[kV], s0[kV], s1[kV];
+        float rstd[kV], less[kV], mul[kV], beta[kV], s0[kV], s1[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
             rstd[i] = st.y;
-            off[i] = -st.x * st.y;
-            gamma[i] = (a.gamma ? a.gamma[ch + i] : 1.0f) * act_scale(a.act);
+            less[i] = -st.x;
+            mul[i] = (a.gamma ? st.y * a.gamma[ch + i] : st.y) * act_scale(a.act);
             beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
             s0[i] = s1[i] = 0.0f;
         }
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
                 for (int k = 0; k < kUnroll; ++k) {
                     if (p0 + k * a.slots >= p_end) break;
                     float u[kV], dz[kV];
-                    in[k].template values<decltype(kind)::value>(a, rstd, off, gamma, beta, dy_scale, u, dz);
+                    in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
 #pragma unroll
                     for (int i = 0; i < kV; ++i) {
                         s0[i] += dz[i];
@@ -306,15 +306,15 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     if (slot >= a.slots || ch >= a.c) return;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
-    float rstd[kV], off[kV], gamma[kV], beta[kV], by[kV], k0[kV], k1[kV];
+    float rstd[kV], less[kV], mul[kV], beta[kV], by[kV], k0[kV], k1[kV];
 #pragma unroll
     for (int i = 0; i < kV; ++i) {
         const size_t g = (size_t)smp * a.groups + (ch + i) / a.cpg;
         const float2 st = a.stats[g], m = a.means[g];
         rstd[i] = st.y;
-        off[i] = -st.x * st.y;
-        gamma[i] = (a.gamma ? a.gamma[ch + i] : 1.0f) * act_scale(a.act);
+        less[i] = -st.x;
         by[i] = a.gamma ? st.y * a.gamma[ch + i] : st.y;
+        mul[i] = by[i] * act_scale(a.act);
         beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
         k0[i] = -st.y * m.x;
         k1[i] = -st.y * m.y;
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
                 const int p = p0 + k * a.slots;
                 if (p >= p_end) break;
                 float u[kV], dz[kV];
-                in[k].template values<decltype(kind)::value>(a, rstd, off, gamma, beta, dy_scale, u, dz);
+                in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
 #pragma unroll
                 for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i], by[i], __fmaf_rn(u[i], k1[i], k0[i]));
                 store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,

@@ -128,12 +128,14 @@ __device__ __forceinline__ void x_values(const Raw<kN * Elem<kType>::kSize> &r, 
 }
 
 // u = (x - mean) rstd and dz = dy act'(gamma u + beta) of kN neighbouring channels; x from the kept tensor, or from its 8-bit form with
-// the byte s of their block; gamma and beta times act_scale().  Of kW neighbouring channels all are of one group: mean and rstd come once
-// for each kW.  off = -mean rstd: the step of the 8-bit form goes into the factor of u (a power of two, so exactly).
+// the byte s of their block.  `less` is minus the mean; mul = gamma rstd and beta come times act_scale().  Of kW neighbouring channels all are of
+// one group: mean and rstd come once for each kW.  The difference is formed first, as in the forward pass (a value that is the mean gives
+// zero, and a mean far from zero costs no digits), and the activation's argument is the forward pass's to the bit wherever x itself is kept:
+// both passes agree on the side of ReLU's gate.  (Scaling by a power of two is exact, so code or sum times its step is rounded with the difference.)
 template <int kAct, int kType, int kN, bool kCodes, int kW>
 __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType>::kSize> &x, int s, const Raw<kN * Elem<GnTypes<kType>::kY>::kSize> &dy,
-                                         float x_scale, float dy_scale, int act, const float (&off)[kN / kW], const float (&rstd)[kN / kW],
-                                         const float (&gamma)[kN], const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
+                                         float x_scale, float dy_scale, int act, const float (&less)[kN / kW], const float (&rstd)[kN / kW],
+                                         const float (&mul)[kN], const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
 {
     float z[kN];
     if constexpr (kCodes) {
@@ -146,13 +148,13 @@ __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType
         Elem<kType>::to_f32(x, u);
     }
     Elem<GnTypes<kType>::kY>::to_f32(dy, dz);
-    const float scale = kCodes ? block_step(s) : kType == EOQ_I32 ? x_scale : 1.0f;
+    const float scale = kCodes ? block_step(s) : x_scale;
 #pragma unroll
     for (int i = 0; i < kPairs<kN>; ++i) {
         const int j = 2 * i / kW, k = kN == 1 ? 0 : (2 * i + 1) / kW;
-        const Pair v = fma2(pair_of(u, i), Pair{rstd[j] * scale, rstd[k] * scale}, Pair{off[j], off[k]});
-        set_pair(u, i, v);
-        set_pair(z, i, fma2(v, pair_of(gamma, i), pair_of(beta, i)));
+        const Pair m = {less[j], less[k]}, d = kCodes || kType == EOQ_I32 ? fma2(pair_of(u, i), both(scale), m) : pair_of(u, i) + m;
+        set_pair(u, i, d * Pair{rstd[j], rstd[k]});
+        set_pair(z, i, fma2(d, pair_of(mul, i), pair_of(beta, i)));
         if (kType == EOQ_I32) set_pair(dz, i, pair_of(dz, i) * both(dy_scale));
     }
     times_slope<kAct>(dz, z, act);
@@ -181,10 +183,10 @@ struct GnInput {
         dy = load_raw<kDyB>(reinterpret_cast<const char *>(a.dy) + (pix * a.dy_stride + ch) * Elem<Types::kY>::kSize);
     }
     template <int kAct>
-    __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&off)[kV], const float (&gamma)[kV],
+    __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&less)[kV], const float (&mul)[kV],
                                            const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
     {
-        gn_terms<kAct, kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
+        gn_terms<kAct, kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, less, rstd, mul, beta, u, dz);
     }
 };
 

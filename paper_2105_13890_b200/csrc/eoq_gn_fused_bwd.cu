@@ -13,8 +13,8 @@ namespace eoq {
 
 namespace {
 
-// shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2); gamma, gamma and beta times
-// act_scale(), gamma times rstd
+// shared memory: cells of the threads, rows of sums by warp, sums of every block of the cluster, of the sample, (S1, S2); gamma, gamma times rstd,
+// that and beta times act_scale()
 template <int kV>
 struct BwdLayout {
     __host__ __device__ static size_t bytes(int cv)
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
     const size_t all = kKeep ? (size_t)a.vecs * kGnThreads : 0;
     float2 *cell = reinterpret_cast<float2 *>(smem + all * (Input::kDyB + Input::kXB));
     float2 *by_warp = cell + kGnThreads * kV, *parts = by_warp + rows * width, *total = parts + 8 * width, *means = total + width;   // parts [rank][channel]
-    float *gamma_s = reinterpret_cast<float *>(means + width), *gamma_z = gamma_s + width, *beta_z = gamma_z + width, *gamma_r = beta_z + width;
+    float *gamma_s = reinterpret_cast<float *>(means + width), *gamma_r = gamma_s + width, *mul_z = gamma_r + width, *beta_z = mul_z + width;
 
     const int id = a.by_cluster(blockIdx.x), rank = blockIdx.x - id * a.cluster, set = a.by_chunks(id), chunk = id - set * a.chunks;
     const int samples = a.by_ranks(a.cluster), own = a.by_ranks(rank), smp = set * samples + own, part = rank - own * a.ranks;
@@ -62,14 +62,14 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
 #pragma unroll 4
         for (int i = 0; i < vecs; ++i, p += bytes.step) ptx::prefetch_l1(p);
     }
-    float off[kG], rstd[kG];
+    float less[kG], rstd[kG];
     const int g0 = a.by_cpg(cv * kV), in_g0 = cv * kV - g0 * a.cpg;   // group of the first channel within the chunk, and where in it
     const float2 *stats = a.stats + (size_t)smp * a.groups + a.by_cpg(ch0);
     int g = g0, in_g = in_g0;
 #pragma unroll
     for (int k = 0; k < kG; ++k) {
         const float2 st = active ? __ldg(stats + g) : make_float2(0.0f, 0.0f);
-        off[k] = -st.x * st.y;
+        less[k] = -st.x;
         rstd[k] = st.y;
         in_g += kW;
         if (in_g == a.cpg) {
@@ -81,9 +81,9 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
         const bool in = k < channels;
         const float gamma = in && a.gamma ? __ldg(a.gamma + ch0 + k) : 1.0f, r = in ? __ldg(stats + a.by_cpg(k)).y : 0.0f;
         gamma_s[k] = gamma;
-        gamma_z[k] = gamma * act_scale(a.act);
-        beta_z[k] = (in && a.beta ? __ldg(a.beta + ch0 + k) : 0.0f) * act_scale(a.act);
         gamma_r[k] = gamma * r;
+        mul_z[k] = gamma * r * act_scale(a.act);   // (as the forward pass has it)
+        beta_z[k] = (in && a.beta ? __ldg(a.beta + ch0 + k) : 0.0f) * act_scale(a.act);
     }
     const float dy_scale = error_scale<kType>(a);
 
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
     __syncthreads();   // (gamma and beta)
 
     // Both looks: a few vectors at a time.  use(u, dz, gamma rstd) gets what a vector holds.
-    const float *const gamma_at = gamma_z + cv * kV, *const beta_at = beta_z + cv * kV, *const gamma_r_at = gamma_r + cv * kV;
+    const float *const mul_at = mul_z + cv * kV, *const beta_at = beta_z + cv * kV, *const gamma_r_at = gamma_r + cv * kV;
     // back: from the last vector to the first, so that what is read again was read a short while ago (64 channels 112 x 112, 64 bf16
     // samples: 110 us instead of 120).
     auto look = [&](auto kind, auto back, auto use) {
@@ -123,17 +123,17 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
                 }
                 s_at -= kCount * bytes.step;
             }
-            float gamma[kV], beta[kV], by[kV];
+            float mul[kV], beta[kV], by[kV];
 #pragma unroll
             for (int j = 0; j < kV; ++j) {
-                gamma[j] = gamma_at[j];
+                mul[j] = mul_at[j];
                 beta[j] = beta_at[j];
                 by[j] = gamma_r_at[j];
             }
 #pragma unroll
             for (int j = 0; j < kCount; ++j) {
                 float u[kV], dz[kV];
-                gn_terms<decltype(kind)::value, kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, off, rstd, gamma, beta, u, dz);
+                gn_terms<decltype(kind)::value, kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, less, rstd, mul, beta, u, dz);
                 if constexpr (kBack) use(i + j, u, dz, by);
                 else use(0, u, dz, by);
             }
