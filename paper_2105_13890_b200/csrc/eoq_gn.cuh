@@ -104,8 +104,18 @@ __device__ __forceinline__ void times_slope(float (&e)[kN], const float (&z)[kN]
 {
     const int act = kAct == kAnyAct ? any_act : kAct;
     if (act == EOQ_ACT_RELU) {
+        // A product, so that a NaN or an infinity of the error stays, plus a NaN where z is one.  (Two comparisons and half an instruction an element:
+        // 28 x 28 x 512, 32 bf16 samples from the 8-bit form, 33.7 us; nested selections and the product 40.6.)
+        float open[kN], lost[kN];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) e[i] = z[i] > 0.0f ? e[i] : z[i] != z[i] ? z[i] : 0.0f;
+        for (int i = 0; i < kN; ++i) {
+            uint32_t nan;
+            asm("set.gt.f32.f32 %0, %1, 0f00000000;" : "=f"(open[i]) : "f"(z[i]));
+            asm("set.nan.u32.f32 %0, %1, %1;" : "=r"(nan) : "f"(z[i]));   // (all ones: the bits of a NaN)
+            lost[i] = __uint_as_float(nan);
+        }
+#pragma unroll
+        for (int i = 0; i < kPairs<kN>; ++i) set_pair(e, i, fma2(pair_of(e, i), pair_of(open, i), pair_of(lost, i)));
     } else if (act == EOQ_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < kPairs<kN>; ++i) {
