@@ -30,46 +30,56 @@ __global__ void __launch_bounds__(kThreads) gn_stats_kernel(const __grid_constan
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
     constexpr int kB = kV * Elem<kType>::kSize;
-    float mean[kV], sq[kV];
-#pragma unroll
-    for (int i = 0; i < kV; ++i) mean[i] = sq[i] = 0.0f;
     if (slot < a.slots && ch < a.c) {
         const char *src = reinterpret_cast<const char *>(a.x) + ((size_t)smp * a.hw * a.x_stride + ch) * Elem<kType>::kSize;
-        int count = 0;
-        for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-            Raw<kB> raw[kUnroll];
-            float v[kUnroll][kV];
-            int m = 0;
+        int in_cell = 0, p0 = p_begin + slot;   // pixels that the cell holds
+        do {
+            float mean[kV], sq[kV];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
-                const int p = p0 + u * a.slots;
-                raw[u] = p < p_end ? load_raw<kB>(src + (size_t)p * a.x_stride * Elem<kType>::kSize) : zero_raw<kB>();
-                m += p < p_end;
-            }
-#pragma unroll
-            for (int u = 0; u < kUnroll; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
-            const float inv_m = 1.0f / (float)m, share = (float)m / (float)(count + m), both = (float)count * share;
-            count += m;
-#pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                // about the first pixel: equal values have exactly themselves as their mean
-                const float k = v[0][i];
-                float s = 0.0f, q = 0.0f;
-#pragma unroll
-                for (int u = 1; u < kUnroll; ++u) s += u < m ? v[u][i] - k : 0.0f;   // (the valid pixels come first)
-                s = __fmaf_rn(s, inv_m, k);
+            for (int i = 0; i < kV; ++i) mean[i] = sq[i] = 0.0f;
+            int count = 0;
+            for (; p0 < p_end && count < a.run; p0 += kUnroll * a.slots) {
+                Raw<kB> raw[kUnroll];
+                float v[kUnroll][kV];
+                int m = 0;
 #pragma unroll
                 for (int u = 0; u < kUnroll; ++u) {
-                    const float d = u < m ? v[u][i] - s : 0.0f;
-                    q = __fmaf_rn(d, d, q);
+                    const int p = p0 + u * a.slots;
+                    raw[u] = p < p_end ? load_raw<kB>(src + (size_t)p * a.x_stride * Elem<kType>::kSize) : zero_raw<kB>();
+                    m += p < p_end;
                 }
-                const float d = s - mean[i];
-                mean[i] = __fmaf_rn(d, share, mean[i]);
-                sq[i] += __fmaf_rn(d * d, both, q);
-            }
-        }
 #pragma unroll
-        for (int i = 0; i < kV; ++i) cell[(slot * a.cv + cv) * kV + i] = make_float2(mean[i], sq[i]);
+                for (int u = 0; u < kUnroll; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
+                const float inv_m = 1.0f / (float)m, share = (float)m / (float)(count + m), both = (float)count * share;
+                count += m;
+#pragma unroll
+                for (int i = 0; i < kV; ++i) {
+                    // about the first pixel: equal values have exactly themselves as their mean
+                    const float k = v[0][i];
+                    float s = 0.0f, q = 0.0f;
+#pragma unroll
+                    for (int u = 1; u < kUnroll; ++u) s += u < m ? v[u][i] - k : 0.0f;   // (the valid pixels come first)
+                    s = __fmaf_rn(s, inv_m, k);
+#pragma unroll
+                    for (int u = 0; u < kUnroll; ++u) {
+                        const float d = u < m ? v[u][i] - s : 0.0f;
+                        q = __fmaf_rn(d, d, q);
+                    }
+                    const float d = s - mean[i];
+                    mean[i] = __fmaf_rn(d, share, mean[i]);
+                    sq[i] += __fmaf_rn(d * d, both, q);
+                }
+            }
+            const float share = in_cell ? (float)count / (float)(in_cell + count) : 1.0f, both = (float)in_cell * share;
+#pragma unroll
+            for (int i = 0; i < kV; ++i) {
+                float2 &at = cell[(slot * a.cv + cv) * kV + i];
+                const float2 was = in_cell ? at : make_float2(0.0f, 0.0f);
+                const float d = mean[i] - was.x;
+                at = in_cell ? make_float2(__fmaf_rn(d, share, was.x), was.y + __fmaf_rn(d * d, both, sq[i])) : make_float2(mean[i], sq[i]);
+            }
+            in_cell += count;
+        } while (p0 < p_end);
     }
     __syncthreads();
     // a thread per channel joins the slots: the mean of the means by their counts, then the squares about it
@@ -193,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
     const int cv = threadIdx.x % a.cv, slot = threadIdx.x / a.cv, ch = (blockIdx.y * a.cv + cv) * kV;
     const int p_begin = split * a.per_split, p_end = min(a.hw, p_begin + a.per_split);
     if (slot < a.slots && ch < a.c) {
-        float rstd[kV], less[kV], mul[kV], beta[kV], s0[kV], s1[kV];
+        float rstd[kV], less[kV], mul[kV], beta[kV];
 #pragma unroll
         for (int i = 0; i < kV; ++i) {
             const float2 st = a.stats[(size_t)smp * a.groups + (ch + i) / a.cpg];
@@ -201,30 +211,41 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
             less[i] = -st.x;
             mul[i] = (a.gamma ? st.y * a.gamma[ch + i] : st.y) * act_scale(a.act);
             beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
-            s0[i] = s1[i] = 0.0f;
         }
         const float dy_scale = error_scale<kType>(a);
         const size_t pix0 = (size_t)smp * a.hw;
         with_act(a.act, [&](auto kind) {
-            for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
-                GnInput<kType, kV, kCodes> in[kUnroll];
+            int p0 = p_begin + slot;
+            bool first = true;
+            do {
+                float s0[kV], s1[kV];
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
+                for (int i = 0; i < kV; ++i) s0[i] = s1[i] = 0.0f;
+                for (int count = 0; p0 < p_end && count < a.run; count += kUnroll, p0 += kUnroll * a.slots) {
+                    GnInput<kType, kV, kCodes> in[kUnroll];
 #pragma unroll
-                for (int k = 0; k < kUnroll; ++k) {
-                    if (p0 + k * a.slots >= p_end) break;
-                    float u[kV], dz[kV];
-                    in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
+                    for (int u = 0; u < kUnroll; ++u) in[u].load(a, pix0 + p0 + u * a.slots, ch, p0 + u * a.slots < p_end);
 #pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        s0[i] += dz[i];
-                        s1[i] = __fmaf_rn(dz[i], u[i], s1[i]);
+                    for (int k = 0; k < kUnroll; ++k) {
+                        if (p0 + k * a.slots >= p_end) break;
+                        float u[kV], dz[kV];
+                        in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
+#pragma unroll
+                        for (int i = 0; i < kV; ++i) {
+                            s0[i] += dz[i];
+                            s1[i] = __fmaf_rn(dz[i], u[i], s1[i]);
+                        }
                     }
                 }
-            }
-        });
 #pragma unroll
-        for (int i = 0; i < kV; ++i) cell[(slot * a.cv + cv) * kV + i] = make_float2(s0[i], s1[i]);
+                for (int i = 0; i < kV; ++i) {
+                    float2 &at = cell[(slot * a.cv + cv) * kV + i];
+                    const float2 was = first ? make_float2(0.0f, 0.0f) : at;
+                    at = make_float2(was.x + s0[i], was.y + s1[i]);
+                }
+                first = false;
+            } while (p0 < p_end);
+        });
     }
     __syncthreads();
     const int width = a.cv * kV;
@@ -242,7 +263,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
 }
 
 // Blocks in front: a warp per (sample, group) forms S1 and S2.  Blocks behind: kJoin channels each, dgamma and dbeta over samples and
-// splits, 32 threads a channel in a fixed order.
+// splits, 32 threads a channel in a fixed order.  Both in 64 bits where there are many, since nothing bounds the numbers of samples and splits.
 constexpr int kJoin = 8;
 __global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_constant__ GnArgs a, int group_blocks)
 {
@@ -253,32 +274,48 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_cons
         if (id >= (size_t)a.n * a.groups) return;
         const int smp = (int)(id / a.groups), g = (int)(id % a.groups), cells = a.splits * a.cpg;
         const float2 *part = a.part + (size_t)smp * a.splits * a.c + (size_t)g * a.cpg;
-        float s0 = 0.0f, s1 = 0.0f;
+        double s0 = 0.0, s1 = 0.0;
         for (int i = lane; i < cells; i += 32) {
             const float2 e = part[(size_t)(i / a.cpg) * a.c + i % a.cpg];
-            const float gamma = a.gamma ? a.gamma[g * a.cpg + i % a.cpg] : 1.0f;
-            s0 = __fmaf_rn(gamma, e.x, s0);
-            s1 = __fmaf_rn(gamma, e.y, s1);
+            const double gamma = a.gamma ? a.gamma[g * a.cpg + i % a.cpg] : 1.0f;
+            s0 += gamma * e.x;
+            s1 += gamma * e.y;
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) {
             s0 += __shfl_xor_sync(0xffffffffu, s0, d);
             s1 += __shfl_xor_sync(0xffffffffu, s1, d);
         }
-        const float total = (float)((double)a.hw * a.cpg);
-        if (lane == 0) a.means[id] = make_float2(s0 / total, s1 / total);
+        const double total = (double)a.hw * a.cpg;
+        if (lane == 0) a.means[id] = make_float2((float)(s0 / total), (float)(s1 / total));
         return;
     }
     __shared__ float2 red[kThreads / 32][kJoin];
     const int k = threadIdx.x % kJoin, j = threadIdx.x / kJoin, c = ((int)blockIdx.x - group_blocks) * kJoin + k;
-    float2 t = make_float2(0.0f, 0.0f);
-    if (c < a.c)
+    constexpr int kRows = kThreads / kJoin, kRun = 32;
+    const size_t rows = (size_t)a.n * a.splits;
+    auto sum = [&](size_t from, size_t to) {
+        float2 t = make_float2(0.0f, 0.0f);
 #pragma unroll 4
-        for (size_t r = j; r < (size_t)a.n * a.splits; r += kThreads / kJoin) {
+        for (size_t r = from; r < to; r += kRows) {
             const float2 e = a.part[r * a.c + c];
             t.x += e.x;
             t.y += e.y;
         }
+        return t;
+    };
+    float2 t = make_float2(0.0f, 0.0f);
+    if (c < a.c && rows <= kRun * kRows) {
+        t = sum(j, rows);
+    } else if (c < a.c) {
+        double2 far = make_double2(0.0, 0.0);
+        for (size_t r0 = j; r0 < rows; r0 += kRun * kRows) {
+            t = sum(r0, min(rows, r0 + kRun * kRows));
+            far.x += t.x;
+            far.y += t.y;
+        }
+        t = make_float2((float)far.x, (float)far.y);
+    }
 #pragma unroll
     for (int d = kJoin; d < 32; d *= 2) {
         t.x += __shfl_xor_sync(0xffffffffu, t.x, d);
@@ -374,6 +411,7 @@ void use_plan(GnArgs &a, const GnPlan &p)
     a.slots = p.slots;
     a.splits = p.splits;
     a.per_split = p.per_split;
+    a.run = run_of(p.per_split / p.slots);
 }
 
 size_t parts_bytes(int n, int hw, int c, int dtype)

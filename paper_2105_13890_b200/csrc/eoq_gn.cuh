@@ -210,6 +210,16 @@ __device__ __forceinline__ float error_scale(const GnArgs &a)
     return ldexpf(1.0f, clampi(e, -120, 120));
 }
 
+// Sums of a thread's vectors go in two steps: of `run` vectors in registers, which then join what the thread's cell in shared memory holds.  A sum of
+// k terms of one sign is off by up to k / 2 roundings of itself, and equal terms, such as the errors behind an average over all pixels, come near
+// that: 0.1 added up 2,048 times in one step is off by 270, in two of 64 and 32 terms by 14.  (A power of two, run * run >= vecs.)
+inline int run_of(int vecs)
+{
+    int run = 64;
+    while ((long long)run * run < vecs) run *= 2;
+    return run;
+}
+
 inline bool aligned_at(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 }  // namespace eoq

@@ -55,16 +55,15 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
     // ---- the thread's vectors
     {
         constexpr int kA = kW == 1 ? kPairs<kV> : kG;   // accumulators: a channel to a lane of a pair, or a group to a pair
-        Pair mean[kA], sq[kA];   // mean: with its sign turned
-#pragma unroll
-        for (int j = 0; j < kA; ++j) mean[j] = sq[j] = both(0.0f);
+        Pair mean[kA], sq[kA];   // of a run of vectors; mean: with its sign turned
         auto acc = [](int i) { return kW == 1 ? i : 2 * i / kW; };   // of pair i of a vector
-        auto batch = [&](const char *&at, int i0, auto count, float inv) {   // inv: 1 / values of the batch
+        // i0: vectors of the run in front of the batch; inv: 1 / values of the batch
+        auto batch = [&](const char *&at, int i, int i0, auto count, float inv) {
             constexpr int kCount = decltype(count)::value;
             Raw<kB> raw[kCount];
             float v[kCount][kV];
             Pair s[kA], q[kA], first[kA];
-            x.get(raw, i0, at);
+            x.get(raw, i, at);
 #pragma unroll
             for (int u = 0; u < kCount; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
             // (about the first value, so that equal values have themselves as their mean; sums of a few 16-bit values are exact anyway)
@@ -100,19 +99,35 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
             }
         };
         const char *at = x.first();
-        int i = 0;
-        for (; i + kGnBatch <= vecs; i += kGnBatch) batch(at, i, std::integral_constant<int, kGnBatch>(), 1.0f / (kGnBatch * kW));
-        if (i + 2 <= vecs) {
-            batch(at, i, std::integral_constant<int, 2>(), 0.5f / kW);
-            i += 2;
-        }
-        if (i < vecs) batch(at, i, std::integral_constant<int, 1>(), 1.0f / kW);
-        if (slot < a.slots)
+        int done = 0;   // vectors in the cells (kept ones are few: a single run)
+        do {
+            const int end = kKeep ? vecs : min(vecs, done + a.run);
 #pragma unroll
-            for (int j = 0; j < kG; ++j) {
-                const Pair m = mean[kW == 1 ? j / 2 : j], e = sq[kW == 1 ? j / 2 : j];
-                cell[(slot * a.cv + cv) * kG + j] = kW == 1 ? (j % 2 ? make_float2(-m.y, e.y) : make_float2(-m.x, e.x)) : make_float2(-m.x, e.x + e.y);
+            for (int j = 0; j < kA; ++j) mean[j] = sq[j] = both(0.0f);
+            int i = done;
+            for (; i + kGnBatch <= end; i += kGnBatch) batch(at, i, i - done, std::integral_constant<int, kGnBatch>(), 1.0f / (kGnBatch * kW));
+            if (i + 2 <= end) {
+                batch(at, i, i - done, std::integral_constant<int, 2>(), 0.5f / kW);
+                i += 2;
             }
+            if (i < end) batch(at, i, i - done, std::integral_constant<int, 1>(), 1.0f / kW);
+            if (slot < a.slots) {
+                const float share = kKeep || done == 0 ? 1.0f : __fdividef((float)(end - done), (float)end), between = (float)(done * kW) * share;
+#pragma unroll
+                for (int j = 0; j < kG; ++j) {
+                    const Pair m = mean[kW == 1 ? j / 2 : j], e = sq[kW == 1 ? j / 2 : j];
+                    float2 c = kW == 1 ? (j % 2 ? make_float2(-m.y, e.y) : make_float2(-m.x, e.x)) : make_float2(-m.x, e.x + e.y);
+                    float2 &at_cell = cell[(slot * a.cv + cv) * kG + j];
+                    if (!kKeep && done > 0) {
+                        const float2 was = at_cell;
+                        const float d = c.x - was.x;
+                        c = make_float2(__fmaf_rn(d, share, was.x), was.y + __fmaf_rn(d * d, between, c.y));
+                    }
+                    at_cell = c;
+                }
+            }
+            done = end;
+        } while (!kKeep && done < vecs);
     }
     if (!kKeep) copy_wait();
     __syncthreads();

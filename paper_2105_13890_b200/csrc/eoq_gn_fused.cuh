@@ -122,6 +122,7 @@ inline void use_plan(GnArgs &a, const FusedPlan &p, int kw)
     a.ranks = p.ranks;
     a.vecs = p.vecs;
     a.per = (a.hw + p.ranks - 1) / p.ranks;
+    a.run = run_of(p.vecs);
     a.by_slots = FastDiv(p.slots);
     a.by_chunks = FastDiv(p.chunks);
     a.by_ranks = FastDiv(p.ranks);

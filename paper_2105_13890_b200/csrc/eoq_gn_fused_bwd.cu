@@ -91,11 +91,11 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
 
     __syncthreads();   // (gamma and beta)
 
-    // Both looks: a few vectors at a time.  use(u, dz, gamma rstd) gets what a vector holds.
+    // Both looks: a few vectors at a time.  use(u, dz, gamma rstd) gets what a vector holds; first to last, after(i) follows the batch in front of vector i.
     const float *const mul_at = mul_z + cv * kV, *const beta_at = beta_z + cv * kV, *const gamma_r_at = gamma_r + cv * kV;
     // back: from the last vector to the first, so that what is read again was read a short while ago (64 channels 112 x 112, 64 bf16
     // samples: 110 us instead of 120).
-    auto look = [&](auto kind, auto back, auto use) {
+    auto look = [&](auto kind, auto back, auto use, auto after) {
         constexpr bool kBack = decltype(back)::value;
         const char *dy_at = dys.first(), *x_at = xs.first(), *s_at = bytes.first();
         if (kBack) {
@@ -147,7 +147,10 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
         } else {
             int i = 0;
 #pragma unroll 1
-            for (; i + kGnBatch <= vecs; i += kGnBatch) batch(i, std::integral_constant<int, kGnBatch>());
+            for (; i + kGnBatch <= vecs; i += kGnBatch) {
+                batch(i, std::integral_constant<int, kGnBatch>());
+                after(i + kGnBatch);
+            }
 #pragma unroll 1
             for (; i < vecs; ++i) batch(i, std::integral_constant<int, 1>());
         }
@@ -165,6 +168,15 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
         float s0[kV], s1[kV];
 #pragma unroll
         for (int j = 0; j < kV; ++j) s0[j] = s1[j] = 0.0f;
+        float2 *const own = cell + (slot * a.cv + cv) * kV;
+        auto to_cell = [&](bool first) {
+#pragma unroll
+            for (int j = 0; j < kV; ++j) {
+                const float2 was = first ? make_float2(0.0f, 0.0f) : own[j];
+                own[j] = make_float2(was.x + s0[j], was.y + s1[j]);
+                s0[j] = s1[j] = 0.0f;
+            }
+        };
         by_act([&](auto kind) {
             look(kind, std::false_type(), [&](int, const float (&u)[kV], const float (&dz)[kV], const float (&)[kV]) {
 #pragma unroll
@@ -172,11 +184,11 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
                     set_pair(s0, j, pair_of(s0, j) + pair_of(dz, j));
                     set_pair(s1, j, fma2(pair_of(dz, j), pair_of(u, j), pair_of(s1, j)));
                 }
+            }, [&](int i) {
+                if (!kKeep && (i & (a.run - 1)) == 0) to_cell(i == a.run);   // (kept vectors are few)
             });
         });
-        if (slot < a.slots)
-#pragma unroll
-            for (int j = 0; j < kV; ++j) cell[(slot * a.cv + cv) * kV + j] = make_float2(s0[j], s1[j]);
+        if (slot < a.slots) to_cell(kKeep || vecs < a.run);
     }
     __syncthreads();
     // channels by lanes, slots by warps; then the warps' rows
@@ -277,7 +289,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
             } else {
                 store_raw(dx + i * dx_step, Elem<Types::kDx>::from_f32(dz));
             }
-        });
+        }, [](int) {});
     });
 }
 

@@ -579,6 +579,7 @@ struct GnArgs {
 
     float2 *part, *means;               // workspace
     int cv, slots, splits, per_split;   // lanes of a chunk of channels, pixels at a time, pixel ranges of a sample, pixels of a range
+    int run;                            // vectors that a thread adds up before its sums join those in its cell
     // the one-launch kernels: chunks of channels, blocks of a cluster, of them those of a sample
     int chunks, cluster, ranks, vecs, per;   // vecs: vectors of a thread; per: pixels of a block
     FastDiv by_cv, by_cpg, by_part, by_slots, by_chunks, by_ranks, by_cluster;   // by_part: cells of a group in a pixel
