@@ -474,7 +474,8 @@ EOQ_API int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_
  *   same u).  gamma, beta, stats as in the forward pass.  With dz = dy * act'(z):
  *   dgamma = sum dz u, dbeta = sum dz (fp32 [c], each may be NULL), dx = rstd (gamma dz - S1 - u S2), S1 and S2 the means of
  *   gamma dz and gamma dz u over the sample's group.
- * All arithmetic in fp32 and more; sums run in an order that depends on the sizes alone, so results are reproducible bit for bit.
+ * All arithmetic in fp32 and more; sums run in an order that depends on the sizes alone, so results are reproducible bit for bit.  The
+ * variance of a floating-point x has to be an fp32 number: a spread above 2^63 has an infinite one, rstd 0.  Integer sums have no such limit.
  * NaN and infinity spread to their sample's group and to the sums that hold them: of x, and of dy, behind a closed ReLU too (0 times
  * either is a NaN).  A marked block of the 8-bit form counts as NaN in every group that it holds channels of.  Tensors must not overlap.
  * workspace: eoq_gn_workspace_size() bytes, 256-byte aligned, the same for both directions; nothing is kept in it between calls.

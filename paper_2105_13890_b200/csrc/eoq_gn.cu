@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kThreads) gn_stats_kernel(const __grid_constan
                     m += p < p_end;
                 }
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
+                for (int u = 0; u < kUnroll; ++u) Elem<kType>::to_f32(raw[u], v[u]);   // (integer sums as they are)
                 const float inv_m = 1.0f / (float)m, share = (float)m / (float)(count + m), both = (float)count * share;
                 count += m;
 #pragma unroll
@@ -101,7 +101,8 @@ __global__ void __launch_bounds__(kThreads) gn_stats_kernel(const __grid_constan
     }
 }
 
-// a warp per (sample, group): mean and 1 / sqrt(variance + eps)
+// a warp per (sample, group): mean and 1 / sqrt(variance + eps), in 64 bits.  The partial results of integer sums are those of the sums as they are:
+// with their exponent the squares may be beyond fp32.
 __global__ void __launch_bounds__(kThreads) gn_join_kernel(const __grid_constant__ GnArgs a)
 {
     ptx::grid_dep_wait_launch_small();
@@ -123,7 +124,8 @@ __global__ void __launch_bounds__(kThreads) gn_join_kernel(const __grid_constant
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-    if (lane == 0) a.stats[id] = make_float2((float)mean, (float)(1.0 / sqrt(q / total + (double)a.eps)));
+    const double scale = a.x_scale;   // (of integer sums)
+    if (lane == 0) a.stats[id] = make_float2((float)(mean * scale), (float)(1.0 / sqrt(q / total * scale * scale + (double)a.eps)));
 }
 
 template <int kType, int kV, bool kSave>

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
             Pair s[kA], q[kA], first[kA];
             x.get(raw, i, at);
 #pragma unroll
-            for (int u = 0; u < kCount; ++u) x_values<kType, kV>(raw[u], a.x_scale, v[u]);
+            for (int u = 0; u < kCount; ++u) Elem<kType>::to_f32(raw[u], v[u]);   // (integer sums as they are)
             // (about the first value, so that equal values have themselves as their mean; sums of a few 16-bit values are exact anyway)
             constexpr bool kShift = kE > 2;
 #pragma unroll
@@ -174,7 +174,12 @@ __global__ void __launch_bounds__(kGnThreads, 4) gn_fused_fwd_kernel(const __gri
             const float2 e = parts[r * most + g];
             if (count(r) > 0.0f) q += __fmaf_rn((e.x - s) * (e.x - s), count(r) * (float)a.cpg, e.y);
         }
-        const float rstd = __frsqrt_rn(q / ((float)a.hw * (float)a.cpg) + a.eps);
+        const float var = q / ((float)a.hw * (float)a.cpg);
+        float rstd = __frsqrt_rn(var + a.eps);
+        if constexpr (kType == EOQ_I32) {   // (squares of sums at exponent 60 are no fp32 numbers: what the exponent adds comes in 64 bits)
+            s *= a.x_scale;
+            rstd = (float)(1.0 / sqrt((double)var * a.x_scale * a.x_scale + (double)a.eps));
+        }
         final[g] = make_float2(s, rstd);
         if (rank == 0 && a.stats) a.stats[(size_t)smp * a.groups + a.by_cpg(ch0) + g] = make_float2(s, rstd);
     }
