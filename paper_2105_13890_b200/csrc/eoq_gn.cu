@@ -214,7 +214,6 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
             mul[i] = (a.gamma ? st.y * a.gamma[ch + i] : st.y) * act_scale(a.act);
             beta[i] = a.beta ? a.beta[ch + i] * act_scale(a.act) : 0.0f;
         }
-        const float dy_scale = error_scale<kType>(a);
         const size_t pix0 = (size_t)smp * a.hw;
         with_act(a.act, [&](auto kind) {
             int p0 = p_begin + slot;
@@ -231,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_sums_kernel(const __grid_cons
                     for (int k = 0; k < kUnroll; ++k) {
                         if (p0 + k * a.slots >= p_end) break;
                         float u[kV], dz[kV];
-                        in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
+                        in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, u, dz);
 #pragma unroll
                         for (int i = 0; i < kV; ++i) {
                             s0[i] += dz[i];
@@ -331,8 +330,9 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_join_kernel(const __grid_cons
             t.x += red[i][k].x;
             t.y += red[i][k].y;
         }
-        if (a.dbeta) a.dbeta[c] = t.x;
-        if (a.dgamma) a.dgamma[c] = t.y;
+        const float scale = error_scale(a);
+        if (a.dbeta) a.dbeta[c] = t.x * scale;
+        if (a.dgamma) a.dgamma[c] = t.y * scale;
     }
 }
 
@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
         k0[i] = -st.y * m.x;
         k1[i] = -st.y * m.y;
     }
-    const float dy_scale = error_scale<kType>(a);
+    const float dy_scale = kType == EOQ_I32 ? error_scale(a) : 1.0f;
     const size_t pix0 = (size_t)smp * a.hw;
     with_act(a.act, [&](auto kind) {
         for (int p0 = p_begin + slot; p0 < p_end; p0 += kUnroll * a.slots) {
@@ -370,9 +370,9 @@ __global__ void __launch_bounds__(kThreads) gn_bwd_apply_kernel(const __grid_con
                 const int p = p0 + k * a.slots;
                 if (p >= p_end) break;
                 float u[kV], dz[kV];
-                in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, dy_scale, u, dz);
+                in[k].template values<decltype(kind)::value>(a, rstd, less, mul, beta, u, dz);
 #pragma unroll
-                for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i], by[i], __fmaf_rn(u[i], k1[i], k0[i]));
+                for (int i = 0; i < kV; ++i) dz[i] = __fmaf_rn(dz[i], by[i], __fmaf_rn(u[i], k1[i], k0[i])) * dy_scale;
                 store_raw(reinterpret_cast<char *>(a.dx) + ((pix0 + p) * a.dx_stride + ch) * Elem<Types::kDx>::kSize,
                           Elem<Types::kDx>::from_f32(dz));
             }

@@ -144,7 +144,7 @@ __device__ __forceinline__ void x_values(const Raw<kN * Elem<kType>::kSize> &r, 
 // both passes agree on the side of ReLU's gate.  (Scaling by a power of two is exact, so code or sum times its step is rounded with the difference.)
 template <int kAct, int kType, int kN, bool kCodes, int kW>
 __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType>::kSize> &x, int s, const Raw<kN * Elem<GnTypes<kType>::kY>::kSize> &dy,
-                                         float x_scale, float dy_scale, int act, const float (&less)[kN / kW], const float (&rstd)[kN / kW],
+                                         float x_scale, int act, const float (&less)[kN / kW], const float (&rstd)[kN / kW],
                                          const float (&mul)[kN], const float (&beta)[kN], float (&u)[kN], float (&dz)[kN])
 {
     float z[kN];
@@ -165,7 +165,6 @@ __device__ __forceinline__ void gn_terms(const Raw<kCodes ? kN : kN * Elem<kType
         const Pair m = {less[j], less[k]}, d = kCodes || kType == EOQ_I32 ? fma2(pair_of(u, i), both(scale), m) : pair_of(u, i) + m;
         set_pair(u, i, d * Pair{rstd[j], rstd[k]});
         set_pair(z, i, fma2(d, pair_of(mul, i), pair_of(beta, i)));
-        if (kType == EOQ_I32) set_pair(dz, i, pair_of(dz, i) * both(dy_scale));
     }
     times_slope<kAct>(dz, z, act);
 }
@@ -194,17 +193,17 @@ struct GnInput {
     }
     template <int kAct>
     __device__ __forceinline__ void values(const GnArgs &a, const float (&rstd)[kV], const float (&less)[kV], const float (&mul)[kV],
-                                           const float (&beta)[kV], float dy_scale, float (&u)[kV], float (&dz)[kV]) const
+                                           const float (&beta)[kV], float (&u)[kV], float (&dz)[kV]) const
     {
-        gn_terms<kAct, kType, kV, kCodes, 1>(x, s, dy, a.x_scale, dy_scale, a.act, less, rstd, mul, beta, u, dz);
+        gn_terms<kAct, kType, kV, kCodes, 1>(x, s, dy, a.x_scale, a.act, less, rstd, mul, beta, u, dz);
     }
 };
 
-// 2^*dy_exp of int8 errors
-template <int kType>
+// 2^*dy_exp of int8 errors.  Every gradient is linear in the errors, so codes are worked on as they are and dx, dgamma and dbeta scaled at the end:
+// sums of errors at exponent 120 would leave fp32 on their way to a result that does not.
 __device__ __forceinline__ float error_scale(const GnArgs &a)
 {
-    if (kType != EOQ_I32) return 1.0f;
+    if (!a.dy_exp) return 1.0f;
     const int e = *a.dy_exp;
     if ((e < -120 || e > 120) && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) atomicOr(&a.dev->status, EOQ_DEV_RANGE);
     return ldexpf(1.0f, clampi(e, -120, 120));

@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
         mul_z[k] = gamma * r * act_scale(a.act);   // (as the forward pass has it)
         beta_z[k] = (in && a.beta ? __ldg(a.beta + ch0 + k) : 0.0f) * act_scale(a.act);
     }
-    const float dy_scale = error_scale<kType>(a);
+    const float dy_scale = kType == EOQ_I32 ? error_scale(a) : 1.0f;
 
     if (kKeep) copy_wait();
 
@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
 #pragma unroll
             for (int j = 0; j < kCount; ++j) {
                 float u[kV], dz[kV];
-                gn_terms<decltype(kind)::value, kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, dy_scale, a.act, less, rstd, mul, beta, u, dz);
+                gn_terms<decltype(kind)::value, kType, kV, kCodes, kW>(x[j], s[j].w, dy[j], a.x_scale, a.act, less, rstd, mul, beta, u, dz);
                 if constexpr (kBack) use(i + j, u, dz, by);
                 else use(0, u, dz, by);
             }
@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
         if (whole) {
             if (rank == 0) {
                 for (int r = a.ranks; r < a.cluster; ++r) add(r);
-                if (a.dbeta) a.dbeta[ch0 + k] = t.x;
-                if (a.dgamma) a.dgamma[ch0 + k] = t.y;
+                if (a.dbeta) a.dbeta[ch0 + k] = t.x * dy_scale;
+                if (a.dgamma) a.dgamma[ch0 + k] = t.y * dy_scale;
             }
         } else if (part == 0) {
             a.part[(size_t)smp * a.c + ch0 + k] = t;
@@ -282,6 +282,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
             for (int j = 0; j < kPairs<kV>; ++j) {
                 const int l = 2 * j / kW, h = kV == 1 ? 0 : (2 * j + 1) / kW;
                 set_pair(dz, j, fma2(pair_of(dz, j), pair_of(by, j), fma2(pair_of(u, j), Pair{k1[l], k1[h]}, Pair{k0[l], k0[h]})));
+                if (kType == EOQ_I32) set_pair(dz, j, pair_of(dz, j) * both(dy_scale));
             }
             if constexpr (kKeep) {
                 store_raw(dx, Elem<Types::kDx>::from_f32(dz));

@@ -54,3 +54,26 @@ def test_every_exponent_of_the_sums(n, hw, c, groups, x_exp, eps, kept):
     r = R.gn_bwd(e.astype(np.float64) * 2.0 ** -12, xw, stats[..., 0], stats[..., 1], g, b, "silu")
     for got, at in ((dx, 0), (dg, 1), (db, 2)):
         R.within(got, r[at], r[at + 3])
+
+
+@pytest.mark.parametrize("kept", ["input", "codes"])
+@pytest.mark.parametrize("e_exp", [120, -120])
+@pytest.mark.parametrize("n,hw,c,groups", SHAPES)
+def test_every_exponent_of_the_errors(n, hw, c, groups, e_exp, kept):
+    """Errors of one sign in one channel and of the other in the next: at 120 the sums of either are no fp32 numbers, dx is one."""
+    acc, e, gamma, beta = make(n, hw, c, 7 + c)
+    acc, e = acc * 8, (np.abs(e) + 64).clip(max=127).astype(np.int8)
+    e[..., 1::2] = -e[..., 1::2]
+    _, stats, dx, dg, db = call(acc, e, e_exp, gamma, beta, groups, -14, 1e-5, kept, eoq.EOQ_ACT_NONE)
+    xw = acc.astype(np.float64) * 2.0 ** -14
+    if kept == "codes":
+        xw = R.block_form(xw.reshape(-1, c))[2].reshape(xw.shape)
+    r = R.gn_bwd(e.astype(np.float64) * 2.0 ** e_exp, xw, stats[..., 0], stats[..., 1], gamma.astype(np.float64), beta.astype(np.float64), "none")
+    assert np.abs(r[0]).max() < 2.0 ** 128
+    R.within(dx, r[0], r[3])
+    for got, at in ((dg, 1), (db, 2)):
+        # what is certain to be beyond the largest number, and what is not near it
+        beyond, inside = np.abs(r[at]) - r[at + 3] > 2.0 ** 128, np.abs(r[at]) + r[at + 3] < 2.0 ** 128 * (1 - 2.0 ** -20)
+        assert (got[beyond] == np.copysign(np.inf, r[at][beyond])).all()
+        R.within(got[inside], r[at][inside], r[at + 3][inside])
+    assert e_exp < 0 or np.isinf(db).any()
