@@ -275,8 +275,11 @@ cudaError_t launch(GnArgs a, const FusedPlan &p, cudaStream_t st)
     return launch_chained_clusters(p.ranks, kernel, dim3((unsigned)((size_t)a.n * p.chunks * p.ranks)), dim3(kGnThreads), p.smem, st, a);
 }
 
+// whether a plan is taken that leaves SMs without a block, or vectors unkept
+constexpr int kAlways = 0, kAllSms = 1, kKept = 2;
+
 template <int kType, int kV, int kW>
-bool of_part(const GnArgs &a, cudaError_t *result, cudaStream_t st, bool all_sms)
+bool of_part(const GnArgs &a, cudaError_t *result, cudaStream_t st, int only)
 {
     constexpr int kB = kV * Elem<kType>::kSize;
     const bool save = a.codes_out != nullptr && a.c % kBlock8 == 0;
@@ -287,23 +290,23 @@ bool of_part(const GnArgs &a, cudaError_t *result, cudaStream_t st, bool all_sms
     auto fixed = [&](int cv) { return FwdLayout<kV, kW>::bytes(cv, cv * kV / a.cpg); };
     if (!fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kFour, fixed)) return false;
     if (!p.keep && !fused_plan(p, a.n, a.hw, a.c, kV, unit, kB, kB, kTwo, fixed)) return false;
-    if (all_sms && (size_t)a.n * p.chunks * p.ranks < kPartSms) return false;
+    if ((only == kAllSms && (size_t)a.n * p.chunks * p.ranks < kPartSms) || (only == kKept && !p.keep)) return false;
     if (p.keep) *result = save ? launch<kType, kV, kW, true, true>(a, p, st) : launch<kType, kV, kW, false, true>(a, p, st);
     else *result = save ? launch<kType, kV, kW, true, false>(a, p, st) : launch<kType, kV, kW, false, false>(a, p, st);
     return true;
 }
 
 template <int kType, int kV>
-bool of_width(const GnArgs &a, cudaError_t *result, cudaStream_t st, bool all_sms = false)
+bool of_width(const GnArgs &a, cudaError_t *result, cudaStream_t st, int only = kAlways)
 {
     const int w = gcd_of(a.cpg, kV);
     if constexpr (kV == 8)
-        if (w == 8) return of_part<kType, kV, 8>(a, result, st, all_sms);
+        if (w == 8) return of_part<kType, kV, 8>(a, result, st, only);
     if constexpr (kV >= 4)
-        if (w == 4) return of_part<kType, kV, 4>(a, result, st, all_sms);
+        if (w == 4) return of_part<kType, kV, 4>(a, result, st, only);
     if constexpr (kV >= 2)
-        if (w == 2) return of_part<kType, kV, 2>(a, result, st, all_sms);
-    return of_part<kType, kV, 1>(a, result, st, all_sms);
+        if (w == 2) return of_part<kType, kV, 2>(a, result, st, only);
+    return of_part<kType, kV, 1>(a, result, st, only);
 }
 
 template <int kType>
@@ -317,7 +320,10 @@ bool of_type(const GnArgs &a, cudaError_t *result, cudaStream_t st)
     if (of(kWide)) {
         // Narrower vectors where groups then fall into more chunks and the call has no block for every SM otherwise (13 samples 45 x 45, 120 fp16
         // channels in groups of 15: 8.5 us, 11.3 with 16-byte vectors).
-        if (a.cpg % kWide != 0) return of_width<kType, kWide>(a, result, st, true) || of_width<kType, kWide / 2>(a, result, st);
+        // Whole blocks of the 8-bit form may make a group too wide for narrower vectors alone: few blocks then, which are worth it where they
+        // keep their vectors (1,056 fp16 channels in 32 groups, one sample 7 x 7: 10.4 us, 13.6 in three launches; 112 x 112, read again: 1048 and 308).
+        if (a.cpg % kWide != 0)
+            return of_width<kType, kWide>(a, result, st, kAllSms) || of_width<kType, kWide / 2>(a, result, st) || of_width<kType, kWide>(a, result, st, kKept);
         return of_width<kType, kWide>(a, result, st);
     }
     if (of(2)) return of_width<kType, 2>(a, result, st);
