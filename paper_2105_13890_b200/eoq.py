@@ -65,14 +65,19 @@ def conv_desc(n, h, w, c_in, c_out, kh, kw, stride=1, pad=0, x_wmargin=0) -> eoq
     return eoq_conv_desc_t(n, h, w, c_in, c_out, kh, kw, stride, pad, x_wmargin)
 
 
+def _fits(what, ints, sizes) -> None:
+    """ctypes cuts what an int or a size_t does not hold; this raises."""
+    if not all(-(1 << 31) <= v < 1 << 31 for v in ints) or not all(0 <= v < 1 << 64 for v in sizes):
+        raise OverflowError(what + ": a size that its field does not hold")
+
+
 class eoq_gn_desc_t(C.Structure):
     _fields_ = [(k, C.c_int) for k in ("n", "hw", "c", "groups", "dtype", "x_exp", "act")] + [("eps", C.c_float)] + \
                [(k, C.c_size_t) for k in ("x_stride", "y_stride", "dy_stride", "dx_stride")]
 
 
 def gn_desc(n, hw, c, groups, dtype, act=EOQ_ACT_NONE, eps=1e-5, x_exp=0, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0) -> eoq_gn_desc_t:
-    if max(abs(v) for v in (n, hw, c, groups, dtype, x_exp, act)) >= 1 << 31 or min(x_stride, y_stride, dy_stride, dx_stride) < 0:
-        raise OverflowError("gn_desc: a size that its field does not hold")   # (ctypes would cut it)
+    _fits("gn_desc", (n, hw, c, groups, dtype, x_exp, act), (x_stride, y_stride, dy_stride, dx_stride))
     return eoq_gn_desc_t(n, hw, c, groups, dtype, x_exp, act, eps, x_stride, y_stride, dy_stride, dx_stride)
 
 
@@ -511,6 +516,7 @@ def eoq_ckpt_load(handle, codes, exps, rows, cols, dst, dtype, stride, stream=No
 
 
 def eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, dtype) -> int:
+    _fits("eoq_ckpt_wgrad_workspace_size", (c_out, c_in, dtype), (rows,))
     out = C.c_size_t(0)
     _check(lib().eoq_ckpt_wgrad_workspace_size(rows, c_out, c_in, dtype, C.byref(out)), "eoq_ckpt_wgrad_workspace_size")
     return out.value
