@@ -444,7 +444,7 @@ EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_
  * device in : dy [rows][dy_stride] (dtype EOQ_F32, EOQ_F16 or EOQ_BF16; dy_stride >= c_out elements, 0 = c_out); codes
  *             [rows][c_in] and exps as eoq_ckpt_save wrote them.
  * device out: dw fp32 [c_out][c_in], 16-byte aligned.
- * Every product is exact (dy in two or three bf16 parts where its type has more bits; fp32 errors below 2^-110 to 2^-133), sums are
+ * Every product is exact (dy in two or three bf16 parts where its type has more bits; fp32 errors below 2^-110 to within 2^-133), sums are
  * fp32, in an order that depends on the sizes alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
  * workspace: eoq_ckpt_wgrad_workspace_size() bytes (may be 0), 256-byte aligned; nothing is kept in it between calls.
  * eoq_set_gemm_ctas does not apply.  16-byte aligned tensors with c_out a multiple of 8, c_in of 16 and dy_stride of 16 bytes run
@@ -471,7 +471,8 @@ EOQ_API int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_
  *   codes and exps (both or neither): the 8-bit form of x, as eoq_ckpt_save(x, rows = n * hw, cols = c) writes it.
  * eoq_gn_bwd: either x, or codes and exps with x = NULL: the gradients are then those at the values the 8-bit form stands for, with the
  *   forward pass's mean and rstd (an element is off by at most half a step of its block times rstd in u; ReLU's gate goes by the
- *   same u).  gamma, beta, stats as in the forward pass.  With dz = dy * act'(z):
+ *   same u).  From x itself, u and the activation's argument are the forward pass's: an element that is its group's mean
+ *   has u = 0.  gamma, beta, stats as in the forward pass.  With dz = dy * act'(z):
  *   dgamma = sum dz u, dbeta = sum dz (fp32 [c], each may be NULL), dx = rstd (gamma dz - S1 - u S2), S1 and S2 the means of
  *   gamma dz and gamma dz u over the sample's group.
  * All arithmetic in fp32 and more; sums run in an order that depends on the sizes alone, so results are reproducible bit for bit.  The

@@ -123,9 +123,11 @@ __device__ __forceinline__ void commit_both(uint32_t bar, uint32_t leader)
     else
         ptx::mma_commit(bar, leader);
 }
-// An arrival at the first block's barrier.  (In the default scope: what it announces lies in this block's shared memory, written and fenced
-// towards the asynchronous proxy by then.  With the scope of the cluster, which waits for more than that, the kernel took 288 us instead of
-// 135: 1024 to 4096 channels, 16,384 rows.)
+// An arrival at the first block's barrier, in the default scope: whatever it announces lies in this block's own SM, where this SM's half of the MMA
+// reads or writes it, and is done by then.  Operands (full_bar) are written to shared memory and fenced towards the asynchronous proxy; tensor memory
+// (moved_bar) has been read and written, both waited for, with the fence of tcgen05 in front of the arrival and behind the first block's wait.  No data passes
+// between the blocks' threads themselves.  In the scope of the cluster, which waits for more than that, the kernel took 288 us for the operands (269 with
+// one warp passing a barrier of the block on) and 147 for tensor memory, instead of 135: 1024 to 4096 channels, 16,384 rows.
 template <bool kPair>
 __device__ __forceinline__ void arrive_first(uint32_t bar)
 {
@@ -134,7 +136,7 @@ __device__ __forceinline__ void arrive_first(uint32_t bar)
     else
         ptx::mbar_arrive(bar);
 }
-// wait_bar for a barrier that threads of both blocks arrive at: what they wrote before is visible behind it
+// wait_bar for a barrier that threads of both blocks arrive at, in the scope of the cluster
 template <bool kPair>
 __device__ __forceinline__ bool wait_both(uint32_t bar, uint32_t parity, const RoleCtx &c)
 {

@@ -6,9 +6,11 @@
 //   S1 and S2 the means of gamma dz and gamma dz u over the (sample, group).
 //
 // The kernels here serve what the one-launch forms (eoq_gn_fused.cu, eoq_gn_fused_bwd.cu) leave: groups wider than a thread block, or than
-// its shared memory.  A pass that reduces, a small one that joins, a pass that writes; for calls that both forms take they are the slower
-// ones (256 channels 56 x 56, 32 fp16 samples, forward: 43 us against 25; 64 channels 112 x 112, 64 bf16 samples, both passes: 303 against
-// 181), since everything is read from memory twice and a call is three launches.  A thread owns kV
+// its shared memory.  A pass that reduces, a small one that joins, a pass that writes.  For calls that both forms take they are the slower ones
+// where there are samples for every SM (256 channels 56 x 56, 32 fp16 samples, forward: 43 us against 25; 64 channels 112 x 112, 64 bf16 samples,
+// both passes: 303 against 181), since everything is read from memory twice and a call is three launches.  They would be the faster ones for a few
+// large images, whose pixels they deal to all SMs instead of eight for each chunk of channels (one 512 x 512 of 64 channels in 16 groups, bf16: 62 and 68
+// us against 373 and 488; in one group 480 and 215 against 502 and 974): such calls take the one-launch form all the same.  A thread owns kV
 // neighbouring channels (16 bytes of x, or one element where widths or addresses rule that out) and walks pixels of one sample, so
 // that what depends on the channel stays in registers.  Sums never leave the thread as raw squares: a batch of pixels gives its mean
 // and its squares about that mean, and (count, mean, squares) are joined pairwise, so a mean far from zero costs no digits.

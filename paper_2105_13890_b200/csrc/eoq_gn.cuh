@@ -53,6 +53,9 @@ __device__ __forceinline__ void set_pair(float (&v)[kN], int i, Pair p)
 }
 template <int kN> constexpr int kPairs = (kN + 1) / 2;
 
+// The activation is arithmetic of fp32's class, not correctly rounded: ex2.approx and rcp.approx are off by two steps of fp32 and one, and values below
+// the normal numbers are 0 (SiLU of z < -87, which is above -2e-36).  The exact functions take several times the instructions of a kernel that is
+// short of issue slots, and every 16-bit output is rounded 2^13 times as coarsely; the quotients by counts (__fdividef, two steps) only weight means.
 __device__ __forceinline__ float ex2_approx(float v)
 {
     float r;

@@ -2,9 +2,11 @@
 // Batches of a thread's vectors give their mean and the squares about it; (count, mean, squares) are joined pairwise, so a mean far from
 // zero costs no digits, and a group of equal values has exactly that value as its mean.
 //
-// Bound by memory where samples are kept (256 channels 56 x 56, 32 fp16 samples, ReLU: 25 us, 4.1 TB/s; the reads and the writes of a block do
-// not overlap), by the launch and a cluster barrier where they are small (512 channels 7 x 7, one sample: 3.6 us).  With SiLU and the 8-bit
-// form (64 channels 112 x 112, 64 bf16 samples: 72 us, 3.6 TB/s) issue slots are busy for 44% of the cycles.
+// Where samples are kept, a block reads, joins, then writes, so that reads and writes overlap only between blocks: 256 channels 56 x 56, 32 fp16 samples,
+// ReLU: 25 us, 4.1 TB/s in 1,024 blocks for 592 places.  Small calls take the launch and a cluster barrier (512 channels 7 x 7, one
+// sample: 3.7 us).  With SiLU and the 8-bit form (64 channels 112 x 112, 64 bf16 samples: 72 us, 3.6 TB/s) issue slots are busy for 44% of the cycles.
+// The form that reads again and writes the 8-bit form holds three unrolled batches in 64 registers and spills 300 to 570 bytes a thread of 16-bit
+// types (16 samples 150 x 150 x 64: 49 us, of which memory needs 18).
 #include <type_traits>
 
 #include "eoq_gn_fused.cuh"

@@ -5,7 +5,7 @@
 // Between the two looks the vectors stay in shared memory where that leaves room for four blocks on an SM, forward also where it leaves
 // room for two; larger samples are read again, from the L2 cache as far as what the resident clusters work on has room there.  (256
 // channels 56 x 56, 32 fp16 samples: 25 us kept, 30 read again; 64 channels 112 x 112, 64 bf16 samples: kept in 104 KB by two blocks an
-// SM 72 us forward and 209 backward, read again 83 and 110.)
+// SM 72 us forward and 209 backward, read again 83 and 110.  Samples that do not fit go to eight blocks whether or not the SMs need as many.)
 #pragma once
 #include "eoq_gn.cuh"
 

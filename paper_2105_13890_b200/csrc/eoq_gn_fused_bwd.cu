@@ -3,8 +3,10 @@
 // second writes dx.  When all samples of a chunk fit a cluster it also adds dgamma and dbeta over them, and the call is one launch;
 // otherwise a small kernel behind adds the samples in their order.
 //
-// Bound by instruction issue and the special functions of two looks at every element (38 to 47 instructions, SiLU's slope in each: 52% and 43% of
-// the cycles, the rest waits for loads): 64 channels 112 x 112, 64 bf16 samples from the 8-bit form: 110 us, 2.3 TB/s of what has to move.
+// 64 channels 112 x 112, 64 bf16 samples from the 8-bit form, SiLU: 109 us, 2.4 TB/s of what has to move (3.0 TB/s with what is read a second time).
+// No unit is full: 38 instructions per element keep issue 58% and the exponentials' unit 48% busy, 27 of 64 warps are there, and
+// their longest wait is for loads (3.3 per issue; next 1.7 for dependent arithmetic).  Registers allow four blocks on an SM; fp32 vectors read again
+// spill at that bound (116 bytes a thread stored, 48 from the 8-bit form; the 16-bit types 8 to 16).
 #include <type_traits>
 
 #include "eoq_gn_fused.cuh"
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(kGnThreads, kW == kV ? 4 : 3) gn_fused_bwd_ker
     // Both looks: a few vectors at a time.  use(u, dz, gamma rstd) gets what a vector holds; first to last, after(i) follows the batch in front of vector i.
     const float *const mul_at = mul_z + cv * kV, *const beta_at = beta_z + cv * kV, *const gamma_r_at = gamma_r + cv * kV;
     // back: from the last vector to the first, so that what is read again was read a short while ago (64 channels 112 x 112, 64 bf16
-    // samples: 110 us instead of 120).
+    // samples: 109 us instead of 120).
     auto look = [&](auto kind, auto back, auto use, auto after) {
         constexpr bool kBack = decltype(back)::value;
         const char *dy_at = dys.first(), *x_at = xs.first(), *s_at = bytes.first();
