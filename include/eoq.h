@@ -445,7 +445,7 @@ EOQ_API int eoq_ckpt_load(eoq_handle_t handle, const int8_t *codes, const uint8_
  *             [rows][c_in] and exps as eoq_ckpt_save wrote them.
  * device out: dw fp32 [c_out][c_in], 16-byte aligned.
  * Every product is exact (dy in two or three bf16 parts where its type has more bits; fp32 errors below 2^-110 to within 2^-133), sums are
- * fp32, in an order that depends on the sizes alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
+ * fp32, in an order that depends on the sizes and alignments alone.  An infinity or NaN in dy, or a marked block, reaches the weights of its row and column.
  * workspace: eoq_ckpt_wgrad_workspace_size() bytes (may be 0), 256-byte aligned; nothing is kept in it between calls.
  * eoq_set_gemm_ctas does not apply.  16-byte aligned tensors with c_out a multiple of 8, c_in of 16 and dy_stride of 16 bytes run
  * several times faster.
@@ -475,8 +475,8 @@ EOQ_API int eoq_ckpt_wgrad(eoq_handle_t handle, const void *dy, int dtype, size_
  *   has u = 0.  gamma, beta, stats as in the forward pass.  With dz = dy * act'(z):
  *   dgamma = sum dz u, dbeta = sum dz (fp32 [c], each may be NULL), dx = rstd (gamma dz - S1 - u S2), S1 and S2 the means of
  *   gamma dz and gamma dz u over the sample's group.
- * All arithmetic in fp32 and more; sums run in an order that depends on the sizes alone, so results are reproducible bit for bit.  The
- * variance of a floating-point x has to be an fp32 number: a spread above 2^63 has an infinite one, rstd 0.  Integer sums have no such limit.
+ * All arithmetic in fp32 and more; sums run in an order that depends on the sizes, strides and alignments alone, so results are reproducible
+ * bit for bit.  The variance of a floating-point x has to be an fp32 number: a spread above 2^63 has an infinite one, rstd 0.  Integer sums have no such limit.
  * NaN and infinity spread to their sample's group and to the sums that hold them: of x, and of dy, behind a closed ReLU too (0 times
  * either is a NaN).  A marked block of the 8-bit form counts as NaN in every group that it holds channels of.  Tensors must not overlap.
  * workspace: eoq_gn_workspace_size() bytes, 256-byte aligned, the same for both directions; nothing is kept in it between calls.
