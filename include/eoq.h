@@ -67,7 +67,7 @@ typedef enum {
 
 /* Bits of the device status word returned by eoq_last_status(). */
 #define EOQ_DEV_TIMEOUT 1u   /* a bounded wait inside a kernel ran out; results of that call are invalid */
-#define EOQ_DEV_NONFINITE 2u /* eoq_quantize, eoq_ckpt_save or eoq_gn_fwd (its 8-bit form) met a NaN or an infinity */
+#define EOQ_DEV_NONFINITE 2u /* eoq_quantize, eoq_ckpt_save, eoq_gn_fwd (its 8-bit form), eoq_lin_* or eoq_grad_* met a NaN or an infinity */
 #define EOQ_DEV_SQ_ZERO 4u   /* a scale quantizer saw an all-zero tensor (codes 0, exponent passed through) */
 #define EOQ_DEV_RANGE 8u     /* an input exponent outside the supported range */
 
@@ -497,6 +497,64 @@ EOQ_API int eoq_gn_fwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const voi
 EOQ_API int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const void *dy, const int32_t *dy_exp, const void *x,
                const int8_t *codes, const uint8_t *exps, const float *gamma, const float *beta, const float *stats, void *dx,
                float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Linear layers in 8-bit integers with a scale for each token and channel: the layer beside the convolutions of Sec. 3.2.1 whose three passes are products of
+ * 8-bit integers too, for tensors that one exponent does not serve.
+ * Codes of a row v of floating-point values (a token of the input, a channel of the weights): top = max(largest |v|, 2^-119),
+ *   scale = top / 127,  code = R(v * per),  per = 127 / top,  both quotients rounded to fp32, the product exact.
+ * A row that holds a NaN or an infinity has the scale NaN and codes 0 (EOQ_DEV_NONFINITE); what is computed from it is NaN.
+ * A matrix of codes [rows][cols] has rows of `pitch` = cols rounded up to 16 bytes; what is behind cols is not read.
+ *
+ * eoq_lin_desc_t: rows tokens, c_in to c_out channels; dtype of x, y, dy and dx: EOQ_F32, EOQ_F16 or EOQ_BF16.  Strides: elements from row to row, so that a
+ * tensor may be part of a wider one; 0 = its channels.
+ * eoq_lin_quantize: codes [rows][pitch] and scales (fp32 [rows]) of src [rows][stride], tokens or weights [c_out][c_in].
+ * eoq_lin_fwd: y[t][o] = x_scales[t] w_scales[o] sum over i of x_codes[t][i] w_codes[o][i]  (+ bias[o], fp32 [c_out], NULL = 0).
+ *   With x, the call codes it first; x_codes and x_scales then receive its codes (both NULL when no backward pass follows).  With x = NULL they are the input.
+ * eoq_lin_bwd: gradients at the values that the codes stand for, the errors dy [rows][dy_stride] coded twice:
+ *   u[t][o] = dy[t][o] w_scales[o], rounded to fp32, coded by tokens:   dx[t][i] = scale_u[t] sum over o of code_u[t][o] w_codes[o][i]
+ *   v[t][o] = dy[t][o] x_scales[t], rounded to fp32, coded by channels: dw[o][i] = scale_v[o] sum over t of code_v[t][o] x_codes[t][i]  (fp32 [c_out][c_in], 16-byte aligned)
+ *   dbias[o] = sum over t of dy[t][o]  (fp32).  Each of the three may be NULL; w_codes and w_scales are needed for dx, x_codes and x_scales for dw.
+ * Integer sums are exact at any length; an output is rounded four times (three in fp32).  Sums of dbias run in an order that depends on the sizes, strides and alignments
+ * alone.  Results are reproducible bit for bit.  An infinity or NaN in dy[t][o] makes row t of dx and row o of dw NaN; a scale that is NaN makes NaN whatever it enters: all of
+ * dw for a token's, all of dx for a channel's.
+ * Tensors must not overlap.  workspace: eoq_lin_workspace_size(desc, EOQ_LIN_FWD or EOQ_LIN_BWD) bytes, 256-byte aligned; nothing is kept in it between calls.
+ * Pointers aligned to their elements, codes and dw to 16 bytes; 16-byte aligned tensors with strides of 16 bytes run several times faster.
+ * eoq_set_gemm_ctas and the reduce hook do not apply.
+ * Errors: BAD_ARG (null pointer, non-positive size, stride below the channels, unknown type, x_codes without x_scales, the handle's device not the current one), ALIGNMENT,
+ * UNSUPPORTED (rows or a stride > 2^30, channels > 2^20, a tensor of more than 2^40 elements, weights of more than 2^34), WORKSPACE.
+ */
+typedef struct {
+    size_t rows;
+    int c_in, c_out, dtype;
+    size_t x_stride, y_stride, dy_stride, dx_stride;
+} eoq_lin_desc_t;
+#define EOQ_LIN_FWD 0
+#define EOQ_LIN_BWD 1
+EOQ_API int eoq_lin_workspace_size(const eoq_lin_desc_t *desc, int which, size_t *bytes);
+EOQ_API int eoq_lin_quantize(eoq_handle_t handle, const void *src, int dtype, size_t rows, int cols, size_t stride, int8_t *codes, float *scales, void *stream);
+EOQ_API int eoq_lin_fwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, const void *x, int8_t *x_codes, float *x_scales, const int8_t *w_codes,
+                const float *w_scales, const float *bias, void *y, void *workspace, size_t workspace_bytes, void *stream);
+EOQ_API int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, const void *dy, const int8_t *x_codes, const float *x_scales, const int8_t *w_codes,
+                const float *w_scales, void *dx, float *dw, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The norm of a step's floating-point gradients (eoq_lin_bwd, eoq_gn_bwd, eoq_ckpt_wgrad) together, and their clipping in front of an update:
+ *   norm = sqrt(sum of g^2 over all elements of all tensors),  out = g * min(1, max_norm / norm).
+ * Host arrays of num tensors: g (device), sizes in elements (0: left out), dtypes (EOQ_F32, EOQ_F16, EOQ_BF16).  out: tensors of the same types, which may be g's own, or NULL
+ * for in place; otherwise tensors must not overlap.  norm: fp32, device.
+ * Sums run in 64 bits, in an order that depends on the sizes and alignments alone: results are reproducible bit for bit.  The factor is an fp32 number, 1 where the norm is
+ * at most max_norm.  A norm that no fp32 number holds, or NaN, raises EOQ_DEV_NONFINITE, is written as it is, and the factor is 1: the program skips the step.
+ * workspace: eoq_grad_workspace_size(num) bytes, 256-byte aligned; nothing is kept in it between calls.
+ * Errors: BAD_ARG (null pointer, num <= 0, unknown type, max_norm negative or NaN, the handle's device not the current one), ALIGNMENT (of an element, norm),
+ * UNSUPPORTED (num > 2^20, more than 2^40 elements), WORKSPACE.
+ */
+EOQ_API int eoq_grad_workspace_size(int num, size_t *bytes);
+EOQ_API int eoq_grad_norm(eoq_handle_t handle, int num, const void *const *g, const size_t *sizes, const int *dtypes, float *norm, void *workspace,
+                  size_t workspace_bytes, void *stream);
+EOQ_API int eoq_grad_clip(eoq_handle_t handle, int num, const void *const *g, void *const *out, const size_t *sizes, const int *dtypes, float max_norm, float *norm,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * Update of `num` scalar parameters (gamma, b1, b2; Sec. 3.2.3 applied to a single value): g = Q_g({total}) with
  * total the exact sum behind the gradient at exponent *total_exp[i] + exp_bias[i]; u = Q_u(lr g);
@@ -526,7 +584,7 @@ EOQ_API int eoq_last_status(eoq_handle_t handle, void *stream, unsigned *bits);
 #define EOQ_PROF_DGRAD_AUX 4     /* Q_e phase 2 */
 #define EOQ_PROF_WGRAD_AUX 5     /* slice sum + b1 term + Q_g behind the weight-gradient GEMM */
 #define EOQ_PROF_FWD_AUX 6       /* b1 weight table, weight row padding (eoq_weight_prep, or per call without it) */
-#define EOQ_PROF_OTHER 7         /* eoq_quantize, eoq_bn_*, eoq_gn_*, eoq_ckpt_* */
+#define EOQ_PROF_OTHER 7         /* eoq_quantize, eoq_bn_*, eoq_gn_*, eoq_ckpt_*, eoq_lin_*, eoq_grad_* */
 #define EOQ_PROF_UPDATE 8        /* eoq_update */
 #define EOQ_PROF_INPUT_Q 9       /* eoq_quantize_image */
 #define EOQ_PROF_WGRAD_TAPS 10   /* b1 error sums of the weight gradient (none for a layer without a bias in front) */

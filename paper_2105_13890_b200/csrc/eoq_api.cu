@@ -854,6 +854,18 @@ bool eoq::tiled_map_2d(CUtensorMap *map, const void *ptr, bool bf16, size_t cols
                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool eoq::tiled_map_of(CUtensorMap *map, const void *ptr, int elem, size_t cols, size_t rows, size_t pitch, int box_cols, int box_rows, int swizzle)
+{
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    return g_encode_tiled(map, elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT32, 2,
+                          const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // ================================================================================= handle
 
 extern "C" int eoq_create(eoq_handle_t *handle, int device)
@@ -2464,6 +2476,277 @@ extern "C" int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const 
     const cudaError_t err = launch_gn_bwd(a, d.dtype, workspace, &launches, s);
     count_launches(h, launches);
     return record(h, err);
+}
+
+// ================================================================================= linear layers in 8-bit integers
+
+static size_t lin_pitch(size_t cols) { return (cols + 15) & ~(size_t)15; }
+
+// The descriptor of a call with its strides filled in.
+static int lin_check(const eoq_lin_desc_t *desc, eoq_lin_desc_t *d)
+{
+    if (!desc) return EOQ_ERR_BAD_ARG;
+    *d = *desc;
+    if (d->rows == 0 || d->c_in <= 0 || d->c_out <= 0 || d->dtype < EOQ_F32 || d->dtype > EOQ_BF16) return EOQ_ERR_BAD_ARG;
+    // (no tensor of such a layer has 2^40 elements or its weights 2^34, so that tiles and parts of a reduction are counted in 31 bits)
+    if (d->rows > (size_t)1 << 30 || d->c_in > 1 << 20 || d->c_out > 1 << 20 || d->rows * (size_t)d->c_in > (size_t)1 << 40 ||
+        d->rows * (size_t)d->c_out > (size_t)1 << 40 || (size_t)d->c_in * d->c_out > (size_t)1 << 34)
+        return EOQ_ERR_UNSUPPORTED;
+    size_t *strides[4] = {&d->x_stride, &d->y_stride, &d->dy_stride, &d->dx_stride};
+    for (int i = 0; i < 4; ++i) {
+        const size_t c = i == 0 || i == 3 ? d->c_in : d->c_out;
+        if (*strides[i] == 0) *strides[i] = c;
+        if (*strides[i] < c) return EOQ_ERR_BAD_ARG;
+        if (*strides[i] > (size_t)1 << 30) return EOQ_ERR_UNSUPPORTED;
+    }
+    return EOQ_OK;
+}
+
+// Places in the workspace of a call.
+struct LinSpace {
+    size_t row_codes, row_scales, col_codes, col_scales, tops, strip_sums, parts, bytes;
+};
+static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
+{
+    LinSpace s = {};
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += round256(bytes);
+        return here;
+    };
+    if (which == EOQ_LIN_FWD) {
+        s.row_codes = take(d.rows * lin_pitch(d.c_in));
+        s.row_scales = take(d.rows * 4);
+        s.parts = take(lin_gemm_workspace_bytes(d.rows, d.c_out, d.c_in));
+    } else {
+        const size_t codes = d.rows * lin_pitch(d.c_out), strips = (d.rows + lin_strip_rows(d.rows) - 1) / lin_strip_rows(d.rows);
+        s.row_codes = take(codes);
+        s.row_scales = take(d.rows * 4);
+        s.col_codes = take(codes);
+        s.col_scales = take((size_t)d.c_out * 4);
+        s.tops = take((size_t)d.c_out * 4);
+        s.strip_sums = take(strips * d.c_out * 4);
+        const size_t dx = lin_gemm_workspace_bytes(d.rows, d.c_in, d.c_out), dw = lin_gemm_workspace_bytes(d.c_out, d.c_in, d.rows);
+        s.parts = take(dx > dw ? dx : dw);
+    }
+    s.bytes = at;
+    return s;
+}
+
+extern "C" int eoq_lin_workspace_size(const eoq_lin_desc_t *desc, int which, size_t *bytes)
+{
+    eoq_lin_desc_t d;
+    if (!bytes || (which != EOQ_LIN_FWD && which != EOQ_LIN_BWD)) return EOQ_ERR_BAD_ARG;
+    const int chk = lin_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    *bytes = lin_space(d, which).bytes;
+    return EOQ_OK;
+}
+
+extern "C" int eoq_lin_quantize(eoq_handle_t handle, const void *src, int dtype, size_t rows, int cols, size_t stride, int8_t *codes, float *scales, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    if (stride == 0 && cols > 0) stride = cols;
+    if (!src || !codes || !scales || rows == 0 || cols <= 0 || stride < (size_t)cols || dtype < EOQ_F32 || dtype > EOQ_BF16) return EOQ_ERR_BAD_ARG;
+    if (rows > (size_t)1 << 30 || cols > 1 << 20 || stride > (size_t)1 << 30) return EOQ_ERR_UNSUPPORTED;
+    if (!aligned_to(src, dtype_size(dtype)) || !aligned16(codes) || !aligned_to(scales, 4)) return EOQ_ERR_ALIGNMENT;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    LinCodeArgs a = {};
+    a.src = src;
+    a.rows = rows;
+    a.stride = stride;
+    a.cols = cols;
+    a.codes = codes;
+    a.pitch = lin_pitch(cols);
+    a.scales = scales;
+    a.dev = h->dev;
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    const cudaError_t err = launch_lin_rows(a, dtype, &launches, s);
+    count_launches(h, launches);
+    return record(h, err);
+}
+
+extern "C" int eoq_lin_fwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, const void *x, int8_t *x_codes, float *x_scales, const int8_t *w_codes,
+                           const float *w_scales, const float *bias, void *y, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    eoq_lin_desc_t d;
+    const int chk = lin_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    if (!w_codes || !w_scales || !y || (x_codes == nullptr) != (x_scales == nullptr) || (!x && !x_codes)) return EOQ_ERR_BAD_ARG;
+    const size_t e = dtype_size(d.dtype);
+    if (!aligned_to(x, e) || !aligned_to(y, e) || !aligned16(x_codes) || !aligned_to(x_scales, 4) || !aligned16(w_codes) || !aligned_to(w_scales, 4) ||
+        !aligned_to(bias, 4))
+        return EOQ_ERR_ALIGNMENT;
+    const LinSpace space = lin_space(d, EOQ_LIN_FWD);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < space.bytes) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    char *ws = reinterpret_cast<char *>(workspace);
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    cudaError_t err = cudaSuccess;
+    if (!x_codes) {
+        x_codes = reinterpret_cast<int8_t *>(ws + space.row_codes);
+        x_scales = reinterpret_cast<float *>(ws + space.row_scales);
+    }
+    if (x) {
+        LinCodeArgs a = {};
+        a.src = x;
+        a.rows = d.rows;
+        a.stride = d.x_stride;
+        a.cols = d.c_in;
+        a.codes = x_codes;
+        a.pitch = lin_pitch(d.c_in);
+        a.scales = x_scales;
+        a.dev = h->dev;
+        err = launch_lin_rows(a, d.dtype, &launches, s);
+    }
+    if (err == cudaSuccess) {
+        LinGemmArgs g = {};
+        g.m = (int)d.rows;
+        g.n = d.c_out;
+        g.row_scale = x_scales;
+        g.col_scale = w_scales;
+        g.bias = bias;
+        g.out = y;
+        g.out_pitch = d.y_stride * e;
+        g.out_type = d.dtype;
+        g.sm_count = h->sm_count;
+        g.dev = h->dev;
+        err = launch_lin_gemm(g, EOQ_PASS_FWD, x_codes, lin_pitch(d.c_in), w_codes, lin_pitch(d.c_in), d.c_in, ws + space.parts, &launches, s);
+    }
+    count_launches(h, launches);
+    return record(h, err);
+}
+
+extern "C" int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, const void *dy, const int8_t *x_codes, const float *x_scales, const int8_t *w_codes,
+                           const float *w_scales, void *dx, float *dw, float *dbias, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    eoq_lin_desc_t d;
+    const int chk = lin_check(desc, &d);
+    if (chk != EOQ_OK) return chk;
+    if (!dy || (!dx && !dw && !dbias) || (dx && (!w_codes || !w_scales)) || (dw && (!x_codes || !x_scales))) return EOQ_ERR_BAD_ARG;
+    const size_t e = dtype_size(d.dtype);
+    if (!aligned_to(dy, e) || !aligned_to(dx, e) || !aligned16(x_codes) || !aligned_to(x_scales, 4) || !aligned16(w_codes) || !aligned_to(w_scales, 4) ||
+        !aligned16(dw) || !aligned_to(dbias, 4))
+        return EOQ_ERR_ALIGNMENT;
+    const LinSpace space = lin_space(d, EOQ_LIN_BWD);
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < space.bytes) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    char *ws = reinterpret_cast<char *>(workspace);
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    cudaError_t err = cudaSuccess;
+    LinCodeArgs a = {};
+    a.src = dy;
+    a.rows = d.rows;
+    a.stride = d.dy_stride;
+    a.cols = d.c_out;
+    a.pitch = lin_pitch(d.c_out);
+    a.dev = h->dev;
+    LinGemmArgs g = {};
+    g.sm_count = h->sm_count;
+    g.dev = h->dev;
+    if (dx) {
+        a.factors = w_scales;
+        a.codes = reinterpret_cast<int8_t *>(ws + space.row_codes);
+        a.scales = reinterpret_cast<float *>(ws + space.row_scales);
+        err = launch_lin_rows(a, d.dtype, &launches, s);
+        if (err == cudaSuccess) {
+            g.m = (int)d.rows;
+            g.n = d.c_in;
+            g.row_scale = a.scales;
+            g.out = dx;
+            g.out_pitch = d.dx_stride * e;
+            g.out_type = d.dtype;
+            err = launch_lin_gemm(g, EOQ_PASS_DGRAD, a.codes, a.pitch, w_codes, lin_pitch(d.c_in), d.c_out, ws + space.parts, &launches, s);
+        }
+    }
+    if (err == cudaSuccess && (dw || dbias)) {
+        a.factors = dw ? x_scales : nullptr;
+        a.codes = reinterpret_cast<int8_t *>(ws + space.col_codes);
+        a.scales = reinterpret_cast<float *>(ws + space.col_scales);
+        a.tops = dw ? reinterpret_cast<uint32_t *>(ws + space.tops) : nullptr;
+        a.sums = dbias;
+        a.strip_sums = reinterpret_cast<float *>(ws + space.strip_sums);
+        err = launch_lin_columns(a, d.dtype, &launches, s);
+        if (err == cudaSuccess && dw) {
+            g.m = d.c_out;
+            g.n = d.c_in;
+            g.row_scale = a.scales;
+            g.out = dw;
+            g.out_pitch = (size_t)d.c_in * 4;
+            g.out_type = EOQ_F32;
+            err = launch_lin_gemm(g, EOQ_PASS_WGRAD, a.codes, a.pitch, x_codes, lin_pitch(d.c_in), d.rows, ws + space.parts, &launches, s);
+        }
+    }
+    count_launches(h, launches);
+    return record(h, err);
+}
+
+// ================================================================================= norm and clipping of gradients
+
+static int grad_check(int num, const void *const *g, void *const *out, const size_t *sizes, const int *dtypes)
+{
+    if (num <= 0 || !g || !sizes || !dtypes) return EOQ_ERR_BAD_ARG;
+    if (num > 1 << 20) return EOQ_ERR_UNSUPPORTED;
+    size_t pieces = 0;
+    bool odd = false;
+    for (int i = 0; i < num; ++i) {
+        if (dtypes[i] < EOQ_F32 || dtypes[i] > EOQ_BF16) return EOQ_ERR_BAD_ARG;
+        if (sizes[i] == 0) continue;
+        if (!g[i] || (out && !out[i])) return EOQ_ERR_BAD_ARG;
+        if (sizes[i] > (size_t)1 << 40) return EOQ_ERR_UNSUPPORTED;
+        pieces += (sizes[i] + kGradPiece - 1) / kGradPiece;
+        odd = odd || !aligned_to(g[i], dtype_size(dtypes[i])) || (out && !aligned_to(out[i], dtype_size(dtypes[i])));
+    }
+    if (pieces > (size_t)1 << 31) return EOQ_ERR_UNSUPPORTED;
+    return odd ? EOQ_ERR_ALIGNMENT : EOQ_OK;
+}
+
+extern "C" int eoq_grad_workspace_size(int num, size_t *bytes)
+{
+    if (!bytes || num <= 0) return EOQ_ERR_BAD_ARG;
+    if (num > 1 << 20) return EOQ_ERR_UNSUPPORTED;
+    *bytes = round256(grad_workspace_bytes(num));
+    return EOQ_OK;
+}
+
+static int grad_call(eoq_handle_t handle, bool clip, int num, const void *const *g, void *const *out, const size_t *sizes, const int *dtypes, float max_norm,
+                     float *norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    Handle *h = reinterpret_cast<Handle *>(handle);
+    const int chk = grad_check(num, g, out, sizes, dtypes);
+    if (chk != EOQ_OK) return chk;
+    if (!norm || (clip && !(max_norm >= 0.0f))) return EOQ_ERR_BAD_ARG;
+    if (!aligned_to(norm, 4)) return EOQ_ERR_ALIGNMENT;
+    if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < grad_workspace_bytes(num)) return EOQ_ERR_WORKSPACE;
+    if (!on_handle_device(h)) return EOQ_ERR_BAD_ARG;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    ProfScope prof(h, EOQ_PROF_OTHER, s);
+    int launches = 0;
+    const GradList l = {num, g, out, sizes, dtypes};
+    const cudaError_t err = launch_grad(l, clip, max_norm, norm, workspace, h->dev, &launches, s);
+    count_launches(h, launches);
+    return record(h, err);
+}
+
+extern "C" int eoq_grad_norm(eoq_handle_t handle, int num, const void *const *g, const size_t *sizes, const int *dtypes, float *norm, void *workspace,
+                             size_t workspace_bytes, void *stream)
+{
+    return grad_call(handle, false, num, g, nullptr, sizes, dtypes, 0.0f, norm, workspace, workspace_bytes, stream);
+}
+
+extern "C" int eoq_grad_clip(eoq_handle_t handle, int num, const void *const *g, void *const *out, const size_t *sizes, const int *dtypes, float max_norm,
+                             float *norm, void *workspace, size_t workspace_bytes, void *stream)
+{
+    return grad_call(handle, true, num, g, out, sizes, dtypes, max_norm, norm, workspace, workspace_bytes, stream);
 }
 
 extern "C" int eoq_aux_avgpool_sum(eoq_handle_t handle, const int8_t *x, int n, int hw, int c, int32_t *sums, void *stream)

@@ -331,10 +331,96 @@ static PyObject *gn_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
                     (const float *)p[5], (const float *)p[6], (const float *)p[7], p[8], (float *)p[9], (float *)p[10], p[11], bytes, p[12]));
 }
 
+static int get_lin_desc(PyObject *o, eoq_lin_desc_t *out)
+{
+    Py_buffer view;
+    if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE)) return 0;
+    const int ok = view.len == (Py_ssize_t)sizeof(*out);
+    if (ok) memcpy(out, view.buf, sizeof(*out));
+    else PyErr_SetString(PyExc_TypeError, "not a linear layer descriptor");
+    PyBuffer_Release(&view);
+    return ok;
+}
+
+static PyObject *lin_quantize(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle src dtype rows cols stride | codes scales stream */
+    void *h, *src, *p[3];
+    int dtype, cols;
+    long long rows, stride;
+    if (!want(n, 9) || !get_ptr(a[0], &h) || !get_ptr(a[1], &src) || !get_i32(a[2], &dtype) || !get_int(a[3], &rows) || !get_i32(a[4], &cols) ||
+        !get_int(a[5], &stride))
+        return NULL;
+    PTRS(6, 3);
+    CALL(eoq_lin_quantize((eoq_handle_t)h, src, dtype, (size_t)rows, cols, (size_t)stride, (int8_t *)p[0], (float *)p[1], p[2]));
+}
+
+static PyObject *lin_fwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle desc | x x_codes x_scales w_codes w_scales bias y workspace stream */
+    void *h, *p[9];
+    eoq_lin_desc_t d;
+    size_t bytes;
+    if (!want(n, 11) || !get_ptr(a[0], &h) || !get_lin_desc(a[1], &d) || !get_bytes(a[9], &bytes)) return NULL;
+    PTRS(2, 9);
+    CALL(eoq_lin_fwd((eoq_handle_t)h, &d, p[0], (int8_t *)p[1], (float *)p[2], (const int8_t *)p[3], (const float *)p[4], (const float *)p[5], p[6], p[7],
+                     bytes, p[8]));
+}
+
+static PyObject *lin_bwd(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle desc | dy x_codes x_scales w_codes w_scales dx dw dbias workspace stream */
+    void *h, *p[10];
+    eoq_lin_desc_t d;
+    size_t bytes;
+    if (!want(n, 12) || !get_ptr(a[0], &h) || !get_lin_desc(a[1], &d) || !get_bytes(a[10], &bytes)) return NULL;
+    PTRS(2, 10);
+    CALL(eoq_lin_bwd((eoq_handle_t)h, &d, p[0], (const int8_t *)p[1], (const float *)p[2], (const int8_t *)p[3], (const float *)p[4], p[5], (float *)p[6],
+                     (float *)p[7], p[8], bytes, p[9]));
+}
+
+/* a buffer of num elements of `size` bytes (None: NULL) */
+static int get_array(PyObject *o, Py_ssize_t num, size_t size, Py_buffer *view)
+{
+    view->obj = NULL;
+    view->buf = NULL;
+    if (o == Py_None) return 1;
+    if (PyObject_GetBuffer(o, view, PyBUF_SIMPLE)) return 0;
+    if (view->len == (Py_ssize_t)(num * size)) return 1;
+    PyErr_SetString(PyExc_ValueError, "an array of another length");
+    PyBuffer_Release(view);
+    return 0;
+}
+
+static PyObject *grad_clip(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    /* handle clip num | g out sizes dtypes (arrays) | max_norm norm workspace stream */
+    void *h, *p[3];
+    int clip, num, st = EOQ_OK;
+    size_t bytes;
+    if (!want(n, 11) || !get_ptr(a[0], &h) || !get_i32(a[1], &clip) || !get_i32(a[2], &num) || !get_bytes(a[9], &bytes)) return NULL;
+    const double max_norm = PyFloat_AsDouble(a[7]);
+    if (max_norm == -1.0 && PyErr_Occurred()) return NULL;
+    PTRS(8, 3);
+    Py_buffer v[4];
+    const size_t size[4] = {sizeof(void *), sizeof(void *), sizeof(size_t), sizeof(int)};
+    int got = 0;
+    while (got < 4 && get_array(a[3 + got], num, size[got], &v[got])) ++got;
+    if (got == 4) {
+        Py_BEGIN_ALLOW_THREADS
+        st = clip ? eoq_grad_clip((eoq_handle_t)h, num, v[0].buf, v[1].buf, v[2].buf, v[3].buf, (float)max_norm, p[0], p[1], bytes, p[2])
+                  : eoq_grad_norm((eoq_handle_t)h, num, v[0].buf, v[2].buf, v[3].buf, p[0], p[1], bytes, p[2]);
+        Py_END_ALLOW_THREADS
+    }
+    for (int i = 0; i < got; ++i)
+        if (v[i].obj) PyBuffer_Release(&v[i]);
+    return got == 4 ? PyLong_FromLong(st) : NULL;
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD(conv_fwd_dev), METHOD(conv_dgrad), METHOD(conv_wgrad_dev), METHOD(err_prescale_dev),
                                 METHOD(quantize), METHOD(update_dev), METHOD(weight_prep), METHOD(ckpt_save), METHOD(ckpt_load), METHOD(ckpt_wgrad),
-                                METHOD(gn_fwd), METHOD(gn_bwd), {NULL, NULL, 0, NULL}};
+                                METHOD(gn_fwd), METHOD(gn_bwd), METHOD(lin_quantize), METHOD(lin_fwd), METHOD(lin_bwd), METHOD(grad_clip), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_eoqbind", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__eoqbind(void)

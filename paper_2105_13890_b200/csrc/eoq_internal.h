@@ -550,6 +550,70 @@ struct CkptWgradArgs {
 size_t ckpt_wgrad_workspace_bytes(size_t rows, int c_out, int c_in, int dtype);
 cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *workspace, int *launches, cudaStream_t st);
 
+// Linear layers in 8-bit integers (eoq_lin_*).  A tiled tensor map of any element size (1: bytes, 2: 16-bit, 4: 32-bit words) and swizzle (bytes of a row: 32, 64, 128).
+bool tiled_map_of(CUtensorMap *map, const void *ptr, int elem, size_t cols, size_t rows, size_t pitch, int box_cols, int box_rows, int swizzle);
+
+// Coding of rows or columns with a scale each.
+struct LinCodeArgs {
+    const void *src;
+    size_t rows, stride;            // stride in elements
+    int cols;
+    const float *factors;           // multiplied in before the coding: of the columns when rows are coded (may be null), of the rows when columns are
+    int8_t *codes;
+    size_t pitch;                   // bytes of a row of codes
+    float *scales;
+    DeviceState *dev;
+    // of columns
+    uint32_t *tops;                 // [cols] largest magnitudes; null: no codes wanted, sums alone
+    float *sums, *strip_sums;       // [cols] sums of the values and their parts by strips of rows; null: not wanted
+    size_t strip;                   // filled in by the launcher: rows of a strip, strips
+    int strips;
+};
+size_t lin_strip_rows(size_t rows);
+cudaError_t launch_lin_rows(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
+cudaError_t launch_lin_columns(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
+
+// out[m][n] = row_scale[m] col_scale[n] sum_k A B + bias[n]
+struct LinGemmArgs {
+    int m, n;
+    const float *row_scale, *col_scale, *bias;   // the last two may be null
+    void *out;
+    size_t out_pitch;               // bytes
+    int out_type;
+    int sm_count;
+    DeviceState *dev;
+    // filled in by the launcher
+    int m_tiles, n_tiles, splits, k_stages, stages_per_split;
+    int split_rows;                 // rows from one part's sums to the next one's
+    bool tensor_store, launch_early;
+};
+size_t lin_gemm_workspace_bytes(size_t m, size_t n, size_t k);
+// pass: EOQ_PASS_FWD (A [m][k], B [n][k]), EOQ_PASS_DGRAD (A [m][k], B [k][n]), EOQ_PASS_WGRAD (A [k][m], B [k][n]); pitches in bytes, multiples of 16
+cudaError_t launch_lin_gemm(LinGemmArgs a, int pass, const int8_t *pa, size_t pitch_a, const int8_t *pb, size_t pitch_b, size_t k, void *workspace, int *launches,
+                            cudaStream_t st);
+
+// Norm and clipping of gradients (eoq_grad_*).
+constexpr int kGradTensors = 256, kGradPiece = 8192;   // tensors of a launch; elements of a piece
+struct GradBatch {                  // a launch's tensors
+    const void *in[kGradTensors];
+    void *out[kGradTensors];
+    unsigned long long size[kGradTensors];
+    unsigned first[kGradTensors];   // pieces of the tensors before
+    uint8_t dtype[kGradTensors];
+    double *sums;                   // a block's sum of squares each
+    unsigned pieces;
+    int num;
+};
+struct GradList {                   // a call's, in host memory
+    int num;
+    const void *const *in;
+    void *const *out;               // null: in place
+    const size_t *size;
+    const int *dtype;
+};
+size_t grad_workspace_bytes(int num);
+cudaError_t launch_grad(const GradList &l, bool clip, float max_norm, float *norm, void *workspace, DeviceState *dev, int *launches, cudaStream_t st);
+
 // Division by a number that a launch keeps: exact as long as dividend times divisor stays below 2^32.
 struct FastDiv {
     unsigned d, m;

@@ -25,6 +25,7 @@ EOQ_ROUND_RNE, EOQ_ROUND_STOCHASTIC = 0, 1
 EOQ_F32, EOQ_F16, EOQ_BF16, EOQ_I32 = range(4)
 EOQ_ACT_NONE, EOQ_ACT_RELU, EOQ_ACT_SILU = range(3)
 EOQ_CKPT_BLOCK = 32
+EOQ_LIN_FWD, EOQ_LIN_BWD = 0, 1
 EOQ_PASS_FWD, EOQ_PASS_DGRAD, EOQ_PASS_WGRAD = 0, 1, 2
 
 EXPORTS = [
@@ -35,6 +36,7 @@ EXPORTS = [
     "eoq_err_prescale_dev", "eoq_update_dev", "eoq_update_part", "eoq_describe_plan", "eoq_debug_force_wait_timeout", "eoq_probe_mma_i8", "eoq_profile_gemm_only", "eoq_aux_maxpool_fwd", "eoq_aux_maxpool_bwd",
     "eoq_aux_maxpool_bwd_head", "eoq_aux_avgpool_sum", "eoq_aux_join", "eoq_aux_join_head", "eoq_conv_dgrad_head", "eoq_conv_dgrad_join_head", "eoq_conv_wgrad_gemm", "eoq_wgrad_finish", "eoq_aux_head_workspace_size", "eoq_aux_head", "eoq_aux_head_update", "eoq_aux_head_error", "eoq_aux_scalar_update", "eoq_update_wide", "eoq_set_reduce_hook", "eoq_bn_workspace_size", "eoq_bn_fwd", "eoq_bn_bwd",
     "eoq_ckpt_save", "eoq_ckpt_load", "eoq_ckpt_wgrad_workspace_size", "eoq_ckpt_wgrad", "eoq_gn_workspace_size", "eoq_gn_fwd", "eoq_gn_bwd",
+    "eoq_lin_workspace_size", "eoq_lin_quantize", "eoq_lin_fwd", "eoq_lin_bwd", "eoq_grad_workspace_size", "eoq_grad_norm", "eoq_grad_clip",
 ]
 EOQ_STATIC_SCRATCH_BYTES = 16 << 20
 EOQ_PROF_IGEMM_FWD, EOQ_PROF_IGEMM_DGRAD, EOQ_PROF_WGRAD = 0, 1, 2
@@ -79,6 +81,42 @@ class eoq_gn_desc_t(C.Structure):
 def gn_desc(n, hw, c, groups, dtype, act=EOQ_ACT_NONE, eps=1e-5, x_exp=0, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0) -> eoq_gn_desc_t:
     _fits("gn_desc", (n, hw, c, groups, dtype, x_exp, act), (x_stride, y_stride, dy_stride, dx_stride))
     return eoq_gn_desc_t(n, hw, c, groups, dtype, x_exp, act, eps, x_stride, y_stride, dy_stride, dx_stride)
+
+
+class eoq_lin_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_size_t)] + [(k, C.c_int) for k in ("c_in", "c_out", "dtype")] + \
+               [(k, C.c_size_t) for k in ("x_stride", "y_stride", "dy_stride", "dx_stride")]
+
+
+def lin_desc(rows, c_in, c_out, dtype, x_stride=0, y_stride=0, dy_stride=0, dx_stride=0) -> eoq_lin_desc_t:
+    _fits("lin_desc", (c_in, c_out, dtype), (rows, x_stride, y_stride, dy_stride, dx_stride))
+    return eoq_lin_desc_t(rows, c_in, c_out, dtype, x_stride, y_stride, dy_stride, dx_stride)
+
+
+def lin_pitch(cols: int) -> int:
+    """Bytes of a row of `cols` codes."""
+    return -(-cols // 16) * 16
+
+
+class grad_list:
+    """The gradients of a step as eoq_grad_norm and eoq_grad_clip take them: contiguous tensors, and where the clipped ones go (None: in place).  Holds on to the
+    tensors; a program whose gradients keep their places makes one and uses it in every step."""
+
+    def __init__(self, tensors: Sequence, out: Optional[Sequence] = None):
+        self.tensors, self.out = list(tensors), None if out is None else list(out)
+        self.num = len(self.tensors)
+        if out is not None and len(self.out) != self.num:
+            raise ValueError("grad_list: as many tensors to clip into as gradients")
+        for i, t in enumerate(self.tensors):
+            if not t.is_contiguous() or (out is not None and (not self.out[i].is_contiguous() or self.out[i].dtype != t.dtype or self.out[i].numel() != t.numel())):
+                raise ValueError("grad_list: contiguous tensors, of the same type and size where they are clipped into others")
+        types = {"torch.float32": EOQ_F32, "torch.float16": EOQ_F16, "torch.bfloat16": EOQ_BF16}
+        if any(str(t.dtype) not in types for t in self.tensors):
+            raise TypeError("grad_list: gradients in fp32, fp16 or bf16")
+        self.g = (C.c_void_p * self.num)(*[t.data_ptr() for t in self.tensors])
+        self.to = None if out is None else (C.c_void_p * self.num)(*[t.data_ptr() for t in self.out])
+        self.sizes = (C.c_size_t * self.num)(*[t.numel() for t in self.tensors])
+        self.dtypes = (C.c_int * self.num)(*[types[str(t.dtype)] for t in self.tensors])
 
 
 _lib = None
@@ -158,6 +196,8 @@ def lib() -> C.CDLL:
         L.eoq_ckpt_wgrad_workspace_size.argtypes = [sz, ci, ci, ci, C.POINTER(sz)]
         L.eoq_ckpt_wgrad.argtypes = [vp, vp, ci, sz, ci, sz, vp, vp, ci, vp, vp, sz, vp]
         L.eoq_gn_workspace_size.argtypes = [gp, C.POINTER(sz)]
+        L.eoq_lin_workspace_size.argtypes = [C.POINTER(eoq_lin_desc_t), C.c_int, C.POINTER(sz)]
+        L.eoq_grad_workspace_size.argtypes = [C.c_int, C.POINTER(sz)]
         L.eoq_gn_fwd.argtypes = [vp, gp] + [vp] * 8 + [sz, vp]
         L.eoq_gn_bwd.argtypes = [vp, gp] + [vp] * 12 + [sz, vp]
         L.eoq_profile_gemm_only.argtypes = [vp, C.c_int]
@@ -548,6 +588,55 @@ def eoq_gn_bwd(handle, desc, dy, dy_exp, x, codes, exps, gamma, beta, stats, dx,
                                       _stream(stream))
     if check:
         _check(st, "eoq_gn_bwd")
+    return st
+
+
+# ------------------------------------------------------------------------------- linear layers in 8-bit integers, norm and clipping of gradients
+
+def eoq_lin_workspace_size(desc: eoq_lin_desc_t, which: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().eoq_lin_workspace_size(C.byref(desc), int(which), C.byref(out)), "eoq_lin_workspace_size")
+    return out.value
+
+
+def eoq_lin_quantize(handle, src, dtype, rows, cols, stride, codes, scales, stream=None, check: bool = True) -> int:
+    st = (_native or native()).lin_quantize(handle, src, dtype, rows, cols, stride, codes, scales, _stream(stream))
+    if check:
+        _check(st, "eoq_lin_quantize")
+    return st
+
+
+def eoq_lin_fwd(handle, desc, x, x_codes, x_scales, w_codes, w_scales, bias, y, workspace, stream=None, check: bool = True) -> int:
+    st = (_native or native()).lin_fwd(handle, desc, x, x_codes, x_scales, w_codes, w_scales, bias, y, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_lin_fwd")
+    return st
+
+
+def eoq_lin_bwd(handle, desc, dy, x_codes, x_scales, w_codes, w_scales, dx, dw, dbias, workspace, stream=None, check: bool = True) -> int:
+    st = (_native or native()).lin_bwd(handle, desc, dy, x_codes, x_scales, w_codes, w_scales, dx, dw, dbias, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_lin_bwd")
+    return st
+
+
+def eoq_grad_workspace_size(grads: grad_list) -> int:
+    out = C.c_size_t(0)
+    _check(lib().eoq_grad_workspace_size(grads.num, C.byref(out)), "eoq_grad_workspace_size")
+    return out.value
+
+
+def eoq_grad_norm(handle, grads: grad_list, norm, workspace, stream=None, check: bool = True) -> int:
+    st = (_native or native()).grad_clip(handle, 0, grads.num, grads.g, None, grads.sizes, grads.dtypes, 0.0, norm, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_grad_norm")
+    return st
+
+
+def eoq_grad_clip(handle, grads: grad_list, max_norm, norm, workspace, stream=None, check: bool = True) -> int:
+    st = (_native or native()).grad_clip(handle, 1, grads.num, grads.g, grads.to, grads.sizes, grads.dtypes, max_norm, norm, workspace, _stream(stream))
+    if check:
+        _check(st, "eoq_grad_clip")
     return st
 
 
