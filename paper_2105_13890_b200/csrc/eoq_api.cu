@@ -2504,7 +2504,7 @@ static int lin_check(const eoq_lin_desc_t *desc, eoq_lin_desc_t *d)
 
 // Places in the workspace of a call.
 struct LinSpace {
-    size_t row_codes, row_scales, col_codes, col_scales, tops, strip_sums, parts, bytes;
+    size_t row_codes, row_scales, row_tops, row_per, col_codes, col_scales, col_per, strip_tops, strip_sums, parts, bytes;
 };
 static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
 {
@@ -2520,13 +2520,17 @@ static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
         s.row_scales = take(d.rows * 4);
         s.parts = take(lin_gemm_workspace_bytes(d.rows, d.c_out, d.c_in));
     } else {
-        const size_t codes = d.rows * lin_pitch(d.c_out), strips = (d.rows + lin_strip_rows(d.rows) - 1) / lin_strip_rows(d.rows);
+        const size_t codes = d.rows * lin_pitch(d.c_out);
+        const LinStrips l = lin_strips(d.rows, d.c_out);
         s.row_codes = take(codes);
         s.row_scales = take(d.rows * 4);
+        s.row_per = take(d.rows * 4);
         s.col_codes = take(codes);
-        s.col_scales = take((size_t)d.c_out * 4);
-        s.tops = take((size_t)d.c_out * 4);
-        s.strip_sums = take(strips * d.c_out * 4);
+        s.col_scales = take(l.col_pitch * 4);
+        s.col_per = take(l.col_pitch * 4);
+        s.strip_tops = take(l.floats * 4);
+        s.strip_sums = take(l.floats * 4);
+        s.row_tops = take(l.row_floats * 4);
         const size_t dx = lin_gemm_workspace_bytes(d.rows, d.c_in, d.c_out), dw = lin_gemm_workspace_bytes(d.c_out, d.c_in, d.rows);
         s.parts = take(dx > dw ? dx : dw);
     }
@@ -2642,49 +2646,52 @@ extern "C" int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
     char *ws = reinterpret_cast<char *>(workspace);
     ProfScope prof(h, EOQ_PROF_OTHER, s);
     int launches = 0;
-    cudaError_t err = cudaSuccess;
-    LinCodeArgs a = {};
+    LinErrorArgs a = {};
     a.src = dy;
     a.rows = d.rows;
     a.stride = d.dy_stride;
     a.cols = d.c_out;
     a.pitch = lin_pitch(d.c_out);
     a.dev = h->dev;
-    LinGemmArgs g = {};
-    g.sm_count = h->sm_count;
-    g.dev = h->dev;
     if (dx) {
         a.factors = w_scales;
         a.codes = reinterpret_cast<int8_t *>(ws + space.row_codes);
         a.scales = reinterpret_cast<float *>(ws + space.row_scales);
-        err = launch_lin_rows(a, d.dtype, &launches, s);
-        if (err == cudaSuccess) {
-            g.m = (int)d.rows;
-            g.n = d.c_in;
-            g.row_scale = a.scales;
-            g.out = dx;
-            g.out_pitch = d.dx_stride * e;
-            g.out_type = d.dtype;
-            err = launch_lin_gemm(g, EOQ_PASS_DGRAD, a.codes, a.pitch, w_codes, lin_pitch(d.c_in), d.c_out, ws + space.parts, &launches, s);
-        }
+        a.row_tops = reinterpret_cast<float *>(ws + space.row_tops);
+        a.row_per = reinterpret_cast<float *>(ws + space.row_per);
     }
-    if (err == cudaSuccess && (dw || dbias)) {
-        a.factors = dw ? x_scales : nullptr;
-        a.codes = reinterpret_cast<int8_t *>(ws + space.col_codes);
-        a.scales = reinterpret_cast<float *>(ws + space.col_scales);
-        a.tops = dw ? reinterpret_cast<uint32_t *>(ws + space.tops) : nullptr;
+    if (dw) {
+        a.row_factors = x_scales;
+        a.col_codes = reinterpret_cast<int8_t *>(ws + space.col_codes);
+        a.col_scales = reinterpret_cast<float *>(ws + space.col_scales);
+        a.strip_tops = reinterpret_cast<float *>(ws + space.strip_tops);
+        a.col_per = reinterpret_cast<float *>(ws + space.col_per);
+    }
+    if (dbias) {
         a.sums = dbias;
         a.strip_sums = reinterpret_cast<float *>(ws + space.strip_sums);
-        err = launch_lin_columns(a, d.dtype, &launches, s);
-        if (err == cudaSuccess && dw) {
-            g.m = d.c_out;
-            g.n = d.c_in;
-            g.row_scale = a.scales;
-            g.out = dw;
-            g.out_pitch = (size_t)d.c_in * 4;
-            g.out_type = EOQ_F32;
-            err = launch_lin_gemm(g, EOQ_PASS_WGRAD, a.codes, a.pitch, x_codes, lin_pitch(d.c_in), d.rows, ws + space.parts, &launches, s);
-        }
+    }
+    cudaError_t err = launch_lin_errors(a, d.dtype, &launches, s);
+    LinGemmArgs g = {};
+    g.sm_count = h->sm_count;
+    g.dev = h->dev;
+    if (err == cudaSuccess && dw) {
+        g.m = d.c_out;
+        g.n = d.c_in;
+        g.row_scale = a.col_scales;
+        g.out = dw;
+        g.out_pitch = (size_t)d.c_in * 4;
+        g.out_type = EOQ_F32;
+        err = launch_lin_gemm(g, EOQ_PASS_WGRAD, a.col_codes, a.pitch, x_codes, lin_pitch(d.c_in), d.rows, ws + space.parts, &launches, s);
+    }
+    if (err == cudaSuccess && dx) {
+        g.m = (int)d.rows;
+        g.n = d.c_in;
+        g.row_scale = a.scales;
+        g.out = dx;
+        g.out_pitch = d.dx_stride * e;
+        g.out_type = d.dtype;
+        err = launch_lin_gemm(g, EOQ_PASS_DGRAD, a.codes, a.pitch, w_codes, lin_pitch(d.c_in), d.c_out, ws + space.parts, &launches, s);
     }
     count_launches(h, launches);
     return record(h, err);

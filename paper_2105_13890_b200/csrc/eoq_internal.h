@@ -553,25 +553,41 @@ cudaError_t launch_ckpt_wgrad(CkptWgradArgs a, int dtype, float *dw, void *works
 // Linear layers in 8-bit integers (eoq_lin_*).  A tiled tensor map of any element size (1: bytes, 2: 16-bit, 4: 32-bit words) and swizzle (bytes of a row: 32, 64, 128).
 bool tiled_map_of(CUtensorMap *map, const void *ptr, int elem, size_t cols, size_t rows, size_t pitch, int box_cols, int box_rows, int swizzle);
 
-// Coding of rows or columns with a scale each.
+// Coding of rows with a scale each.
 struct LinCodeArgs {
     const void *src;
     size_t rows, stride;            // stride in elements
     int cols;
-    const float *factors;           // multiplied in before the coding: of the columns when rows are coded (may be null), of the rows when columns are
+    const float *factors;           // of the columns, multiplied in before the coding; may be null
     int8_t *codes;
     size_t pitch;                   // bytes of a row of codes
     float *scales;
     DeviceState *dev;
-    // of columns
-    uint32_t *tops;                 // [cols] largest magnitudes; null: no codes wanted, sums alone
-    float *sums, *strip_sums;       // [cols] sums of the values and their parts by strips of rows; null: not wanted
-    size_t strip;                   // filled in by the launcher: rows of a strip, strips
-    int strips;
 };
-size_t lin_strip_rows(size_t rows);
+// Coding of a layer's errors by rows, by columns, and the columns' sums.
+struct LinErrorArgs {
+    const void *src;
+    size_t rows, stride;
+    int cols;
+    size_t pitch;                   // bytes of a row of either codes
+    DeviceState *dev;
+    const float *factors;           // of the columns, for the rows' codes; null codes: not wanted
+    int8_t *codes;
+    float *scales, *row_tops, *row_per;   // row_tops [chunks][rows]: largest magnitudes of parts of rows; row_per [rows]: from a value to its code
+    const float *row_factors;       // of the rows, for the columns' codes; null strip_tops: not wanted
+    int8_t *col_codes;
+    float *col_scales, *strip_tops, *col_per;   // strip_tops [strips][col_pitch]: of parts of columns; col_per [col_pitch]
+    float *sums, *strip_sums;       // of the values; null strip_sums: not wanted
+    size_t strip, col_pitch;        // filled in by the launcher: rows of a strip, floats from strip to strip
+    int strips, chunks;
+};
+struct LinStrips {
+    size_t rows, col_pitch;         // of a strip; floats from strip to strip
+    size_t floats, row_floats;      // of all strips; of the parts of all rows
+};
+LinStrips lin_strips(size_t rows, int cols);
 cudaError_t launch_lin_rows(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
-cudaError_t launch_lin_columns(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
+cudaError_t launch_lin_errors(const LinErrorArgs &a, int dtype, int *launches, cudaStream_t st);
 
 // out[m][n] = row_scale[m] col_scale[n] sum_k A B + bias[n]
 struct LinGemmArgs {
