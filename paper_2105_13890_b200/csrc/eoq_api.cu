@@ -2521,7 +2521,7 @@ static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
         s.parts = take(lin_gemm_workspace_bytes(d.rows, d.c_out, d.c_in));
     } else {
         const size_t codes = d.rows * lin_pitch(d.c_out);
-        const LinStrips l = lin_strips(d.rows, d.c_out);
+        const LinStrips l = lin_strips(d.rows, d.c_out, d.dtype);
         s.row_codes = take(codes);
         s.row_scales = take(d.rows * 4);
         s.row_per = take(d.rows * 4);

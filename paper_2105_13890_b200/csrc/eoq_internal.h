@@ -585,7 +585,7 @@ struct LinStrips {
     size_t rows, col_pitch;         // of a strip; floats from strip to strip
     size_t floats, row_floats;      // of all strips; of the parts of all rows
 };
-LinStrips lin_strips(size_t rows, int cols);
+LinStrips lin_strips(size_t rows, int cols, int dtype);
 cudaError_t launch_lin_rows(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
 cudaError_t launch_lin_errors(const LinErrorArgs &a, int dtype, int *launches, cudaStream_t st);
 

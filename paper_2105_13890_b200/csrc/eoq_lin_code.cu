@@ -15,62 +15,114 @@ namespace eoq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFoldStrips = 32;   // strips whose maxima the second look finds by itself; more take a kernel between the two
+// Strips, and elements of a tensor, whose maxima the second look puts together by itself; others take a kernel between the two.
+constexpr int kFoldStrips = 32;
+constexpr size_t kFoldSize = 1 << 20;
 
 // magnitudes as unsigned bits: their order, with infinity and then NaN above all numbers
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// the largest magnitude among the elements of a vector, as an fp32's bits
-template <int kType, int kBytes>
-__device__ __forceinline__ uint32_t raw_top(const Raw<kBytes> &r, uint32_t top)
+// the largest magnitude among the elements of 16 bytes, as an fp32's bits
+template <int kType>
+__device__ __forceinline__ uint32_t raw_top(const Raw<16> &r, uint32_t top)
 {
     if constexpr (kType == EOQ_F32) {
 #pragma unroll
-        for (int i = 0; i < kBytes / 4; ++i) top = max(top, raw_word(r, i) & 0x7fffffffu);
+        for (int i = 0; i < 4; ++i) top = max(top, raw_word(r, i) & 0x7fffffffu);
         return top;
     } else {
-        // the halves of a word side by side
-        uint32_t m = 0;
-        if constexpr (kBytes == 2) {
-            m = raw_word(r, 0) & 0x7fffu;
-        } else {
+        uint32_t m = 0;   // the halves of a word side by side
 #pragma unroll
-            for (int i = 0; i < kBytes / 4; ++i) m = __vmaxs2(m, raw_word(r, i) & 0x7fff7fffu);
-            m = max(m & 0xffffu, m >> 16);
-        }
+        for (int i = 0; i < 4; ++i) m = __vmaxs2(m, raw_word(r, i) & 0x7fff7fffu);
+        m = max(m & 0xffffu, m >> 16);
         if constexpr (kType == EOQ_BF16) return max(top, m << 16);
         else return max(top, abs_bits(__half2float(__ushort_as_half((unsigned short)m))));
     }
 }
 
-// a vector of a row from `col` on, zeros behind the row's end
-template <int kType, int kV>
-__device__ __forceinline__ Raw<kV * Elem<kType>::kSize> get_raw(const char *row, int col, int cols, bool mine)
-{
-    constexpr int kE = Elem<kType>::kSize;
-    if (mine && col + kV <= cols) return load_raw<kV * kE>(row + (size_t)col * kE);
-    Raw<kV * kE> r = zero_raw<kV * kE>();
-    if constexpr (kV > 1) {
-        if (mine && col < cols) {
+// A thread's 16 bytes of a row.  kWide: kN neighbouring elements, a vector; otherwise (rows that are not 16-byte aligned) kN elements `lanes` columns apart, so
+// that a warp's loads of each are neighbouring.  Threads of a row share groups of lanes * kN columns.
+template <int kType, bool kWide>
+struct Span {
+    static constexpr int kE = Elem<kType>::kSize, kN = 16 / kE;
+    int first, step, cols;   // the thread's column 0 of a group; to its next one; columns of a row
+    __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_)
+        : first(group * lanes * kN + (kWide ? lane * kN : lane)), step(kWide ? 1 : lanes), cols(cols_)
+    {
+    }
+    __device__ __forceinline__ int column(int i) const { return first + i * step; }
+    __device__ __forceinline__ bool any() const { return first < cols; }
+    // zeros behind the row's end
+    __device__ __forceinline__ Raw<16> get(const char *row, bool mine) const
+    {
+        if (kWide && mine && first + kN <= cols) return load_raw<16>(row + (size_t)first * kE);
+        Raw<16> r = zero_raw<16>();
+        if (!kWide) {
+            uint32_t w[kN];
 #pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                if (col + i >= cols) break;
-                const uint32_t w = raw_word(load_raw<kE>(row + (size_t)(col + i) * kE), 0);
-                if constexpr (kE == 4) set_word(r, i, w);
-                else set_word(r, i / 2, i & 1 ? raw_word(r, i / 2) | w << 16 : w);
+            for (int i = 0; i < kN; ++i) w[i] = mine && column(i) < cols ? raw_word(load_raw<kE>(row + (size_t)column(i) * kE), 0) : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) set_word(r, i, kE == 4 ? w[i] : w[2 * i % kN] | w[(2 * i + 1) % kN] << 16);
+        } else if (mine) {
+            // the last elements of a row whose end cuts a vector, last one first
+#pragma unroll 1
+            for (int c = cols - 1; c >= first; --c) {
+                const uint32_t w = raw_word(load_raw<kE>(row + (size_t)c * kE), 0);
+                if (kE == 4) r.w = make_uint4(w, r.w.x, r.w.y, r.w.z);
+                else r.w = make_uint4(r.w.x << 16 | w, __funnelshift_l(r.w.x, r.w.y, 16), __funnelshift_l(r.w.y, r.w.z, 16), __funnelshift_l(r.w.z, r.w.w, 16));
             }
         }
+        return r;
     }
-    return r;
-}
-
-// factors of kV columns; ones (of nothing) behind the end
-template <int kV>
-__device__ __forceinline__ void get_factors(const float *factors, int col, int cols, float (&f)[kV])
-{
+    // of an array with an element for each column (whole vectors of them: padded to eight); nothing (ones) behind the end
+    __device__ __forceinline__ void get_padded(const float *p, float (&v)[kN]) const
+    {
+        if constexpr (kWide) {
 #pragma unroll
-    for (int i = 0; i < kV; ++i) f[i] = col + i < cols ? __ldg(factors + col + i) : 1.0f;
-}
+            for (int i = 0; i < kN; i += 4) {
+                const float4 w = any() ? __ldg(reinterpret_cast<const float4 *>(p + first + i)) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                v[i] = w.x;
+                v[i + 1] = w.y;
+                v[i + 2] = w.z;
+                v[i + 3] = w.w;
+            }
+        } else {
+            get_exact(p, v);
+        }
+    }
+    __device__ __forceinline__ void get_exact(const float *p, float (&v)[kN]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = column(i) < cols ? __ldg(p + column(i)) : 1.0f;
+    }
+    __device__ __forceinline__ void put_padded(float *p, const float (&v)[kN]) const
+    {
+        if constexpr (kWide) {
+#pragma unroll
+            for (int i = 0; i < kN; i += 4)
+                if (any()) *reinterpret_cast<float4 *>(p + first + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+        } else {
+            put_exact(p, v);
+        }
+    }
+    __device__ __forceinline__ void put_exact(float *p, const float (&v)[kN]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            if (column(i) < cols) p[column(i)] = v[i];
+    }
+    // the low bytes of q as codes (a row of codes is whole pieces of 16 bytes)
+    __device__ __forceinline__ void put_codes(int8_t *row, const uint32_t (&q)[kN]) const
+    {
+        if constexpr (kWide) {
+            if (any()) store_raw(row + first, pack_codes(q));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+                if (column(i) < cols) row[column(i)] = (int8_t)q[i];
+        }
+    }
+};
 
 // the largest of `lanes` neighbouring threads' values, a power of two; of more than a warp by way of `cells`, one for each of the block's warps
 __device__ __forceinline__ uint32_t lanes_top(uint32_t top, int lanes, uint32_t *cells)
@@ -90,58 +142,52 @@ __device__ __forceinline__ uint32_t lanes_top(uint32_t top, int lanes, uint32_t 
     return top;
 }
 
-template <int kV>
-__device__ __forceinline__ void put_codes(int8_t *row, int col, const float (&v)[kV], float per, bool fine)
-{
-    uint32_t q[kV];
-#pragma unroll
-    for (int i = 0; i < kV; ++i) q[i] = row_code(v[i], per);
-    Raw<kV> r = pack_codes(q);
-    store_raw(row + col, fine ? r : zero_raw<kV>());   // (a row of codes is whole pieces of 16 bytes)
-}
-
-// Rows: kHold vectors of kV elements a lane of each of kRows rows at a time.
-template <int kType, int kV, int kHold, int kRows>
+// Rows: kHold groups of each of kRows rows at a time.
+template <int kType, bool kWide, int kHold, int kRows>
 __global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constant__ LinCodeArgs a, const int lanes)
 {
-    constexpr int kE = Elem<kType>::kSize;
+    using S = Span<kType, kWide>;
+    constexpr int kN = S::kN;
     __shared__ uint32_t cells[kThreads / 32];
     ptx::grid_dep_wait_launch_small();
-    const int lane = threadIdx.x % lanes, slots = kThreads / lanes;
+    const int lane = threadIdx.x % lanes, slots = kThreads / lanes, groups = (a.cols + lanes * kN - 1) / (lanes * kN);
     const size_t row0 = (size_t)blockIdx.x * kRows * slots + threadIdx.x / lanes;
-    const char *src = reinterpret_cast<const char *>(a.src) + row0 * a.stride * kE;
-    const size_t step = slots * a.stride * kE;
-    auto scaled = [&](const Raw<kV * kE> &r, int col, float (&v)[kV]) {
+    const char *src = reinterpret_cast<const char *>(a.src) + row0 * a.stride * S::kE;
+    const size_t step = slots * a.stride * S::kE;
+    auto scaled = [&](const Raw<16> &r, const S &at, float (&v)[kN]) {
         Elem<kType>::to_f32(r, v);
         if (a.factors) {
-            float f[kV];
-            get_factors(a.factors, col, a.cols, f);
+            float f[kN];
+            at.get_exact(a.factors, f);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) v[i] *= f[i];
+            for (int i = 0; i < kN; ++i) v[i] *= f[i];
         }
     };
-    auto more = [&](uint32_t top, const Raw<kV * kE> &r, int col) {
-        if (!a.factors) return raw_top<kType, kV * kE>(r, top);
-        float v[kV];
-        scaled(r, col, v);
+    auto more = [&](uint32_t top, const Raw<16> &r, const S &at) {
+        if (!a.factors) return raw_top<kType>(r, top);
+        float v[kN];
+        scaled(r, at, v);
 #pragma unroll
-        for (int i = 0; i < kV; ++i) top = max(top, abs_bits(v[i]));
+        for (int i = 0; i < kN; ++i) top = max(top, abs_bits(v[i]));
         return top;
     };
-    Raw<kV * kE> held[kRows][kHold];
+    Raw<16> held[kRows][kHold];
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) held[u][h] = get_raw<kType, kV>(src + u * step, (h * lanes + lane) * kV, a.cols, row0 + u * slots < a.rows);
+        for (int h = 0; h < kHold; ++h) held[u][h] = S(h, lane, lanes, a.cols).get(src + u * step, row0 + u * slots < a.rows);
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
         const size_t row = row0 + u * slots;
         const bool mine = row < a.rows;
         uint32_t top = 0;
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) top = more(top, held[u][h], (h * lanes + lane) * kV);
+        for (int h = 0; h < kHold; ++h) top = more(top, held[u][h], S(h, lane, lanes, a.cols));
         if (mine)
-            for (int col = (kHold * lanes + lane) * kV; col < a.cols; col += lanes * kV) top = more(top, get_raw<kType, kV>(src + u * step, col, a.cols, true), col);
+            for (int g = kHold; g < groups; ++g) {
+                const S at(g, lane, lanes, a.cols);
+                top = more(top, at.get(src + u * step, true), at);
+            }
         const float t = __uint_as_float(lanes_top(top, lanes, cells));
         if (kRows > 1 && lanes > 32) __syncthreads();   // (the cells are read)
         if (!mine) continue;
@@ -151,123 +197,140 @@ __global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constan
             a.scales[row] = row_scale_of(t);
             if (!fine) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
         }
-        int8_t *dst = a.codes + row * a.pitch;
+        auto put = [&](const Raw<16> &r, const S &at) {
+            float v[kN];
+            uint32_t q[kN];
+            scaled(r, at, v);
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) {
-            const int col = (h * lanes + lane) * kV;
-            if (col >= a.cols) break;
-            float v[kV];
-            scaled(held[u][h], col, v);
-            put_codes(dst, col, v, per, fine);
-        }
-        for (int col = (kHold * lanes + lane) * kV; col < a.cols; col += lanes * kV) {
-            float v[kV];
-            scaled(get_raw<kType, kV>(src + u * step, col, a.cols, true), col, v);
-            put_codes(dst, col, v, per, fine);
+            for (int i = 0; i < kN; ++i) q[i] = fine ? row_code(v[i], per) : 0u;
+            at.put_codes(a.codes + row * a.pitch, q);
+        };
+#pragma unroll
+        for (int h = 0; h < kHold; ++h) put(held[u][h], S(h, lane, lanes, a.cols));
+        for (int g = kHold; g < groups; ++g) {
+            const S at(g, lane, lanes, a.cols);
+            put(at.get(src + u * step, true), at);
         }
     }
 }
 
 // ------------------------------------------------------------------ the errors of a layer
 
-// kV floats from an address that is a multiple of their size
-template <int kV>
-__device__ __forceinline__ void get_floats(const float *p, float (&v)[kV])
-{
-    if constexpr (kV % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < kV; i += 4) {
-            const float4 w = __ldg(reinterpret_cast<const float4 *>(p + i));
-            v[i] = w.x;
-            v[i + 1] = w.y;
-            v[i + 2] = w.z;
-            v[i + 3] = w.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < kV; ++i) v[i] = __ldg(p + i);
-    }
-}
-template <int kV>
-__device__ __forceinline__ void put_floats(float *p, const float (&v)[kV])
-{
-    if constexpr (kV % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < kV; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kV; ++i) p[i] = v[i];
-    }
-}
-
 constexpr int kAhead = 4;   // rows of a thread in flight
 
-// Block (x, y): strip x of the rows, `lanes` (at most 32) vectors of columns.  kRows: the rows' maxima too.
-template <int kType, int kV, bool kRows>
-__global__ void __launch_bounds__(kThreads) lin_look_kernel(const __grid_constant__ LinErrorArgs a, const int lanes)
+// Block (x, y): strip x of the rows, group y of the columns, `lanes` (at most 32) threads a row.  kRows: the rows' maxima too.
+// Vectors come in by asynchronous copies, each read back by the thread that copied it, six to eight rows ahead.  16,384 x 4096 of bf16: 43 us, 3.1 TB/s, bound by
+// issue (15 instructions an element, of which the products, maxima and the sum are five).
+template <int kType, bool kWide, bool kRows>
+__global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_constant__ LinErrorArgs a, const int lanes)
 {
-    constexpr int kE = Elem<kType>::kSize;
-    __shared__ float tops_s[kThreads][kV], sums_s[kThreads][kV];
+    using S = Span<kType, kWide>;
+    constexpr int kN = S::kN, kRing = kWide ? 4 : 1, kPair = 2;   // stages of two rows
+    __shared__ __align__(16) uint4 ring[kRing * kPair][kThreads];
     ptx::grid_dep_wait_launch_small();
-    const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes, col = (blockIdx.y * lanes + lane) * kV;
+    const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes;
+    const S at(blockIdx.y, lane, lanes, a.cols);
     const size_t begin = (size_t)blockIdx.x * a.strip, end = min(a.rows, begin + a.strip);
-    const char *src = reinterpret_cast<const char *>(a.src) + (begin + slot) * a.stride * kE;
-    const size_t step = slots * a.stride * kE;
-    float w[kV], top[kV] = {}, sum[kV] = {};
-    if (kRows) get_factors(a.factors, col, a.cols, w);
-    Raw<kV * kE> next[kAhead];
-    float next_f[kAhead];
-    auto fetch = [&](size_t row) {
+    const size_t step = slots * a.stride * S::kE;
+    const char *src = reinterpret_cast<const char *>(a.src) + (begin + slot) * a.stride * S::kE;
+    const int stages = (int)((end - begin + kPair * slots - 1) / (kPair * slots));   // (the same for every lane)
+    int left = (int)(end - begin) - slot;                                           // rows from `src` on
+    Raw<16> now[kPair];
+    float f[kPair] = {}, next_f[kPair] = {};
+    const float *factor = a.row_factors + begin + slot;
+    // the next stage's copies or, without a ring, loads
+    auto fetch = [&](int stage) {
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const bool mine = row + u * slots < end;
-            next[u] = get_raw<kType, kV>(src + u * step, col, a.cols, mine);
-            next_f[u] = mine && a.row_factors ? __ldg(a.row_factors + row + u * slots) : 0.0f;
-        }
-        src += kAhead * step;
-    };
-    fetch(begin + slot);
-    for (size_t row0 = begin; row0 < end; row0 += kAhead * slots) {   // (the same rounds for every lane)
-        Raw<kV * kE> held[kAhead];
-        float f[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            held[u] = next[u];
-            f[u] = next_f[u];
-        }
-        fetch(row0 + slot + kAhead * slots);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            float v[kV], m = 0.0f;
-            Elem<kType>::to_f32(held[u], v);
-#pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                if (kRows) m = max_abs(m, v[i] * w[i]);
-                top[i] = max_abs(top[i], v[i] * f[u]);
-                sum[i] += v[i];
+        for (int u = 0; u < kPair; ++u) {
+            const bool mine = u * slots < left;
+            if constexpr (kWide) {
+                const int bytes = mine ? min(16, max(0, (a.cols - at.first) * S::kE)) : 0;   // (zeros behind them)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(&ring[stage % kRing * kPair + u][threadIdx.x])),
+                             "l"(bytes ? src + u * step + (size_t)at.first * S::kE : reinterpret_cast<const char *>(a.strip_tops ? a.strip_tops : a.strip_sums)), "r"(bytes)
+                             : "memory");
+            } else {
+                now[u] = at.get(src + u * step, mine);
             }
-            if (kRows) {
-                const uint32_t t = lanes_top(__float_as_uint(m), lanes, nullptr);
-                const size_t row = row0 + slot + u * slots;
+        }
+        src += kPair * step;
+        left -= kPair * slots;
+        if constexpr (kWide) asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int f_left = left;
+    auto fetch_factors = [&](float (&to)[kPair]) {
+#pragma unroll
+        for (int u = 0; u < kPair; ++u) to[u] = a.row_factors && u * slots < f_left ? __ldg(factor + u * slots) : 0.0f;
+        factor += kPair * slots;
+        f_left -= kPair * slots;
+    };
+    // Factors are scales, so a magnitude times one has the sign bit 0 (a NaN too), and magnitudes are compared as integers: three at a time.
+    float w[kN], sum[kN] = {};
+    int top[kN] = {};
+    if constexpr (kWide)
+        for (int j = 0; j < kRing - 1; ++j) fetch(j);   // (nothing but empty groups past the last one)
+    fetch_factors(next_f);
+    if (kRows) at.get_exact(a.factors, w);
+    for (int j = 0; j < stages; ++j) {
+#pragma unroll
+        for (int u = 0; u < kPair; ++u) f[u] = next_f[u];
+        fetch_factors(next_f);
+        if constexpr (kWide) {
+            fetch(j + kRing - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) now[u].w = ring[j % kRing * kPair + u][threadIdx.x];
+        } else {
+            fetch(j);
+        }
+        float v[kPair][kN];
+        Elem<kType>::to_f32(now[0], v[0]);
+        Elem<kType>::to_f32(now[1], v[1]);
+        auto times = [](float x, float y) { return __float_as_int(fabsf(x) * y); };
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            top[i] = __vimax3_s32(top[i], times(v[0][i], f[0]), times(v[1][i], f[1]));
+            sum[i] += v[0][i];
+            sum[i] += v[1][i];
+        }
+        if (kRows) {
+#pragma unroll
+            for (int u = 0; u < kPair; ++u) {
+                int m = 0;
+#pragma unroll
+                for (int i = 0; i < kN; i += 2) m = __vimax3_s32(m, times(v[u][i], w[i]), times(v[u][i + 1], w[i + 1]));
+                const uint32_t t = lanes_top((uint32_t)m, lanes, nullptr);
+                const size_t row = begin + slot + (size_t)(j * kPair + u) * slots;
                 if (lane == 0 && row < end) a.row_tops[blockIdx.y * a.rows + row] = __uint_as_float(t);
             }
         }
     }
-    put_floats(tops_s[threadIdx.x], top);
-    put_floats(sums_s[threadIdx.x], sum);
-    __syncthreads();
-    if (slot == 0 && col < a.cols) {
-        for (int s = 1; s < slots; ++s) {
-            const int at = s * lanes + lane;
+    if constexpr (kWide) asm volatile("cp.async.wait_all;" ::: "memory");
+    // threads of the same columns meet
+    auto meet = [&](auto value, auto add) {
+        int *cells = reinterpret_cast<int *>(&ring[0][0]);
+        constexpr int kAtOnce = kRing * kPair * 4 < kN ? kRing * kPair * 4 : kN;
 #pragma unroll
-            for (int i = 0; i < kV; ++i) {
-                top[i] = max_abs(top[i], tops_s[at][i]);
-                sum[i] += sums_s[at][i];
-            }
+        for (int i0 = 0; i0 < kN; i0 += kAtOnce) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) cells[i * kThreads + threadIdx.x] = value(i0 + i);
+            __syncthreads();
+            if (slot == 0)
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                    for (int s = 1; s < slots; ++s) add(i0 + i, cells[i * kThreads + s * lanes + lane]);
         }
-        const size_t at = (size_t)blockIdx.x * a.col_pitch + col;
-        if (a.strip_tops) put_floats(a.strip_tops + at, top);
-        if (a.strip_sums) put_floats(a.strip_sums + at, sum);
+    };
+    if (a.strip_tops) {
+        meet([&](int i) { return top[i]; }, [&](int i, int v) { top[i] = max(top[i], v); });
+        float tops[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) tops[i] = __int_as_float(top[i]);
+        if (slot == 0) at.put_padded(a.strip_tops + blockIdx.x * a.col_pitch, tops);
+    }
+    if (a.strip_sums) {
+        meet([&](int i) { return __float_as_int(sum[i]); }, [&](int i, int v) { sum[i] += __int_as_float(v); });
+        if (slot == 0) at.put_padded(a.strip_sums + blockIdx.x * a.col_pitch, sum);
     }
 }
 
@@ -322,89 +385,74 @@ __global__ void __launch_bounds__(kJoinThreads) lin_join_looks_kernel(const __gr
     }
 }
 
-// The second look.  Block (x, y): `range` rows from x * range on, `lanes` vectors of columns.  kFold: what the parts left is put together here, column by
+// The second look.  Block (x, y): `range` rows from x * range on, group y of the columns.  kFold: what the parts left is put together here, column by
 // column and row by row, by every thread that needs it.
-template <int kType, int kV, bool kRows, bool kFold>
-__global__ void __launch_bounds__(kThreads) lin_codes_kernel(const __grid_constant__ LinErrorArgs a, const int lanes, const size_t range)
+template <int kType, bool kWide, bool kRows, bool kFold>
+__global__ void __launch_bounds__(kThreads, 3) lin_codes_kernel(const __grid_constant__ LinErrorArgs a, const int lanes, const size_t range)
 {
-    constexpr int kE = Elem<kType>::kSize;
+    using S = Span<kType, kWide>;
+    constexpr int kN = S::kN;
     ptx::grid_dep_wait_launch_small();
-    const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes, col = (blockIdx.y * lanes + lane) * kV;
+    const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes;
+    const S at(blockIdx.y, lane, lanes, a.cols);
     const size_t begin = (size_t)blockIdx.x * range, end = min(a.rows, begin + range);
-    if (col >= a.cols) return;
-    const char *src = reinterpret_cast<const char *>(a.src) + (begin + slot) * a.stride * kE;
-    const size_t step = slots * a.stride * kE;
-    Raw<kV * kE> next[kAhead];
-    float next_f[kAhead], next_per[kAhead];
-    auto fetch = [&](size_t row0) {
+    if (!at.any()) return;
+    const char *src = reinterpret_cast<const char *>(a.src) + (begin + slot) * a.stride * S::kE;
+    const size_t step = slots * a.stride * S::kE;
+    float w[kN], per[kN];
+    if (kRows) at.get_exact(a.factors, w);
+    if (kFold) {
+        float top[kN] = {};
+#pragma unroll 4
+        for (int s = 0; s < a.strips; ++s) {
+            float t[kN];
+            at.get_padded(a.strip_tops + s * a.col_pitch, t);
+#pragma unroll
+            for (int i = 0; i < kN; ++i) top[i] = max_abs(top[i], t[i]);
+        }
+        const bool writes = blockIdx.x == 0 && slot == 0;
+        if (writes && a.strip_sums) {
+            float sum[kN] = {};
+#pragma unroll 4
+            for (int s = 0; s < a.strips; ++s) {
+                float t[kN];
+                at.get_padded(a.strip_sums + s * a.col_pitch, t);
+#pragma unroll
+                for (int i = 0; i < kN; ++i) sum[i] += t[i];
+            }
+            at.put_exact(a.sums, sum);
+        }
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            if (writes && at.column(i) < a.cols) finish_top(top[i], a.col_scales + at.column(i), a.dev);
+            per[i] = finite_top(top[i]) ? row_per_of(top[i]) : 0.0f;
+        }
+    } else {
+        at.get_padded(a.col_per, per);
+    }
+    for (size_t row0 = begin + slot; row0 < end; row0 += kAhead * slots, src += kAhead * step) {
+        Raw<16> raw[kAhead];
+        float f[kAhead], row_per[kAhead] = {};
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const size_t row = row0 + u * slots;
             const bool mine = row < end;
-            next[u] = get_raw<kType, kV>(src + u * step, col, a.cols, mine);
-            next_f[u] = mine ? __ldg(a.row_factors + row) : 0.0f;
-            if (kRows && !kFold) next_per[u] = mine ? __ldg(a.row_per + row) : 0.0f;
-            if (kRows && kFold) {
-                next_per[u] = 0.0f;
-                if (mine)
-                    for (int c = 0; c < a.chunks; ++c) next_per[u] = max_abs(next_per[u], __ldg(a.row_tops + c * a.rows + row));
-            }
+            raw[u] = at.get(src + u * step, mine);
+            f[u] = mine ? __ldg(a.row_factors + row) : 0.0f;
+            if (kRows && !kFold) row_per[u] = mine ? __ldg(a.row_per + row) : 0.0f;
+            if (kRows && kFold && mine)
+                for (int c = 0; c < a.chunks; ++c) row_per[u] = max_abs(row_per[u], __ldg(a.row_tops + c * a.rows + row));
         }
-        src += kAhead * step;
-    };
-    fetch(begin + slot);
-    float w[kV], per[kV];
-    if (kRows) get_factors(a.factors, col, a.cols, w);
-    if (kFold) {
-        float top[kV] = {}, sum[kV] = {};
-#pragma unroll 4
-        for (int s = 0; s < a.strips; ++s) {
-            float t[kV];
-            get_floats(a.strip_tops + (size_t)s * a.col_pitch + col, t);
-#pragma unroll
-            for (int i = 0; i < kV; ++i) top[i] = max_abs(top[i], t[i]);
-        }
-        const bool writes = blockIdx.x == 0 && slot == 0;
-        if (writes && a.strip_sums) {
-#pragma unroll 4
-            for (int s = 0; s < a.strips; ++s) {
-                float t[kV];
-                get_floats(a.strip_sums + (size_t)s * a.col_pitch + col, t);
-#pragma unroll
-                for (int i = 0; i < kV; ++i) sum[i] += t[i];
-            }
-#pragma unroll
-            for (int i = 0; i < kV; ++i)
-                if (col + i < a.cols) a.sums[col + i] = sum[i];
-        }
-#pragma unroll
-        for (int i = 0; i < kV; ++i) {
-            if (writes && col + i < a.cols) finish_top(top[i], a.col_scales + col + i, a.dev);
-            per[i] = finite_top(top[i]) ? row_per_of(top[i]) : 0.0f;
-        }
-    } else {
-        get_floats(a.col_per + col, per);
-    }
-    for (size_t row0 = begin + slot; row0 < end; row0 += kAhead * slots) {
-        Raw<kV * kE> held[kAhead];
-        float f[kAhead], row_per[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            held[u] = next[u];
-            f[u] = next_f[u];
-            row_per[u] = next_per[u];
-        }
-        fetch(row0 + kAhead * slots);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const size_t row = row0 + u * slots;
             if (row >= end) break;
-            float v[kV];
-            Elem<kType>::to_f32(held[u], v);
-            uint32_t q[kV];
+            float v[kN];
+            uint32_t q[kN];
+            Elem<kType>::to_f32(raw[u], v);
 #pragma unroll
-            for (int i = 0; i < kV; ++i) q[i] = row_code(v[i] * f[u], per[i]);
-            store_raw(a.col_codes + row * a.pitch + col, pack_codes(q));
+            for (int i = 0; i < kN; ++i) q[i] = row_code(v[i] * f[u], per[i]);
+            at.put_codes(a.col_codes + row * a.pitch, q);
             if (kRows) {
                 if (kFold) {
                     const float t = row_per[u];
@@ -412,18 +460,11 @@ __global__ void __launch_bounds__(kThreads) lin_codes_kernel(const __grid_consta
                     if (blockIdx.y == 0 && lane == 0) finish_top(t, a.scales + row, a.dev);
                 }
 #pragma unroll
-                for (int i = 0; i < kV; ++i) q[i] = row_code(v[i] * w[i], row_per[u]);
-                store_raw(a.codes + row * a.pitch + col, pack_codes(q));
+                for (int i = 0; i < kN; ++i) q[i] = row_code(v[i] * w[i], row_per[u]);
+                at.put_codes(a.codes + row * a.pitch, q);
             }
         }
     }
-}
-
-// elements of the widest vectors that every row begins and ends pieces of
-int vector_of(const void *src, size_t stride, int e)
-{
-    const size_t at = reinterpret_cast<uintptr_t>(src) | stride * e;
-    return at % 16 == 0 ? 16 / e : e == 2 && at % 4 == 0 ? 2 : 1;
 }
 
 // the power of two of lanes that hold `vectors`, `hold` each
@@ -434,36 +475,37 @@ int lanes_of(int vectors, int hold)
     return lanes;
 }
 
-template <int kType, int kV, int kHold, int kRows>
+template <int kType, bool kWide, int kHold, int kRows>
 cudaError_t launch_rows(const LinCodeArgs &a, int vectors, cudaStream_t st)
 {
     const int lanes = lanes_of(vectors, kHold);
     const size_t at_once = (size_t)kThreads / lanes * kRows;
-    return launch_chained(lin_rows_kernel<kType, kV, kHold, kRows>, dim3((unsigned)((a.rows + at_once - 1) / at_once)), dim3(kThreads), 0, st, a, lanes);
+    return launch_chained(lin_rows_kernel<kType, kWide, kHold, kRows>, dim3((unsigned)((a.rows + at_once - 1) / at_once)), dim3(kThreads), 0, st, a, lanes);
 }
 
 // 64 bytes a thread in flight (128 for the longest rows), of one row or of four; rows that leave SMs without a block are spread over more threads.
-template <int kType, int kV>
+template <int kType, bool kWide>
 cudaError_t rows_of(const LinCodeArgs &a, cudaStream_t st)
 {
-    const int vectors = (a.cols + kV - 1) / kV;
+    const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
     const bool few = a.rows * vectors < (size_t)kPartSms * kThreads * 4;
-    if (vectors > 4 * kThreads) return launch_rows<kType, kV, 8, 1>(a, vectors, st);
-    if (few && vectors <= kThreads) return launch_rows<kType, kV, 1, 1>(a, vectors, st);
-    if (vectors <= 32) return launch_rows<kType, kV, 1, 4>(a, vectors, st);
-    if (vectors <= 64) return launch_rows<kType, kV, 2, 2>(a, vectors, st);
-    return launch_rows<kType, kV, 4, 1>(a, vectors, st);
+    if (vectors > 4 * kThreads) return launch_rows<kType, kWide, 8, 1>(a, vectors, st);
+    if (few && vectors <= kThreads) return launch_rows<kType, kWide, 1, 1>(a, vectors, st);
+    if (vectors <= 32) return launch_rows<kType, kWide, 1, 4>(a, vectors, st);
+    if (vectors <= 64) return launch_rows<kType, kWide, 2, 2>(a, vectors, st);
+    return launch_rows<kType, kWide, 4, 1>(a, vectors, st);
 }
 
-template <int kType, int kV, bool kRows>
-cudaError_t looks_of(LinErrorArgs a, int vectors, int *launches, cudaStream_t st)
+template <int kType, bool kWide, bool kRows>
+cudaError_t looks_of(LinErrorArgs a, int *launches, cudaStream_t st)
 {
+    const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
     const int lanes = vectors < 32 ? lanes_of(vectors, 1) : 32, across = (vectors + lanes - 1) / lanes, slots = kThreads / lanes;
     a.chunks = across;
     ++*launches;
-    cudaError_t e = launch_chained(lin_look_kernel<kType, kV, kRows>, dim3((unsigned)a.strips, across), dim3(kThreads), 0, st, a, lanes);
+    cudaError_t e = launch_chained(lin_look_kernel<kType, kWide, kRows>, dim3((unsigned)a.strips, across), dim3(kThreads), 0, st, a, lanes);
     if (e != cudaSuccess) return e;
-    const bool fold = a.strip_tops && a.strips <= kFoldStrips && across <= kFoldStrips;
+    const bool fold = a.strip_tops && a.strips <= kFoldStrips && a.rows * a.cols <= kFoldSize;
     if (!fold) {
         const size_t rows = kRows ? (a.rows + kJoinThreads - 1) / kJoinThreads : 0;
         ++*launches;
@@ -475,19 +517,18 @@ cudaError_t looks_of(LinErrorArgs a, int vectors, int *launches, cudaStream_t st
     while (range > (size_t)slots && (a.rows + range - 1) / range * across < 4 * kPartSms) range /= 2;
     const dim3 grid((unsigned)((a.rows + range - 1) / range), across);
     ++*launches;
-    if (fold) return launch_chained(lin_codes_kernel<kType, kV, kRows, true>, grid, dim3(kThreads), 0, st, a, lanes, range);
-    return launch_chained(lin_codes_kernel<kType, kV, kRows, false>, grid, dim3(kThreads), 0, st, a, lanes, range);
+    if (fold) return launch_chained(lin_codes_kernel<kType, kWide, kRows, true>, grid, dim3(kThreads), 0, st, a, lanes, range);
+    return launch_chained(lin_codes_kernel<kType, kWide, kRows, false>, grid, dim3(kThreads), 0, st, a, lanes, range);
 }
 
-template <int kType, int kV>
+template <int kType, bool kWide>
 cudaError_t errors_of(LinErrorArgs a, int *launches, cudaStream_t st)
 {
-    const int vectors = (a.cols + kV - 1) / kV;
-    const LinStrips s = lin_strips(a.rows, a.cols);
+    const LinStrips s = lin_strips(a.rows, a.cols, kType);
     a.strip = s.rows;
     a.strips = (int)((a.rows + s.rows - 1) / s.rows);
     a.col_pitch = s.col_pitch;
-    if (a.codes && a.strip_tops) return looks_of<kType, kV, true>(a, vectors, launches, st);
+    if (a.codes && a.strip_tops) return looks_of<kType, kWide, true>(a, launches, st);
     if (a.codes) {
         LinCodeArgs r = {};
         r.src = a.src;
@@ -500,43 +541,43 @@ cudaError_t errors_of(LinErrorArgs a, int *launches, cudaStream_t st)
         r.scales = a.scales;
         r.dev = a.dev;
         ++*launches;
-        const cudaError_t e = rows_of<kType, kV>(r, st);
+        const cudaError_t e = rows_of<kType, kWide>(r, st);
         if (e != cudaSuccess) return e;
     }
-    return a.strip_tops || a.strip_sums ? looks_of<kType, kV, false>(a, vectors, launches, st) : cudaSuccess;
+    return a.strip_tops || a.strip_sums ? looks_of<kType, kWide, false>(a, launches, st) : cudaSuccess;
 }
 
 template <int kType, typename F>
-cudaError_t with_vectors(const void *src, size_t stride, F &&f)
+cudaError_t with_width(const void *src, size_t stride, F &&f)
 {
-    constexpr int kWide = 16 / Elem<kType>::kSize;
-    const int v = vector_of(src, stride, Elem<kType>::kSize);
-    if (v == kWide) return f(std::integral_constant<int, kType>(), std::integral_constant<int, kWide>());
-    if constexpr (kWide == 8)
-        if (v == 2) return f(std::integral_constant<int, kType>(), std::integral_constant<int, 2>());
-    return f(std::integral_constant<int, kType>(), std::integral_constant<int, 1>());
+    const size_t at = reinterpret_cast<uintptr_t>(src) | stride * Elem<kType>::kSize;
+    if (at % 16 == 0) return f(std::integral_constant<int, kType>(), std::true_type());
+    return f(std::integral_constant<int, kType>(), std::false_type());
 }
 template <typename F>
 cudaError_t with_type(const void *src, size_t stride, int dtype, F &&f)
 {
-    if (dtype == EOQ_F32) return with_vectors<EOQ_F32>(src, stride, f);
-    if (dtype == EOQ_F16) return with_vectors<EOQ_F16>(src, stride, f);
-    return with_vectors<EOQ_BF16>(src, stride, f);
+    if (dtype == EOQ_F32) return with_width<EOQ_F32>(src, stride, f);
+    if (dtype == EOQ_F16) return with_width<EOQ_F16>(src, stride, f);
+    return with_width<EOQ_BF16>(src, stride, f);
 }
 
 }  // namespace
 
-// Strips of rows: some eight blocks of 256 columns for each SM, of at least eight rows; at most 512, so that what they leave stays small beside the tensor.
-LinStrips lin_strips(size_t rows, int cols)
+// Strips of rows: as many as let every block run at once, three on an SM, of at least eight rows; at most 512, so that what they leave stays small beside the tensor.
+LinStrips lin_strips(size_t rows, int cols, int dtype)
 {
-    size_t strips = (8 * kPartSms + (cols + 255) / 256 - 1) / ((cols + 255) / 256);
+    const int wide = dtype == EOQ_F32 ? 128 : 256;   // columns of a block
+    const size_t chunks = (cols + wide - 1) / wide;
+    size_t strips = 3 * kPartSms / chunks;
+    if (strips < 1) strips = 1;
     if (strips > 512) strips = 512;
     LinStrips s;
     s.rows = (rows + strips - 1) / strips;
     if (s.rows < 8) s.rows = 8;
     s.col_pitch = ((size_t)cols + 7) & ~(size_t)7;
     s.floats = (rows + s.rows - 1) / s.rows * s.col_pitch;
-    s.row_floats = rows * ((cols + 31) / 32);   // (of the narrowest vectors: chunks of 32 columns)
+    s.row_floats = rows * chunks;
     return s;
 }
 
