@@ -2710,7 +2710,7 @@ static int grad_check(int num, const void *const *g, void *const *out, const siz
         if (sizes[i] == 0) continue;
         if (!g[i] || (out && !out[i])) return EOQ_ERR_BAD_ARG;
         if (sizes[i] > (size_t)1 << 40) return EOQ_ERR_UNSUPPORTED;
-        pieces += (sizes[i] + kGradPiece - 1) / kGradPiece;
+        pieces += sizes[i] / kGradPiece + 2;
         odd = odd || !aligned_to(g[i], dtype_size(dtypes[i])) || (out && !aligned_to(out[i], dtype_size(dtypes[i])));
     }
     if (pieces > (size_t)1 << 31) return EOQ_ERR_UNSUPPORTED;

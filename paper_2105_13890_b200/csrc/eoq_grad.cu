@@ -1,26 +1,56 @@
 // Norm of the gradients of a step, of many tensors together, and their clipping (eoq_grad_norm, eoq_grad_clip):
 //   norm = sqrt(sum of squares over all elements),  g <- g * min(1, max_norm / norm).
 //
-// Bound: memory, or the launches where the gradients are few.  The tensors are cut into pieces of kPiece elements, dealt out to blocks in turn; a block's squares
-// are added in 64 bits (no overflow, no digits lost over long sums) in an order that depends on the sizes and alignments alone, the blocks' sums by the block that comes last.
+// Bound: memory, or the launches where the gradients are few.  The tensors are cut into pieces, dealt out to blocks in turn; the squares of 16 bytes are added in
+// 32 bits and these sums in 64, in an order that depends on the sizes and alignments alone, the blocks' sums by the block that comes last.  (Every square in 64 bits:
+// the conversions hold the kernel at 1.5 T elements a second, 133 us for 200 M of two types.)  A thread has 64 bytes on their way before it uses the first: with load
+// and store in turn, that many took 240 us to scale instead of 179.
 #include "eoq_block8.cuh"
 
 namespace eoq {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kFlight = 4;        // vectors of a thread in flight
+constexpr unsigned kAddBlocks = 6 * kPartSms, kScaleBlocks = 4 * kPartSms;   // of a launch, all at once on the part; the order of the sums depends on the sizes alone
+constexpr int kFewTensors = 128, kMostTensors = 1024, kRanges = 512;
 
-// the tensor that holds piece `p`
-__device__ __forceinline__ int tensor_of(const GradBatch &b, unsigned p)
+template <int kTensors>
+struct GradBatch {                     // a launch's tensors
+    const void *in[kTensors];
+    void *out[kTensors];
+    unsigned long long size[kTensors];
+    unsigned first[kTensors];          // pieces of the tensors before
+    uint8_t dtype[kTensors];
+    uint16_t start[kRanges];           // tensor of the first piece of every range of 2^shift pieces
+    unsigned pieces;
+    int num, shift;
+};
+
+// What the launches of a call share.
+struct GradSums {
+    double *sums;                      // a block's sum of squares each, of all launches
+    int before;                        // blocks of the launches before this one
+    bool last;                         // this one is the last of a norm without clipping, which adds them
+    float *norm;
+    DeviceState *dev;
+};
+
+// Elements of a piece: what the threads of a block have in flight.  Pieces begin at multiples of 16 bytes: a tensor's first one has `skew` elements less.
+__host__ __device__ inline unsigned piece_of(int dtype) { return kFlight * kThreads * (dtype == EOQ_F32 ? 4 : 8); }
+__host__ __device__ inline unsigned skew_of(const void *p, int dtype) { return (unsigned)(reinterpret_cast<uintptr_t>(p) % 16) / (dtype == EOQ_F32 ? 4 : 2); }
+
+// f(tensor, place of a piece in it) for the block's pieces, every gridDim.x-th one, forwards or backwards.  The tensor is looked up in a table of the pieces' ranges and
+// then among the few that share one: parameters are read one at a time, and a search by halves waits for ten such reads one after the other.
+template <bool kBack, int kTensors, typename F>
+__device__ __forceinline__ void for_pieces(const GradBatch<kTensors> &b, F &&f)
 {
-    int lo = 0, hi = b.num - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (b.first[mid] <= p) lo = mid;
-        else hi = mid - 1;
+    for (unsigned k = blockIdx.x; k < b.pieces; k += gridDim.x) {
+        const unsigned p = kBack ? b.pieces - 1 - k : k;
+        int t = b.start[p >> b.shift];
+        while (t + 1 < b.num && b.first[t + 1] <= p) ++t;
+        f(t, p - b.first[t]);
     }
-    return lo;
 }
 
 template <typename F>
@@ -31,6 +61,7 @@ __device__ __forceinline__ void with_type(int dtype, F &&f)
     else f(Elem<EOQ_BF16>());
 }
 
+// sum over the block, in every thread
 __device__ __forceinline__ double block_sum(double v)
 {
     __shared__ double sum_s[kThreads / 32];
@@ -40,161 +71,239 @@ __device__ __forceinline__ double block_sum(double v)
     if (threadIdx.x % 32 == 0) sum_s[threadIdx.x / 32] = v;
     __syncthreads();
     v = sum_s[0];
+#pragma unroll
     for (int w = 1; w < kThreads / 32; ++w) v += sum_s[w];
     return v;
 }
 
-// Of elements [0, n) at p: the first ones up to a 16-byte boundary and the last ones behind one go one at a time, the others 16 bytes at a time.
+// The squares of 16 bytes in fp32: off by 5 * 2^-24 of their sum at most, as long as that is a good one.
 template <typename E>
-__device__ __forceinline__ int head_of(const void *p, int n)
+__device__ __forceinline__ float squares(const Raw<16> &r)
 {
-    return min(n, (int)((16 - reinterpret_cast<uintptr_t>(p) % 16) % 16) / E::kSize);
+    constexpr int kV = 16 / E::kSize;
+    float v[kV];
+    E::to_f32(r, v);
+    float even = v[0] * v[0], odd = v[1] * v[1];
+#pragma unroll
+    for (int j = 2; j < kV; j += 2) {
+        even = __fmaf_rn(v[j], v[j], even);
+        odd = __fmaf_rn(v[j + 1], v[j + 1], odd);
+    }
+    return even + odd;
+}
+// Neither so small that squares may have been lost among the smallest numbers (2^-123 of 2^-76 together, above that) nor too large for fp32, infinite or NaN; those
+// are added in 64 bits.
+__device__ __forceinline__ bool good_sum(float s) { return s >= 0x1p-76f && s <= 0x1p126f; }
+template <typename E>
+__device__ __noinline__ double wide_squares(Raw<16> r)
+{
+    constexpr int kV = 16 / E::kSize;
+    float v[kV];
+    E::to_f32(r, v);
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < kV; ++j) sum += (double)v[j] * v[j];
+    return sum;
 }
 
-__global__ void __launch_bounds__(kThreads) grad_squares_kernel(const __grid_constant__ GradBatch b)
+// This thread's vectors of piece `k` of a tensor of n elements: f(vectors, bytes from `p` to the first, whether they are a whole piece's or the first alone counts); of those whose
+// elements are not all the tensor's, g(element).
+template <typename E, typename F, typename G>
+__device__ __forceinline__ void piece_vectors(const char *p, unsigned long long n, unsigned skew, unsigned k, F &&f, G &&g)
 {
+    constexpr int kV = 16 / E::kSize;
+    const long long begin = (long long)k * kFlight * kThreads * kV - skew;   // (of the piece, in elements)
+    const char *at = p + begin * E::kSize + threadIdx.x * 16;
+    Raw<16> r[kFlight];
+    if (begin >= 0 && begin + kFlight * kThreads * kV <= (long long)n) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) r[u] = *reinterpret_cast<const Raw<16> *>(at + u * kThreads * 16);
+        f(r, at - p, true);
+        return;
+    }
+#pragma unroll 1
+    for (int u = 0; u < kFlight; ++u) {
+        const long long e = begin + (long long)(u * kThreads + threadIdx.x) * kV;
+        if (e >= 0 && e + kV <= (long long)n) {
+            r[0] = *reinterpret_cast<const Raw<16> *>(at + u * kThreads * 16);
+            f(r, at + u * kThreads * 16 - p, false);
+        } else {
+            for (long long i = e < 0 ? 0 : e; i < e + kV && i < (long long)n; ++i) g(i);
+        }
+    }
+}
+
+// root of the sum of the blocks' sums, in every thread
+__device__ __forceinline__ double whole_norm(const double *sums, int blocks)
+{
+    double v[4] = {};
+    for (int i = threadIdx.x; i < blocks; i += 4 * kThreads)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * kThreads < blocks) v[u] += __ldcg(sums + i + u * kThreads);
+    return sqrt(block_sum((v[0] + v[1]) + (v[2] + v[3])));
+}
+__device__ __forceinline__ void write_norm(double whole, float *norm, DeviceState *dev)
+{
+    if (threadIdx.x != 0) return;
+    *norm = (float)whole;
+    if (!(whole <= 3.402823466e38)) atomicOr(&dev->status, EOQ_DEV_NONFINITE);
+}
+
+template <int kTensors>
+__global__ void __launch_bounds__(kThreads, 6) grad_squares_kernel(const __grid_constant__ GradBatch<kTensors> b, const GradSums s)
+{
+    __shared__ bool last_s;
     ptx::grid_dep_wait_launch_small();
     double sum = 0.0;
-    for (unsigned p = blockIdx.x; p < b.pieces; p += gridDim.x) {
-        const int t = tensor_of(b, p);
-        const size_t at = (size_t)(p - b.first[t]) * kGradPiece;
-        const int n = (int)min((unsigned long long)kGradPiece, (unsigned long long)(b.size[t] - at));
+    for_pieces<false>(b, [&](int t, unsigned k) {
         with_type(b.dtype[t], [&](auto type) {
             using E = decltype(type);
-            constexpr int kV = 16 / E::kSize;
-            const char *src = reinterpret_cast<const char *>(b.in[t]) + at * E::kSize;
-            const int head = head_of<E>(src, n), body = (n - head) / kV;
-            auto one = [&](int i) {
-                float v[1];
-                E::to_f32(load_raw<E::kSize>(src + (size_t)i * E::kSize), v);
-                sum += (double)v[0] * v[0];
-            };
-            if ((int)threadIdx.x < head) one(threadIdx.x);
-            if ((int)threadIdx.x < n - head - body * kV) one(head + body * kV + threadIdx.x);
-#pragma unroll 4
-            for (int i = threadIdx.x; i < body; i += kThreads) {
-                float v[kV];
-                E::to_f32(load_raw<16>(src + ((size_t)head + (size_t)i * kV) * E::kSize), v);
+            const char *src = reinterpret_cast<const char *>(b.in[t]);
+            piece_vectors<E>(
+                src, b.size[t], skew_of(src, b.dtype[t]), k,
+                [&](const Raw<16> (&r)[kFlight], long long, bool whole) {
+                    float q[kFlight];
+                    bool good = true;
 #pragma unroll
-                for (int j = 0; j < kV; ++j) sum += (double)v[j] * v[j];
-            }
+                    for (int u = 0; u < kFlight; ++u)
+                        if (u == 0 || whole) good = good_sum(q[u] = squares<E>(r[u])) && good;
+#pragma unroll
+                    for (int u = 0; u < kFlight; ++u) {
+                        if (u > 0 && !whole) break;
+                        if (good) sum += (double)q[u];
+                        else if ((r[u].w.x | r[u].w.y | r[u].w.z | r[u].w.w) != 0) sum += wide_squares<E>(r[u]);
+                    }
+                },
+                [&](long long i) {
+                    float v[1];
+                    E::to_f32(load_raw<E::kSize>(src + i * E::kSize), v);
+                    sum += (double)v[0] * v[0];
+                });
         });
-    }
-    sum = block_sum(sum);
-    if (threadIdx.x == 0) b.sums[blockIdx.x] = sum;
-}
-
-__device__ __forceinline__ double whole_sum(const double *sums, int blocks)
-{
-    double s = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += kThreads) s += sums[i];
-    return block_sum(s);
-}
-
-__global__ void __launch_bounds__(kThreads) grad_norm_kernel(const double *sums, int blocks, float *norm, DeviceState *dev)
-{
-    ptx::grid_dep_wait_launch_small();
-    const double s = whole_sum(sums, blocks);
+    });
+    const double own = block_sum(sum);
     if (threadIdx.x == 0) {
-        const float n = (float)sqrt(s);
-        *norm = n;
-        if (!(n <= 3.402823466e38f)) atomicOr(&dev->status, EOQ_DEV_NONFINITE);
+        s.sums[s.before + blockIdx.x] = own;
+        __threadfence();
+        last_s = s.last && atomicInc(&s.dev->ticket, gridDim.x - 1) == gridDim.x - 1;   // (back to zero by itself)
     }
+    __syncthreads();
+    if (!last_s) return;
+    __threadfence();
+    write_norm(whole_norm(s.sums, s.before + gridDim.x), s.norm, s.dev);
 }
 
-__global__ void __launch_bounds__(kThreads) grad_scale_kernel(const __grid_constant__ GradBatch b, const double *sums, int blocks, float max_norm, float *norm, DeviceState *dev)
+// A block's pieces last to first: what the norm read last is still in the L2.
+template <int kTensors>
+__global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_constant__ GradBatch<kTensors> b, const GradSums s, float max_norm)
 {
     ptx::grid_dep_wait_launch_small();
-    const double whole = sqrt(whole_sum(sums, blocks));
-    const bool fine = whole <= 3.402823466e38;
-    if (blockIdx.x == 0 && threadIdx.x == 0 && norm) {
-        *norm = (float)whole;
-        if (!fine) atomicOr(&dev->status, EOQ_DEV_NONFINITE);
-    }
-    const float scale = fine && whole > max_norm ? (float)(max_norm / whole) : 1.0f;
-    for (unsigned p = blockIdx.x; p < b.pieces; p += gridDim.x) {
-        const int t = tensor_of(b, p);
-        if (b.in[t] == b.out[t] && scale == 1.0f) continue;
-        const size_t at = (size_t)(p - b.first[t]) * kGradPiece;
-        const int n = (int)min((unsigned long long)kGradPiece, (unsigned long long)(b.size[t] - at));
+    const double whole = whole_norm(s.sums, s.before);
+    if (blockIdx.x == 0 && s.last) write_norm(whole, s.norm, s.dev);
+    const float scale = whole <= 3.402823466e38 && whole > max_norm ? (float)(max_norm / whole) : 1.0f;
+    for_pieces<true>(b, [&](int t, unsigned k) {
+        if (b.in[t] == b.out[t] && scale == 1.0f) return;
         with_type(b.dtype[t], [&](auto type) {
             using E = decltype(type);
             constexpr int kV = 16 / E::kSize;
-            const char *src = reinterpret_cast<const char *>(b.in[t]) + at * E::kSize;
-            char *dst = reinterpret_cast<char *>(b.out[t]) + at * E::kSize;
-            const bool together = reinterpret_cast<uintptr_t>(src) % 16 == reinterpret_cast<uintptr_t>(dst) % 16;
-            const int head = together ? head_of<E>(src, n) : n, body = (n - head) / kV;
-            auto one = [&](int i) {
-                float v[1];
-                E::to_f32(*reinterpret_cast<const Raw<E::kSize> *>(src + (size_t)i * E::kSize), v);
-                v[0] *= scale;
-                store_raw(dst + (size_t)i * E::kSize, E::from_f32(v));
-            };
-            for (int i = threadIdx.x; i < head; i += kThreads) one(i);
-            for (int i = head + body * kV + threadIdx.x; i < n; i += kThreads) one(i);
-#pragma unroll 4
-            for (int i = threadIdx.x; i < body; i += kThreads) {
-                const size_t o = ((size_t)head + (size_t)i * kV) * E::kSize;
-                float v[kV];
-                E::to_f32(*reinterpret_cast<const Raw<16> *>(src + o), v);
+            const char *src = reinterpret_cast<const char *>(b.in[t]);
+            char *dst = reinterpret_cast<char *>(b.out[t]);
+            const unsigned skew = skew_of(src, b.dtype[t]);
+            const bool together = skew == skew_of(dst, b.dtype[t]);
+            piece_vectors<E>(
+                src, b.size[t], skew, k,
+                [&](const Raw<16> (&r)[kFlight], long long at, bool whole_piece) {
 #pragma unroll
-                for (int j = 0; j < kV; ++j) v[j] *= scale;
-                store_raw(dst + o, E::from_f32(v));
-            }
+                    for (int u = 0; u < kFlight; ++u) {
+                        if (u > 0 && !whole_piece) break;
+                        float v[kV];
+                        E::to_f32(r[u], v);
+#pragma unroll
+                        for (int j = 0; j < kV; ++j) v[j] *= scale;
+                        char *to = dst + at + u * kThreads * 16;
+                        const Raw<16> w = E::from_f32(v);
+                        if (together) {
+                            store_raw(to, w);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kV; ++j) {
+                                const float one[1] = {v[j]};
+                                store_raw(to + j * E::kSize, E::from_f32(one));
+                            }
+                        }
+                    }
+                },
+                [&](long long i) {
+                    float v[1];
+                    E::to_f32(*reinterpret_cast<const Raw<E::kSize> *>(src + i * E::kSize), v);
+                    v[0] *= scale;
+                    store_raw(dst + i * E::kSize, E::from_f32(v));
+                });
         });
+    });
+}
+
+// tensors [first, first + kTensors) as a launch takes them, those without elements left out; the blocks it takes
+template <int kTensors>
+unsigned batch_of(const GradList &l, int first, unsigned most, GradBatch<kTensors> &b)
+{
+    b.num = 0;
+    b.pieces = 0;
+    for (int i = first; i < l.num && i < first + kTensors; ++i) {
+        if (l.size[i] == 0) continue;
+        b.in[b.num] = l.in[i];
+        b.out[b.num] = l.out ? l.out[i] : const_cast<void *>(l.in[i]);
+        b.size[b.num] = l.size[i];
+        b.dtype[b.num] = (uint8_t)l.dtype[i];
+        b.first[b.num] = b.pieces;
+        b.pieces += (unsigned)((l.size[i] + skew_of(l.in[i], l.dtype[i]) + piece_of(l.dtype[i]) - 1) / piece_of(l.dtype[i]));
+        ++b.num;
     }
+    b.shift = 0;
+    while (b.pieces >> b.shift >= kRanges) ++b.shift;
+    for (unsigned r = 0, t = 0; r << b.shift < b.pieces; ++r) {
+        while ((int)t + 1 < b.num && b.first[t + 1] <= r << b.shift) ++t;
+        b.start[r] = (uint16_t)t;
+    }
+    return b.pieces == 0 ? 1 : b.pieces < most ? b.pieces : most;   // (a launch without elements has a block that adds nothing)
+}
+
+template <int kTensors>
+cudaError_t launch(const GradList &l, bool clip, float max_norm, float *norm, double *sums, DeviceState *dev, int *launches, cudaStream_t st)
+{
+    GradBatch<kTensors> b;
+    GradSums s = {sums, 0, false, norm, dev};
+    for (int first = 0; first < l.num; first += kTensors) {
+        const unsigned grid = batch_of(l, first, kAddBlocks, b);
+        s.last = !clip && l.num - first <= kTensors;
+        ++*launches;
+        const cudaError_t e = launch_chained(grad_squares_kernel<kTensors>, dim3(grid), dim3(kThreads), 0, st, b, s);
+        if (e != cudaSuccess) return e;
+        s.before += (int)grid;
+    }
+    if (!clip) return cudaSuccess;
+    for (int first = (l.num - 1) / kTensors * kTensors; first >= 0; first -= kTensors) {
+        const unsigned grid = batch_of(l, first, kScaleBlocks, b);
+        s.last = first == 0;   // (of several launches the last one writes the norm)
+        if (b.pieces == 0 && !s.last) continue;
+        ++*launches;
+        const cudaError_t e = launch_chained(grad_scale_kernel<kTensors>, dim3(grid), dim3(kThreads), 0, st, b, s, max_norm);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
 
-constexpr unsigned kMostBlocks = 4u * kPartSms;   // of a launch: the order of the sums depends on the sizes alone
+size_t grad_workspace_bytes(int num) { return sizeof(double) * kAddBlocks * (((size_t)num + kMostTensors - 1) / kMostTensors); }
 
-static size_t batches_of(int num) { return ((size_t)num + kGradTensors - 1) / kGradTensors; }
-size_t grad_workspace_bytes(int num) { return sizeof(double) * kMostBlocks * batches_of(num); }
-
+// (a launch's parameters are copied with it: short lists take the small form)
 cudaError_t launch_grad(const GradList &l, bool clip, float max_norm, float *norm, void *workspace, DeviceState *dev, int *launches, cudaStream_t st)
 {
     double *sums = reinterpret_cast<double *>(workspace);
-    int blocks = 0;
-    // tensors [first, first + kGradTensors) as a launch takes them; those without elements are left out
-    auto batch = [&](int first, GradBatch &b) {
-        b.num = 0;
-        b.pieces = 0;
-        for (int i = first; i < l.num && i < first + kGradTensors; ++i) {
-            if (l.size[i] == 0) continue;
-            b.in[b.num] = l.in[i];
-            b.out[b.num] = l.out ? l.out[i] : const_cast<void *>(l.in[i]);
-            b.size[b.num] = l.size[i];
-            b.dtype[b.num] = (uint8_t)l.dtype[i];
-            b.first[b.num] = b.pieces;
-            b.pieces += (unsigned)((l.size[i] + kGradPiece - 1) / kGradPiece);
-            ++b.num;
-        }
-        return b.pieces < kMostBlocks ? b.pieces : kMostBlocks;
-    };
-    GradBatch b;
-    for (int first = 0; first < l.num; first += kGradTensors) {
-        const unsigned grid = batch(first, b);
-        if (grid == 0) continue;
-        b.sums = sums + blocks;
-        ++*launches;
-        const cudaError_t e = launch_chained(grad_squares_kernel, dim3(grid), dim3(kThreads), 0, st, b);
-        if (e != cudaSuccess) return e;
-        blocks += (int)grid;
-    }
-    if (!clip) {
-        ++*launches;
-        return launch_chained(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, (const double *)sums, blocks, norm, dev);
-    }
-    for (int first = 0, done = 0; first < l.num || !done; first += kGradTensors, ++done) {
-        const unsigned grid = batch(first, b);
-        if (grid == 0 && done) continue;
-        ++*launches;
-        const cudaError_t e = launch_chained(grad_scale_kernel, dim3(grid ? grid : 1), dim3(kThreads), 0, st, b, (const double *)sums, blocks, max_norm,
-                                             done ? (float *)nullptr : norm, dev);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    if (l.num <= kFewTensors) return launch<kFewTensors>(l, clip, max_norm, norm, sums, dev, launches, st);
+    return launch<kMostTensors>(l, clip, max_norm, norm, sums, dev, launches, st);
 }
 
 }  // namespace eoq

@@ -609,17 +609,7 @@ cudaError_t launch_lin_gemm(LinGemmArgs a, int pass, const int8_t *pa, size_t pi
                             cudaStream_t st);
 
 // Norm and clipping of gradients (eoq_grad_*).
-constexpr int kGradTensors = 256, kGradPiece = 8192;   // tensors of a launch; elements of a piece
-struct GradBatch {                  // a launch's tensors
-    const void *in[kGradTensors];
-    void *out[kGradTensors];
-    unsigned long long size[kGradTensors];
-    unsigned first[kGradTensors];   // pieces of the tensors before
-    uint8_t dtype[kGradTensors];
-    double *sums;                   // a block's sum of squares each
-    unsigned pieces;
-    int num;
-};
+constexpr int kGradPiece = 4096;   // elements that a block takes at a time, at least
 struct GradList {                   // a call's, in host memory
     int num;
     const void *const *in;

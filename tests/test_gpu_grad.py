@@ -14,6 +14,9 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 TYPES = (torch.float32, torch.float16, torch.bfloat16)
 F32 = ref.HALF[torch.float32]
+# The squares of eight elements are added in fp32: four in a row in each of two chains, then both, 5 roundings of at most F32 of the sum; these sums in 64 bits.  A
+# root halves what the sum is off by, and its result is rounded to fp32: 2.5 + 1 roundings.
+SUM, NORM = 1.01 * 2.5 * F32, 1.01 * 3.5 * F32
 
 
 def tensors(sizes, seed=0, types=TYPES, spread=1.0):
@@ -53,7 +56,7 @@ def test_norm(sizes):
     ts = tensors(sizes)
     status_clear()
     got, want = float(call(ts)), norm_of(ts)
-    assert abs(got - want) <= 1.01 * F32 * want and status_clear() == 0
+    assert abs(got - want) <= NORM * want and status_clear() == 0
 
 
 @pytest.mark.parametrize("inside", [False, True])
@@ -69,27 +72,27 @@ def test_clip(sizes, limit, inside):
     ats = [rng.randrange(9) for _ in ts]
     out = None if inside else [r[a:a + t.numel()] for r, a, t in zip(room, ats, ts)]
     norm = float(call(ts, max_norm, out))
-    assert abs(norm - whole) <= 1.01 * F32 * whole
+    assert abs(norm - whole) <= NORM * whole
     factor = min(1.0, max_norm / whole)
     for b, t, o in zip(before, ts, ts if inside else out):
         want = b.double() * factor
         if factor == 1.0:
             assert torch.equal(o, b)
         else:
-            # the factor is an fp32 number, the product one, the output its type's
-            ref.near(o, want, 1.01 * (2 * F32 + ref.HALF[b.dtype]) * want.abs() + 2 * ref.LEAST[b.dtype])
+            # the factor is an fp32 number and as far off as the norm, the product one, the output its type's
+            ref.near(o, want, 1.01 * (SUM + 2 * F32 + ref.HALF[b.dtype]) * want.abs() + 2 * ref.LEAST[b.dtype])
         assert inside or torch.equal(t, b)
     if not inside:
         assert all(bool((r[:a] == 7).all() and (r[a + t.numel():] == 7).all()) for r, a, t in zip(room, ats, ts))
 
 
-@pytest.mark.parametrize("size", [1e-30, 1e-20, 1e18, 3e37])
+@pytest.mark.parametrize("size", [1e-36, 1e-30, 1e-20, 1e-12, 1e-11, 1e18, 1e19, 3e37])
 def test_sizes_of_gradients(size):
     """Squares of small and large gradients are numbers too."""
     for t in (torch.float32, torch.bfloat16):
         ts = [(torch.linspace(-1, 1, 100, device=DEV) * size).to(t), torch.full((3,), size, device=DEV).to(t)]
         want = norm_of(ts)
-        assert abs(float(call(ts)) - want) <= 1.01 * F32 * want
+        assert abs(float(call(ts)) - want) <= NORM * want
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38])
@@ -149,6 +152,6 @@ def test_a_step_of_two_layers():
     before = [g.clone() for g in grads]
     whole = norm_of(grads)
     norm = float(call(grads, 0.5))
-    assert abs(norm - whole) <= 1.01 * F32 * whole and whole > 0.5
+    assert abs(norm - whole) <= NORM * whole and whole > 0.5
     for g, p in zip(grads, before):
-        ref.near(g, p.double() * (0.5 / whole), 4 * F32 * p.double().abs() + 2.0 ** -149)
+        ref.near(g, p.double() * (0.5 / whole), (SUM + 4 * F32) * p.double().abs() + 2.0 ** -149)
