@@ -2593,11 +2593,12 @@ extern "C" int eoq_lin_fwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
     ProfScope prof(h, EOQ_PROF_OTHER, s);
     int launches = 0;
     cudaError_t err = cudaSuccess;
+    const bool few = lin_few_fits(d.rows, d.c_in), code_there = few && x && !x_codes;
     if (!x_codes) {
         x_codes = reinterpret_cast<int8_t *>(ws + space.row_codes);
         x_scales = reinterpret_cast<float *>(ws + space.row_scales);
     }
-    if (x) {
+    if (x && !code_there) {
         LinCodeArgs a = {};
         a.src = x;
         a.rows = d.rows;
@@ -2609,7 +2610,25 @@ extern "C" int eoq_lin_fwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
         a.dev = h->dev;
         err = launch_lin_rows(a, d.dtype, &launches, s);
     }
-    if (err == cudaSuccess) {
+    if (err == cudaSuccess && few) {
+        LinFewArgs f = {};
+        f.x = code_there ? x : nullptr;
+        f.x_stride = d.x_stride;
+        f.x_codes = x_codes;
+        f.x_scales = x_scales;
+        f.rows = (int)d.rows;
+        f.c_in = d.c_in;
+        f.c_out = d.c_out;
+        f.pitch = lin_pitch(d.c_in);
+        f.w_codes = w_codes;
+        f.w_scales = w_scales;
+        f.bias = bias;
+        f.y = y;
+        f.y_stride = d.y_stride;
+        f.dev = h->dev;
+        ++launches;
+        err = launch_lin_few(f, d.dtype, h->sm_count, s);
+    } else if (err == cudaSuccess) {
         LinGemmArgs g = {};
         g.m = (int)d.rows;
         g.n = d.c_out;

@@ -608,6 +608,23 @@ size_t lin_gemm_workspace_bytes(size_t m, size_t n, size_t k);
 cudaError_t launch_lin_gemm(LinGemmArgs a, int pass, const int8_t *pa, size_t pitch_a, const int8_t *pb, size_t pitch_b, size_t k, void *workspace, int *launches,
                             cudaStream_t st);
 
+// Forward pass for a few tokens.
+struct LinFewArgs {
+    const void *x;                  // coded in the kernel; null: x_codes and x_scales are the input
+    size_t x_stride;
+    const int8_t *x_codes;
+    const float *x_scales;
+    int rows, c_in, c_out;
+    size_t pitch;                   // bytes of a row of either codes
+    const int8_t *w_codes;
+    const float *w_scales, *bias;   // the last may be null
+    void *y;
+    size_t y_stride;
+    DeviceState *dev;
+};
+bool lin_few_fits(size_t rows, int c_in);
+cudaError_t launch_lin_few(const LinFewArgs &a, int dtype, int sm_count, cudaStream_t st);
+
 // Norm and clipping of gradients (eoq_grad_*).
 constexpr int kGradPiece = 4096;   // elements that a block takes at a time, at least
 struct GradList {                   // a call's, in host memory

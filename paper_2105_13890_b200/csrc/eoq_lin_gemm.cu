@@ -21,7 +21,7 @@ namespace {
 constexpr int kEpiWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 320;
 constexpr int kStageK = 128;                   // bytes of the reduction in a stage
 constexpr int kMaxSmem = 224 * 1024;           // of dynamic shared memory: some 2.3 KB are static
-constexpr int kStageBytes = 4096;              // staging of an epilogue warp: 32 rows of 128 bytes
+constexpr int kUnit = 2048, kStageBytes = 2 * kUnit;   // staging of an epilogue warp: twice 32 rows of 64 bytes, on their way out and being filled
 
 enum Major { kBothK = 0, kBMn = 1, kBothMn = 2 };
 
@@ -67,22 +67,29 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// 32 sums of a row with their scales and, rounded to the output's type, into the row's place of the warp's staging: pieces of 16 bytes in the order that
-// tensor copies expect of rows of 64 (16-bit types) or 128 bytes.  `scales`: of the 32 columns, and their biases 128 bytes on.
-__device__ __forceinline__ void stage_row(uint32_t (&r)[32], int type, float row_scale, uint32_t scales, uint32_t staged, int lane)
+// 32 sums of a row with their scales.  `scales`: of the 32 columns, and their biases 128 bytes on.
+__device__ __forceinline__ void scale_row(uint32_t (&r)[32], float row_scale, uint32_t scales)
 {
-    if (type != EOQ_I32) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const int4 s = ptx::ld_shared_128(scales + j * 4), b = ptx::ld_shared_128(scales + 128 + j * 4);
-            const int sv[4] = {s.x, s.y, s.z, s.w}, bv[4] = {b.x, b.y, b.z, b.w};
+    for (int j = 0; j < 32; j += 4) {
+        const int4 s = ptx::ld_shared_128(scales + j * 4), b = ptx::ld_shared_128(scales + 128 + j * 4);
+        const int sv[4] = {s.x, s.y, s.z, s.w}, bv[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                r[j + i] = __float_as_uint(__fmaf_rn(__int2float_rn((int)r[j + i]) * row_scale, __int_as_float(sv[i]), __int_as_float(bv[i])));
-        }
+        for (int i = 0; i < 4; ++i)
+            r[j + i] = __float_as_uint(__fmaf_rn(__int2float_rn((int)r[j + i]) * row_scale, __int_as_float(sv[i]), __int_as_float(bv[i])));
     }
+}
+
+// 64 bytes of a row to the lane's place in a unit of staging: pieces of 16 bytes in the order that tensor copies expect of such rows.
+__device__ __forceinline__ void stage_piece(uint32_t unit, int lane, int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    st_shared_v4(unit + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), a, b, c, d);
+}
+// kPart: which 16 of the 32 words (of 16-bit types: all of them, rounded)
+template <int kPart>
+__device__ __forceinline__ void stage_row(const uint32_t (&r)[32], int type, uint32_t unit, int lane)
+{
     if (type == EOQ_F16 || type == EOQ_BF16) {
-        const uint32_t row = staged + lane * 64;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t w[4];
@@ -97,31 +104,31 @@ __device__ __forceinline__ void stage_row(uint32_t (&r)[32], int type, float row
                     w[i] = *reinterpret_cast<const uint32_t *>(&h);
                 }
             }
-            st_shared_v4(row + ((j ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+            stage_piece(unit, lane, j, w[0], w[1], w[2], w[3]);
         }
     } else {
-        const uint32_t row = staged + lane * 128;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) st_shared_v4(row + ((j ^ (lane & 7)) << 4), r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+        for (int j = 0; j < 4; ++j) stage_piece(unit, lane, j, r[16 * kPart + 4 * j], r[16 * kPart + 4 * j + 1], r[16 * kPart + 4 * j + 2], r[16 * kPart + 4 * j + 3]);
     }
 }
 
-// The staged rows to rows of the output that tensor copies cannot address, a row at a time: a lane a column.
-__device__ __forceinline__ void store_rows(const LinGemmArgs &a, uint32_t staged, size_t out_row, int rows, int col0, int lane)
+// The staged rows to rows of the output that tensor copies cannot address: 32 columns of a row at a time, or 16 of two.
+__device__ __forceinline__ void store_rows(const LinGemmArgs &a, uint32_t unit, size_t out_row, int rows, int col0, int lane)
 {
-    const int col = col0 + lane;
-    const bool in = col < a.n;
     if (a.out_type == EOQ_F16 || a.out_type == EOQ_BF16) {
+        const int col = col0 + lane;
+        const bool in = col < a.n;
         for (int i = 0; i < rows; ++i) {
             uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staged + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(unit + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) : "memory");
             if (in) *reinterpret_cast<uint16_t *>(reinterpret_cast<char *>(a.out) + (out_row + i) * a.out_pitch + (size_t)col * 2) = v;
         }
     } else {
-        for (int i = 0; i < rows; ++i) {
+        const int c = lane & 15, col = col0 + c;
+        for (int i = lane >> 4; i < rows; i += 2) {
             uint32_t v;
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(staged + i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) : "memory");
-            if (in) *reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(a.out) + (out_row + i) * a.out_pitch + (size_t)col * 4) = v;
+            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(unit + i * 64 + (((c >> 2) ^ ((i >> 1) & 3)) << 4) + (c & 3) * 4) : "memory");
+            if (col < a.n) *reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(a.out) + (out_row + i) * a.out_pitch + (size_t)col * 4) = v;
         }
     }
 }
@@ -195,11 +202,14 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
             int m0, n0, split;
             place(u, m0, n0, split);
             const int n_own = n0 + rank * S::kOwnN, stages = stages_of(split), k_first = split * a.stages_per_split;
-            for (int it = 0; it < stages; ++it) {
+            // Blocks that work side by side begin at different places of the reduction (integer sums do not mind): in step, all of them asked for the same rows of a few
+            // tokens at once, and 16 tokens 4096 to 4096 took 16.8 us where 32 took 11.0.
+            int at = kPair ? 0 : (int)((unsigned)u % (unsigned)stages);
+            for (int it = 0; it < stages; ++it, at = at + 1 == stages ? 0 : at + 1) {
                 if (!(ok = __all_sync(0xffffffffu, wait_bar(empty_bar(slot), phase ^ 1u, ctx)))) break;
                 if (lane == 0) {
                     const uint32_t dst = smem_base + slot * S::kStage;
-                    const int k = (k_first + it) * kStageK;
+                    const int k = (k_first + at) * kStageK;
                     if (rank == 0) ptx::mbar_expect_tx(full_bar(slot), S::kBlocks * S::kStage);
                     if (kMajor == kBothMn) load_tile<kPair>(dst, &map_a, full_bar(slot), m0, k);
                     else load_tile<kPair>(dst, &map_a, full_bar(slot), k, m0);
@@ -258,58 +268,69 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;
-        constexpr int kHalfN = kN >= 64 ? kN / 2 : kN;                    // columns of a warp (of 32, the second four warps have none)
-        const int e = a.out_type == EOQ_F16 || a.out_type == EOQ_BF16 ? 2 : 4;
-        const uint32_t scales = ptx::smem_u32(&scales_s[warp][0]);
-        int turn = 0, staged = 0;
+        constexpr int kHalfN = kN >= 64 ? kN / 2 : kN, kChunks = kHalfN / 32;   // columns of a warp (of 32, the second four warps have none)
+        const bool narrow = a.out_type == EOQ_F16 || a.out_type == EOQ_BF16;
+        const uint32_t scales = ptx::smem_u32(&scales_s[warp][0]), staging_w = staging + warp * kStageBytes;
+        int turn = 0, units_out = 0;
         for (int u = first; u < units; u += step, ++turn) {
             int m0, n0, split;
             place(u, m0, n0, split);
-            const int acc = turn & 1, row0 = m0 + quad * 32, row = row0 + lane;
+            const int acc = turn & 1, row0 = m0 + quad * 32, row = row0 + lane, first_col = n0 + half * kHalfN;
             const bool mine = row0 < a.m && (kN >= 64 || half == 0);
-            float row_scale = 0.0f;
-            if (a.row_scale && row < a.m) row_scale = __ldg(a.row_scale + row);
+            // scales and biases of the tile arrive beside its MMAs
+            float row_scale = 0.0f, s[kChunks], b[kChunks];
+            if (a.out_type != EOQ_I32) {
+                row_scale = row < a.m ? __ldg(a.row_scale + row) : 0.0f;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const int col = first_col + c * 32 + lane;
+                    s[c] = mine && col < a.n ? a.col_scale ? __ldg(a.col_scale + col) : 1.0f : 0.0f;
+                    b[c] = mine && col < a.n && a.bias ? __ldg(a.bias + col) : 0.0f;
+                }
+            }
             if (!__all_sync(0xffffffffu, wait_bar<32>(sums_bar(acc), (turn >> 1) & 1, ctx))) break;
             ptx::tc_fence_after();
             const size_t out_row = (size_t)split * a.split_rows + row0;
-#pragma unroll 1
-            for (int c = 0; c < kHalfN; c += 32) {
-                const int col0 = n0 + half * kHalfN + c;
-                if (!mine || col0 >= a.n) break;
-                uint32_t r[32];
-                ptx::tmem_ld_32x32(tmem_base + acc * kN + half * kHalfN + c + ((uint32_t)(quad * 32) << 16), r);
-                if (a.out_type != EOQ_I32) {
-                    const int col = col0 + lane;
-                    const float s = col < a.n ? a.col_scale ? __ldg(a.col_scale + col) : 1.0f : 0.0f;
-                    const float b = col < a.n && a.bias ? __ldg(a.bias + col) : 0.0f;
-                    __syncwarp();
-                    scales_s[warp][lane] = s;
-                    scales_s[warp][32 + lane] = b;
-                    __syncwarp();
-                }
-                // 16-bit rows leave room for two of these
-                const uint32_t at = staging + warp * kStageBytes + (e == 2 ? (staged & 1) * 2048 : 0);
-                if (a.tensor_store) {
-                    if (lane == 0) {
-                        if (e == 2) store_wait_read<1>();
-                        else store_wait_read<0>();
-                    }
-                }
-                __syncwarp();
-                ptx::tmem_ld_wait();
-                stage_row(r, a.out_type, row_scale, scales, at, lane);
+            const uint32_t t_row = tmem_base + acc * kN + half * kHalfN + ((uint32_t)(quad * 32) << 16);
+            const int chunks = !mine || first_col >= a.n ? 0 : min(kChunks, (a.n - first_col + 31) / 32);
+            // a unit of staging to memory
+            auto out = [&](int col) {
+                const uint32_t unit = staging_w + (units_out & 1) * kUnit;
+                ++units_out;
                 if (a.tensor_store) {
                     ptx::fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) {
-                        store_tile_2d(&map_out, at, col0, (int)out_row);
+                        if (col < a.n) store_tile_2d(&map_out, unit, col, (int)out_row);
                         store_commit();
+                        store_wait_read<1>();   // (the other unit is free)
                     }
+                    __syncwarp();
                 } else {
                     __syncwarp();
-                    store_rows(a, at, out_row, min(32, a.m - row0), col0, lane);
+                    store_rows(a, unit, out_row, min(32, a.m - row0), col, lane);
+                    __syncwarp();
                 }
-                ++staged;
+            };
+            uint32_t r[2][32];
+            if (chunks > 0) ptx::tmem_ld_32x32(t_row, r[0]);
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                if (c >= chunks) break;
+                ptx::tmem_ld_wait();
+                if (c + 1 < chunks) ptx::tmem_ld_32x32(t_row + (c + 1) * 32, r[(c + 1) & 1]);   // (on its way beside this chunk's arithmetic)
+                if (a.out_type != EOQ_I32) {
+                    scales_s[warp][lane] = s[c];
+                    scales_s[warp][32 + lane] = b[c];
+                    __syncwarp();
+                    scale_row(r[c & 1], row_scale, scales);
+                }
+                stage_row<0>(r[c & 1], a.out_type, staging_w + (units_out & 1) * kUnit, lane);
+                out(first_col + c * 32);
+                if (!narrow) {
+                    stage_row<1>(r[c & 1], a.out_type, staging_w + (units_out & 1) * kUnit, lane);
+                    out(first_col + c * 32 + 16);
+                }
             }
             ptx::tc_fence_before();
             __syncwarp();
@@ -410,7 +431,7 @@ GemmPlan plan_of(size_t m, size_t n, size_t k)
             p.splits = (k_stages + p.stages_per_split - 1) / p.stages_per_split;
             const double waves = (double)((tiles * p.splits + room - 1) / room);
             double time = 6000.0 + waves * ((double)p.stages_per_split * kStage[w] + 8.0 * p.tile_n);
-            if (p.splits > 1) time += 4000.0 + (double)p.splits * m * n * 4.0 * 2.0 / 2500.0;
+            if (p.splits > 1) time += 7000.0 + (double)p.splits * m * n * 4.0 * 2.0 / 2500.0;
             if (best_time == 0.0 || time < best_time) {
                 best = p;
                 best_time = time;
@@ -432,7 +453,7 @@ cudaError_t launch(const LinGemmArgs &a, const void *pa, size_t pitch_a, const v
     if (!got) return cudaErrorInvalidValue;
     if (a.tensor_store) {
         const int e = a.out_type == EOQ_F16 || a.out_type == EOQ_BF16 ? 2 : 4;
-        if (!tiled_map_of(&mo, out, e, a.n, a.out_type == EOQ_I32 ? a.splits * a.split_rows : (size_t)a.m, a.out_pitch, 32, 32, 32 * e)) return cudaErrorInvalidValue;
+        if (!tiled_map_of(&mo, out, e, a.n, a.out_type == EOQ_I32 ? a.splits * a.split_rows : (size_t)a.m, a.out_pitch, 64 / e, 32, 64)) return cudaErrorInvalidValue;
     }
     static_assert(S::kBytes <= kMaxSmem && S::kStages >= 4, "shared memory of a block");
     static std::atomic<unsigned long long> allowed;

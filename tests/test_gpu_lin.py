@@ -121,6 +121,27 @@ def test_parts_of_wider_rows(rows, c_in, c_out, beside, offset, dtype):
     l.untouched()
 
 
+@pytest.mark.parametrize("dtype", list(TYPES), ids=str)
+@pytest.mark.parametrize("beside,offset", [(0, 0), (8, 8), (5, 3)])
+@pytest.mark.parametrize("rows", [1, 2, 3, 5, 8, 9, 12, 16, 17, 25, 32, 33])
+@pytest.mark.parametrize("c_in,c_out", [(16, 8), (63, 17), (64, 200), (130, 5000), (1000, 333), (4096, 64)])
+def test_few_tokens(rows, c_in, c_out, beside, offset, dtype):
+    """Coded by the call or beforehand: the same bits, whichever kernel does it."""
+    l = Layer(rows, c_in, c_out, dtype, c_in % 2 == 0, beside, offset)
+    l.code_weights()
+    l.w_codes[:, c_in:] = 99
+    l.forward(keep=False)
+    l.check_forward()
+    y = l.y.clone()
+    l.forward()
+    l.check_codes()
+    assert torch.equal(l.y, y)
+    l.x_codes[:, c_in:] = -5
+    eoq.eoq_lin_fwd(handle(), l.desc, None, l.x_codes, l.x_scales, l.w_codes, l.w_scales, l.bias, l.y, l.ws)
+    assert torch.equal(l.y, y)
+    l.untouched()
+
+
 @pytest.mark.parametrize("dtype,rows,c_in,c_out", [(torch.bfloat16, 2048, 1024, 1536), (torch.float16, 6272, 64, 256), (torch.float32, 1111, 2000, 999), (torch.bfloat16, 700, 8200, 300),
                                                    (torch.bfloat16, 6, 20000, 40), (torch.float32, 40, 9000, 70), (torch.float16, 257, 256, 6000)])
 def test_large(dtype, rows, c_in, c_out):
@@ -174,8 +195,15 @@ def test_rows_without_codes(rows, c_in, c_out):
     assert status_clear() == 0
     l.check_codes()
     l.x[rows - 1] = 1.0
-    l.forward()
+    for keep in (True, False):
+        l.forward(keep)
+        l.check_forward()
+    l.x[0, 3] = float("nan")
+    l.forward(keep=False)
+    assert status_clear() == eoq.EOQ_DEV_NONFINITE
     l.check_forward()
+    l.x[0, 3] = 0.0
+    l.forward()
     l.backward()
     assert status_clear() == eoq.EOQ_DEV_NONFINITE
     l.check_backward()
