@@ -2481,6 +2481,8 @@ extern "C" int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const 
 // ================================================================================= linear layers in 8-bit integers
 
 static size_t lin_pitch(size_t cols) { return (cols + 15) & ~(size_t)15; }
+// of codes in the workspace: rows that lie in as few lines of 128 bytes as they can, which tensor copies are charged by
+static size_t lin_line_pitch(size_t cols) { return cols > 64 ? (cols + 127) & ~(size_t)127 : cols > 32 ? 64 : cols > 16 ? 32 : 16; }
 
 // The descriptor of a call with its strides filled in.
 static int lin_check(const eoq_lin_desc_t *desc, eoq_lin_desc_t *d)
@@ -2502,6 +2504,27 @@ static int lin_check(const eoq_lin_desc_t *desc, eoq_lin_desc_t *d)
     return EOQ_OK;
 }
 
+// The products of a call, without addresses: forward, or backward with what is asked for.
+static LinGemmArgs lin_products(const eoq_lin_desc_t &d, bool forward, bool dx, bool dw)
+{
+    LinGemmArgs g = {};
+    auto add = [&](size_t m, size_t n, size_t k, size_t pitch_a, size_t pitch_b, bool a_mn, bool b_mn) {
+        LinProduct &p = g.p[g.count++];
+        p.m = (int)m;
+        p.n = (int)n;
+        p.k = k;
+        p.pitch_a = pitch_a;
+        p.pitch_b = pitch_b;
+        p.a_mn = a_mn;
+        p.b_mn = b_mn;
+    };
+    const size_t in = lin_pitch(d.c_in), errors = lin_line_pitch(d.c_out);
+    if (forward) add(d.rows, d.c_out, d.c_in, in, in, false, false);
+    if (dw) add(d.c_out, d.c_in, d.rows, errors, in, true, true);
+    if (dx) add(d.rows, d.c_in, d.c_out, errors, in, false, true);
+    return g;
+}
+
 // Places in the workspace of a call.
 struct LinSpace {
     size_t row_codes, row_scales, row_tops, row_per, col_codes, col_scales, col_per, strip_tops, strip_sums, parts, bytes;
@@ -2518,9 +2541,9 @@ static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
     if (which == EOQ_LIN_FWD) {
         s.row_codes = take(d.rows * lin_pitch(d.c_in));
         s.row_scales = take(d.rows * 4);
-        s.parts = take(lin_gemm_workspace_bytes(d.rows, d.c_out, d.c_in));
+        s.parts = take(lin_gemm_workspace_bytes(lin_products(d, true, false, false)));
     } else {
-        const size_t codes = d.rows * lin_pitch(d.c_out);
+        const size_t codes = d.rows * lin_line_pitch(d.c_out);
         const LinStrips l = lin_strips(d.rows, d.c_out, d.dtype);
         s.row_codes = take(codes);
         s.row_scales = take(d.rows * 4);
@@ -2531,8 +2554,13 @@ static LinSpace lin_space(const eoq_lin_desc_t &d, int which)
         s.strip_tops = take(l.floats * 4);
         s.strip_sums = take(l.floats * 4);
         s.row_tops = take(l.row_floats * 4);
-        const size_t dx = lin_gemm_workspace_bytes(d.rows, d.c_in, d.c_out), dw = lin_gemm_workspace_bytes(d.c_out, d.c_in, d.rows);
-        s.parts = take(dx > dw ? dx : dw);
+        // (each alone may be cut into more parts than the two together)
+        size_t parts = 0;
+        for (int k = 1; k < 4; ++k) {
+            const size_t bytes = lin_gemm_workspace_bytes(lin_products(d, false, (k & 1) != 0, (k & 2) != 0));
+            if (bytes > parts) parts = bytes;
+        }
+        s.parts = take(parts);
     }
     s.bytes = at;
     return s;
@@ -2629,18 +2657,19 @@ extern "C" int eoq_lin_fwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
         ++launches;
         err = launch_lin_few(f, d.dtype, h->sm_count, s);
     } else if (err == cudaSuccess) {
-        LinGemmArgs g = {};
-        g.m = (int)d.rows;
-        g.n = d.c_out;
-        g.row_scale = x_scales;
-        g.col_scale = w_scales;
-        g.bias = bias;
-        g.out = y;
-        g.out_pitch = d.y_stride * e;
-        g.out_type = d.dtype;
+        LinGemmArgs g = lin_products(d, true, false, false);
         g.sm_count = h->sm_count;
         g.dev = h->dev;
-        err = launch_lin_gemm(g, EOQ_PASS_FWD, x_codes, lin_pitch(d.c_in), w_codes, lin_pitch(d.c_in), d.c_in, ws + space.parts, &launches, s);
+        LinProduct &p = g.p[0];
+        p.a = x_codes;
+        p.b = w_codes;
+        p.row_scale = x_scales;
+        p.col_scale = w_scales;
+        p.bias = bias;
+        p.out = y;
+        p.out_pitch = d.y_stride * e;
+        p.out_type = d.dtype;
+        err = launch_lin_gemm(g, ws + space.parts, &launches, s);
     }
     count_launches(h, launches);
     return record(h, err);
@@ -2670,7 +2699,7 @@ extern "C" int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
     a.rows = d.rows;
     a.stride = d.dy_stride;
     a.cols = d.c_out;
-    a.pitch = lin_pitch(d.c_out);
+    a.pitch = lin_line_pitch(d.c_out);
     a.dev = h->dev;
     if (dx) {
         a.factors = w_scales;
@@ -2691,27 +2720,28 @@ extern "C" int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, cons
         a.strip_sums = reinterpret_cast<float *>(ws + space.strip_sums);
     }
     cudaError_t err = launch_lin_errors(a, d.dtype, &launches, s);
-    LinGemmArgs g = {};
+    LinGemmArgs g = lin_products(d, false, dx != nullptr, dw != nullptr);
     g.sm_count = h->sm_count;
     g.dev = h->dev;
-    if (err == cudaSuccess && dw) {
-        g.m = d.c_out;
-        g.n = d.c_in;
-        g.row_scale = a.col_scales;
-        g.out = dw;
-        g.out_pitch = (size_t)d.c_in * 4;
-        g.out_type = EOQ_F32;
-        err = launch_lin_gemm(g, EOQ_PASS_WGRAD, a.col_codes, a.pitch, x_codes, lin_pitch(d.c_in), d.rows, ws + space.parts, &launches, s);
+    if (dw) {
+        LinProduct &p = g.p[0];
+        p.a = a.col_codes;
+        p.b = x_codes;
+        p.row_scale = a.col_scales;
+        p.out = dw;
+        p.out_pitch = (size_t)d.c_in * 4;
+        p.out_type = EOQ_F32;
     }
-    if (err == cudaSuccess && dx) {
-        g.m = (int)d.rows;
-        g.n = d.c_in;
-        g.row_scale = a.scales;
-        g.out = dx;
-        g.out_pitch = d.dx_stride * e;
-        g.out_type = d.dtype;
-        err = launch_lin_gemm(g, EOQ_PASS_DGRAD, a.codes, a.pitch, w_codes, lin_pitch(d.c_in), d.c_out, ws + space.parts, &launches, s);
+    if (dx) {
+        LinProduct &p = g.p[g.count - 1];
+        p.a = a.codes;
+        p.b = w_codes;
+        p.row_scale = a.scales;
+        p.out = dx;
+        p.out_pitch = d.dx_stride * e;
+        p.out_type = d.dtype;
     }
+    if (err == cudaSuccess && g.count) err = launch_lin_gemm(g, ws + space.parts, &launches, s);
     count_launches(h, launches);
     return record(h, err);
 }

@@ -589,24 +589,34 @@ LinStrips lin_strips(size_t rows, int cols, int dtype);
 cudaError_t launch_lin_rows(const LinCodeArgs &a, int dtype, int *launches, cudaStream_t st);
 cudaError_t launch_lin_errors(const LinErrorArgs &a, int dtype, int *launches, cudaStream_t st);
 
-// out[m][n] = row_scale[m] col_scale[n] sum_k A B + bias[n]
-struct LinGemmArgs {
+// out[m][n] = row_scale[m] col_scale[n] sum_k A B + bias[n].  A is [m][k], or [k][m] where a_mn; B [n][k], or [k][n] where b_mn.
+struct LinProduct {
     int m, n;
+    size_t k;
+    const int8_t *a, *b;
+    size_t pitch_a, pitch_b;        // bytes from row to row, multiples of 16
+    bool a_mn, b_mn;
     const float *row_scale, *col_scale, *bias;   // the last two may be null
     void *out;
     size_t out_pitch;               // bytes
     int out_type;
+    // filled in by the launcher
+    int m_tiles, n_tiles, splits, k_stages, stages_per_split, units;
+    int split_rows;                 // rows from one part's sums to the next one's
+    int a_rows;                     // of A that a tile's copies bring in
+    bool tensor_store;              // the output goes out by tensor copies
+};
+struct LinGemmArgs {                // one launch: a product, or two that do not depend on one another
+    LinProduct p[2];
+    int count;
     int sm_count;
     DeviceState *dev;
     // filled in by the launcher
-    int m_tiles, n_tiles, splits, k_stages, stages_per_split;
-    int split_rows;                 // rows from one part's sums to the next one's
-    bool tensor_store, launch_early;
+    int catch_up, groups;
+    bool launch_early;
 };
-size_t lin_gemm_workspace_bytes(size_t m, size_t n, size_t k);
-// pass: EOQ_PASS_FWD (A [m][k], B [n][k]), EOQ_PASS_DGRAD (A [m][k], B [k][n]), EOQ_PASS_WGRAD (A [k][m], B [k][n]); pitches in bytes, multiples of 16
-cudaError_t launch_lin_gemm(LinGemmArgs a, int pass, const int8_t *pa, size_t pitch_a, const int8_t *pb, size_t pitch_b, size_t k, void *workspace, int *launches,
-                            cudaStream_t st);
+size_t lin_gemm_workspace_bytes(LinGemmArgs a);   // (sizes alone)
+cudaError_t launch_lin_gemm(LinGemmArgs a, void *workspace, int *launches, cudaStream_t st);
 
 // Forward pass for a few tokens.
 struct LinFewArgs {

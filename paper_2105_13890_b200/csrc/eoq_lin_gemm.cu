@@ -8,9 +8,10 @@
 // bits.  One product of scales and one addition per output remain: three roundings in fp32 and the one to the output's type.
 //
 // Bound: the tensor pipe (128 cycles for 128 x 256 x 32 a block) where tiles are full.  Persistent blocks walk tiles of 128 x kN, or pairs of blocks tiles of
-// 256 x 256 as one (each loads half of either operand: 64 bytes a cycle and SM instead of 96 for tiles of 128 x 256).  Roles: eight epilogue warps, a
-// warp for the tensor copies, one for the MMAs.  Two accumulators in tensor memory let a tile's epilogue run beside the next one's MMAs.
-// All waits are bounded.
+// 256 x 256 as one (each loads half of either operand: 64 bytes a cycle and SM instead of 96 for tiles of 128 x 256).  Roles: sixteen epilogue warps, a warp for the
+// tensor copies, one for the MMAs.  Accumulators in tensor memory, two of a pair, four otherwise, let tiles' epilogues run beside the next ones' MMAs: what an epilogue
+// takes is mostly waiting (for scales, tensor memory, stores), so that blocks with several tiles give them to two or four groups of warps in turn.  The two products of a
+// backward pass share a launch: alone, 64 and 256 tiles leave 74 pairs idle for an eighth of the time each.  All waits are bounded.
 #include "eoq_lin.cuh"
 #include "eoq_pair.cuh"
 
@@ -18,20 +19,20 @@ namespace eoq {
 
 namespace {
 
-constexpr int kEpiWarps = 8, kLoadWarp = 8, kMmaWarp = 9, kThreads = 320;
 constexpr int kStageK = 128;                   // bytes of the reduction in a stage
+constexpr int kUnit = 2048;                    // staging of an epilogue warp: 32 rows of 64 bytes
 constexpr int kMaxSmem = 224 * 1024;           // of dynamic shared memory: some 2.3 KB are static
-constexpr int kUnit = 2048, kStageBytes = 2 * kUnit;   // staging of an epilogue warp: twice 32 rows of 64 bytes, on their way out and being filled
-
-enum Major { kBothK = 0, kBMn = 1, kBothMn = 2 };
 
 template <int kN, bool kPair>
 struct GemmShape {
     static constexpr int kBlocks = kPair ? 2 : 1, kOwnN = kN / kBlocks;   // columns of B that a block loads
-    static constexpr int kA = kTileM * kStageK, kB = kOwnN * kStageK, kStage = kA + kB;
-    static constexpr int kFit = (kMaxSmem - 1024 - kEpiWarps * kStageBytes) / kStage, kStages = kFit < 8 ? kFit : 8;
-    static constexpr int kBytes = kStages * kStage + kEpiWarps * kStageBytes + 1024;
-    static constexpr uint32_t kColumns = 2 * kN;                          // of tensor memory: two accumulators
+    static constexpr int kEpiWarps = 16, kLoadWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
+    static constexpr int kSums = kPair ? 2 : 4;                           // accumulators
+    static constexpr int kLeastGroups = kPair || kN == 128 ? 1 : kN == 64 ? 2 : 4;   // so that no epilogue warp has less than a chunk
+    static constexpr int kA = kTileM * kStageK, kB = kOwnN * kStageK, kStage = kA + kB, kStaging = kEpiWarps * kUnit;
+    static constexpr int kFit = (kMaxSmem - 1024 - kStaging) / kStage, kStages = kFit < 8 ? kFit : 8;
+    static constexpr int kBytes = kStages * kStage + kStaging + 1024;
+    static constexpr uint32_t kColumns = kSums * kN;                      // of tensor memory
 };
 
 __device__ __forceinline__ void mma_i8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate, uint32_t leader)
@@ -59,89 +60,162 @@ __device__ __forceinline__ void store_tile_2d(const void *map, uint32_t src, int
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
+// two fp32 operations in one instruction, each rounded as it is alone
+__device__ __forceinline__ uint64_t pair_of(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 // 32 sums of a row with their scales.  `scales`: of the 32 columns, and their biases 128 bytes on.
 __device__ __forceinline__ void scale_row(uint32_t (&r)[32], float row_scale, uint32_t scales)
 {
+    const uint64_t rs = pair_of(row_scale, row_scale);
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
-        const int4 s = ptx::ld_shared_128(scales + j * 4), b = ptx::ld_shared_128(scales + 128 + j * 4);
-        const int sv[4] = {s.x, s.y, s.z, s.w}, bv[4] = {b.x, b.y, b.z, b.w};
+        uint64_t s[2], b[2];
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(s[0]), "=l"(s[1]) : "r"(scales + j * 4) : "memory");
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(b[0]), "=l"(b[1]) : "r"(scales + 128 + j * 4) : "memory");
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            r[j + i] = __float_as_uint(__fmaf_rn(__int2float_rn((int)r[j + i]) * row_scale, __int_as_float(sv[i]), __int_as_float(bv[i])));
+        for (int i = 0; i < 2; ++i) {
+            const uint64_t v = fma_2(mul_2(pair_of(__int2float_rn((int)r[j + 2 * i]), __int2float_rn((int)r[j + 2 * i + 1])), rs), s[i], b[i]);
+            asm("mov.b64 {%0, %1}, %2;" : "=r"(r[j + 2 * i]), "=r"(r[j + 2 * i + 1]) : "l"(v));
+        }
     }
 }
 
-// 64 bytes of a row to the lane's place in a unit of staging: pieces of 16 bytes in the order that tensor copies expect of such rows.
-__device__ __forceinline__ void stage_piece(uint32_t unit, int lane, int j, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+// 64 bytes of a row to the lane's place in the staging: pieces of 16 bytes in the order that tensor copies expect of such rows.  kPart: which 16 of the 32 words (of
+// 16-bit types: all of them, rounded).
+template <int kType, int kPart>
+__device__ __forceinline__ void stage_row(const uint32_t (&r)[32], uint32_t unit, int lane)
 {
-    st_shared_v4(unit + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), a, b, c, d);
-}
-// kPart: which 16 of the 32 words (of 16-bit types: all of them, rounded)
-template <int kPart>
-__device__ __forceinline__ void stage_row(const uint32_t (&r)[32], int type, uint32_t unit, int lane)
-{
-    if (type == EOQ_F16 || type == EOQ_BF16) {
+    const uint32_t row = unit + lane * 64, turn = (uint32_t)((lane >> 1) & 3) << 4;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
+    for (int j = 0; j < 4; ++j) {
+        uint32_t w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float lo = __uint_as_float(r[8 * j + 2 * i]), hi = __uint_as_float(r[8 * j + 2 * i + 1]);
-                if (type == EOQ_F16) {
-                    const __half2 h = __floats2half2_rn(lo, hi);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&h);
-                } else {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-                    w[i] = *reinterpret_cast<const uint32_t *>(&h);
-                }
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (kType == EOQ_F16) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(r[8 * j + 2 * i]), __uint_as_float(r[8 * j + 2 * i + 1]));
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            } else if constexpr (kType == EOQ_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(r[8 * j + 2 * i]), __uint_as_float(r[8 * j + 2 * i + 1]));
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                w[i] = r[16 * kPart + 4 * j + i];
             }
-            stage_piece(unit, lane, j, w[0], w[1], w[2], w[3]);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) stage_piece(unit, lane, j, r[16 * kPart + 4 * j], r[16 * kPart + 4 * j + 1], r[16 * kPart + 4 * j + 2], r[16 * kPart + 4 * j + 3]);
+        st_shared_v4(row + ((uint32_t)(j << 4) ^ turn), w[0], w[1], w[2], w[3]);
     }
 }
 
 // The staged rows to rows of the output that tensor copies cannot address: 32 columns of a row at a time, or 16 of two.
-__device__ __forceinline__ void store_rows(const LinGemmArgs &a, uint32_t unit, size_t out_row, int rows, int col0, int lane)
+template <int kE>
+__device__ __forceinline__ void store_rows(const LinProduct &a, uint32_t unit, size_t out_row, int rows, int col0, int lane)
 {
-    if (a.out_type == EOQ_F16 || a.out_type == EOQ_BF16) {
+    if constexpr (kE == 2) {
         const int col = col0 + lane;
         const bool in = col < a.n;
-        for (int i = 0; i < rows; ++i) {
+        char *to = reinterpret_cast<char *>(a.out) + out_row * a.out_pitch + (size_t)col * 2;
+#pragma unroll 8
+        for (int i = 0; i < rows; ++i, to += a.out_pitch) {
             uint16_t v;
             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(unit + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) : "memory");
-            if (in) *reinterpret_cast<uint16_t *>(reinterpret_cast<char *>(a.out) + (out_row + i) * a.out_pitch + (size_t)col * 2) = v;
+            if (in) *reinterpret_cast<uint16_t *>(to) = v;
         }
     } else {
         const int c = lane & 15, col = col0 + c;
-        for (int i = lane >> 4; i < rows; i += 2) {
+        char *to = reinterpret_cast<char *>(a.out) + (out_row + (lane >> 4)) * a.out_pitch + (size_t)col * 4;
+#pragma unroll 8
+        for (int i = lane >> 4; i < rows; i += 2, to += 2 * a.out_pitch) {
             uint32_t v;
             asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(unit + i * 64 + (((c >> 2) ^ ((i >> 1) & 3)) << 4) + (c & 3) * 4) : "memory");
-            if (col < a.n) *reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(a.out) + (out_row + i) * a.out_pitch + (size_t)col * 4) = v;
+            if (col < a.n) *reinterpret_cast<uint32_t *>(to) = v;
         }
     }
 }
 
-template <int kMajor, int kN, bool kPair>
-__global__ void __launch_bounds__(kThreads, 1)
-lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ CUtensorMap map_out)
+// A warp's 32 rows and 32 columns of scaled sums to memory, by way of its staging.
+template <int kType>
+__device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorMap *map, const uint32_t (&r)[32], uint32_t unit, size_t out_row, int rows, int col0, int lane)
+{
+    constexpr int kE = kType == EOQ_F16 || kType == EOQ_BF16 ? 2 : 4;
+    auto out = [&](int col) {
+        if (a.tensor_store) {
+            ptx::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                if (col < a.n) store_tile_2d(map, unit, col, (int)out_row);
+                store_commit();
+                store_wait_read();
+            }
+        } else {
+            __syncwarp();
+            store_rows<kE>(a, unit, out_row, rows, col, lane);
+        }
+        __syncwarp();
+    };
+    stage_row<kType, 0>(r, unit, lane);
+    out(col0);
+    if constexpr (kE == 4) {
+        stage_row<kType, 1>(r, unit, lane);
+        out(col0 + 16);
+    }
+}
+
+// The calling pair or block's units in turn: next(product, unit) is false behind the last one.  Those of the first product are dealt out one by one; where some
+// blocks get one more than the others, those others take `catch_up` units of the second product in the meantime, then all take theirs in turn.
+struct Turns {
+    int me, me_light, all, own0, first1, catch_up, light, units1, round;
+    __device__ __forceinline__ Turns(const LinGemmArgs &a, int me_, int all_) : me(me_), all(all_), round(0)
+    {
+        const int units0 = a.p[0].units, each = units0 / all, more = units0 - each * all;
+        own0 = each + (me < more ? 1 : 0);
+        light = all - more;
+        catch_up = me >= more && more > 0 ? a.catch_up : 0;
+        first1 = more > 0 ? a.catch_up * light : 0;
+        units1 = a.count > 1 ? a.p[1].units : 0;
+        me_light = me - more;
+    }
+    __device__ __forceinline__ bool next(int &product, int &unit)
+    {
+        const int r = round++, k = r - own0;
+        product = k < 0 ? 0 : 1;
+        unit = k < 0 ? me + r * all : k < catch_up ? k * light + me_light : first1 + (k - catch_up) * all + me;
+        return k < 0 || unit < units1;
+    }
+};
+
+struct Maps {
+    CUtensorMap a[2], b[2], out[2];
+};
+
+template <int kN, bool kPair>
+__global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_kernel(const __grid_constant__ LinGemmArgs args, const __grid_constant__ Maps maps)
 {
     using S = GemmShape<kN, kPair>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 5];
-    __shared__ __align__(16) float scales_s[kEpiWarps][64];
+    __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kSums + 1];
+    __shared__ __align__(16) float scales_s[S::kEpiWarps][64];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t abort_s;
 
@@ -152,69 +226,71 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
     auto full_bar = [&](int s) { return bar0 + 8u * s; };
     auto empty_bar = [&](int s) { return bar0 + 8u * (S::kStages + s); };
     auto sums_bar = [&](int i) { return bar0 + 8u * (2 * S::kStages + i); };
-    auto read_bar = [&](int i) { return bar0 + 8u * (2 * S::kStages + 2 + i); };
-    const uint32_t drain_bar = bar0 + 8u * (2 * S::kStages + 4);
+    auto read_bar = [&](int i) { return bar0 + 8u * (2 * S::kStages + S::kSums + i); };
+    const uint32_t drain_bar = bar0 + 8u * (2 * S::kStages + 2 * S::kSums);
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             ptx::mbar_init(full_bar(s), 1);
             ptx::mbar_init(empty_bar(s), 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < S::kSums; ++i) {
             ptx::mbar_init(sums_bar(i), 1);
-            ptx::mbar_init(read_bar(i), S::kBlocks * kEpiWarps);
+            ptx::mbar_init(read_bar(i), S::kBlocks * (S::kEpiWarps / args.groups));
         }
         ptx::mbar_init(drain_bar, 1);
         abort_s = 0;
         ptx::fence_barrier_init();
-        ptx::prefetch_tensormap(&map_a);
-        ptx::prefetch_tensormap(&map_b);
-        if (a.tensor_store) ptx::prefetch_tensormap(&map_out);
+        for (int i = 0; i < args.count; ++i) {
+            ptx::prefetch_tensormap(&maps.a[i]);
+            ptx::prefetch_tensormap(&maps.b[i]);
+        }
     }
-    if (warp == kMmaWarp) tmem_take<kPair>(ptx::smem_u32(&tmem_base_s), S::kColumns);
-    const int rank = kPair ? blockIdx.x & 1 : 0, first = blockIdx.x / S::kBlocks, step = gridDim.x / S::kBlocks;
-    const int tiles = a.m_tiles * a.n_tiles, units = tiles * a.splits;
-    // Unit u: a tile and a part of its reduction.  Tiles go in bands of kBand tiles of n, down m inside a band, so that what runs at a time
+    if (warp == S::kMmaWarp) tmem_take<kPair>(ptx::smem_u32(&tmem_base_s), S::kColumns);
+    const int rank = kPair ? blockIdx.x & 1 : 0;
+    // A unit: a tile and a part of its reduction.  Tiles go in bands of kBand tiles of n, down m inside a band, so that what runs at a time
     // shares operands in the L2.
-    auto place = [&](int u, int &m0, int &n0, int &split) {
+    auto place = [&](const LinProduct &p, int u, int &m0, int &n0, int &split) {
         constexpr int kBand = 8;
+        const int tiles = p.m_tiles * p.n_tiles;
         split = u / tiles;
-        const int t = u - split * tiles, per_band = kBand * a.m_tiles, band = t / per_band, in = t - band * per_band;
-        const int width = min(kBand, a.n_tiles - band * kBand);
+        const int t = u - split * tiles, per_band = kBand * p.m_tiles, band = t / per_band, in = t - band * per_band;
+        const int width = min(kBand, p.n_tiles - band * kBand);
         const int mt = in / width;
         m0 = mt * S::kBlocks * kTileM + rank * kTileM;
         n0 = (band * kBand + in - mt * width) * kN;
     };
-    auto stages_of = [&](int split) { return min(a.stages_per_split, a.k_stages - split * a.stages_per_split); };
+    auto stages_of = [&](const LinProduct &p, int split) { return min(p.stages_per_split, p.k_stages - split * p.stages_per_split); };
     ptx::tc_fence_before();
     if (kPair) ptx::cluster_sync();   // (the other block's barriers are ready)
     else __syncthreads();
     ptx::tc_fence_after();
     ptx::grid_dep_wait();
-    if (a.launch_early) ptx::grid_dep_launch();
+    if (args.launch_early) ptx::grid_dep_launch();
     const uint32_t tmem_base = tmem_base_s;
-    const RoleCtx ctx{&abort_s, a.dev};
+    const RoleCtx ctx{&abort_s, args.dev};
+    Turns turns(args, blockIdx.x / S::kBlocks, gridDim.x / S::kBlocks);
+    int which, u;
 
-    if (warp == kLoadWarp) {
+    if (warp == S::kLoadWarp) {
         bool ok = true;
         int slot = 0, started = 0;
         uint32_t phase = 0;
-        for (int u = first; u < units && ok; u += step) {
+        while (ok && turns.next(which, u)) {
+            const LinProduct &p = args.p[which];
+            const CUtensorMap *map_a = &maps.a[which], *map_b = &maps.b[which];
+            const bool a_mn = p.a_mn, b_mn = p.b_mn;
             int m0, n0, split;
-            place(u, m0, n0, split);
-            const int n_own = n0 + rank * S::kOwnN, stages = stages_of(split), k_first = split * a.stages_per_split;
-            // Blocks that work side by side begin at different places of the reduction (integer sums do not mind): in step, all of them asked for the same rows of a few
-            // tokens at once, and 16 tokens 4096 to 4096 took 16.8 us where 32 took 11.0.
-            int at = kPair ? 0 : (int)((unsigned)u % (unsigned)stages);
-            for (int it = 0; it < stages; ++it, at = at + 1 == stages ? 0 : at + 1) {
+            place(p, u, m0, n0, split);
+            const int n_own = n0 + rank * S::kOwnN, stages = stages_of(p, split), k_first = split * p.stages_per_split;
+            const uint32_t bytes = S::kBlocks * (S::kB + p.a_rows * kStageK);
+            for (int it = 0; it < stages; ++it) {
                 if (!(ok = __all_sync(0xffffffffu, wait_bar(empty_bar(slot), phase ^ 1u, ctx)))) break;
                 if (lane == 0) {
                     const uint32_t dst = smem_base + slot * S::kStage;
-                    const int k = (k_first + at) * kStageK;
-                    if (rank == 0) ptx::mbar_expect_tx(full_bar(slot), S::kBlocks * S::kStage);
-                    if (kMajor == kBothMn) load_tile<kPair>(dst, &map_a, full_bar(slot), m0, k);
-                    else load_tile<kPair>(dst, &map_a, full_bar(slot), k, m0);
-                    if (kMajor == kBothK) load_tile<kPair>(dst + S::kA, &map_b, full_bar(slot), k, n_own);
-                    else load_tile<kPair>(dst + S::kA, &map_b, full_bar(slot), n_own, k);
+                    const int k = (k_first + it) * kStageK;
+                    if (rank == 0) ptx::mbar_expect_tx(full_bar(slot), bytes);
+                    load_tile<kPair>(dst, map_a, full_bar(slot), a_mn ? m0 : k, a_mn ? k : m0);
+                    load_tile<kPair>(dst + S::kA, map_b, full_bar(slot), b_mn ? n_own : k, b_mn ? k : n_own);
                 }
                 __syncwarp();
                 ++started;
@@ -227,23 +303,25 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
             for (int it = started > S::kStages ? started - S::kStages : 0; it < started; ++it)
                 for (uint32_t i = 0; i < kSpinLimit; ++i)
                     if (ptx::mbar_try_wait(full_bar(it % S::kStages), (uint32_t)(it / S::kStages) & 1u)) break;
-    } else if (warp == kMmaWarp) {
+    } else if (warp == S::kMmaWarp) {
         if (rank == 0) {
             const uint32_t leader = elect_one();
-            const uint32_t idesc = make_idesc_i8(S::kBlocks * kTileM, kN, kMajor == kBothMn, kMajor != kBothK);
-            // K-major: rows of 128 bytes, groups of eight 1024 bytes apart, 32 bytes along the row to the next step of the reduction.  MN-major: a row of the
-            // reduction is 128 (or kN) bytes, groups of eight rows lie behind one another, 32 rows to the next step.
-            constexpr int kBRow = kMajor == kBothK ? 128 : S::kOwnN < 128 ? S::kOwnN : 128;
-            constexpr uint32_t kAStep = kMajor == kBothMn ? 32 * 128 / 16 : 2, kBStep = kMajor == kBothK ? 2 : 32 * kBRow / 16;
-            const uint32_t a_hi = smem_desc_hi(1024, 2), b_hi = smem_desc_hi(8 * kBRow, layout_type_for(kBRow));
-            const uint32_t a_lead = (S::kA >> 4) << 16, b_lead = (S::kB >> 4) << 16;
             bool ok = true;
             int slot = 0, turn = 0;
             uint32_t phase = 0;
-            for (int u = first; u < units && ok; u += step, ++turn) {
-                const int stages = stages_of(u / tiles), acc = turn & 1;
+            for (; ok && turns.next(which, u); ++turn) {
+                const LinProduct &p = args.p[which];
+                const bool a_mn = p.a_mn, b_mn = p.b_mn;
+                // K-major: rows of 128 bytes, groups of eight 1024 bytes apart, 32 bytes along the row to the next step of the reduction.  MN-major: a row of the
+                // reduction is 128 (or kN) bytes, groups of eight rows lie behind one another, 32 rows to the next step.
+                constexpr int kBMnRow = S::kOwnN < 128 ? S::kOwnN : 128;
+                const uint32_t idesc = make_idesc_i8(S::kBlocks * kTileM, kN, a_mn, b_mn);
+                const uint32_t a_step = a_mn ? 32 * 128 / 16 : 2, b_step = b_mn ? 32 * kBMnRow / 16 : 2;
+                const uint32_t a_hi = smem_desc_hi(1024, 2), b_hi = b_mn ? smem_desc_hi(8 * kBMnRow, layout_type_for(kBMnRow)) : a_hi;
+                const uint32_t a_lead = (S::kA >> 4) << 16, b_lead = (S::kB >> 4) << 16;
+                const int stages = stages_of(p, u / (p.m_tiles * p.n_tiles)), acc = turn % S::kSums;
                 const uint32_t d = tmem_base + acc * kN;
-                if (!(ok = __all_sync(0xffffffffu, wait_both<kPair>(read_bar(acc), ((turn >> 1) & 1) ^ 1, ctx)))) break;
+                if (!(ok = __all_sync(0xffffffffu, wait_both<kPair>(read_bar(acc), (turn / S::kSums & 1) ^ 1, ctx)))) break;
                 ptx::tc_fence_after();
                 for (int it = 0; it < stages; ++it) {
                     if (!(ok = __all_sync(0xffffffffu, wait_both<kPair>(full_bar(slot), phase, ctx)))) break;
@@ -251,7 +329,7 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
                     const uint32_t a16 = ((smem_base + slot * S::kStage) >> 4) | a_lead, b16 = ((smem_base + slot * S::kStage + S::kA) >> 4) | b_lead;
 #pragma unroll
                     for (int k = 0; k < kStageK / 32; ++k) {
-                        const uint64_t ad = smem_desc_join(a16 + k * kAStep, a_hi), bd = smem_desc_join(b16 + k * kBStep, b_hi);
+                        const uint64_t ad = smem_desc_join(a16 + k * a_step, a_hi), bd = smem_desc_join(b16 + k * b_step, b_hi);
                         const uint32_t more = (k | it) != 0 ? 1u : 0u;
                         if constexpr (kPair) mma_i8_pair(d, ad, bd, idesc, more, leader);
                         else ptx::mma_i8(d, ad, bd, idesc, more, leader);
@@ -267,81 +345,59 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
                     if (ptx::mbar_try_wait(drain_bar, 0)) break;
         }
     } else {
-        const int quad = warp & 3, half = warp >> 2;
-        constexpr int kHalfN = kN >= 64 ? kN / 2 : kN, kChunks = kHalfN / 32;   // columns of a warp (of 32, the second four warps have none)
-        const bool narrow = a.out_type == EOQ_F16 || a.out_type == EOQ_BF16;
-        const uint32_t scales = ptx::smem_u32(&scales_s[warp][0]), staging_w = staging + warp * kStageBytes;
-        int turn = 0, units_out = 0;
-        for (int u = first; u < units; u += step, ++turn) {
+        const int group_warps = S::kEpiWarps / args.groups, quad = warp & 3, group = warp / group_warps, part = warp % group_warps / 4, warp_n = kN * 4 / group_warps;
+        const uint32_t scales = ptx::smem_u32(&scales_s[warp][0]), unit = staging + warp * kUnit;
+        for (int turn = 0; turns.next(which, u); ++turn) {
+            if (turn % args.groups != group) continue;
+            const LinProduct &p = args.p[which];
+            const CUtensorMap *map_out = &maps.out[which];
+            const int type = p.out_type;
             int m0, n0, split;
-            place(u, m0, n0, split);
-            const int acc = turn & 1, row0 = m0 + quad * 32, row = row0 + lane, first_col = n0 + half * kHalfN;
-            const bool mine = row0 < a.m && (kN >= 64 || half == 0);
-            // scales and biases of the tile arrive beside its MMAs
-            float row_scale = 0.0f, s[kChunks], b[kChunks];
-            if (a.out_type != EOQ_I32) {
-                row_scale = row < a.m ? __ldg(a.row_scale + row) : 0.0f;
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    const int col = first_col + c * 32 + lane;
-                    s[c] = mine && col < a.n ? a.col_scale ? __ldg(a.col_scale + col) : 1.0f : 0.0f;
-                    b[c] = mine && col < a.n && a.bias ? __ldg(a.bias + col) : 0.0f;
-                }
-            }
-            if (!__all_sync(0xffffffffu, wait_bar<32>(sums_bar(acc), (turn >> 1) & 1, ctx))) break;
-            ptx::tc_fence_after();
-            const size_t out_row = (size_t)split * a.split_rows + row0;
-            const uint32_t t_row = tmem_base + acc * kN + half * kHalfN + ((uint32_t)(quad * 32) << 16);
-            const int chunks = !mine || first_col >= a.n ? 0 : min(kChunks, (a.n - first_col + 31) / 32);
-            // a unit of staging to memory
-            auto out = [&](int col) {
-                const uint32_t unit = staging_w + (units_out & 1) * kUnit;
-                ++units_out;
-                if (a.tensor_store) {
-                    ptx::fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (col < a.n) store_tile_2d(&map_out, unit, col, (int)out_row);
-                        store_commit();
-                        store_wait_read<1>();   // (the other unit is free)
-                    }
-                    __syncwarp();
-                } else {
-                    __syncwarp();
-                    store_rows(a, unit, out_row, min(32, a.m - row0), col, lane);
-                    __syncwarp();
-                }
+            place(p, u, m0, n0, split);
+            const int acc = turn % S::kSums, row0 = m0 + quad * 32, first_col = n0 + part * warp_n, rows = min(32, p.m - row0);
+            const int chunks = rows <= 0 || first_col >= p.n ? 0 : min(warp_n / 32, (p.n - first_col + 31) / 32);
+            // the row's scale and the first columns' arrive beside the tile's MMAs, the next columns' beside the arithmetic
+            float row_scale = 0.0f, s = 0.0f, b = 0.0f;
+            auto fetch = [&](int c) {
+                const int col = first_col + c * 32 + lane;
+                s = c < chunks && col < p.n ? p.col_scale ? __ldg(p.col_scale + col) : 1.0f : 0.0f;
+                b = c < chunks && col < p.n && p.bias ? __ldg(p.bias + col) : 0.0f;
             };
-            uint32_t r[2][32];
-            if (chunks > 0) ptx::tmem_ld_32x32(t_row, r[0]);
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                if (c >= chunks) break;
-                ptx::tmem_ld_wait();
-                if (c + 1 < chunks) ptx::tmem_ld_32x32(t_row + (c + 1) * 32, r[(c + 1) & 1]);   // (on its way beside this chunk's arithmetic)
-                if (a.out_type != EOQ_I32) {
-                    scales_s[warp][lane] = s[c];
-                    scales_s[warp][32 + lane] = b[c];
+            if (type != EOQ_I32) {
+                row_scale = lane < rows ? __ldg(p.row_scale + row0 + lane) : 0.0f;
+                fetch(0);
+            }
+            if (!__all_sync(0xffffffffu, wait_bar<32>(sums_bar(acc), turn / S::kSums & 1, ctx))) break;
+            ptx::tc_fence_after();
+            const size_t out_row = (size_t)split * p.split_rows + row0;
+            const uint32_t t_row = tmem_base + acc * kN + part * warp_n + ((uint32_t)(quad * 32) << 16);
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                const int col0 = first_col + c * 32;
+                uint32_t r[32];
+                ptx::tmem_ld_32x32(t_row + c * 32, r);
+                if (type != EOQ_I32) {
+                    scales_s[warp][lane] = s;
+                    scales_s[warp][32 + lane] = b;
                     __syncwarp();
-                    scale_row(r[c & 1], row_scale, scales);
+                    fetch(c + 1);
                 }
-                stage_row<0>(r[c & 1], a.out_type, staging_w + (units_out & 1) * kUnit, lane);
-                out(first_col + c * 32);
-                if (!narrow) {
-                    stage_row<1>(r[c & 1], a.out_type, staging_w + (units_out & 1) * kUnit, lane);
-                    out(first_col + c * 32 + 16);
-                }
+                ptx::tmem_ld_wait();
+                if (type != EOQ_I32) scale_row(r, row_scale, scales);
+                if (type == EOQ_BF16) write_chunk<EOQ_BF16>(p, map_out, r, unit, out_row, rows, col0, lane);
+                else if (type == EOQ_F16) write_chunk<EOQ_F16>(p, map_out, r, unit, out_row, rows, col0, lane);
+                else write_chunk<EOQ_F32>(p, map_out, r, unit, out_row, rows, col0, lane);   // (words as they are)
             }
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_first<kPair>(read_bar(acc));
         }
-        if (a.tensor_store && lane == 0) store_wait_all();
+        if (lane == 0) store_wait_all();
     }
     ptx::tc_fence_before();
     if (kPair) ptx::cluster_sync();   // (neither block ends while the other's MMAs, copies or arrivals may reach it)
     else __syncthreads();
-    if (warp == kMmaWarp) {
+    if (warp == S::kMmaWarp) {
         ptx::tc_fence_after();
         tmem_return<kPair>(tmem_base, S::kColumns);
     }
@@ -349,7 +405,7 @@ lin_gemm_kernel(const __grid_constant__ LinGemmArgs a, const __grid_constant__ C
 
 // The parts of a split reduction, which stand `pitch` words apart row by row and `split_rows` rows apart, added and scaled: four columns a thread.
 template <bool kLong>
-__global__ void __launch_bounds__(256) lin_join_kernel(const __grid_constant__ LinGemmArgs a, const int32_t *__restrict__ part, size_t pitch)
+__global__ void __launch_bounds__(256) lin_join_kernel(const __grid_constant__ LinProduct a, const int32_t *__restrict__ part, size_t pitch)
 {
     ptx::grid_dep_wait_launch_small();
     const int per_row = (a.n + 3) / 4;
@@ -394,124 +450,186 @@ __global__ void __launch_bounds__(256) lin_join_kernel(const __grid_constant__ L
     }
 }
 
-struct GemmPlan {
-    bool pair;
-    int tile_n, m_tiles, n_tiles, splits, k_stages, stages_per_split;
-};
-
 constexpr int kMostStages = 1023;   // of a part: 130,944 products of codes, at most 2^14 each, are an int32
 
-int tile_m(const GemmPlan &p) { return p.pair ? 2 * kTileM : kTileM; }
+// Bytes of `splits` parts of a product's sums, their rows and columns.
 size_t partial_pitch(int n) { return ((size_t)n + 3) & ~(size_t)3; }
+size_t parts_bytes(const LinProduct &p) { return p.splits > 1 ? sizeof(int32_t) * (size_t)p.splits * p.split_rows * partial_pitch(p.n) : 0; }
 
-// Tiles and splits that take the least time by a model of waves of blocks: cycles of a stage (the MMAs', or what its loads take), and some 6000 cycles in front
-// of and behind a block's work.
-GemmPlan plan_of(size_t m, size_t n, size_t k)
+struct Plan {
+    int tile_n;       // 32, 64, 128, or 256: a pair's
+    int catch_up;
+};
+
+// Cycles of a stage of a tile of width 32 << w: its MMAs, or what a block's copies take, two cycles for each line of 128 bytes that a row of a tile lies in.
+double stage_cycles(const LinProduct &p, int w)
 {
-    const int k_stages = (int)((k + kStageK - 1) / kStageK), least = (k_stages + kMostStages - 1) / kMostStages;
-    GemmPlan best = {};
+    static const double kMma[4] = {230.0, 230.0, 280.0, 520.0};
+    const int own_n = w == 3 ? 128 : 32 << w;
+    auto lines = [](size_t pitch) { return pitch % 128 == 0 || 128 % pitch == 0 ? 1.0 : 1.75; };
+    const double copies = 2.0 * ((p.a_mn || p.m >= 128 ? 128.0 : p.m) * lines(p.pitch_a) + (p.b_mn ? 128.0 : own_n) * lines(p.pitch_b));
+    return copies > kMma[w] ? copies : kMma[w];
+}
+
+// Tiles and splits of the products of a launch, by a model of what takes how long: cycles of a stage, of a tile's epilogue, of a
+// launch that joins parts.  The time of a launch is that of its busiest block.
+Plan plan_of(LinProduct *p, int count)
+{
+    LinProduct best[2] = {};
+    Plan plan = {};
     double best_time = 0.0;
     for (int w = 0; w < 4; ++w) {
-        GemmPlan p;
-        p.tile_n = 32 << w;
-        p.pair = p.tile_n == 256;
-        if (p.pair && (m <= kTileM || n <= 128)) continue;
-        if (w > 0 && !p.pair && n <= (size_t)p.tile_n / 2) continue;
-        p.m_tiles = (int)((m + tile_m(p) - 1) / tile_m(p));
-        p.n_tiles = (int)((n + p.tile_n - 1) / p.tile_n);
-        p.k_stages = k_stages;
-        const size_t tiles = (size_t)p.m_tiles * p.n_tiles, room = kPartSms / (p.pair ? 2 : 1);
-        static const double kStage[4] = {260.0, 290.0, 380.0, 560.0};
+        const int tile_n = 32 << w, blocks = tile_n == 256 ? 2 : 1, tile_m = blocks * kTileM;
+        const int room = kPartSms / blocks;
+        bool fits = true, wider = w == 0;
+        for (int i = 0; i < count; ++i) {
+            if (blocks == 2 && (p[i].m <= kTileM || p[i].n <= 128)) fits = false;
+            if (p[i].n > tile_n / 2) wider = true;   // (some product has columns for tiles this wide)
+        }
+        if (!fits || !wider) continue;
         for (int fill = 0; fill <= 2; ++fill) {
-            size_t splits = fill == 0 ? 1 : fill * room / tiles;
-            if (fill > 0 && splits <= 1) continue;
-            if (splits < (size_t)least) splits = least;
-            if (splits > (size_t)k_stages) splits = k_stages;
-            p.stages_per_split = (int)((k_stages + splits - 1) / splits);
-            p.splits = (k_stages + p.stages_per_split - 1) / p.stages_per_split;
-            const double waves = (double)((tiles * p.splits + room - 1) / room);
-            double time = 6000.0 + waves * ((double)p.stages_per_split * kStage[w] + 8.0 * p.tile_n);
-            if (p.splits > 1) time += 7000.0 + (double)p.splits * m * n * 4.0 * 2.0 / 2500.0;
+            LinProduct q[2];
+            double work[2] = {}, unit[2] = {}, join = 0.0;
+            bool splits_any = fill == 0;
+            for (int i = 0; i < count; ++i) {
+                q[i] = p[i];
+                q[i].m_tiles = (p[i].m + tile_m - 1) / tile_m;
+                q[i].n_tiles = (p[i].n + tile_n - 1) / tile_n;
+                q[i].split_rows = q[i].m_tiles * tile_m;
+                const size_t tiles = (size_t)q[i].m_tiles * q[i].n_tiles, least = (q[i].k_stages + kMostStages - 1) / kMostStages;
+                size_t splits = fill == 0 ? 1 : (size_t)fill * room / tiles;
+                if (splits < least) splits = least;
+                if (splits > (size_t)q[i].k_stages) splits = q[i].k_stages;
+                q[i].stages_per_split = (int)((q[i].k_stages + splits - 1) / splits);
+                q[i].splits = (q[i].k_stages + q[i].stages_per_split - 1) / q[i].stages_per_split;
+                if (q[i].splits > 1) splits_any = true;
+                q[i].units = (int)(tiles * q[i].splits);
+                unit[i] = (double)q[i].stages_per_split * stage_cycles(q[i], w);
+                if (unit[i] < 20.0 * tile_n + 400.0) unit[i] = 20.0 * tile_n + 400.0;   // (its epilogue)
+                work[i] = unit[i] * q[i].units;
+                if (q[i].splits > 1) join += 7000.0 + (double)q[i].splits * q[i].m * q[i].n * 4.0 * 2.0 / 2500.0;
+            }
+            if (!splits_any) continue;
+            int catch_up = 0;
+            double time;
+            if (count == 1) {
+                time = (double)((q[0].units + room - 1) / room) * unit[0];
+            } else {
+                // the product with the longer units goes first
+                if (unit[1] > unit[0]) {
+                    const LinProduct t = q[0];
+                    q[0] = q[1];
+                    q[1] = t;
+                    const double d = unit[0];
+                    unit[0] = unit[1];
+                    unit[1] = d;
+                }
+                const int more = q[0].units % room, light = room - more;
+                if (more > 0) catch_up = (int)(unit[0] / unit[1] + 0.5);
+                if ((long long)catch_up * light > q[1].units) catch_up = (q[1].units + light - 1) / light;
+                const long long left = q[1].units - (long long)catch_up * (more > 0 ? light : 0);
+                const double whole = (double)(q[0].units / room) * unit[0] + (more > 0 ? unit[0] > catch_up * unit[1] ? unit[0] : catch_up * unit[1] : 0.0);
+                time = whole + (left > 0 ? (double)((left + room - 1) / room) * unit[1] : 0.0);
+            }
+            time += 6000.0 + join;
             if (best_time == 0.0 || time < best_time) {
-                best = p;
                 best_time = time;
+                for (int i = 0; i < count; ++i) best[i] = q[i];
+                plan.tile_n = tile_n;
+                plan.catch_up = catch_up;
             }
         }
     }
-    return best;
+    for (int i = 0; i < count; ++i) p[i] = best[i];
+    return plan;
 }
 
-template <int kMajor, int kN, bool kPair>
-cudaError_t launch(const LinGemmArgs &a, const void *pa, size_t pitch_a, const void *pb, size_t pitch_b, size_t k, const void *out, cudaStream_t st)
+template <int kN, bool kPair>
+cudaError_t launch(LinGemmArgs a, cudaStream_t st)
 {
     using S = GemmShape<kN, kPair>;
-    CUtensorMap ma, mb, mo = {};
-    const bool got =
-        (kMajor == kBothMn ? tiled_map_of(&ma, pa, 1, a.m, k, pitch_a, 128, kStageK, 128) : tiled_map_of(&ma, pa, 1, k, a.m, pitch_a, kStageK, kTileM, 128)) &&
-        (kMajor == kBothK ? tiled_map_of(&mb, pb, 1, k, a.n, pitch_b, kStageK, S::kOwnN, 128)
-                          : tiled_map_of(&mb, pb, 1, a.n, k, pitch_b, S::kOwnN, kStageK, S::kOwnN));
-    if (!got) return cudaErrorInvalidValue;
-    if (a.tensor_store) {
-        const int e = a.out_type == EOQ_F16 || a.out_type == EOQ_BF16 ? 2 : 4;
-        if (!tiled_map_of(&mo, out, e, a.n, a.out_type == EOQ_I32 ? a.splits * a.split_rows : (size_t)a.m, a.out_pitch, 64 / e, 32, 64)) return cudaErrorInvalidValue;
+    Maps maps = {};
+    size_t units = 0;
+    for (int i = 0; i < a.count; ++i) {
+        const LinProduct &p = a.p[i];
+        const bool got =
+            (p.a_mn ? tiled_map_of(&maps.a[i], p.a, 1, p.m, p.k, p.pitch_a, 128, kStageK, 128) : tiled_map_of(&maps.a[i], p.a, 1, p.k, p.m, p.pitch_a, kStageK, p.a_rows, 128)) &&
+            (p.b_mn ? tiled_map_of(&maps.b[i], p.b, 1, p.n, p.k, p.pitch_b, S::kOwnN, kStageK, S::kOwnN)
+                    : tiled_map_of(&maps.b[i], p.b, 1, p.k, p.n, p.pitch_b, kStageK, S::kOwnN, 128));
+        if (!got) return cudaErrorInvalidValue;
+        if (p.tensor_store) {
+            const int e = p.out_type == EOQ_F16 || p.out_type == EOQ_BF16 ? 2 : 4;
+            if (!tiled_map_of(&maps.out[i], p.out, e, p.n, p.out_type == EOQ_I32 ? (size_t)p.splits * p.split_rows : (size_t)p.m, p.out_pitch, 64 / e, 32, 64))
+                return cudaErrorInvalidValue;
+        }
+        units += p.units;
     }
     static_assert(S::kBytes <= kMaxSmem && S::kStages >= 4, "shared memory of a block");
     static std::atomic<unsigned long long> allowed;
-    const cudaError_t e = allow_smem((const void *)lin_gemm_kernel<kMajor, kN, kPair>, S::kBytes, allowed);
+    const cudaError_t e = allow_smem((const void *)lin_gemm_kernel<kN, kPair>, S::kBytes, allowed);
     if (e != cudaSuccess) return e;
-    const size_t units = (size_t)a.m_tiles * a.n_tiles * a.splits, room = a.sm_count / S::kBlocks;
+    const size_t room = a.sm_count / S::kBlocks;
     const unsigned grid = (unsigned)(units < room ? units : room) * S::kBlocks;
-    return launch_chained_clusters(S::kBlocks, lin_gemm_kernel<kMajor, kN, kPair>, dim3(grid), dim3(kThreads), S::kBytes, st, a, ma, mb, mo);
-}
-
-template <int kMajor>
-cudaError_t of_width(const LinGemmArgs &a, int tile_n, const void *pa, size_t pitch_a, const void *pb, size_t pitch_b, size_t k, const void *out, cudaStream_t st)
-{
-    if (tile_n == 32) return launch<kMajor, 32, false>(a, pa, pitch_a, pb, pitch_b, k, out, st);
-    if (tile_n == 64) return launch<kMajor, 64, false>(a, pa, pitch_a, pb, pitch_b, k, out, st);
-    if (tile_n == 128) return launch<kMajor, 128, false>(a, pa, pitch_a, pb, pitch_b, k, out, st);
-    return launch<kMajor, 256, true>(a, pa, pitch_a, pb, pitch_b, k, out, st);
+    a.groups = S::kLeastGroups;
+    while (!kPair && a.groups < 4 && units >= 2 * a.groups * room) a.groups *= 2;
+    return launch_chained_clusters(S::kBlocks, lin_gemm_kernel<kN, kPair>, dim3(grid), dim3(S::kThreads), S::kBytes, st, a, maps);
 }
 
 }  // namespace
 
-size_t lin_gemm_workspace_bytes(size_t m, size_t n, size_t k)
+// Products as a pass describes them, with tiles and splits.
+static Plan planned(LinGemmArgs &a)
 {
-    const GemmPlan p = plan_of(m, n, k);
-    return p.splits > 1 ? sizeof(int32_t) * (size_t)p.splits * p.m_tiles * tile_m(p) * partial_pitch((int)n) : 0;
+    for (int i = 0; i < a.count; ++i) a.p[i].k_stages = (int)((a.p[i].k + kStageK - 1) / kStageK);
+    return plan_of(a.p, a.count);
 }
 
-cudaError_t launch_lin_gemm(LinGemmArgs a, int pass, const int8_t *pa, size_t pitch_a, const int8_t *pb, size_t pitch_b, size_t k, void *workspace, int *launches,
-                            cudaStream_t st)
+size_t lin_gemm_workspace_bytes(LinGemmArgs a)
 {
-    const GemmPlan p = plan_of(a.m, a.n, k);
-    a.m_tiles = p.m_tiles;
-    a.n_tiles = p.n_tiles;
-    a.splits = p.splits;
-    a.k_stages = p.k_stages;
-    a.stages_per_split = p.stages_per_split;
-    a.split_rows = p.m_tiles * tile_m(p);
-    LinGemmArgs g = a;
-    // (a tensor copy writes whole pieces of 16 bytes at the end of a row, past the last column)
-    g.tensor_store = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_pitch % 16 == 0 && (size_t)a.n * (a.out_type == EOQ_F32 ? 4 : 2) % 16 == 0;
-    if (p.splits > 1) {
-        g.out = workspace;
-        g.out_type = EOQ_I32;
-        g.out_pitch = partial_pitch(a.n) * 4;
-        g.tensor_store = true;
-        g.launch_early = true;
+    planned(a);
+    size_t bytes = 0;
+    for (int i = 0; i < a.count; ++i) bytes += (parts_bytes(a.p[i]) + 255) / 256 * 256;
+    return bytes;
+}
+
+cudaError_t launch_lin_gemm(LinGemmArgs a, void *workspace, int *launches, cudaStream_t st)
+{
+    const Plan plan = planned(a);
+    a.catch_up = plan.catch_up;
+    LinProduct whole[2];
+    char *part = reinterpret_cast<char *>(workspace);
+    for (int i = 0; i < a.count; ++i) {
+        LinProduct &p = a.p[i];
+        // Of few tokens, only their rows are brought in; what stands in the others of a tile is nobody's.  (16 tokens, 4096 to 4096: 18.6 us with boxes of 128 rows, most of them
+        // behind the end.)
+        p.a_rows = p.a_mn || p.m >= kTileM ? kTileM : (p.m + 7) / 8 * 8;
+        // (a tensor copy writes whole pieces of 16 bytes at the end of a row, past the last column)
+        p.tensor_store = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_pitch % 16 == 0 && (size_t)p.n * (p.out_type == EOQ_F32 ? 4 : 2) % 16 == 0;
+        whole[i] = p;
+        if (p.splits == 1) continue;
+        p.out = part;
+        part += (parts_bytes(p) + 255) / 256 * 256;
+        p.out_type = EOQ_I32;
+        p.out_pitch = partial_pitch(p.n) * 4;
+        p.tensor_store = true;
+        a.launch_early = true;
     }
-    const cudaError_t err = pass == EOQ_PASS_FWD     ? of_width<kBothK>(g, p.tile_n, pa, pitch_a, pb, pitch_b, k, g.out, st)
-                            : pass == EOQ_PASS_DGRAD ? of_width<kBMn>(g, p.tile_n, pa, pitch_a, pb, pitch_b, k, g.out, st)
-                                                     : of_width<kBothMn>(g, p.tile_n, pa, pitch_a, pb, pitch_b, k, g.out, st);
+    cudaError_t e = plan.tile_n == 32    ? launch<32, false>(a, st)
+                    : plan.tile_n == 64  ? launch<64, false>(a, st)
+                    : plan.tile_n == 128 ? launch<128, false>(a, st)
+                                         : launch<256, true>(a, st);
     ++*launches;
-    if (err != cudaSuccess || p.splits == 1) return err;
-    ++*launches;
-    const size_t pieces = (size_t)a.m * ((a.n + 3) / 4), blocks = (pieces + 255) / 256, cap = 8 * (size_t)a.sm_count;
-    const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
-    const int32_t *part = reinterpret_cast<const int32_t *>(workspace);
-    if (p.k_stages > kMostStages) return launch_chained(lin_join_kernel<true>, grid, dim3(256), 0, st, a, part, partial_pitch(a.n));
-    return launch_chained(lin_join_kernel<false>, grid, dim3(256), 0, st, a, part, partial_pitch(a.n));
+    for (int i = 0; i < a.count && e == cudaSuccess; ++i) {
+        const LinProduct &p = whole[i];
+        if (p.splits == 1) continue;
+        ++*launches;
+        const size_t pieces = (size_t)p.m * ((p.n + 3) / 4), blocks = (pieces + 255) / 256, cap = 8 * (size_t)a.sm_count;
+        const dim3 grid((unsigned)(blocks < cap ? blocks : cap));
+        const int32_t *from = reinterpret_cast<const int32_t *>(a.p[i].out);
+        e = p.k_stages > kMostStages ? launch_chained(lin_join_kernel<true>, grid, dim3(256), 0, st, p, from, partial_pitch(p.n))
+                                     : launch_chained(lin_join_kernel<false>, grid, dim3(256), 0, st, p, from, partial_pitch(p.n));
+    }
+    return e;
 }
 
 }  // namespace eoq
