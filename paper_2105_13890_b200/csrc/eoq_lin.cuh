@@ -60,6 +60,7 @@ template <int kType, bool kWide>
 struct Span {
     static constexpr int kE = Elem<kType>::kSize, kN = 16 / kE;
     int first, step, cols;   // the thread's column 0 of a group; to its next one; columns of a row
+    Span() = default;
     __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_)
         : first(group * lanes * kN + (kWide ? lane * kN : lane)), step(kWide ? 1 : lanes), cols(cols_)
     {

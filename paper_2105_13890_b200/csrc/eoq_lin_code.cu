@@ -15,6 +15,8 @@ namespace eoq {
 namespace {
 
 constexpr int kThreads = 256;
+// blocks of the rows' kernel on an SM, by the vectors that a thread holds
+template <int kHeld> constexpr int kRowBlocks = kHeld <= 1 ? 6 : kHeld <= 4 ? 4 : 2;
 // Strips, and elements of a tensor, whose maxima the second look puts together by itself; others take a kernel between the two.
 constexpr int kFoldStrips = 32;
 constexpr size_t kFoldSize = 1 << 20;
@@ -37,18 +39,16 @@ __device__ __forceinline__ uint32_t lanes_top(uint32_t top, int lanes, uint32_t 
     return top;
 }
 
-// Rows: kHold groups of each of kRows rows at a time.
-template <int kType, bool kWide, int kHold, int kRows>
-__global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constant__ LinCodeArgs a, const int lanes)
+// Rows: kHold groups of a row at a time, the next row's on their way meanwhile.
+template <int kType, bool kWide, int kHold>
+__global__ void __launch_bounds__(kThreads, kRowBlocks<kHold>) lin_rows_kernel(const __grid_constant__ LinCodeArgs a, const int lanes)
 {
     using S = Span<kType, kWide>;
     constexpr int kN = S::kN;
-    __shared__ uint32_t cells[kThreads / 32];
+    __shared__ uint32_t cells[2][kThreads / 32];
     ptx::grid_dep_wait_launch_small();
     const int lane = threadIdx.x % lanes, slots = kThreads / lanes, groups = (a.cols + lanes * kN - 1) / (lanes * kN);
-    const size_t row0 = (size_t)blockIdx.x * kRows * slots + threadIdx.x / lanes;
-    const char *src = reinterpret_cast<const char *>(a.src) + row0 * a.stride * S::kE;
-    const size_t step = slots * a.stride * S::kE;
+    const size_t at_once = slots, stride = a.stride * S::kE;
     auto scaled = [&](const Raw<16> &r, const S &at, float (&v)[kN]) {
         Elem<kType>::to_f32(r, v);
         if (a.factors) {
@@ -66,28 +66,34 @@ __global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constan
         for (int i = 0; i < kN; ++i) top = max(top, abs_bits(v[i]));
         return top;
     };
-    Raw<16> held[kRows][kHold];
+    Raw<16> next[kHold];
+    auto fetch = [&](size_t row) {
 #pragma unroll
-    for (int u = 0; u < kRows; ++u)
+        for (int h = 0; h < kHold; ++h) next[h] = S(h, lane, lanes, a.cols).get(reinterpret_cast<const char *>(a.src) + row * stride, row < a.rows);
+    };
+    const size_t step = gridDim.x * at_once;
+    size_t row = blockIdx.x * at_once + threadIdx.x / lanes;
+    int turn = 0;
+    fetch(row);
+    for (size_t first = blockIdx.x * at_once; first < a.rows; first += step, row += step, turn ^= 1) {   // (the same rounds for every thread)
+        Raw<16> held[kHold];
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) held[u][h] = S(h, lane, lanes, a.cols).get(src + u * step, row0 + u * slots < a.rows);
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        const size_t row = row0 + u * slots;
+        for (int h = 0; h < kHold; ++h) held[h] = next[h];
+        if (first + step < a.rows) fetch(row + step);
         const bool mine = row < a.rows;
+        const char *src = reinterpret_cast<const char *>(a.src) + row * stride;
         uint32_t top = 0;
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) top = more(top, held[u][h], S(h, lane, lanes, a.cols));
+        for (int h = 0; h < kHold; ++h) top = more(top, held[h], S(h, lane, lanes, a.cols));
         if (mine)
             for (int g = kHold; g < groups; ++g) {
                 const S at(g, lane, lanes, a.cols);
-                top = more(top, at.get(src + u * step, true), at);
+                top = more(top, at.get(src, true), at);
             }
-        const float t = __uint_as_float(lanes_top(top, lanes, cells));
-        if (kRows > 1 && lanes > 32) __syncthreads();   // (the cells are read)
+        const float t = __uint_as_float(lanes_top(top, lanes, cells[turn]));
         if (!mine) continue;
         const bool fine = finite_top(t);
-        const float per = row_per_of(t);
+        const float per = fine ? row_per_of(t) : 0.0f;
         if (lane == 0) {
             a.scales[row] = row_scale_of(t);
             if (!fine) atomicOr(&a.dev->status, EOQ_DEV_NONFINITE);
@@ -97,14 +103,18 @@ __global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constan
             uint32_t q[kN];
             scaled(r, at, v);
 #pragma unroll
-            for (int i = 0; i < kN; ++i) q[i] = fine ? row_code(v[i], per) : 0u;
+            for (int i = 0; i < kN; ++i) q[i] = row_code(v[i], per);
+            if (!fine) {
+#pragma unroll
+                for (int i = 0; i < kN; ++i) q[i] = 0;
+            }
             at.put_codes(a.codes + row * a.pitch, q);
         };
 #pragma unroll
-        for (int h = 0; h < kHold; ++h) put(held[u][h], S(h, lane, lanes, a.cols));
+        for (int h = 0; h < kHold; ++h) put(held[h], S(h, lane, lanes, a.cols));
         for (int g = kHold; g < groups; ++g) {
             const S at(g, lane, lanes, a.cols);
-            put(at.get(src + u * step, true), at);
+            put(at.get(src, true), at);
         }
     }
 }
@@ -113,44 +123,106 @@ __global__ void __launch_bounds__(kThreads) lin_rows_kernel(const __grid_constan
 
 constexpr int kAhead = 4;   // rows of a thread in flight
 
-// Block (x, y): strip x of the rows, group y of the columns, `lanes` (at most 32) threads a row.  kRows: the rows' maxima too.
-// Vectors come in by asynchronous copies, each read back by the thread that copied it, six to eight rows ahead.  16,384 x 4096 of bf16: 43 us, 3.1 TB/s, bound by
-// issue (15 instructions an element, of which the products, maxima and the sum are five).
-template <int kType, bool kWide, bool kRows>
+// the largest magnitude of three, NaN if one is; two products or sums of neighbouring values in one instruction, each rounded as it is alone
+__device__ __forceinline__ float max3_abs(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float2 mul_2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 c, a, b;\n\t"
+        "mov.b64 {%0, %1}, c;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add_2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n\t.reg .b64 a, b, c;\n\t"
+        "mov.b64 a, {%2, %3};\n\t"
+        "mov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 c, a, b;\n\t"
+        "mov.b64 {%0, %1}, c;\n\t}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+// The values of the block's threads that have the same lane, put together in those of slot 0, by way of kCells arrays of a value a thread.
+template <int kN, int kCells, bool kMax>
+__device__ __forceinline__ void meet_threads(float *cells, float (&mine)[kN], int lane, int slot, int slots, int lanes)
+{
+    constexpr int kAtOnce = kCells < kN ? kCells : kN;
+#pragma unroll
+    for (int i0 = 0; i0 < kN; i0 += kAtOnce) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) cells[i * kThreads + threadIdx.x] = mine[i0 + i];
+        __syncthreads();
+        if (slot == 0)
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i)
+                for (int s = 1; s < slots; ++s) {
+                    const float v = cells[i * kThreads + s * lanes + lane];
+                    mine[i0 + i] = kMax ? max_abs(mine[i0 + i], v) : mine[i0 + i] + v;
+                }
+    }
+}
+
+// Block (x, y): strip x of the rows, kVec groups of the columns from y * kVec on, `lanes` (at most 32) threads a row.  kRows: the rows' maxima too.
+// Vectors come in by asynchronous copies, each read back by the thread that copied it, some rows ahead.  What bounds it is issue: two vectors of a row a thread share the
+// row's own work (its factor, its maximum, what is ahead).  16,384 x 4096 of bf16: 36 us; 43 with one.
+template <int kType, bool kWide, int kVec, bool kRows>
 __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_constant__ LinErrorArgs a, const int lanes)
 {
     using S = Span<kType, kWide>;
-    constexpr int kN = S::kN, kRing = kWide ? 4 : 1, kPair = 2;   // stages of two rows
-    __shared__ __align__(16) uint4 ring[kRing * kPair][kThreads];
+    constexpr int kN = S::kN, kRing = kWide ? (kVec == 2 ? 3 : 4) : 1, kPair = 2;   // stages of two rows
+    __shared__ __align__(16) uint4 ring[kRing * kPair * kVec][kThreads];
     ptx::grid_dep_wait_launch_small();
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes;
-    const S at(blockIdx.y, lane, lanes, a.cols);
     const size_t begin = (size_t)blockIdx.x * a.strip, end = min(a.rows, begin + a.strip);
     const size_t step = slots * a.stride * S::kE;
     const char *src = reinterpret_cast<const char *>(a.src) + (begin + slot) * a.stride * S::kE;
     const int stages = (int)((end - begin + kPair * slots - 1) / (kPair * slots));   // (the same for every lane)
     int left = (int)(end - begin) - slot;                                           // rows from `src` on
-    Raw<16> now[kPair];
-    float f[kPair] = {}, next_f[kPair] = {};
-    const float *factor = a.row_factors + begin + slot;
+    S at[kVec];
+    int bytes[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+        at[j] = S(blockIdx.y * kVec + j, lane, lanes, a.cols);
+        bytes[j] = min(16, max(0, (a.cols - at[j].first) * S::kE));   // (of a vector; zeros behind them)
+    }
+    Raw<16> now[kPair][kVec];
     // the next stage's copies or, without a ring, loads
-    auto fetch = [&](int stage) {
+    auto fetch = [&](int slot_) {
 #pragma unroll
         for (int u = 0; u < kPair; ++u) {
             const bool mine = u * slots < left;
-            if constexpr (kWide) {
-                const int bytes = mine ? min(16, max(0, (a.cols - at.first) * S::kE)) : 0;   // (zeros behind them)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(&ring[stage % kRing * kPair + u][threadIdx.x])),
-                             "l"(bytes ? src + u * step + (size_t)at.first * S::kE : reinterpret_cast<const char *>(a.strip_tops ? a.strip_tops : a.strip_sums)), "r"(bytes)
-                             : "memory");
-            } else {
-                now[u] = at.get(src + u * step, mine);
+            const char *row = mine ? src + u * step : reinterpret_cast<const char *>(a.src);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                if constexpr (kWide) {
+                    const int n = mine ? bytes[j] : 0;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(&ring[(slot_ * kPair + u) * kVec + j][threadIdx.x])),
+                                 "l"(row + (n ? (size_t)at[j].first * S::kE : 0)), "r"(n)
+                                 : "memory");
+                } else {
+                    now[u][j] = at[j].get(row, mine);
+                }
             }
         }
         src += kPair * step;
         left -= kPair * slots;
         if constexpr (kWide) asm volatile("cp.async.commit_group;" ::: "memory");
     };
+    const float *factor = a.row_factors + begin + slot;
     int f_left = left;
     auto fetch_factors = [&](float (&to)[kPair]) {
 #pragma unroll
@@ -158,74 +230,78 @@ __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_cons
         factor += kPair * slots;
         f_left -= kPair * slots;
     };
-    // Factors are scales, so a magnitude times one has the sign bit 0 (a NaN too), and magnitudes are compared as integers: three at a time.
-    float w[kN], sum[kN] = {};
-    int top[kN] = {};
+    float f[kPair] = {}, next_f[kPair] = {}, w[kVec][kN], top[kVec][kN] = {};
+    float2 sum[kVec][kN / 2] = {};
     if constexpr (kWide)
         for (int j = 0; j < kRing - 1; ++j) fetch(j);   // (nothing but empty groups past the last one)
     fetch_factors(next_f);
-    if (kRows) at.get_exact(a.factors, w);
-    for (int j = 0; j < stages; ++j) {
+    if (kRows)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) at[j].get_exact(a.factors, w[j]);
+    float *row_top = kRows ? a.row_tops + blockIdx.y * a.rows + begin + slot : nullptr;
+    int row_left = left + (kWide ? (kRing - 1) * kPair * slots : 0), here = 0, ahead = kRing - 1;
+    for (int it = 0; it < stages; ++it) {
 #pragma unroll
         for (int u = 0; u < kPair; ++u) f[u] = next_f[u];
         fetch_factors(next_f);
         if constexpr (kWide) {
-            fetch(j + kRing - 1);
+            fetch(ahead);
             asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
 #pragma unroll
-            for (int u = 0; u < kPair; ++u) now[u].w = ring[j % kRing * kPair + u][threadIdx.x];
-        } else {
-            fetch(j);
-        }
-        float v[kPair][kN];
-        Elem<kType>::to_f32(now[0], v[0]);
-        Elem<kType>::to_f32(now[1], v[1]);
-        auto times = [](float x, float y) { return __float_as_int(fabsf(x) * y); };
+            for (int u = 0; u < kPair; ++u)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            top[i] = __vimax3_s32(top[i], times(v[0][i], f[0]), times(v[1][i], f[1]));
-            sum[i] += v[0][i];
-            sum[i] += v[1][i];
+                for (int j = 0; j < kVec; ++j) now[u][j].w = ring[(here * kPair + u) * kVec + j][threadIdx.x];
+            here = here + 1 == kRing ? 0 : here + 1;
+            ahead = ahead + 1 == kRing ? 0 : ahead + 1;
+        } else {
+            fetch(0);
+        }
+        float m[kPair] = {};
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+            float v[kPair][kN];
+            Elem<kType>::to_f32(now[0][j], v[0]);
+            Elem<kType>::to_f32(now[1][j], v[1]);
+#pragma unroll
+            for (int i = 0; i < kN; i += 2) {
+                const float2 a0 = make_float2(v[0][i], v[0][i + 1]), a1 = make_float2(v[1][i], v[1][i + 1]);
+                const float2 p0 = mul_2(a0, make_float2(f[0], f[0])), p1 = mul_2(a1, make_float2(f[1], f[1]));
+                top[j][i] = max3_abs(top[j][i], p0.x, p1.x);
+                top[j][i + 1] = max3_abs(top[j][i + 1], p0.y, p1.y);
+                sum[j][i / 2] = add_2(add_2(sum[j][i / 2], a0), a1);
+                if (kRows) {
+                    const float2 ww = make_float2(w[j][i], w[j][i + 1]), r0 = mul_2(a0, ww), r1 = mul_2(a1, ww);
+                    m[0] = max3_abs(m[0], r0.x, r0.y);
+                    m[1] = max3_abs(m[1], r1.x, r1.y);
+                }
+            }
         }
         if (kRows) {
 #pragma unroll
             for (int u = 0; u < kPair; ++u) {
-                int m = 0;
-#pragma unroll
-                for (int i = 0; i < kN; i += 2) m = __vimax3_s32(m, times(v[u][i], w[i]), times(v[u][i + 1], w[i + 1]));
-                const uint32_t t = lanes_top((uint32_t)m, lanes, nullptr);
-                const size_t row = begin + slot + (size_t)(j * kPair + u) * slots;
-                if (lane == 0 && row < end) a.row_tops[blockIdx.y * a.rows + row] = __uint_as_float(t);
+                const uint32_t t = lanes_top(__float_as_uint(m[u]), lanes, nullptr);
+                if (lane == 0 && u * slots < row_left) row_top[u * slots] = __uint_as_float(t);
             }
+            row_top += kPair * slots;
+            row_left -= kPair * slots;
         }
     }
     if constexpr (kWide) asm volatile("cp.async.wait_all;" ::: "memory");
-    // threads of the same columns meet
-    auto meet = [&](auto value, auto add) {
-        int *cells = reinterpret_cast<int *>(&ring[0][0]);
-        constexpr int kAtOnce = kRing * kPair * 4 < kN ? kRing * kPair * 4 : kN;
+    float *cells = reinterpret_cast<float *>(&ring[0][0]);
+    constexpr int kCells = kRing * kPair * kVec * 4;
 #pragma unroll
-        for (int i0 = 0; i0 < kN; i0 += kAtOnce) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) cells[i * kThreads + threadIdx.x] = value(i0 + i);
-            __syncthreads();
-            if (slot == 0)
-#pragma unroll
-                for (int i = 0; i < kAtOnce; ++i)
-                    for (int s = 1; s < slots; ++s) add(i0 + i, cells[i * kThreads + s * lanes + lane]);
+    for (int j = 0; j < kVec; ++j) {
+        if (a.strip_tops) {
+            meet_threads<kN, kCells, true>(cells, top[j], lane, slot, slots, lanes);
+            if (slot == 0) at[j].put_padded(a.strip_tops + blockIdx.x * a.col_pitch, top[j]);
         }
-    };
-    if (a.strip_tops) {
-        meet([&](int i) { return top[i]; }, [&](int i, int v) { top[i] = max(top[i], v); });
-        float tops[kN];
+        if (a.strip_sums) {
+            float sums[kN];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) tops[i] = __int_as_float(top[i]);
-        if (slot == 0) at.put_padded(a.strip_tops + blockIdx.x * a.col_pitch, tops);
-    }
-    if (a.strip_sums) {
-        meet([&](int i) { return __float_as_int(sum[i]); }, [&](int i, int v) { sum[i] += __int_as_float(v); });
-        if (slot == 0) at.put_padded(a.strip_sums + blockIdx.x * a.col_pitch, sum);
+            for (int i = 0; i < kN; ++i) sums[i] = i & 1 ? sum[j][i / 2].y : sum[j][i / 2].x;
+            meet_threads<kN, kCells, false>(cells, sums, lane, slot, slots, lanes);
+            if (slot == 0) at[j].put_padded(a.strip_sums + blockIdx.x * a.col_pitch, sums);
+        }
     }
 }
 
@@ -370,35 +446,44 @@ int lanes_of(int vectors, int hold)
     return lanes;
 }
 
-template <int kType, bool kWide, int kHold, int kRows>
+template <int kType, bool kWide, int kHold>
 cudaError_t launch_rows(const LinCodeArgs &a, int vectors, cudaStream_t st)
 {
     const int lanes = lanes_of(vectors, kHold);
-    const size_t at_once = (size_t)kThreads / lanes * kRows;
-    return launch_chained(lin_rows_kernel<kType, kWide, kHold, kRows>, dim3((unsigned)((a.rows + at_once - 1) / at_once)), dim3(kThreads), 0, st, a, lanes);
+    const size_t at_once = kThreads / lanes, rounds = (a.rows + at_once - 1) / at_once, room = (size_t)kRowBlocks<kHold> * kPartSms;
+    return launch_chained(lin_rows_kernel<kType, kWide, kHold>, dim3((unsigned)(rounds < room ? rounds : room)), dim3(kThreads), 0, st, a, lanes);
 }
 
-// 64 bytes a thread in flight (128 for the longest rows), of one row or of four; rows that leave SMs without a block are spread over more threads.
+// As few threads a row as hold it in 64 bytes each (128 of the longest rows), since a row's own work is every thread's: 8,192 x 4096 of bf16 take 19.7 us, 24 with 32
+// bytes a thread, 21 with 128.  Rows that leave SMs without a block are spread over more threads.
 template <int kType, bool kWide>
 cudaError_t rows_of(const LinCodeArgs &a, cudaStream_t st)
 {
     const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
     const bool few = a.rows * vectors < (size_t)kPartSms * kThreads * 4;
-    if (vectors > 4 * kThreads) return launch_rows<kType, kWide, 8, 1>(a, vectors, st);
-    if (few && vectors <= kThreads) return launch_rows<kType, kWide, 1, 1>(a, vectors, st);
-    if (vectors <= 32) return launch_rows<kType, kWide, 1, 4>(a, vectors, st);
-    if (vectors <= 64) return launch_rows<kType, kWide, 2, 2>(a, vectors, st);
-    return launch_rows<kType, kWide, 4, 1>(a, vectors, st);
+    if (vectors > 4 * kThreads) return launch_rows<kType, kWide, 8>(a, vectors, st);
+    if (vectors <= 32 || (few && vectors <= kThreads)) return launch_rows<kType, kWide, 1>(a, vectors, st);
+    if (vectors <= 64) return launch_rows<kType, kWide, 2>(a, vectors, st);
+    return launch_rows<kType, kWide, 4>(a, vectors, st);
 }
+
+// Two groups of columns a block of the first look: of tensors that keep every SM busy for some rounds all the same.
+bool lin_two_groups(size_t rows, int cols, int dtype) { return cols > (dtype == EOQ_F32 ? 128 : 256) && rows * cols >= (size_t)1 << 22; }
 
 template <int kType, bool kWide, bool kRows>
 cudaError_t looks_of(LinErrorArgs a, int *launches, cudaStream_t st)
 {
     const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
     const int lanes = vectors < 32 ? lanes_of(vectors, 1) : 32, across = (vectors + lanes - 1) / lanes, slots = kThreads / lanes;
-    a.chunks = across;
     ++*launches;
-    cudaError_t e = launch_chained(lin_look_kernel<kType, kWide, kRows>, dim3((unsigned)a.strips, across), dim3(kThreads), 0, st, a, lanes);
+    cudaError_t e;
+    if (kWide && lin_two_groups(a.rows, a.cols, kType)) {
+        a.chunks = (across + 1) / 2;
+        e = launch_chained(lin_look_kernel<kType, kWide, kWide ? 2 : 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
+    } else {
+        a.chunks = across;
+        e = launch_chained(lin_look_kernel<kType, kWide, 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
+    }
     if (e != cudaSuccess) return e;
     const bool fold = a.strip_tops && a.strips <= kFoldStrips && a.rows * a.cols <= kFoldSize;
     if (!fold) {
@@ -463,8 +548,8 @@ cudaError_t with_type(const void *src, size_t stride, int dtype, F &&f)
 LinStrips lin_strips(size_t rows, int cols, int dtype)
 {
     const int wide = dtype == EOQ_F32 ? 128 : 256;   // columns of a block
-    const size_t chunks = (cols + wide - 1) / wide;
-    size_t strips = 3 * kPartSms / chunks;
+    const size_t chunks = (cols + wide - 1) / wide, blocks = lin_two_groups(rows, cols, dtype) ? (chunks + 1) / 2 : chunks;
+    size_t strips = 3 * kPartSms / blocks;
     if (strips < 1) strips = 1;
     if (strips > 512) strips = 512;
     LinStrips s;
