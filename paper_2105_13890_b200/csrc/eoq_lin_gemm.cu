@@ -20,8 +20,8 @@ namespace eoq {
 namespace {
 
 constexpr int kStageK = 128;                   // bytes of the reduction in a stage
-constexpr int kUnit = 2048;                    // staging of an epilogue warp: 32 rows of 64 bytes
-constexpr int kMaxSmem = 224 * 1024;           // of dynamic shared memory: some 2.3 KB are static
+constexpr int kUnit = 2048;                    // staging: 32 rows of 64 bytes
+constexpr int kMaxSmem = 225 * 1024;           // of dynamic shared memory: some of a block's 227 KB are static
 
 template <int kN, bool kPair>
 struct GemmShape {
@@ -29,7 +29,7 @@ struct GemmShape {
     static constexpr int kEpiWarps = 16, kLoadWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1, kThreads = 32 * (kEpiWarps + 2);
     static constexpr int kSums = kPair ? 2 : 4;                           // accumulators
     static constexpr int kLeastGroups = kPair || kN == 128 ? 1 : kN == 64 ? 2 : 4;   // so that no epilogue warp has less than a chunk
-    static constexpr int kA = kTileM * kStageK, kB = kOwnN * kStageK, kStage = kA + kB, kStaging = kEpiWarps * kUnit;
+    static constexpr int kA = kTileM * kStageK, kB = kOwnN * kStageK, kStage = kA + kB, kUnits = kPair ? 1 : 2, kStaging = kUnits * kEpiWarps * kUnit;
     static constexpr int kFit = (kMaxSmem - 1024 - kStaging) / kStage, kStages = kFit < 8 ? kFit : 8;
     static constexpr int kBytes = kStages * kStage + kStaging + 1024;
     static constexpr uint32_t kColumns = kSums * kN;                      // of tensor memory
@@ -60,7 +60,8 @@ __device__ __forceinline__ void store_tile_2d(const void *map, uint32_t src, int
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kLeft) : "memory"); }
 __device__ __forceinline__ void store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -154,30 +155,33 @@ __device__ __forceinline__ void store_rows(const LinProduct &a, uint32_t unit, s
     }
 }
 
-// A warp's 32 rows and 32 columns of scaled sums to memory, by way of its staging.
-template <int kType>
-__device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorMap *map, const uint32_t (&r)[32], uint32_t unit, size_t out_row, int rows, int col0, int lane)
+// A warp's 32 rows and 32 columns of scaled sums to memory, by way of its kUnits of staging, one being filled and, of two, one on its way out.  (Of a pair's block there is
+// one: a stage of operands more, six instead of four, is worth a tenth of the time.)
+template <int kType, int kUnits>
+__device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorMap *map, const uint32_t (&r)[32], uint32_t staging, int &units, size_t out_row, int rows, int col0, int lane)
 {
     constexpr int kE = kType == EOQ_F16 || kType == EOQ_BF16 ? 2 : 4;
     auto out = [&](int col) {
+        const uint32_t unit = staging + units % kUnits * kUnit;
         if (a.tensor_store) {
             ptx::fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
                 if (col < a.n) store_tile_2d(map, unit, col, (int)out_row);
                 store_commit();
-                store_wait_read();
+                store_wait_read<kUnits - 1>();
             }
         } else {
             __syncwarp();
             store_rows<kE>(a, unit, out_row, rows, col, lane);
         }
         __syncwarp();
+        ++units;
     };
-    stage_row<kType, 0>(r, unit, lane);
+    stage_row<kType, 0>(r, staging + units % kUnits * kUnit, lane);
     out(col0);
     if constexpr (kE == 4) {
-        stage_row<kType, 1>(r, unit, lane);
+        stage_row<kType, 1>(r, staging + units % kUnits * kUnit, lane);
         out(col0 + 16);
     }
 }
@@ -215,7 +219,6 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
     using S = GemmShape<kN, kPair>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * S::kStages + 2 * S::kSums + 1];
-    __shared__ __align__(16) float scales_s[S::kEpiWarps][64];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile uint32_t abort_s;
 
@@ -346,7 +349,8 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
         }
     } else {
         const int group_warps = S::kEpiWarps / args.groups, quad = warp & 3, group = warp / group_warps, part = warp % group_warps / 4, warp_n = kN * 4 / group_warps;
-        const uint32_t scales = ptx::smem_u32(&scales_s[warp][0]), unit = staging + warp * kUnit;
+        const uint32_t staging_w = staging + warp * S::kUnits * kUnit;
+        int units = 0;
         for (int turn = 0; turns.next(which, u); ++turn) {
             if (turn % args.groups != group) continue;
             const LinProduct &p = args.p[which];
@@ -377,16 +381,21 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
                 uint32_t r[32];
                 ptx::tmem_ld_32x32(t_row + c * 32, r);
                 if (type != EOQ_I32) {
-                    scales_s[warp][lane] = s;
-                    scales_s[warp][32 + lane] = b;
+                    // (in the unit that is filled next)
+                    const uint32_t scales = staging_w + units % S::kUnits * kUnit;
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + lane * 4), "f"(s) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(scales + 128 + lane * 4), "f"(b) : "memory");
                     __syncwarp();
                     fetch(c + 1);
                 }
                 ptx::tmem_ld_wait();
-                if (type != EOQ_I32) scale_row(r, row_scale, scales);
-                if (type == EOQ_BF16) write_chunk<EOQ_BF16>(p, map_out, r, unit, out_row, rows, col0, lane);
-                else if (type == EOQ_F16) write_chunk<EOQ_F16>(p, map_out, r, unit, out_row, rows, col0, lane);
-                else write_chunk<EOQ_F32>(p, map_out, r, unit, out_row, rows, col0, lane);   // (words as they are)
+                if (type != EOQ_I32) {
+                    scale_row(r, row_scale, staging_w + units % S::kUnits * kUnit);
+                    __syncwarp();
+                }
+                if (type == EOQ_BF16) write_chunk<EOQ_BF16, S::kUnits>(p, map_out, r, staging_w, units, out_row, rows, col0, lane);
+                else if (type == EOQ_F16) write_chunk<EOQ_F16, S::kUnits>(p, map_out, r, staging_w, units, out_row, rows, col0, lane);
+                else write_chunk<EOQ_F32, S::kUnits>(p, map_out, r, staging_w, units, out_row, rows, col0, lane);   // (words as they are)
             }
             ptx::tc_fence_before();
             __syncwarp();
