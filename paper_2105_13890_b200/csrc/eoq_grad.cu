@@ -12,7 +12,7 @@ namespace eoq {
 namespace {
 
 constexpr int kThreads = 256, kFlight = 4;        // vectors of a thread in flight
-constexpr unsigned kAddBlocks = 6 * kPartSms, kScaleBlocks = 4 * kPartSms;   // of a launch, all at once on the part; the order of the sums depends on the sizes alone
+constexpr unsigned kAddBlocks = 4 * kPartSms, kScaleBlocks = 4 * kPartSms;   // of a launch, all at once on the part; the order of the sums depends on the sizes alone
 constexpr int kFewTensors = 128, kMostTensors = 1024, kRanges = 512;
 
 template <int kTensors>
@@ -36,21 +36,18 @@ struct GradSums {
     DeviceState *dev;
 };
 
-// Elements of a piece: what the threads of a block have in flight.  Pieces begin at multiples of 16 bytes: a tensor's first one has `skew` elements less.
+// Elements of a piece: what the threads of a block have in flight.  Pieces begin at multiples of 128 bytes: a tensor's first one has `skew` elements less.
 __host__ __device__ inline unsigned piece_of(int dtype) { return kFlight * kThreads * (dtype == EOQ_F32 ? 4 : 8); }
-__host__ __device__ inline unsigned skew_of(const void *p, int dtype) { return (unsigned)(reinterpret_cast<uintptr_t>(p) % 16) / (dtype == EOQ_F32 ? 4 : 2); }
+__host__ __device__ inline unsigned skew_of(const void *p, int dtype) { return (unsigned)(reinterpret_cast<uintptr_t>(p) % 128) / (dtype == EOQ_F32 ? 4 : 2); }
 
-// f(tensor, place of a piece in it) for the block's pieces, every gridDim.x-th one, forwards or backwards.  The tensor is looked up in a table of the pieces' ranges and
-// then among the few that share one: parameters are read one at a time, and a search by halves waits for ten such reads one after the other.
-template <bool kBack, int kTensors, typename F>
-__device__ __forceinline__ void for_pieces(const GradBatch<kTensors> &b, F &&f)
+// The tensor of a piece.  It is looked up in a table of the pieces' ranges and then among the few that share one: parameters are read one at a time, and a search by
+// halves waits for ten such reads one after the other.
+template <int kTensors>
+__device__ __forceinline__ int tensor_of(const GradBatch<kTensors> &b, unsigned p)
 {
-    for (unsigned k = blockIdx.x; k < b.pieces; k += gridDim.x) {
-        const unsigned p = kBack ? b.pieces - 1 - k : k;
-        int t = b.start[p >> b.shift];
-        while (t + 1 < b.num && b.first[t + 1] <= p) ++t;
-        f(t, p - b.first[t]);
-    }
+    int t = b.start[p >> b.shift];
+    while (t + 1 < b.num && b.first[t + 1] <= p) ++t;
+    return t;
 }
 
 template <typename F>
@@ -106,30 +103,57 @@ __device__ __noinline__ double wide_squares(Raw<16> r)
     return sum;
 }
 
-// This thread's vectors of piece `k` of a tensor of n elements: f(vectors, bytes from `p` to the first, whether they are a whole piece's or the first alone counts); of those whose
-// elements are not all the tensor's, g(element).
+// A piece on its way: its tensor, its place there, this thread's vectors if they are all the tensor's.
+struct Flight {
+    int t;
+    unsigned k;
+    bool whole;
+    Raw<16> r[kFlight];
+};
+// The block's pieces, every gridDim.x-th one, the next one's vectors on their way while use() has one's: two flights in turn, since a copy of what is on its way would
+// wait for it.
+template <typename F, typename G>
+__device__ __forceinline__ void two_ahead(unsigned pieces, F &&fetch, G &&use)
+{
+    Flight f, g;
+    unsigned p = blockIdx.x;
+    if (p < pieces) fetch(p, f);
+    while (p < pieces) {
+        const unsigned q = p + gridDim.x;
+        if (q < pieces) fetch(q, g);
+        use(f);
+        if (q >= pieces) break;
+        p = q + gridDim.x;
+        if (p < pieces) fetch(p, f);
+        use(g);
+    }
+}
+
+// This thread's vectors of piece `k` of tensor `t`, if they are all the tensor's.
+template <int kTensors>
+__device__ __forceinline__ bool fetch_piece(const GradBatch<kTensors> &b, int t, unsigned k, Raw<16> (&r)[kFlight])
+{
+    const int shift = b.dtype[t] == EOQ_F32 ? 2 : 1;
+    const char *p = reinterpret_cast<const char *>(b.in[t]);
+    constexpr long long kBytes = kFlight * kThreads * 16;
+    const long long begin = (long long)k * kBytes - (long long)(reinterpret_cast<uintptr_t>(p) % 128);   // (of the piece, in bytes)
+    if (begin < 0 || begin + kBytes > (long long)b.size[t] << shift) return false;
+#pragma unroll
+    for (int u = 0; u < kFlight; ++u) r[u] = *reinterpret_cast<const Raw<16> *>(p + begin + (u * kThreads + threadIdx.x) * 16);
+    return true;
+}
+// Of a piece that is not: f(vector, bytes from `p` to it) for those whose elements are, g(element) for the elements of the others.
 template <typename E, typename F, typename G>
-__device__ __forceinline__ void piece_vectors(const char *p, unsigned long long n, unsigned skew, unsigned k, F &&f, G &&g)
+__device__ __forceinline__ void piece_ends(const char *p, unsigned long long n, unsigned skew, unsigned k, F &&f, G &&g)
 {
     constexpr int kV = 16 / E::kSize;
     const long long begin = (long long)k * kFlight * kThreads * kV - skew;   // (of the piece, in elements)
-    const char *at = p + begin * E::kSize + threadIdx.x * 16;
-    Raw<16> r[kFlight];
-    if (begin >= 0 && begin + kFlight * kThreads * kV <= (long long)n) {
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) r[u] = *reinterpret_cast<const Raw<16> *>(at + u * kThreads * 16);
-        f(r, at - p, true);
-        return;
-    }
 #pragma unroll 1
     for (int u = 0; u < kFlight; ++u) {
         const long long e = begin + (long long)(u * kThreads + threadIdx.x) * kV;
-        if (e >= 0 && e + kV <= (long long)n) {
-            r[0] = *reinterpret_cast<const Raw<16> *>(at + u * kThreads * 16);
-            f(r, at + u * kThreads * 16 - p, false);
-        } else {
+        if (e >= 0 && e + kV <= (long long)n) f(*reinterpret_cast<const Raw<16> *>(p + e * E::kSize), e * E::kSize);
+        else
             for (long long i = e < 0 ? 0 : e; i < e + kV && i < (long long)n; ++i) g(i);
-        }
     }
 }
 
@@ -151,35 +175,49 @@ __device__ __forceinline__ void write_norm(double whole, float *norm, DeviceStat
 }
 
 template <int kTensors>
-__global__ void __launch_bounds__(kThreads, 6) grad_squares_kernel(const __grid_constant__ GradBatch<kTensors> b, const GradSums s)
+__global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_constant__ GradBatch<kTensors> b, const GradSums s)
 {
     __shared__ bool last_s;
     ptx::grid_dep_wait_launch_small();
     double sum = 0.0;
-    for_pieces<false>(b, [&](int t, unsigned k) {
+    two_ahead(b.pieces, [&](unsigned p, Flight &f) {
+        f.t = tensor_of(b, p);
+        f.k = p - b.first[f.t];
+        f.whole = fetch_piece(b, f.t, f.k, f.r);
+    }, [&](const Flight &f) {
+        const int t = f.t;
+        const unsigned k = f.k;
+        const bool whole = f.whole;
+        const Raw<16> (&r)[kFlight] = f.r;
         with_type(b.dtype[t], [&](auto type) {
             using E = decltype(type);
-            const char *src = reinterpret_cast<const char *>(b.in[t]);
-            piece_vectors<E>(
-                src, b.size[t], skew_of(src, b.dtype[t]), k,
-                [&](const Raw<16> (&r)[kFlight], long long, bool whole) {
-                    float q[kFlight];
-                    bool good = true;
+            if (whole) {
+                float q[kFlight];
+                bool good = true;
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) good = good_sum(q[u] = squares<E>(r[u])) && good;
+                if (good) {
+                    sum += ((double)q[0] + (double)q[1]) + ((double)q[2] + (double)q[3]);
+                } else {
 #pragma unroll
                     for (int u = 0; u < kFlight; ++u)
-                        if (u == 0 || whole) good = good_sum(q[u] = squares<E>(r[u])) && good;
-#pragma unroll
-                    for (int u = 0; u < kFlight; ++u) {
-                        if (u > 0 && !whole) break;
-                        if (good) sum += (double)q[u];
-                        else if ((r[u].w.x | r[u].w.y | r[u].w.z | r[u].w.w) != 0) sum += wide_squares<E>(r[u]);
-                    }
-                },
-                [&](long long i) {
-                    float v[1];
-                    E::to_f32(load_raw<E::kSize>(src + i * E::kSize), v);
-                    sum += (double)v[0] * v[0];
-                });
+                        if ((r[u].w.x | r[u].w.y | r[u].w.z | r[u].w.w) != 0) sum += wide_squares<E>(r[u]);
+                }
+            } else {
+                const char *src = reinterpret_cast<const char *>(b.in[t]);
+                piece_ends<E>(
+                    src, b.size[t], skew_of(src, b.dtype[t]), k,
+                    [&](const Raw<16> &v, long long) {
+                        const float q = squares<E>(v);
+                        if (good_sum(q)) sum += (double)q;
+                        else if ((v.w.x | v.w.y | v.w.z | v.w.w) != 0) sum += wide_squares<E>(v);
+                    },
+                    [&](long long i) {
+                        float v[1];
+                        E::to_f32(load_raw<E::kSize>(src + i * E::kSize), v);
+                        sum += (double)v[0] * v[0];
+                    });
+            }
         });
     });
     const double own = block_sum(sum);
@@ -202,7 +240,16 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
     const double whole = whole_norm(s.sums, s.before);
     if (blockIdx.x == 0 && s.last) write_norm(whole, s.norm, s.dev);
     const float scale = whole <= 3.402823466e38 && whole > max_norm ? (float)(max_norm / whole) : 1.0f;
-    for_pieces<true>(b, [&](int t, unsigned k) {
+    two_ahead(b.pieces, [&](unsigned back, Flight &f) {
+        const unsigned p = b.pieces - 1 - back;
+        f.t = tensor_of(b, p);
+        f.k = p - b.first[f.t];
+        f.whole = (b.in[f.t] != b.out[f.t] || scale != 1.0f) && fetch_piece(b, f.t, f.k, f.r);
+    }, [&](const Flight &f) {
+        const int t = f.t;
+        const unsigned k = f.k;
+        const bool all = f.whole;
+        const Raw<16> (&r)[kFlight] = f.r;
         if (b.in[t] == b.out[t] && scale == 1.0f) return;
         with_type(b.dtype[t], [&](auto type) {
             using E = decltype(type);
@@ -210,36 +257,34 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
             const char *src = reinterpret_cast<const char *>(b.in[t]);
             char *dst = reinterpret_cast<char *>(b.out[t]);
             const unsigned skew = skew_of(src, b.dtype[t]);
-            const bool together = skew == skew_of(dst, b.dtype[t]);
-            piece_vectors<E>(
-                src, b.size[t], skew, k,
-                [&](const Raw<16> (&r)[kFlight], long long at, bool whole_piece) {
+            const bool together = (reinterpret_cast<uintptr_t>(src) - reinterpret_cast<uintptr_t>(dst)) % 16 == 0;
+            auto put = [&](const Raw<16> &in, long long at) {
+                float v[kV];
+                E::to_f32(in, v);
 #pragma unroll
-                    for (int u = 0; u < kFlight; ++u) {
-                        if (u > 0 && !whole_piece) break;
-                        float v[kV];
-                        E::to_f32(r[u], v);
+                for (int j = 0; j < kV; ++j) v[j] *= scale;
+                if (together) {
+                    store_raw(dst + at, E::from_f32(v));
+                } else {
 #pragma unroll
-                        for (int j = 0; j < kV; ++j) v[j] *= scale;
-                        char *to = dst + at + u * kThreads * 16;
-                        const Raw<16> w = E::from_f32(v);
-                        if (together) {
-                            store_raw(to, w);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < kV; ++j) {
-                                const float one[1] = {v[j]};
-                                store_raw(to + j * E::kSize, E::from_f32(one));
-                            }
-                        }
+                    for (int j = 0; j < kV; ++j) {
+                        const float one[1] = {v[j]};
+                        store_raw(dst + at + j * E::kSize, E::from_f32(one));
                     }
-                },
-                [&](long long i) {
+                }
+            };
+            if (all) {
+                const long long begin = (long long)k * kFlight * kThreads * 16 - (long long)(skew * E::kSize);
+#pragma unroll
+                for (int u = 0; u < kFlight; ++u) put(r[u], begin + (u * kThreads + threadIdx.x) * 16);
+            } else {
+                piece_ends<E>(src, b.size[t], skew, k, put, [&](long long i) {
                     float v[1];
                     E::to_f32(*reinterpret_cast<const Raw<E::kSize> *>(src + i * E::kSize), v);
                     v[0] *= scale;
                     store_raw(dst + i * E::kSize, E::from_f32(v));
                 });
+            }
         });
     });
 }

@@ -210,6 +210,28 @@ def test_rows_without_codes(rows, c_in, c_out):
     assert torch.isnan(l.dx[2]).all() and torch.isnan(l.dw[3]).all() and not torch.isnan(l.dw[c_out - 1]).any() and not torch.isnan(l.dw[2]).any()
 
 
+@pytest.mark.parametrize("rows,c_in,c_out", [(5, 64, 48), (40, 70, 33), (700, 512, 600)])
+@pytest.mark.parametrize("dtype", list(TYPES), ids=str)
+def test_tokens_and_channels_without_codes(rows, c_in, c_out, dtype):
+    """A token that is not finite takes its row of y and all of dw with it, a channel its column of y and all of dx; nothing else, whatever stands between the codes' rows."""
+    for token, channel in ((1, None), (None, 2)):
+        l = Layer(rows, c_in, c_out, dtype)
+        if token is not None:
+            l.x[token, 5] = float("inf")
+        if channel is not None:
+            l.w[channel, 0] = float("nan")
+        status_clear()
+        l.code_weights()
+        l.forward()
+        l.backward()
+        assert status_clear() == eoq.EOQ_DEV_NONFINITE
+        l.check_codes()
+        l.check_forward()
+        l.check_backward()
+        assert bool(torch.isnan(l.dw).all()) == (token is not None) and bool(torch.isnan(l.dx).all()) == (channel is not None)
+        assert int(torch.isnan(l.y).sum()) == (c_out if token is not None else rows)
+
+
 @pytest.mark.parametrize("rows,c_in,c_out", [(6, 140000, 64), (300, 33, 140000), (270000, 40, 48)])
 def test_sums_longer_than_an_int32_holds(rows, c_in, c_out):
     """Codes at -128 (which a program may hand over), reductions beyond 131,071: the parts are exact and added in 64 bits."""
