@@ -3,8 +3,8 @@
 //
 // Bound: memory, or the launches where the gradients are few.  The tensors are cut into pieces, dealt out to blocks in turn; the squares of 16 bytes are added in
 // 32 bits and these sums in 64, in an order that depends on the sizes and alignments alone, the blocks' sums by the block that comes last.  (Every square in 64 bits:
-// the conversions hold the kernel at 1.5 T elements a second, 133 us for 200 M of two types.)  A thread has 64 bytes on their way before it uses the first: with load
-// and store in turn, that many took 240 us to scale instead of 179.
+// the conversions hold the kernel at 1.5 T elements a second, 133 us for 200 M of two types.)  A thread has 64 bytes on their way while it uses as many: with load
+// and store in turn, that many took 240 us to scale instead of 159.
 #include "eoq_block8.cuh"
 
 namespace eoq {
@@ -13,15 +13,19 @@ namespace {
 
 constexpr int kThreads = 256, kFlight = 4;        // vectors of a thread in flight
 constexpr unsigned kAddBlocks = 4 * kPartSms, kScaleBlocks = 4 * kPartSms;   // of a launch, all at once on the part; the order of the sums depends on the sizes alone
-constexpr int kFewTensors = 128, kMostTensors = 1024, kRanges = 512;
+constexpr int kFewTensors = 128, kMostTensors = 960, kRanges = 512;   // (some 32 KB of parameters at most)
 
+// What a launch has to know of a tensor, side by side: parameters come from far away the first time, a line at a time.
+struct alignas(32) GradTensor {
+    const void *in;
+    void *out;
+    unsigned long long size;
+    unsigned first;                    // pieces of the tensors before
+    int dtype;
+};
 template <int kTensors>
 struct GradBatch {                     // a launch's tensors
-    const void *in[kTensors];
-    void *out[kTensors];
-    unsigned long long size[kTensors];
-    unsigned first[kTensors];          // pieces of the tensors before
-    uint8_t dtype[kTensors];
+    GradTensor tensor[kTensors];
     uint16_t start[kRanges];           // tensor of the first piece of every range of 2^shift pieces
     unsigned pieces;
     int num, shift;
@@ -46,7 +50,7 @@ template <int kTensors>
 __device__ __forceinline__ int tensor_of(const GradBatch<kTensors> &b, unsigned p)
 {
     int t = b.start[p >> b.shift];
-    while (t + 1 < b.num && b.first[t + 1] <= p) ++t;
+    while (t + 1 < b.num && b.tensor[t + 1].first <= p) ++t;
     return t;
 }
 
@@ -133,11 +137,11 @@ __device__ __forceinline__ void two_ahead(unsigned pieces, F &&fetch, G &&use)
 template <int kTensors>
 __device__ __forceinline__ bool fetch_piece(const GradBatch<kTensors> &b, int t, unsigned k, Raw<16> (&r)[kFlight])
 {
-    const int shift = b.dtype[t] == EOQ_F32 ? 2 : 1;
-    const char *p = reinterpret_cast<const char *>(b.in[t]);
+    const int shift = b.tensor[t].dtype == EOQ_F32 ? 2 : 1;
+    const char *p = reinterpret_cast<const char *>(b.tensor[t].in);
     constexpr long long kBytes = kFlight * kThreads * 16;
     const long long begin = (long long)k * kBytes - (long long)(reinterpret_cast<uintptr_t>(p) % 128);   // (of the piece, in bytes)
-    if (begin < 0 || begin + kBytes > (long long)b.size[t] << shift) return false;
+    if (begin < 0 || begin + kBytes > (long long)b.tensor[t].size << shift) return false;
 #pragma unroll
     for (int u = 0; u < kFlight; ++u) r[u] = *reinterpret_cast<const Raw<16> *>(p + begin + (u * kThreads + threadIdx.x) * 16);
     return true;
@@ -182,14 +186,14 @@ __global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_
     double sum = 0.0;
     two_ahead(b.pieces, [&](unsigned p, Flight &f) {
         f.t = tensor_of(b, p);
-        f.k = p - b.first[f.t];
+        f.k = p - b.tensor[f.t].first;
         f.whole = fetch_piece(b, f.t, f.k, f.r);
     }, [&](const Flight &f) {
         const int t = f.t;
         const unsigned k = f.k;
         const bool whole = f.whole;
         const Raw<16> (&r)[kFlight] = f.r;
-        with_type(b.dtype[t], [&](auto type) {
+        with_type(b.tensor[t].dtype, [&](auto type) {
             using E = decltype(type);
             if (whole) {
                 float q[kFlight];
@@ -204,9 +208,9 @@ __global__ void __launch_bounds__(kThreads, 4) grad_squares_kernel(const __grid_
                         if ((r[u].w.x | r[u].w.y | r[u].w.z | r[u].w.w) != 0) sum += wide_squares<E>(r[u]);
                 }
             } else {
-                const char *src = reinterpret_cast<const char *>(b.in[t]);
+                const char *src = reinterpret_cast<const char *>(b.tensor[t].in);
                 piece_ends<E>(
-                    src, b.size[t], skew_of(src, b.dtype[t]), k,
+                    src, b.tensor[t].size, skew_of(src, b.tensor[t].dtype), k,
                     [&](const Raw<16> &v, long long) {
                         const float q = squares<E>(v);
                         if (good_sum(q)) sum += (double)q;
@@ -243,20 +247,20 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
     two_ahead(b.pieces, [&](unsigned back, Flight &f) {
         const unsigned p = b.pieces - 1 - back;
         f.t = tensor_of(b, p);
-        f.k = p - b.first[f.t];
-        f.whole = (b.in[f.t] != b.out[f.t] || scale != 1.0f) && fetch_piece(b, f.t, f.k, f.r);
+        f.k = p - b.tensor[f.t].first;
+        f.whole = (b.tensor[f.t].in != b.tensor[f.t].out || scale != 1.0f) && fetch_piece(b, f.t, f.k, f.r);
     }, [&](const Flight &f) {
         const int t = f.t;
         const unsigned k = f.k;
         const bool all = f.whole;
         const Raw<16> (&r)[kFlight] = f.r;
-        if (b.in[t] == b.out[t] && scale == 1.0f) return;
-        with_type(b.dtype[t], [&](auto type) {
+        if (b.tensor[t].in == b.tensor[t].out && scale == 1.0f) return;
+        with_type(b.tensor[t].dtype, [&](auto type) {
             using E = decltype(type);
             constexpr int kV = 16 / E::kSize;
-            const char *src = reinterpret_cast<const char *>(b.in[t]);
-            char *dst = reinterpret_cast<char *>(b.out[t]);
-            const unsigned skew = skew_of(src, b.dtype[t]);
+            const char *src = reinterpret_cast<const char *>(b.tensor[t].in);
+            char *dst = reinterpret_cast<char *>(b.tensor[t].out);
+            const unsigned skew = skew_of(src, b.tensor[t].dtype);
             const bool together = (reinterpret_cast<uintptr_t>(src) - reinterpret_cast<uintptr_t>(dst)) % 16 == 0;
             auto put = [&](const Raw<16> &in, long long at) {
                 float v[kV];
@@ -278,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
 #pragma unroll
                 for (int u = 0; u < kFlight; ++u) put(r[u], begin + (u * kThreads + threadIdx.x) * 16);
             } else {
-                piece_ends<E>(src, b.size[t], skew, k, put, [&](long long i) {
+                piece_ends<E>(src, b.tensor[t].size, skew, k, put, [&](long long i) {
                     float v[1];
                     E::to_f32(*reinterpret_cast<const Raw<E::kSize> *>(src + i * E::kSize), v);
                     v[0] *= scale;
@@ -297,18 +301,18 @@ unsigned batch_of(const GradList &l, int first, unsigned most, GradBatch<kTensor
     b.pieces = 0;
     for (int i = first; i < l.num && i < first + kTensors; ++i) {
         if (l.size[i] == 0) continue;
-        b.in[b.num] = l.in[i];
-        b.out[b.num] = l.out ? l.out[i] : const_cast<void *>(l.in[i]);
-        b.size[b.num] = l.size[i];
-        b.dtype[b.num] = (uint8_t)l.dtype[i];
-        b.first[b.num] = b.pieces;
+        b.tensor[b.num].in = l.in[i];
+        b.tensor[b.num].out = l.out ? l.out[i] : const_cast<void *>(l.in[i]);
+        b.tensor[b.num].size = l.size[i];
+        b.tensor[b.num].dtype = l.dtype[i];
+        b.tensor[b.num].first = b.pieces;
         b.pieces += (unsigned)((l.size[i] + skew_of(l.in[i], l.dtype[i]) + piece_of(l.dtype[i]) - 1) / piece_of(l.dtype[i]));
         ++b.num;
     }
     b.shift = 0;
     while (b.pieces >> b.shift >= kRanges) ++b.shift;
     for (unsigned r = 0, t = 0; r << b.shift < b.pieces; ++r) {
-        while ((int)t + 1 < b.num && b.first[t + 1] <= r << b.shift) ++t;
+        while ((int)t + 1 < b.num && b.tensor[t + 1].first <= r << b.shift) ++t;
         b.start[r] = (uint16_t)t;
     }
     return b.pieces == 0 ? 1 : b.pieces < most ? b.pieces : most;   // (a launch without elements has a block that adds nothing)
