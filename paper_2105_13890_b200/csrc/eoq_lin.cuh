@@ -54,55 +54,90 @@ __device__ __forceinline__ uint32_t raw_top(const Raw<16> &r, uint32_t top)
     }
 }
 
-// A thread's 16 bytes of a row.  kWide: kN neighbouring elements, a vector; otherwise (rows that are not 16-byte aligned) kN elements `lanes` columns apart, so
-// that a warp's loads of each are neighbouring.  Threads of a row share groups of lanes * kN columns.
-template <int kType, bool kWide>
+// A thread's 16 bytes of a row, as its rows' alignment kU allows.  16: a vector of kN neighbouring elements.  8 or 4: pieces of as many bytes, `lanes` pieces apart, so that a
+// warp's loads of each are neighbouring.  2 (16-bit elements in odd rows): the aligned words around kN neighbouring elements, shifted into place; a word is only touched
+// when it holds part of the row.  Threads of a row share groups of lanes * kN columns.
+template <int kType, int kU>
 struct Span {
-    static constexpr int kE = Elem<kType>::kSize, kN = 16 / kE;
-    int first, step, cols;   // the thread's column 0 of a group; to its next one; columns of a row
+    static constexpr int kE = Elem<kType>::kSize, kN = 16 / kE, kPiece = kU == 2 ? kN : kU / kE;   // elements of a piece
+    static constexpr bool kWhole = kPiece == kN;
+    int first, step, cols;   // the thread's first column of a group; from piece to piece; columns of a row
     Span() = default;
-    __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_)
-        : first(group * lanes * kN + (kWide ? lane * kN : lane)), step(kWide ? 1 : lanes), cols(cols_)
-    {
-    }
-    __device__ __forceinline__ int column(int i) const { return first + i * step; }
+    __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_) : first(group * lanes * kN + lane * kPiece), step(lanes * kPiece), cols(cols_) {}
+    __device__ __forceinline__ int column(int i) const { return first + i / kPiece * step + i % kPiece; }
     __device__ __forceinline__ bool any() const { return first < cols; }
+    // elements from column c on, fewer than kCount, last one first (zeros behind them): for ends of rows
+    template <int kCount>
+    __device__ __forceinline__ void tail(const char *row, int c0, uint32_t (&w)[kCount * kE / 4]) const
+    {
+#pragma unroll 1
+        for (int c = cols - 1; c >= c0; --c) {
+            const uint32_t v = raw_word(load_raw<kE>(row + (size_t)c * kE), 0);
+#pragma unroll
+            for (int k = kCount * kE / 4 - 1; k > 0; --k) w[k] = kE == 4 ? w[k - 1] : __funnelshift_l(w[k - 1], w[k], 16);
+            w[0] = kE == 4 ? v : w[0] << 16 | v;
+        }
+    }
     // zeros behind the row's end
     __device__ __forceinline__ Raw<16> get(const char *row, bool mine) const
     {
-        if (kWide && mine && first + kN <= cols) return load_raw<16>(row + (size_t)first * kE);
         Raw<16> r = zero_raw<16>();
-        if (!kWide) {
-            uint32_t w[kN];
+        if (!mine || first >= cols) return r;
+        if constexpr (kU == 16) {
+            if (first + kN <= cols) return load_raw<16>(row + (size_t)first * kE);
+            uint32_t w[4] = {};
+            tail<kN>(row, first, w);
+            r.w = make_uint4(w[0], w[1], w[2], w[3]);
+        } else if constexpr (kU == 2) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(row) + (size_t)first * kE, end = reinterpret_cast<uintptr_t>(row) + (size_t)cols * kE, from = p & ~(uintptr_t)3;
+            uint32_t w[5];
 #pragma unroll
-            for (int i = 0; i < kN; ++i) w[i] = mine && column(i) < cols ? raw_word(load_raw<kE>(row + (size_t)column(i) * kE), 0) : 0u;
+            for (int k = 0; k < 5; ++k) w[k] = from + 4 * k < end ? __ldg(reinterpret_cast<const uint32_t *>(from) + k) : 0u;
+            const int shift = 8 * (int)(p & 2), left = cols - first;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) set_word(r, i, kE == 4 ? w[i] : w[2 * i % kN] | w[(2 * i + 1) % kN] << 16);
-        } else if (mine) {
-            // the last elements of a row whose end cuts a vector, last one first
-#pragma unroll 1
-            for (int c = cols - 1; c >= first; --c) {
-                const uint32_t w = raw_word(load_raw<kE>(row + (size_t)c * kE), 0);
-                if (kE == 4) r.w = make_uint4(w, r.w.x, r.w.y, r.w.z);
-                else r.w = make_uint4(r.w.x << 16 | w, __funnelshift_l(r.w.x, r.w.y, 16), __funnelshift_l(r.w.y, r.w.z, 16), __funnelshift_l(r.w.z, r.w.w, 16));
+            for (int k = 0; k < 4; ++k) {
+                w[k] = __funnelshift_r(w[k], w[k + 1], shift);
+                if (left < 2 * k + 2) w[k] = left <= 2 * k ? 0u : w[k] & 0xffffu;
+            }
+            r.w = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kN / kPiece; ++j) {
+                const int c = first + j * step;
+                uint32_t w[kU / 4] = {};
+                if (c + kPiece <= cols) {
+                    const Raw<kU> v = load_raw<kU>(row + (size_t)c * kE);
+#pragma unroll
+                    for (int k = 0; k < kU / 4; ++k) w[k] = raw_word(v, k);
+                } else if (c < cols) {
+                    tail<kPiece>(row, c, w);
+                }
+#pragma unroll
+                for (int k = 0; k < kU / 4; ++k) set_word(r, j * (kU / 4) + k, w[k]);
             }
         }
         return r;
     }
-    // of an array with an element for each column (whole vectors of them: padded to eight); nothing (ones) behind the end
+    // of an array with an element for each column, in whole pieces (padded to eight); ones of nothing behind the end
     __device__ __forceinline__ void get_padded(const float *p, float (&v)[kN]) const
     {
-        if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < kN; i += 4) {
-                const float4 w = any() ? __ldg(reinterpret_cast<const float4 *>(p + first + i)) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
-                v[i] = w.x;
-                v[i + 1] = w.y;
-                v[i + 2] = w.z;
-                v[i + 3] = w.w;
+        for (int j = 0; j < kN / kPiece; ++j) {
+            const int c = first + j * step;
+            const bool in = c < cols;
+            if constexpr (kPiece % 4 == 0) {
+#pragma unroll
+                for (int i = 0; i < kPiece; i += 4) {
+                    const float4 w = in ? __ldg(reinterpret_cast<const float4 *>(p + c + i)) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                    v[j * kPiece + i] = w.x;
+                    v[j * kPiece + i + 1] = w.y;
+                    v[j * kPiece + i + 2] = w.z;
+                    v[j * kPiece + i + 3] = w.w;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) v[j * kPiece + i] = in ? __ldg(p + c + i) : 1.0f;
             }
-        } else {
-            get_exact(p, v);
         }
     }
     __device__ __forceinline__ void get_exact(const float *p, float (&v)[kN]) const
@@ -112,12 +147,18 @@ struct Span {
     }
     __device__ __forceinline__ void put_padded(float *p, const float (&v)[kN]) const
     {
-        if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < kN; i += 4)
-                if (any()) *reinterpret_cast<float4 *>(p + first + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-        } else {
-            put_exact(p, v);
+        for (int j = 0; j < kN / kPiece; ++j) {
+            const int c = first + j * step;
+            if (c >= cols) continue;
+            if constexpr (kPiece % 4 == 0) {
+#pragma unroll
+                for (int i = 0; i < kPiece; i += 4)
+                    *reinterpret_cast<float4 *>(p + c + i) = make_float4(v[j * kPiece + i], v[j * kPiece + i + 1], v[j * kPiece + i + 2], v[j * kPiece + i + 3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) p[c + i] = v[j * kPiece + i];
+            }
         }
     }
     __device__ __forceinline__ void put_exact(float *p, const float (&v)[kN]) const
@@ -129,14 +170,23 @@ struct Span {
     // the low bytes of q as codes (a row of codes is whole pieces of 16 bytes)
     __device__ __forceinline__ void put_codes(int8_t *row, const uint32_t (&q)[kN]) const
     {
-        if constexpr (kWide) {
-            if (any()) store_raw(row + first, pack_codes(q));
-        } else {
 #pragma unroll
-            for (int i = 0; i < kN; ++i)
-                if (column(i) < cols) row[column(i)] = (int8_t)q[i];
+        for (int j = 0; j < kN / kPiece; ++j) {
+            const int c = first + j * step;
+            if (c >= cols) continue;
+            uint32_t one[kPiece];
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) one[i] = q[j * kPiece + i];
+            store_raw(row + c, pack_codes(one));
         }
     }
 };
+
+// kU of a tensor's rows
+inline int row_alignment(const void *src, size_t stride, int e)
+{
+    const size_t at = reinterpret_cast<uintptr_t>(src) | stride * e;
+    return at % 16 == 0 ? 16 : at % 8 == 0 ? 8 : at % 4 == 0 ? 4 : 2;
+}
 
 }  // namespace eoq

@@ -40,10 +40,10 @@ __device__ __forceinline__ uint32_t lanes_top(uint32_t top, int lanes, uint32_t 
 }
 
 // Rows: kHold groups of a row at a time, the next row's on their way meanwhile.
-template <int kType, bool kWide, int kHold>
+template <int kType, int kU, int kHold>
 __global__ void __launch_bounds__(kThreads, kRowBlocks<kHold>) lin_rows_kernel(const __grid_constant__ LinCodeArgs a, const int lanes)
 {
-    using S = Span<kType, kWide>;
+    using S = Span<kType, kU>;
     constexpr int kN = S::kN;
     __shared__ uint32_t cells[2][kThreads / 32];
     ptx::grid_dep_wait_launch_small();
@@ -179,11 +179,11 @@ __device__ __forceinline__ void meet_threads(float *cells, float (&mine)[kN], in
 // Block (x, y): strip x of the rows, kVec groups of the columns from y * kVec on, `lanes` (at most 32) threads a row.  kRows: the rows' maxima too.
 // Vectors come in by asynchronous copies, each read back by the thread that copied it, some rows ahead.  What bounds it is issue: two vectors of a row a thread share the
 // row's own work (its factor, its maximum, what is ahead).  16,384 x 4096 of bf16: 36 us; 43 with one.
-template <int kType, bool kWide, int kVec, bool kRows>
+template <int kType, int kU, int kVec, bool kRows>
 __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_constant__ LinErrorArgs a, const int lanes)
 {
-    using S = Span<kType, kWide>;
-    constexpr int kN = S::kN, kRing = kWide ? (kVec == 2 ? 3 : 4) : 1, kPair = 2;   // stages of two rows
+    using S = Span<kType, kU>;
+    constexpr int kN = S::kN, kRing = kU == 16 ? (kVec == 2 ? 3 : 4) : 1, kPair = 2;   // stages of two rows
     __shared__ __align__(16) uint4 ring[kRing * kPair * kVec][kThreads];
     ptx::grid_dep_wait_launch_small();
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes;
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_cons
             const char *row = mine ? src + u * step : reinterpret_cast<const char *>(a.src);
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {
-                if constexpr (kWide) {
+                if constexpr (kU == 16) {
                     const int n = mine ? bytes[j] : 0;
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ptx::smem_u32(&ring[(slot_ * kPair + u) * kVec + j][threadIdx.x])),
                                  "l"(row + (n ? (size_t)at[j].first * S::kE : 0)), "r"(n)
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_cons
         }
         src += kPair * step;
         left -= kPair * slots;
-        if constexpr (kWide) asm volatile("cp.async.commit_group;" ::: "memory");
+        if constexpr (kU == 16) asm volatile("cp.async.commit_group;" ::: "memory");
     };
     const float *factor = a.row_factors + begin + slot;
     int f_left = left;
@@ -232,19 +232,19 @@ __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_cons
     };
     float f[kPair] = {}, next_f[kPair] = {}, w[kVec][kN], top[kVec][kN] = {};
     float2 sum[kVec][kN / 2] = {};
-    if constexpr (kWide)
+    if constexpr (kU == 16)
         for (int j = 0; j < kRing - 1; ++j) fetch(j);   // (nothing but empty groups past the last one)
     fetch_factors(next_f);
     if (kRows)
 #pragma unroll
         for (int j = 0; j < kVec; ++j) at[j].get_exact(a.factors, w[j]);
     float *row_top = kRows ? a.row_tops + blockIdx.y * a.rows + begin + slot : nullptr;
-    int row_left = left + (kWide ? (kRing - 1) * kPair * slots : 0), here = 0, ahead = kRing - 1;
+    int row_left = left + (kU == 16 ? (kRing - 1) * kPair * slots : 0), here = 0, ahead = kRing - 1;
     for (int it = 0; it < stages; ++it) {
 #pragma unroll
         for (int u = 0; u < kPair; ++u) f[u] = next_f[u];
         fetch_factors(next_f);
-        if constexpr (kWide) {
+        if constexpr (kU == 16) {
             fetch(ahead);
             asm volatile("cp.async.wait_group %0;" ::"n"(kRing - 1) : "memory");
 #pragma unroll
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_cons
             row_left -= kPair * slots;
         }
     }
-    if constexpr (kWide) asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (kU == 16) asm volatile("cp.async.wait_all;" ::: "memory");
     float *cells = reinterpret_cast<float *>(&ring[0][0]);
     constexpr int kCells = kRing * kPair * kVec * 4;
 #pragma unroll
@@ -358,10 +358,10 @@ __global__ void __launch_bounds__(kJoinThreads) lin_join_looks_kernel(const __gr
 
 // The second look.  Block (x, y): `range` rows from x * range on, group y of the columns.  kFold: what the parts left is put together here, column by
 // column and row by row, by every thread that needs it.
-template <int kType, bool kWide, bool kRows, bool kFold>
+template <int kType, int kU, bool kRows, bool kFold>
 __global__ void __launch_bounds__(kThreads, 3) lin_codes_kernel(const __grid_constant__ LinErrorArgs a, const int lanes, const size_t range)
 {
-    using S = Span<kType, kWide>;
+    using S = Span<kType, kU>;
     constexpr int kN = S::kN;
     ptx::grid_dep_wait_launch_small();
     const int lane = threadIdx.x % lanes, slot = threadIdx.x / lanes, slots = kThreads / lanes;
@@ -446,43 +446,43 @@ int lanes_of(int vectors, int hold)
     return lanes;
 }
 
-template <int kType, bool kWide, int kHold>
+template <int kType, int kU, int kHold>
 cudaError_t launch_rows(const LinCodeArgs &a, int vectors, cudaStream_t st)
 {
     const int lanes = lanes_of(vectors, kHold);
     const size_t at_once = kThreads / lanes, rounds = (a.rows + at_once - 1) / at_once, room = (size_t)kRowBlocks<kHold> * kPartSms;
-    return launch_chained(lin_rows_kernel<kType, kWide, kHold>, dim3((unsigned)(rounds < room ? rounds : room)), dim3(kThreads), 0, st, a, lanes);
+    return launch_chained(lin_rows_kernel<kType, kU, kHold>, dim3((unsigned)(rounds < room ? rounds : room)), dim3(kThreads), 0, st, a, lanes);
 }
 
 // As few threads a row as hold it in 64 bytes each (128 of the longest rows), since a row's own work is every thread's: 8,192 x 4096 of bf16 take 19.7 us, 24 with 32
 // bytes a thread, 21 with 128.  Rows that leave SMs without a block are spread over more threads.
-template <int kType, bool kWide>
+template <int kType, int kU>
 cudaError_t rows_of(const LinCodeArgs &a, cudaStream_t st)
 {
-    const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
+    const int vectors = (a.cols + Span<kType, kU>::kN - 1) / Span<kType, kU>::kN;
     const bool few = a.rows * vectors < (size_t)kPartSms * kThreads * 4;
-    if (vectors > 4 * kThreads) return launch_rows<kType, kWide, 8>(a, vectors, st);
-    if (vectors <= 32 || (few && vectors <= kThreads)) return launch_rows<kType, kWide, 1>(a, vectors, st);
-    if (vectors <= 64) return launch_rows<kType, kWide, 2>(a, vectors, st);
-    return launch_rows<kType, kWide, 4>(a, vectors, st);
+    if (vectors > 4 * kThreads) return launch_rows<kType, kU, 8>(a, vectors, st);
+    if (vectors <= 32 || (few && vectors <= kThreads)) return launch_rows<kType, kU, 1>(a, vectors, st);
+    if (vectors <= 64) return launch_rows<kType, kU, 2>(a, vectors, st);
+    return launch_rows<kType, kU, 4>(a, vectors, st);
 }
 
 // Two groups of columns a block of the first look: of tensors that keep every SM busy for some rounds all the same.
 bool lin_two_groups(size_t rows, int cols, int dtype) { return cols > (dtype == EOQ_F32 ? 128 : 256) && rows * cols >= (size_t)1 << 22; }
 
-template <int kType, bool kWide, bool kRows>
+template <int kType, int kU, bool kRows>
 cudaError_t looks_of(LinErrorArgs a, int *launches, cudaStream_t st)
 {
-    const int vectors = (a.cols + Span<kType, kWide>::kN - 1) / Span<kType, kWide>::kN;
+    const int vectors = (a.cols + Span<kType, kU>::kN - 1) / Span<kType, kU>::kN;
     const int lanes = vectors < 32 ? lanes_of(vectors, 1) : 32, across = (vectors + lanes - 1) / lanes, slots = kThreads / lanes;
     ++*launches;
     cudaError_t e;
-    if (kWide && lin_two_groups(a.rows, a.cols, kType)) {
+    if (kU == 16 && lin_two_groups(a.rows, a.cols, kType)) {
         a.chunks = (across + 1) / 2;
-        e = launch_chained(lin_look_kernel<kType, kWide, kWide ? 2 : 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
+        e = launch_chained(lin_look_kernel<kType, kU, kU == 16 ? 2 : 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
     } else {
         a.chunks = across;
-        e = launch_chained(lin_look_kernel<kType, kWide, 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
+        e = launch_chained(lin_look_kernel<kType, kU, 1, kRows>, dim3((unsigned)a.strips, a.chunks), dim3(kThreads), 0, st, a, lanes);
     }
     if (e != cudaSuccess) return e;
     const bool fold = a.strip_tops && a.strips <= kFoldStrips && a.rows * a.cols <= kFoldSize;
@@ -497,18 +497,18 @@ cudaError_t looks_of(LinErrorArgs a, int *launches, cudaStream_t st)
     while (range > (size_t)slots && (a.rows + range - 1) / range * across < 4 * kPartSms) range /= 2;
     const dim3 grid((unsigned)((a.rows + range - 1) / range), across);
     ++*launches;
-    if (fold) return launch_chained(lin_codes_kernel<kType, kWide, kRows, true>, grid, dim3(kThreads), 0, st, a, lanes, range);
-    return launch_chained(lin_codes_kernel<kType, kWide, kRows, false>, grid, dim3(kThreads), 0, st, a, lanes, range);
+    if (fold) return launch_chained(lin_codes_kernel<kType, kU, kRows, true>, grid, dim3(kThreads), 0, st, a, lanes, range);
+    return launch_chained(lin_codes_kernel<kType, kU, kRows, false>, grid, dim3(kThreads), 0, st, a, lanes, range);
 }
 
-template <int kType, bool kWide>
+template <int kType, int kU>
 cudaError_t errors_of(LinErrorArgs a, int *launches, cudaStream_t st)
 {
     const LinStrips s = lin_strips(a.rows, a.cols, kType);
     a.strip = s.rows;
     a.strips = (int)((a.rows + s.rows - 1) / s.rows);
     a.col_pitch = s.col_pitch;
-    if (a.codes && a.strip_tops) return looks_of<kType, kWide, true>(a, launches, st);
+    if (a.codes && a.strip_tops) return looks_of<kType, kU, true>(a, launches, st);
     if (a.codes) {
         LinCodeArgs r = {};
         r.src = a.src;
@@ -521,18 +521,20 @@ cudaError_t errors_of(LinErrorArgs a, int *launches, cudaStream_t st)
         r.scales = a.scales;
         r.dev = a.dev;
         ++*launches;
-        const cudaError_t e = rows_of<kType, kWide>(r, st);
+        const cudaError_t e = rows_of<kType, kU>(r, st);
         if (e != cudaSuccess) return e;
     }
-    return a.strip_tops || a.strip_sums ? looks_of<kType, kWide, false>(a, launches, st) : cudaSuccess;
+    return a.strip_tops || a.strip_sums ? looks_of<kType, kU, false>(a, launches, st) : cudaSuccess;
 }
 
 template <int kType, typename F>
 cudaError_t with_width(const void *src, size_t stride, F &&f)
 {
-    const size_t at = reinterpret_cast<uintptr_t>(src) | stride * Elem<kType>::kSize;
-    if (at % 16 == 0) return f(std::integral_constant<int, kType>(), std::true_type());
-    return f(std::integral_constant<int, kType>(), std::false_type());
+    const int u = row_alignment(src, stride, Elem<kType>::kSize);
+    if (u == 16) return f(std::integral_constant<int, kType>(), std::integral_constant<int, 16>());
+    if (u == 8) return f(std::integral_constant<int, kType>(), std::integral_constant<int, 8>());
+    if (u == 4 || kType == EOQ_F32) return f(std::integral_constant<int, kType>(), std::integral_constant<int, 4>());
+    return f(std::integral_constant<int, kType>(), std::integral_constant<int, kType == EOQ_F32 ? 4 : 2>());
 }
 template <typename F>
 cudaError_t with_type(const void *src, size_t stride, int dtype, F &&f)

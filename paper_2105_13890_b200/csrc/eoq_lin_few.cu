@@ -33,7 +33,7 @@ __device__ __forceinline__ void mma_16x8x32(int (&d)[4], uint32_t a0, uint32_t a
 }
 
 // kType: of x, y.  kCode: x is coded here.
-template <int kType, bool kCode, bool kWide>
+template <int kType, bool kCode, int kU>
 __global__ void __launch_bounds__(kThreads, 2) lin_few_kernel(const __grid_constant__ FewArgs f)
 {
     using E = Elem<kType>;
@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 2) lin_few_kernel(const __grid_const
 
     if constexpr (kCode) {
         // a token has a share of the warps
-        using S = Span<kType, kWide>;
+        using S = Span<kType, kU>;
         int tokens = 1;
         while (tokens < a.rows) tokens *= 2;
         const int lanes = kThreads / tokens, token = threadIdx.x / lanes, at_lane = threadIdx.x % lanes, span_groups = (a.c_in + lanes * S::kN - 1) / (lanes * S::kN);
@@ -167,20 +167,22 @@ __global__ void __launch_bounds__(kThreads, 2) lin_few_kernel(const __grid_const
     }
 }
 
-template <int kType, bool kCode, bool kWide>
+template <int kType, bool kCode, int kU>
 cudaError_t launch(const FewArgs &f, int sm_count, cudaStream_t st)
 {
     const int per_block = 16 * (kWarps / f.k_warps), units = (f.l.c_out + per_block - 1) / per_block, room = 2 * sm_count;
-    return launch_chained(lin_few_kernel<kType, kCode, kWide>, dim3(units < room ? units : room), dim3(kThreads), (size_t)f.l.rows * f.pitch_s, st, f);
+    return launch_chained(lin_few_kernel<kType, kCode, kU>, dim3(units < room ? units : room), dim3(kThreads), (size_t)f.l.rows * f.pitch_s, st, f);
 }
 
 template <int kType>
 cudaError_t of_type(const FewArgs &f, int sm_count, cudaStream_t st)
 {
     const LinFewArgs &a = f.l;
-    if (!a.x) return launch<kType, false, true>(f, sm_count, st);
-    const size_t at = reinterpret_cast<uintptr_t>(a.x) | a.x_stride * Elem<kType>::kSize;
-    return at % 16 == 0 ? launch<kType, true, true>(f, sm_count, st) : launch<kType, true, false>(f, sm_count, st);
+    if (!a.x) return launch<kType, false, 16>(f, sm_count, st);
+    const int u = row_alignment(a.x, a.x_stride, Elem<kType>::kSize);
+    if (u == 16) return launch<kType, true, 16>(f, sm_count, st);
+    if (u >= 4) return launch<kType, true, 4>(f, sm_count, st);
+    return launch<kType, true, kType == EOQ_F32 ? 4 : 2>(f, sm_count, st);
 }
 
 // the token's codes, then room that has the tokens begin 16 bytes off one another in the banks
