@@ -169,7 +169,6 @@ __device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorM
             if (lane == 0) {
                 if (col < a.n) store_tile_2d(map, unit, col, (int)out_row);
                 store_commit();
-                store_wait_read<kUnits - 1>();
             }
         } else {
             __syncwarp();
@@ -181,6 +180,8 @@ __device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorM
     stage_row<kType, 0>(r, staging + units % kUnits * kUnit, lane);
     out(col0);
     if constexpr (kE == 4) {
+        if (lane == 0) store_wait_read<kUnits - 1>();
+        __syncwarp();
         stage_row<kType, 1>(r, staging + units % kUnits * kUnit, lane);
         out(col0 + 16);
     }
@@ -380,6 +381,9 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
                 const int col0 = first_col + c * 32;
                 uint32_t r[32];
                 ptx::tmem_ld_32x32(t_row + c * 32, r);
+                // what went out of the next unit before has been read by now
+                if (lane == 0) store_wait_read<S::kUnits - 1>();
+                __syncwarp();
                 if (type != EOQ_I32) {
                     // (in the unit that is filled next)
                     const uint32_t scales = staging_w + units % S::kUnits * kUnit;
