@@ -474,12 +474,12 @@ struct Plan {
     int catch_up;
 };
 
-// Cycles of a stage of a tile of width 32 << w: its MMAs, or what a block's copies take, two cycles for each line of 128 bytes that a row of a tile lies in.
+// Cycles of a stage of a tile of width 32 << w: its MMAs, or what a block's copies take, two cycles for a row of a tile, 4.5 where rows straddle lines of 128 bytes.
 double stage_cycles(const LinProduct &p, int w)
 {
     static const double kMma[4] = {230.0, 230.0, 280.0, 520.0};
     const int own_n = w == 3 ? 128 : 32 << w;
-    auto lines = [](size_t pitch) { return pitch % 128 == 0 || 128 % pitch == 0 ? 1.0 : 1.75; };
+    auto lines = [](size_t pitch) { return pitch % 128 == 0 || 128 % pitch == 0 ? 1.0 : 2.25; };
     const double copies = 2.0 * ((p.a_mn || p.m >= 128 ? 128.0 : p.m) * lines(p.pitch_a) + (p.b_mn ? 128.0 : own_n) * lines(p.pitch_b));
     return copies > kMma[w] ? copies : kMma[w];
 }
@@ -517,8 +517,9 @@ Plan plan_of(LinProduct *p, int count)
                 q[i].splits = (q[i].k_stages + q[i].stages_per_split - 1) / q[i].stages_per_split;
                 if (q[i].splits > 1) splits_any = true;
                 q[i].units = (int)(tiles * q[i].splits);
-                unit[i] = (double)q[i].stages_per_split * stage_cycles(q[i], w);
-                if (unit[i] < 20.0 * tile_n + 400.0) unit[i] = 20.0 * tile_n + 400.0;   // (its epilogue)
+                // A tile's epilogue takes 24 cycles a column beside the next tile's stages, of single blocks not quite beside them.
+                const double stages = (double)q[i].stages_per_split * stage_cycles(q[i], w), epilogue = 24.0 * tile_n + (blocks == 2 ? 400.0 : 200.0 + 0.5 * stages);
+                unit[i] = stages > epilogue ? stages : epilogue;
                 work[i] = unit[i] * q[i].units;
                 if (q[i].splits > 1) join += 7000.0 + (double)q[i].splits * q[i].m * q[i].n * 4.0 * 2.0 / 2500.0;
             }
