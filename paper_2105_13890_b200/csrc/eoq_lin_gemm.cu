@@ -174,6 +174,7 @@ __device__ __forceinline__ void write_chunk(const LinProduct &a, const CUtensorM
         } else {
             __syncwarp();
             store_rows<kE>(a, unit, out_row, rows, col, lane);
+            if (lane == 0) store_commit();   // (an empty group: what is waited for counts one for each unit, and the unit before may be another product's, on its way out)
         }
         __syncwarp();
         ++units;
