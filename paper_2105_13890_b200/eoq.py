@@ -99,8 +99,8 @@ def lin_pitch(cols: int) -> int:
 
 
 class grad_list:
-    """The gradients of a step as eoq_grad_norm and eoq_grad_clip take them: contiguous tensors, and where the clipped ones go (None: in place).  Holds on to the
-    tensors; a program whose gradients keep their places makes one and uses it in every step."""
+    """The gradients of a step as eoq_grad_norm and eoq_grad_clip take them: contiguous tensors of one device, and where the clipped ones go (None: in place).  Holds on
+    to the tensors; a program whose gradients keep their places makes one and uses it in every step."""
 
     def __init__(self, tensors: Sequence, out: Optional[Sequence] = None):
         self.tensors, self.out = list(tensors), None if out is None else list(out)
@@ -113,6 +113,10 @@ class grad_list:
         types = {"torch.float32": EOQ_F32, "torch.float16": EOQ_F16, "torch.bfloat16": EOQ_BF16}
         if any(str(t.dtype) not in types for t in self.tensors):
             raise TypeError("grad_list: gradients in fp32, fp16 or bf16")
+        devices = {t.get_device() for t in self.tensors + (self.out or []) if t.numel()}
+        if len(devices) > 1:
+            raise ValueError("grad_list: tensors of one device")
+        self.device = devices.pop() if devices else None   # (-1: host memory, which the calls refuse; None: no elements)
         self.g = (C.c_void_p * self.num)(*[t.data_ptr() for t in self.tensors])
         self.to = None if out is None else (C.c_void_p * self.num)(*[t.data_ptr() for t in self.out])
         self.sizes = (C.c_size_t * self.num)(*[t.numel() for t in self.tensors])
@@ -245,6 +249,16 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     return _current_stream()
+
+
+def _current_device() -> int:
+    """torch's current device, by the getter alone from the second call on."""
+    global _current_device
+    import torch
+
+    value = torch.cuda.current_device()
+    _current_device = torch._C._cuda_getDevice
+    return value
 
 
 def _current_stream() -> int:
@@ -626,7 +640,15 @@ def eoq_grad_workspace_size(grads: grad_list) -> int:
     return out.value
 
 
+def _readable(grads: grad_list, what: str) -> None:
+    """The kernels read the tensors by their addresses: these have to be the current device's, which the calls check to be the handle's too."""
+    device = getattr(grads, "device", None)
+    if device is not None and (device < 0 or device != _current_device()):
+        raise ValueError(what + ": gradients in host memory" if device < 0 else what + ": gradients of another device than the current one")
+
+
 def eoq_grad_norm(handle, grads: grad_list, norm, workspace, stream=None, check: bool = True) -> int:
+    _readable(grads, "eoq_grad_norm")
     st = (_native or native()).grad_clip(handle, 0, grads.num, grads.g, None, grads.sizes, grads.dtypes, 0.0, norm, workspace, _stream(stream))
     if check:
         _check(st, "eoq_grad_norm")
@@ -634,6 +656,7 @@ def eoq_grad_norm(handle, grads: grad_list, norm, workspace, stream=None, check:
 
 
 def eoq_grad_clip(handle, grads: grad_list, max_norm, norm, workspace, stream=None, check: bool = True) -> int:
+    _readable(grads, "eoq_grad_clip")
     st = (_native or native()).grad_clip(handle, 1, grads.num, grads.g, grads.to, grads.sizes, grads.dtypes, max_norm, norm, workspace, _stream(stream))
     if check:
         _check(st, "eoq_grad_clip")
