@@ -515,7 +515,7 @@ EOQ_API int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const voi
  *   u[t][o] = dy[t][o] w_scales[o], rounded to fp32, coded by tokens:   dx[t][i] = scale_u[t] sum over o of code_u[t][o] w_codes[o][i]
  *   v[t][o] = dy[t][o] x_scales[t], rounded to fp32, coded by channels: dw[o][i] = scale_v[o] sum over t of code_v[t][o] x_codes[t][i]  (fp32 [c_out][c_in], 16-byte aligned)
  *   dbias[o] = sum over t of dy[t][o]  (fp32).  Each of the three may be NULL; w_codes and w_scales are needed for dx, x_codes and x_scales for dw.
- * Integer sums are exact at any length; an output is rounded four times (three in fp32).  Sums of dbias run in an order that depends on the sizes, strides and alignments
+ * Integer sums are exact at any length; an output is rounded four times (three in fp32), and infinite only where its type holds no such number, whatever the scales are.  Sums of dbias run in an order that depends on the sizes, strides and alignments
  * alone.  Results are reproducible bit for bit.  An infinity or NaN in dy[t][o] makes row t of dx and row o of dw NaN; a scale that is NaN makes NaN whatever it enters: all of
  * dw for a token's, all of dx for a channel's.
  * Tensors must not overlap.  workspace: eoq_lin_workspace_size(desc, EOQ_LIN_FWD or EOQ_LIN_BWD) bytes, 256-byte aligned; nothing is kept in it between calls.

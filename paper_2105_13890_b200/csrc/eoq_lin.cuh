@@ -15,6 +15,21 @@ __device__ __forceinline__ float row_scale_of(float amax)
 }
 __device__ __forceinline__ float row_per_of(float amax) { return __fdiv_rn(127.0f, fmaxf(amax, kLeastTop)); }   // (of a finite row)
 
+// An output is sum * row * col + bias, each step rounded.  The first one leaves the range of fp32 where the token's scale is large, although a small scale of the channel may
+// bring the output back: rows of scales above 2^93 (sums are at most 2^34 forward: 2^20 products of 2^14) are multiplied by theirs less 64 powers of two, which the
+// columns' scales make up for.  Powers of two change no rounding, so that both ways give the same bits wherever the first one's steps are numbers.  Small scales
+// need no such care: a whole number times an fp32 number is rounded as it should be down to the smallest.
+constexpr float kLargeScale = 9.903520314283042e27f, kLessScale = 5.421010862427522e-20f, kMoreScale = 1.8446744073709552e19f;   // 2^93, 2^-64, 2^64
+constexpr float kMostNumber = 3.4028234663852886e38f;
+__device__ __forceinline__ bool large_scale(float row) { return fabsf(row) > kLargeScale; }
+// the column's scale for such rows; one of 2^64 and more, which would become infinite, the largest number instead: sums other than zero are beyond all numbers with either
+__device__ __forceinline__ float more_scale(float col) { return fabsf(col) >= kMoreScale && fabsf(col) <= kMostNumber ? copysignf(kMostNumber, col) : col * kMoreScale; }
+__device__ __forceinline__ float scaled_sum(float sum, float row, float col, float bias)
+{
+    const bool large = large_scale(row);
+    return __fmaf_rn(sum * (large ? row * kLessScale : row), large ? more_scale(col) : col, bias);
+}
+
 // R(v * per), the product exact: 1.5 * 2^23 + v * per, rounded once at unit spacing.  The low byte is the code.
 __device__ __forceinline__ uint32_t row_code(float v, float per) { return __float_as_uint(__fmaf_rn(v, per, 12582912.0f)); }
 

@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, 2) lin_few_kernel(const __grid_const
             if (o < a.c_out) {
                 const bool first = i == (int)threadIdx.x;
                 const float scale = first ? scale_first : __ldg(a.w_scales + o), bias = first ? bias_first : a.bias ? __ldg(a.bias + o) : 0.0f;
-                const float v[1] = {__fmaf_rn(__int2float_rn(sum) * scales_s[t], scale, bias)};
+                const float v[1] = {scaled_sum(__int2float_rn(sum), scales_s[t], scale, bias)};
                 store_raw(reinterpret_cast<char *>(a.y) + ((size_t)t * a.y_stride + o) * E::kSize, E::from_f32(v));
             }
         }

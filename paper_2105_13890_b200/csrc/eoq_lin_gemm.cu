@@ -88,10 +88,13 @@ __device__ __forceinline__ uint64_t fma_2(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-// 32 sums of a row with their scales.  `scales`: of the 32 columns, and their biases 128 bytes on.
+// 32 sums of a row with their scales (scaled_sum, two at a time).  `scales`: of the 32 columns, and their biases 128 bytes on.  kLarge: some row of the warp's has a large scale.
+template <bool kLarge>
 __device__ __forceinline__ void scale_row(uint32_t (&r)[32], float row_scale, uint32_t scales)
 {
-    const uint64_t rs = pair_of(row_scale, row_scale);
+    const bool large = kLarge && large_scale(row_scale);
+    const float first = large ? row_scale * kLessScale : row_scale;
+    const uint64_t rs = pair_of(first, first);
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
         uint64_t s[2], b[2];
@@ -99,6 +102,11 @@ __device__ __forceinline__ void scale_row(uint32_t (&r)[32], float row_scale, ui
         asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(b[0]), "=l"(b[1]) : "r"(scales + 128 + j * 4) : "memory");
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
+            if (large) {
+                float s0, s1;
+                asm("mov.b64 {%0, %1}, %2;" : "=f"(s0), "=f"(s1) : "l"(s[i]));
+                s[i] = pair_of(more_scale(s0), more_scale(s1));
+            }
             const uint64_t v = fma_2(mul_2(pair_of(__int2float_rn((int)r[j + 2 * i]), __int2float_rn((int)r[j + 2 * i + 1])), rs), s[i], b[i]);
             asm("mov.b64 {%0, %1}, %2;" : "=r"(r[j + 2 * i]), "=r"(r[j + 2 * i + 1]) : "l"(v));
         }
@@ -376,6 +384,7 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
             }
             if (!__all_sync(0xffffffffu, wait_bar<32>(sums_bar(acc), turn / S::kSums & 1, ctx))) break;
             ptx::tc_fence_after();
+            const bool any_large = __any_sync(0xffffffffu, large_scale(row_scale));
             const size_t out_row = (size_t)split * p.split_rows + row0;
             const uint32_t t_row = tmem_base + acc * kN + part * warp_n + ((uint32_t)(quad * 32) << 16);
 #pragma unroll 1
@@ -396,7 +405,9 @@ __global__ void __launch_bounds__((GemmShape<kN, kPair>::kThreads), 1) lin_gemm_
                 }
                 ptx::tmem_ld_wait();
                 if (type != EOQ_I32) {
-                    scale_row(r, row_scale, staging_w + units % S::kUnits * kUnit);
+                    const uint32_t scales = staging_w + units % S::kUnits * kUnit;
+                    if (any_large) scale_row<true>(r, row_scale, scales);
+                    else scale_row<false>(r, row_scale, scales);
                     __syncwarp();
                 }
                 if (type == EOQ_BF16) write_chunk<EOQ_BF16, S::kUnits>(p, map_out, r, staging_w, units, out_row, rows, col0, lane);
@@ -444,7 +455,7 @@ __global__ void __launch_bounds__(256) lin_join_kernel(const __grid_constant__ L
         for (int j = 0; j < 4; ++j) {
             const bool in = col + j < a.n;
             const float f = kLong ? __ll2float_rn((long long)s[j]) : __int2float_rn((int)s[j]);
-            v[j] = __fmaf_rn(f * rs, in && a.col_scale ? __ldg(a.col_scale + col + j) : 1.0f, in && a.bias ? __ldg(a.bias + col + j) : 0.0f);
+            v[j] = scaled_sum(f, rs, in && a.col_scale ? __ldg(a.col_scale + col + j) : 1.0f, in && a.bias ? __ldg(a.bias + col + j) : 0.0f);
         }
         char *dst = reinterpret_cast<char *>(a.out) + row * a.out_pitch;
         auto put = [&](auto type) {
