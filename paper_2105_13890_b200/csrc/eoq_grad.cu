@@ -171,11 +171,13 @@ __device__ __forceinline__ double whole_norm(const double *sums, int blocks)
             if (i + u * kThreads < blocks) v[u] += __ldcg(sums + i + u * kThreads);
     return sqrt(block_sum((v[0] + v[1]) + (v[2] + v[3])));
 }
+// whether an fp32 number holds the norm, which is rounded to it
+__device__ __forceinline__ bool holds(double whole) { return __double2float_rn(whole) <= 3.4028234663852886e38f; }
 __device__ __forceinline__ void write_norm(double whole, float *norm, DeviceState *dev)
 {
     if (threadIdx.x != 0) return;
-    *norm = (float)whole;
-    if (!(whole <= 3.402823466e38)) atomicOr(&dev->status, EOQ_DEV_NONFINITE);
+    *norm = __double2float_rn(whole);
+    if (!holds(whole)) atomicOr(&dev->status, EOQ_DEV_NONFINITE);
 }
 
 template <int kTensors>
@@ -243,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 4) grad_scale_kernel(const __grid_co
     ptx::grid_dep_wait_launch_small();
     const double whole = whole_norm(s.sums, s.before);
     if (blockIdx.x == 0 && s.last) write_norm(whole, s.norm, s.dev);
-    const float scale = whole <= 3.402823466e38 && whole > max_norm ? (float)(max_norm / whole) : 1.0f;
+    const float scale = holds(whole) && whole > max_norm ? (float)(max_norm / whole) : 1.0f;
     two_ahead(b.pieces, [&](unsigned back, Flight &f) {
         const unsigned p = b.pieces - 1 - back;
         f.t = tensor_of(b, p);
