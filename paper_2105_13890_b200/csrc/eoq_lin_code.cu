@@ -315,12 +315,14 @@ __device__ __forceinline__ float finish_top(float top, float *scale, DeviceState
     return 0.0f;
 }
 
-// What the parts left, put together: by the first blocks 32 columns each, a share of the strips a warp, by the others a row a thread.
+// What the parts left, put together: by the first blocks 32 columns each, a share of the strips a warp, by the others a row a thread.  Sums of up to kFoldStrips strips are
+// added one by one, as the second look adds them: the same bits whatever else a call is asked for.
 constexpr int kJoinThreads = 512;
 __global__ void __launch_bounds__(kJoinThreads) lin_join_looks_kernel(const __grid_constant__ LinErrorArgs a)
 {
     constexpr int kWarps = kJoinThreads / 32;
-    __shared__ float tops_s[kWarps][32], sums_s[kWarps][32];
+    static_assert(kFoldStrips == 2 * kWarps, "two strips a warp");
+    __shared__ float tops_s[kWarps][32], sums_s[kFoldStrips][32];
     ptx::grid_dep_wait_launch_small();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, across = (a.cols + 31) / 32;
     if ((int)blockIdx.x >= across) {
@@ -335,24 +337,30 @@ __global__ void __launch_bounds__(kJoinThreads) lin_join_looks_kernel(const __gr
         return;
     }
     const int col = blockIdx.x * 32 + lane;
-    float top = 0.0f, sum = 0.0f;
+    const bool apart = a.strips <= kFoldStrips;
+    float top = 0.0f, sum = 0.0f, second = 0.0f;
     if (col < a.cols) {
 #pragma unroll 4
         for (int s = warp; s < a.strips; s += kWarps) {
             if (a.strip_tops) top = max_abs(top, __ldg(a.strip_tops + (size_t)s * a.col_pitch + col));
-            if (a.strip_sums) sum += __ldg(a.strip_sums + (size_t)s * a.col_pitch + col);
+            if (a.strip_sums) {
+                const float v = __ldg(a.strip_sums + (size_t)s * a.col_pitch + col);
+                if (apart && s >= kWarps) second += v;
+                else sum += v;
+            }
         }
     }
     tops_s[warp][lane] = top;
     sums_s[warp][lane] = sum;
+    sums_s[warp + kWarps][lane] = second;
     __syncthreads();
     if (warp == 0 && col < a.cols) {
-        for (int w = 1; w < kWarps; ++w) {
-            top = max_abs(top, tops_s[w][lane]);
-            sum += sums_s[w][lane];
-        }
+        float whole = 0.0f;
+        for (int w = 1; w < kWarps; ++w) top = max_abs(top, tops_s[w][lane]);
+#pragma unroll
+        for (int s = 0; s < kFoldStrips; ++s) whole += sums_s[s][lane];
         if (a.strip_tops) a.col_per[col] = finish_top(top, a.col_scales + col, a.dev);
-        if (a.strip_sums) a.sums[col] = sum;
+        if (a.strip_sums) a.sums[col] = whole;
     }
 }
 
