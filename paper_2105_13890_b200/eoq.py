@@ -110,17 +110,19 @@ class grad_list:
         for i, t in enumerate(self.tensors):
             if not t.is_contiguous() or (out is not None and (not self.out[i].is_contiguous() or self.out[i].dtype != t.dtype or self.out[i].numel() != t.numel())):
                 raise ValueError("grad_list: contiguous tensors, of the same type and size where they are clipped into others")
-        types = {"torch.float32": EOQ_F32, "torch.float16": EOQ_F16, "torch.bfloat16": EOQ_BF16}
-        if any(str(t.dtype) not in types for t in self.tensors):
+        types, names = [t.dtype for t in self.tensors], {"torch.float32": EOQ_F32, "torch.float16": EOQ_F16, "torch.bfloat16": EOQ_BF16}
+        number = {t: names.get(str(t)) for t in set(types)}
+        if None in number.values():
             raise TypeError("grad_list: gradients in fp32, fp16 or bf16")
-        devices = {t.get_device() for t in self.tensors + (self.out or []) if t.numel()}
+        sizes = [t.numel() for t in self.tensors]
+        devices = {t.get_device() for group in (self.tensors, self.out or ()) for t, n in zip(group, sizes) if n}
         if len(devices) > 1:
             raise ValueError("grad_list: tensors of one device")
         self.device = devices.pop() if devices else None   # (-1: host memory, which the calls refuse; None: no elements)
         self.g = (C.c_void_p * self.num)(*[t.data_ptr() for t in self.tensors])
         self.to = None if out is None else (C.c_void_p * self.num)(*[t.data_ptr() for t in self.out])
-        self.sizes = (C.c_size_t * self.num)(*[t.numel() for t in self.tensors])
-        self.dtypes = (C.c_int * self.num)(*[types[str(t.dtype)] for t in self.tensors])
+        self.sizes = (C.c_size_t * self.num)(*sizes)
+        self.dtypes = (C.c_int * self.num)(*[number[t] for t in types])
 
 
 _lib = None
