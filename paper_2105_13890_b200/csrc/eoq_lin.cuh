@@ -69,70 +69,104 @@ __device__ __forceinline__ uint32_t raw_top(const Raw<16> &r, uint32_t top)
     }
 }
 
+// kBytes (4, 8 or 16) at p if `in`, zeros otherwise: a load under a predicate, not a branch.
+template <int kBytes>
+__device__ __forceinline__ Raw<kBytes> load_if(const void *p, bool in)
+{
+    Raw<kBytes> r;
+    if constexpr (kBytes == 4)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %2, 0;\n\t"
+            "mov.b32 %0, 0;\n\t"
+            "@p ld.global.nc.b32 %0, [%1];\n\t}"
+            : "=&r"(r.w)
+            : "l"(p), "r"((int)in)
+            : "memory");
+    else if constexpr (kBytes == 8)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %3, 0;\n\t"
+            "mov.b32 %0, 0;\n\t"
+            "mov.b32 %1, 0;\n\t"
+            "@p ld.global.nc.v2.b32 {%0, %1}, [%2];\n\t}"
+            : "=&r"(r.w.x), "=&r"(r.w.y)
+            : "l"(p), "r"((int)in)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "setp.ne.b32 p, %5, 0;\n\t"
+            "mov.b32 %0, 0;\n\t"
+            "mov.b32 %1, 0;\n\t"
+            "mov.b32 %2, 0;\n\t"
+            "mov.b32 %3, 0;\n\t"
+            "@p ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+            : "=&r"(r.w.x), "=&r"(r.w.y), "=&r"(r.w.z), "=&r"(r.w.w)
+            : "l"(p), "r"((int)in)
+            : "memory");
+    return r;
+}
+
 // A thread's 16 bytes of a row, as its rows' alignment kU allows.  16: a vector of kN neighbouring elements.  8 or 4: pieces of as many bytes, `lanes` pieces apart, so that a
 // warp's loads of each are neighbouring.  2 (16-bit elements in odd rows): the aligned words around kN neighbouring elements, shifted into place; a word is only touched
 // when it holds part of the row.  Threads of a row share groups of lanes * kN columns.
+// Loads are predicated: threads of a warp that are done with a row's end at different times may stay apart in what follows, maxima of the warp included, which are then those of a part of
+// it.  (A loop over the end's elements had this effect on the errors' rows where two were looked at in turn.)
 template <int kType, int kU>
 struct Span {
     static constexpr int kE = Elem<kType>::kSize, kN = 16 / kE, kPiece = kU == 2 ? kN : kU / kE;   // elements of a piece
-    static constexpr bool kWhole = kPiece == kN;
     int first, step, cols;   // the thread's first column of a group; from piece to piece; columns of a row
+    bool ends;               // the row ends in this group, inside a piece (for all threads alike)
     Span() = default;
-    __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_) : first(group * lanes * kN + lane * kPiece), step(lanes * kPiece), cols(cols_) {}
+    __device__ __forceinline__ Span(int group, int lane, int lanes, int cols_)
+        : first(group * lanes * kN + lane * kPiece), step(lanes * kPiece), cols(cols_), ends(cols_ % kPiece != 0 && (group + 1) * lanes * kN > cols_)
+    {
+    }
     __device__ __forceinline__ int column(int i) const { return first + i / kPiece * step + i % kPiece; }
     __device__ __forceinline__ bool any() const { return first < cols; }
-    // elements from column c on, fewer than kCount, last one first (zeros behind them): for ends of rows
-    template <int kCount>
-    __device__ __forceinline__ void tail(const char *row, int c0, uint32_t (&w)[kCount * kE / 4]) const
-    {
-#pragma unroll 1
-        for (int c = cols - 1; c >= c0; --c) {
-            const uint32_t v = raw_word(load_raw<kE>(row + (size_t)c * kE), 0);
-#pragma unroll
-            for (int k = kCount * kE / 4 - 1; k > 0; --k) w[k] = kE == 4 ? w[k - 1] : __funnelshift_l(w[k - 1], w[k], 16);
-            w[0] = kE == 4 ? v : w[0] << 16 | v;
-        }
-    }
-    // zeros behind the row's end
+    // zeros behind the row's end, or everywhere where the row is not `mine`
     __device__ __forceinline__ Raw<16> get(const char *row, bool mine) const
     {
         Raw<16> r = zero_raw<16>();
-        if (!mine || first >= cols) return r;
-        if constexpr (kU == 16) {
-            if (first + kN <= cols) return load_raw<16>(row + (size_t)first * kE);
-            uint32_t w[4] = {};
-            tail<kN>(row, first, w);
-            r.w = make_uint4(w[0], w[1], w[2], w[3]);
-        } else if constexpr (kU == 2) {
+        if constexpr (kU == 2) {
             const uintptr_t p = reinterpret_cast<uintptr_t>(row) + (size_t)first * kE, end = reinterpret_cast<uintptr_t>(row) + (size_t)cols * kE, from = p & ~(uintptr_t)3;
             uint32_t w[5];
 #pragma unroll
-            for (int k = 0; k < 5; ++k) w[k] = from + 4 * k < end ? __ldg(reinterpret_cast<const uint32_t *>(from) + k) : 0u;
+            for (int k = 0; k < 5; ++k) w[k] = load_if<4>(reinterpret_cast<const void *>(from + 4 * k), mine && first < cols && from + 4 * k < end).w;
             const int shift = 8 * (int)(p & 2), left = cols - first;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                w[k] = __funnelshift_r(w[k], w[k + 1], shift);
-                if (left < 2 * k + 2) w[k] = left <= 2 * k ? 0u : w[k] & 0xffffu;
-            }
-            r.w = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int k = 0; k < 4; ++k) set_word(r, k, up_to(__funnelshift_r(w[k], w[k + 1], shift), left - 2 * k));
         } else {
+            constexpr int kWords = kU / 4, kOfWord = 4 / kE;   // words of a piece, elements of a word
 #pragma unroll
             for (int j = 0; j < kN / kPiece; ++j) {
                 const int c = first + j * step;
-                uint32_t w[kU / 4] = {};
-                if (c + kPiece <= cols) {
-                    const Raw<kU> v = load_raw<kU>(row + (size_t)c * kE);
+                const char *p = row + (size_t)c * kE;
+                const Raw<kU> v = load_if<kU>(p, mine && c + (kWords == 1 ? 1 : kPiece) <= cols);
 #pragma unroll
-                    for (int k = 0; k < kU / 4; ++k) w[k] = raw_word(v, k);
-                } else if (c < cols) {
-                    tail<kPiece>(row, c, w);
+                for (int k = 0; k < kWords; ++k) set_word(r, j * kWords + k, raw_word(v, k));
+            }
+            // the piece that the row ends in, word by word
+            if (kPiece > 1 && ends) {
+#pragma unroll
+                for (int j = 0; j < kN / kPiece; ++j) {
+                    const int c = first + j * step;
+                    const bool part = mine && c < cols && c + kPiece > cols;
+#pragma unroll
+                    for (int k = 0; k < kWords; ++k) {
+                        const int left = cols - c - k * kOfWord;
+                        uint32_t w = raw_word(r, j * kWords + k);
+                        if constexpr (kWords > 1) w |= load_if<4>(row + (size_t)c * kE + 4 * k, part && left > 0).w;
+                        set_word(r, j * kWords + k, up_to(w, left));
+                    }
                 }
-#pragma unroll
-                for (int k = 0; k < kU / 4; ++k) set_word(r, j * (kU / 4) + k, w[k]);
             }
         }
         return r;
     }
+    // the first `left` elements of a word, zeros for the others
+    static __device__ __forceinline__ uint32_t up_to(uint32_t w, int left) { return left <= 0 ? 0u : kE == 2 && left == 1 ? w & 0xffffu : w; }
     // of an array with an element for each column, in whole pieces (padded to eight); ones of nothing behind the end
     __device__ __forceinline__ void get_padded(const float *p, float (&v)[kN]) const
     {
