@@ -515,9 +515,10 @@ EOQ_API int eoq_gn_bwd(eoq_handle_t handle, const eoq_gn_desc_t *desc, const voi
  *   u[t][o] = dy[t][o] w_scales[o], rounded to fp32, coded by tokens:   dx[t][i] = scale_u[t] sum over o of code_u[t][o] w_codes[o][i]
  *   v[t][o] = dy[t][o] x_scales[t], rounded to fp32, coded by channels: dw[o][i] = scale_v[o] sum over t of code_v[t][o] x_codes[t][i]  (fp32 [c_out][c_in], 16-byte aligned)
  *   dbias[o] = sum over t of dy[t][o]  (fp32).  Each of the three may be NULL; w_codes and w_scales are needed for dx, x_codes and x_scales for dw.
- * Integer sums are exact at any length; an output is rounded four times (three in fp32), and infinite only where its type holds no such number, whatever the scales are.  Sums of dbias run in an order that depends on the sizes, strides and alignments
- * alone.  Results are reproducible bit for bit.  An infinity or NaN in dy[t][o] makes row t of dx and row o of dw NaN; a scale that is NaN makes NaN whatever it enters: all of
- * dw for a token's, all of dx for a channel's.
+ * Integer sums are exact at any length; y, dx and dw are rounded four times (three in fp32), and infinite only where their type holds no such number, whatever the scales are.
+ * Sums of dbias run in fp32, in an order that depends on the sizes, strides and alignments alone, not on what else is asked for.  Results are reproducible bit for bit.
+ * An infinity or NaN in dy[t][o], or a u (v) beyond fp32, makes row t of dx (row o of dw) NaN; a scale that is NaN makes NaN whatever it enters: all of dw for a token's, all
+ * of dx for a channel's.
  * Tensors must not overlap.  workspace: eoq_lin_workspace_size(desc, EOQ_LIN_FWD or EOQ_LIN_BWD) bytes, 256-byte aligned; nothing is kept in it between calls.
  * Pointers aligned to their elements, codes and dw to 16 bytes; 16-byte aligned tensors with strides of 16 bytes run several times faster.
  * eoq_set_gemm_ctas and the reduce hook do not apply.
@@ -543,8 +544,9 @@ EOQ_API int eoq_lin_bwd(eoq_handle_t handle, const eoq_lin_desc_t *desc, const v
  *   norm = sqrt(sum of g^2 over all elements of all tensors),  out = g * min(1, max_norm / norm).
  * Host arrays of num tensors: g (device), sizes in elements (0: left out), dtypes (EOQ_F32, EOQ_F16, EOQ_BF16).  out: tensors of the same types, which may be g's own, or NULL
  * for in place; otherwise tensors must not overlap.  norm: fp32, device.
- * Sums run in 64 bits, in an order that depends on the sizes and alignments alone: results are reproducible bit for bit.  The factor is an fp32 number, 1 where the norm is
- * at most max_norm.  A norm that no fp32 number holds, or NaN, raises EOQ_DEV_NONFINITE, is written as it is, and the factor is 1: the program skips the step.
+ * The squares of 16 bytes are added in fp32 (in 64 bits where fp32 would lose some of them or not hold them), these sums in 64 bits, in an order that depends on the sizes and
+ * alignments alone: results are reproducible bit for bit, a norm above 2^-126 is off by 3.5 * 2^-24 of it at most.  The factor is an fp32 number (of fewer bits below 2^-126), 1 where the
+ * norm is at most max_norm.  A norm that no fp32 number holds, or NaN, raises EOQ_DEV_NONFINITE, is written as it is, and the factor is 1: the program skips the step.
  * workspace: eoq_grad_workspace_size(num) bytes, 256-byte aligned; nothing is kept in it between calls.
  * Errors: BAD_ARG (null pointer, num <= 0, unknown type, max_norm negative or NaN, the handle's device not the current one), ALIGNMENT (of an element, norm),
  * UNSUPPORTED (num > 2^20, more than 2^40 elements), WORKSPACE.

@@ -178,7 +178,8 @@ __device__ __forceinline__ void meet_threads(float *cells, float (&mine)[kN], in
 
 // Block (x, y): strip x of the rows, kVec groups of the columns from y * kVec on, `lanes` (at most 32) threads a row.  kRows: the rows' maxima too.
 // Vectors come in by asynchronous copies, each read back by the thread that copied it, some rows ahead.  What bounds it is issue: two vectors of a row a thread share the
-// row's own work (its factor, its maximum, what is ahead).  16,384 x 4096 of bf16: 36 us; 43 with one.
+// row's own work (its factor, its maximum, what is ahead).  16,384 x 4096 of bf16: 36 us; 43 with one.  (That form's 16-bit variants spill 48 bytes at the 80 registers that three
+// blocks an SM leave.)
 template <int kType, int kU, int kVec, bool kRows>
 __global__ void __launch_bounds__(kThreads, 3) lin_look_kernel(const __grid_constant__ LinErrorArgs a, const int lanes)
 {

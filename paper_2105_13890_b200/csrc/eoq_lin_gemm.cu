@@ -12,7 +12,8 @@
 // tensor copies, one for the MMAs.  Accumulators in tensor memory, two of a pair, four otherwise, let tiles' epilogues run beside the next ones' MMAs: what an epilogue
 // takes is mostly waiting (for scales, tensor memory, stores), so that blocks with several tiles give them to two or four groups of warps in turn.  The two products of a
 // backward pass share a launch: alone, 64 and 256 tiles leave 74 pairs idle for an eighth of the time each.  All waits are bounded.
-// 8192 tokens, 4096 to 4096 channels: 80 us, 3.4 POPS; 16,384 tokens, 1024 to 4096: 46 us forward, 87 for the two products backward (87% of the tensor pipe's cycles).
+// In short runs, before the power limit lowers the clock: 8192 tokens, 4096 to 4096 channels 80 us, 3.4 POPS; 16,384 tokens, 1024 to 4096 46 us forward, 87 for the two products
+// backward (87% of the tensor pipe's cycles); these two together take 142 in long ones.
 #include "eoq_lin.cuh"
 #include "eoq_pair.cuh"
 
